@@ -14,7 +14,7 @@ Each pass makes the calls that one data-parallel worker makes of one of them:
 
 A 4-bit block is 32 neighbours of a row: one sign, two exponent and one mantissa bit each (0, 0.5, 1, 1.5, 2, 3, 4, 6),
 to nearest, ties to even, over a common power of two, 2^(floor(log2(largest magnitude)) - 2) held as an exponent of 8 bits.
-A block that holds an infinity or a NaN has the exponent 255 and stands for NaN.  Rows are padded with zeros to 128.
+A block that holds an infinity or a NaN has the exponent 255 and stands for NaN.  Rows are padded with zeros to 256.
 
 A case is a dict of plain values:
   entry   one of the above                         dtype   element type of gradient, matrix, input and weight
@@ -30,7 +30,7 @@ import torch
 own = False
 
 DTYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
-BLOCK, PAD = 32, 128
+BLOCK, PAD = 32, 256
 STEPS, COEF, EPS = 5, (3.4445, -4.7750, 2.0315), 1e-7
 LEARNING_RATE, MOMENTUM, WEIGHT_DECAY = 0.02, 0.95, 0.01
 
@@ -99,7 +99,7 @@ def _up(n, m):
 
 
 def _quantize(x):
-    """Rows of float32 -> (values without their scale, exponent codes), padded to 128 columns."""
+    """Rows of float32 -> (values without their scale, exponent codes), padded to PAD columns."""
     rows, cols = x.shape
     blocks = torch.nn.functional.pad(x, (0, _up(cols, PAD) - cols)).view(rows, -1, BLOCK)
     top = blocks.abs().amax(-1, keepdim=True)
