@@ -471,6 +471,90 @@ int sidco_get_diag(void *stream, sidco_diag *host_out);
 int sidco_set_profiling(int enable);
 int sidco_get_profile(float *ms, const char **names, int cap);
 
+/* ---- 4-bit microscaled numbers ------------------------------------------------
+ *
+ * A block is 32 neighbours of a row under one power of two: with e = floor(log2
+ * of the largest magnitude) its exponent byte is max(e - 2, -127) + 127, and each
+ * number's 4-bit code (sign, two bits of exponent, one of mantissa: 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6) is the nearest to x / 2^(byte - 127), ties to the even code,
+ * magnitudes over 6 taken as 6.  A block of zeros has the byte 0.  A block that
+ * holds an infinity or a NaN has the byte 255 and codes of 0, and stands for NaN
+ * in every one of its places.
+ *
+ * Storage.  A row of n numbers is padded with zeros to a multiple of 256: two
+ * codes a byte, the first in the low half, sidco_mx4_code_bytes(1, n) = 128 *
+ * ceil(n / 256) bytes; and one exponent byte a block, sidco_mx4_scale_bytes(1, n) =
+ * 8 * ceil(n / 256).  Rows follow each other.  Code buffers are 16-byte, exponent
+ * buffers 8-byte aligned (SIDCO_ERR_ALIGN).  A flat gradient is one row.
+ *
+ * Element types are SIDCO_GRAD_F32, _F16 and _BF16.  Results are deterministic:
+ * no sum depends on the order in which blocks finish.                          */
+#define SIDCO_MX4_BLOCK 32
+
+/* Host helpers: bytes of the codes and of the exponents of rows x cols numbers, or
+ * SIDCO_ERR_SIZE.                                                             */
+int64_t sidco_mx4_code_bytes(int64_t rows, int64_t cols);
+int64_t sidco_mx4_scale_bytes(int64_t rows, int64_t cols);
+
+/*
+ * Dense 4-bit compression of one worker's gradient with error feedback: acc = grad
+ * + residual (rounded to fp32, as the residual holds it) becomes codes and
+ * exponents, and residual = acc - what they stand for.  In a block that stands
+ * for NaN the residual keeps acc.  residual may be NULL (memoryless); it must not
+ * alias grad.  1 <= d <= 2^31-1.  Needs no workspace.
+ */
+int sidco_mx4_compress(void *stream, const void *grad, int grad_dtype, float *residual, int64_t d, uint8_t *codes,
+                       uint8_t *scales);
+
+/*
+ * The receiving side: dense_j = scale * sum over w = 0 .. workers-1 of worker w's
+ * numbers, in that order and in fp32 (accumulate = 0), or dense_j += that sum
+ * (accumulate = 1).  Worker w's codes start at codes + w * code_stride and its
+ * exponents at scales + w * scale_stride; strides in bytes, multiples of 16 and 8
+ * and not shorter than the vector's.  Needs no workspace.
+ */
+int sidco_mx4_aggregate(void *stream, const uint8_t *codes, int64_t code_stride, const uint8_t *scales, int64_t scale_stride,
+                        int workers, int64_t d, float scale, int accumulate, float *dense);
+
+/*
+ * A rows x cols matrix (row stride ldx >= cols elements) in 4 bits, read once:
+ *   codes, scales      blocks along the rows: rows of cols numbers
+ *   codes_t, scales_t  blocks along the columns, transposed: cols rows of `rows`
+ *                      numbers
+ * Either pair may be NULL, not both.  A product needs both its operands blocked
+ * along the axis that it sums over: the forward product of a layer takes the
+ * first form of input and weight, the products of its backward pass the others.
+ * Needs no workspace.
+ */
+int sidco_mx4_quantize(void *stream, const void *x, int dtype, int64_t rows, int64_t cols, int64_t ldx, uint8_t *codes,
+                       uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t);
+
+/* What the codes of rows x cols numbers stand for, rounded to `dtype` (exact in fp32
+ * and bf16), with row stride ldo >= cols elements.  Needs no workspace.        */
+int sidco_mx4_dequantize(void *stream, const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, void *out,
+                         int dtype, int64_t ldo);
+
+/*
+ * C = alpha A B^T (accumulate = 0) or C += alpha A B^T (accumulate = 1): A is m x k
+ * and B is n x k, both blocked along k; C is m x n of `c_dtype` with row stride
+ * ldc >= n elements.  Products are exact, sums are fp32 and rounded once.
+ * 1 <= m, n <= 2^31-1, 1 <= k <= 2^24.  C must not overlap A or B.  Needs no
+ * workspace.
+ */
+int sidco_mx4_matmul(void *stream, const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes,
+                     const uint8_t *b_scales, int64_t m, int64_t n, int64_t k, float alpha, int accumulate, void *c, int c_dtype,
+                     int64_t ldc);
+
+/*
+ * A layer with a 4-bit weight on rows as they come: x (rows x k of `x_dtype`, row
+ * stride ldx) is quantised along its rows and multiplied with the n x k weight, c =
+ * alpha x^ W^T (+ c) as in sidco_mx4_matmul.  From one row on.  Uses the stream's
+ * workspace: sidco_workspace_bytes_mx4_linear(rows, k).
+ */
+int sidco_mx4_linear(void *stream, const void *x, int x_dtype, int64_t rows, int64_t k, int64_t ldx, const uint8_t *w_codes,
+                     const uint8_t *w_scales, int64_t n, float alpha, int accumulate, void *c, int c_dtype, int64_t ldc);
+size_t sidco_workspace_bytes_mx4_linear(int64_t rows, int64_t k);
+
 /* Text for an error code; the HIP error string of the last SIDCO_ERR_HIP.     */
 const char *sidco_strerror(int code);
 const char *sidco_last_hip_error(void);

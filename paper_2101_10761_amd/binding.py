@@ -28,6 +28,8 @@ EXPORTS = [
     "sidco_set_delta1", "sidco_get_diag", "sidco_controller_disturbed",
     "sidco_set_speculation", "sidco_read_diag", "sidco_set_profiling",
     "sidco_get_profile", "sidco_strerror", "sidco_last_hip_error", "sidco_version", "sidco_shutdown",
+    "sidco_mx4_code_bytes", "sidco_mx4_scale_bytes", "sidco_mx4_compress", "sidco_mx4_aggregate", "sidco_mx4_quantize",
+    "sidco_mx4_dequantize", "sidco_mx4_matmul", "sidco_mx4_linear", "sidco_workspace_bytes_mx4_linear",
 ]
 
 
@@ -176,6 +178,25 @@ def load() -> C.CDLL:
     lib.sidco_set_profiling.restype = C.c_int
     lib.sidco_get_profile.argtypes = [C.POINTER(C.c_float), C.POINTER(C.c_char_p), C.c_int]
     lib.sidco_get_profile.restype = C.c_int
+    i64, u8p = C.c_int64, C.c_void_p
+    lib.sidco_mx4_code_bytes.argtypes = [i64, i64]
+    lib.sidco_mx4_code_bytes.restype = i64
+    lib.sidco_mx4_scale_bytes.argtypes = [i64, i64]
+    lib.sidco_mx4_scale_bytes.restype = i64
+    lib.sidco_mx4_compress.argtypes = [vp, vp, C.c_int, f32p, i64, u8p, u8p]
+    lib.sidco_mx4_compress.restype = C.c_int
+    lib.sidco_mx4_aggregate.argtypes = [vp, u8p, i64, u8p, i64, C.c_int, i64, C.c_float, C.c_int, f32p]
+    lib.sidco_mx4_aggregate.restype = C.c_int
+    lib.sidco_mx4_quantize.argtypes = [vp, vp, C.c_int, i64, i64, i64, u8p, u8p, u8p, u8p]
+    lib.sidco_mx4_quantize.restype = C.c_int
+    lib.sidco_mx4_dequantize.argtypes = [vp, u8p, u8p, i64, i64, vp, C.c_int, i64]
+    lib.sidco_mx4_dequantize.restype = C.c_int
+    lib.sidco_mx4_matmul.argtypes = [vp, u8p, u8p, u8p, u8p, i64, i64, i64, C.c_float, C.c_int, vp, C.c_int, i64]
+    lib.sidco_mx4_matmul.restype = C.c_int
+    lib.sidco_mx4_linear.argtypes = [vp, vp, C.c_int, i64, i64, i64, u8p, u8p, i64, C.c_float, C.c_int, vp, C.c_int, i64]
+    lib.sidco_mx4_linear.restype = C.c_int
+    lib.sidco_workspace_bytes_mx4_linear.argtypes = [i64, i64]
+    lib.sidco_workspace_bytes_mx4_linear.restype = C.c_size_t
     lib.sidco_strerror.argtypes = [C.c_int]
     lib.sidco_strerror.restype = C.c_char_p
     lib.sidco_last_hip_error.argtypes = []
@@ -657,6 +678,124 @@ def sidco_get_profile() -> list[tuple[str, float]]:
     if n < 0:
         raise SidcoError(n, "sidco_get_profile")
     return [(names[i].decode(), float(ms[i])) for i in range(n)]
+
+
+# ---- 4-bit microscaled numbers ----
+
+
+def sidco_mx4_code_bytes(rows: int, cols: int) -> int:
+    n = load().sidco_mx4_code_bytes(rows, cols)
+    if n < 0:
+        raise SidcoError(int(n), "sidco_mx4_code_bytes")
+    return int(n)
+
+
+def sidco_mx4_scale_bytes(rows: int, cols: int) -> int:
+    n = load().sidco_mx4_scale_bytes(rows, cols)
+    if n < 0:
+        raise SidcoError(int(n), "sidco_mx4_scale_bytes")
+    return int(n)
+
+
+def sidco_workspace_bytes_mx4_linear(rows: int, k: int) -> int:
+    return int(load().sidco_workspace_bytes_mx4_linear(rows, k))
+
+
+def _check_packed(codes, scales, rows, cols, name):
+    torch = _torch or _import_torch()
+    padded = (cols + 255) // 256
+    _check_tensor(codes, torch.uint8, name + " codes", rows * padded * 128)
+    _check_tensor(scales, torch.uint8, name + " scales", rows * padded * 8)
+
+
+def _matrix(x, name, dims=2):
+    """Element code and row stride of a CUDA matrix (or batch of them) whose rows are contiguous."""
+    torch = _torch or _import_torch()
+    codes = {torch.float32: GRAD_F32, torch.float16: GRAD_F16, torch.bfloat16: GRAD_BF16}
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != dims or x.dtype not in codes:
+        raise TypeError(f"{name} must be a CUDA tensor of {dims} dimensions and dtype float32, float16 or bfloat16")
+    code = codes[x.dtype]
+    rows, cols = x.shape[-2:]
+    if cols > 1 and x.stride(-1) != 1:
+        raise TypeError(f"{name} must have contiguous rows")
+    ld = x.stride(-2) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{name}'s rows overlap")
+    return code, ld
+
+
+def sidco_mx4_compress(grad, residual, codes, scales, stream=None) -> None:
+    """Error feedback and 4-bit blocks of one flat gradient (float32, float16 or bfloat16); `residual` (float32) may be
+    None.  codes, scales: uint8 of sidco_mx4_code_bytes(1, d) and sidco_mx4_scale_bytes(1, d)."""
+    torch = _torch or _import_torch()
+    code, d = _grad_code(grad), grad.numel()
+    _check_tensor(grad, grad.dtype, "grad")
+    if residual is not None:
+        _check_tensor(residual, torch.float32, "residual", d)
+    _check_packed(codes, scales, 1, d, "the gradient's")
+    _check(load().sidco_mx4_compress(_stream_handle(stream), _ptr(grad), code, _ptr(residual), d, _ptr(codes), _ptr(scales)),
+           "sidco_mx4_compress")
+
+
+def sidco_mx4_aggregate(codes, scales, dense, scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
+    """dense (+)= scale * the sum of what the workers' blocks stand for; row w of codes and scales is worker w's."""
+    torch = _torch or _import_torch()
+    d = dense.numel()
+    _check_tensor(dense, torch.float32, "dense", 1)
+    if codes.dim() != 2 or scales.dim() != 2 or codes.shape[0] != scales.shape[0]:
+        raise ValueError("codes and scales must have a row for each worker")
+    workers = codes.shape[0]
+    _check_packed(codes, scales, 1, 1, "the workers'")
+    if codes.shape[1] < (d + 255) // 256 * 128 or scales.shape[1] < (d + 255) // 256 * 8:
+        raise ValueError("codes or scales are shorter than dense")
+    _check(load().sidco_mx4_aggregate(_stream_handle(stream), _ptr(codes), codes.shape[1], _ptr(scales), scales.shape[1], workers,
+                                      d, scale, int(accumulate), _ptr(dense)), "sidco_mx4_aggregate")
+
+
+def sidco_mx4_quantize(x, codes, scales, codes_t=None, scales_t=None, stream=None) -> None:
+    """4-bit blocks of a matrix along its rows (codes, scales) and, transposed, along its columns (codes_t, scales_t);
+    either pair may be None."""
+    code, ld = _matrix(x, "x")
+    rows, cols = x.shape
+    if codes is not None or scales is not None:
+        _check_packed(codes, scales, rows, cols, "the rows'")
+    if codes_t is not None or scales_t is not None:
+        _check_packed(codes_t, scales_t, cols, rows, "the columns'")
+    _check(load().sidco_mx4_quantize(_stream_handle(stream), _ptr(x), code, rows, cols, ld, _ptr(codes), _ptr(scales),
+                                     _ptr(codes_t), _ptr(scales_t)), "sidco_mx4_quantize")
+
+
+def sidco_mx4_dequantize(codes, scales, out, stream=None) -> None:
+    """What the blocks of out's rows stand for, in out's type."""
+    code, ld = _matrix(out, "out")
+    rows, cols = out.shape
+    _check_packed(codes, scales, rows, cols, "the matrix's")
+    _check(load().sidco_mx4_dequantize(_stream_handle(stream), _ptr(codes), _ptr(scales), rows, cols, _ptr(out), code, ld),
+           "sidco_mx4_dequantize")
+
+
+def sidco_mx4_matmul(a_codes, a_scales, b_codes, b_scales, k: int, out, alpha: float = 1.0, accumulate: bool = False,
+                     stream=None) -> None:
+    """out (+)= alpha A B^T; A has out's rows, B its columns, both of k numbers blocked along k."""
+    code, ld = _matrix(out, "out")
+    m, n = out.shape
+    _check_packed(a_codes, a_scales, m, k, "A's")
+    _check_packed(b_codes, b_scales, n, k, "B's")
+    _check(load().sidco_mx4_matmul(_stream_handle(stream), _ptr(a_codes), _ptr(a_scales), _ptr(b_codes), _ptr(b_scales), m, n, k,
+                                   alpha, int(accumulate), _ptr(out), code, ld), "sidco_mx4_matmul")
+
+
+def sidco_mx4_linear(x, w_codes, w_scales, out, alpha: float = 1.0, accumulate: bool = False, stream=None) -> None:
+    """out (+)= alpha x^ W^T: x's rows are quantised on the way, W has out's columns as its rows."""
+    x_code, ldx = _matrix(x, "x")
+    code, ld = _matrix(out, "out")
+    rows, k = x.shape
+    if out.shape[0] != rows:
+        raise ValueError("out must have a row for each of x's")
+    n = out.shape[1]
+    _check_packed(w_codes, w_scales, n, k, "the weight's")
+    _check(load().sidco_mx4_linear(_stream_handle(stream), _ptr(x), x_code, rows, k, ldx, _ptr(w_codes), _ptr(w_scales), n, alpha,
+                                   int(accumulate), _ptr(out), code, ld), "sidco_mx4_linear")
 
 
 def sidco_version() -> int:

@@ -635,6 +635,26 @@ int run(void* stream, const void* grad, float* residual, int64_t d, int dist, co
 }
 
 }  // namespace
+
+StreamScratch::StreamScratch(void* stream, size_t bytes) : rc(SIDCO_OK), data(nullptr)
+{
+    g_mu.lock();
+    WsCtx* c = nullptr;
+    rc = pick_ws(stream, true, &c);
+    if (rc == SIDCO_OK) rc = ensure_workspace(*c, head_bytes() + bytes);
+    if (rc == SIDCO_OK) data = (char*)c->ws + head_bytes();
+}
+
+StreamScratch::~StreamScratch() { g_mu.unlock(); }
+
+size_t workspace_with_scratch(size_t bytes) { return head_bytes() + bytes; }
+
+int launched()
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? SIDCO_OK : hip_fail(e, "kernel launch");
+}
+
 }  // namespace sidco
 
 using namespace sidco;
@@ -1730,7 +1750,7 @@ const char* sidco_strerror(int code)
 
 const char* sidco_last_hip_error(void) { return g_hip_msg; }
 
-int sidco_version(void) { return 100; }
+int sidco_version(void) { return 101; }
 
 void sidco_shutdown(void)
 {

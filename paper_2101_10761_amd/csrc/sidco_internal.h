@@ -404,5 +404,22 @@ constexpr int kSelectBlock = 256, kSelectTiles = 16;  // k_select's block, and i
 void launch_select(const Params& p, bool keep, hipStream_t s);
 void launch_gather(const Params& p, hipStream_t s);
 
+// ---- what the C ABI's other source files use of the one that keeps the workspaces ----
+
+// The workspace of `stream` behind its head, of at least `bytes` bytes and 256-byte aligned, for one call: no other call
+// enters the library while this lives.  rc is SIDCO_OK or the error to return.  What a call leaves there, later calls
+// may write over.
+class StreamScratch {
+  public:
+    StreamScratch(void* stream, size_t bytes);
+    ~StreamScratch();
+    StreamScratch(const StreamScratch&) = delete;
+    StreamScratch& operator=(const StreamScratch&) = delete;
+    int rc;
+    char* data;
+};
+size_t workspace_with_scratch(size_t bytes);  // bytes of a workspace whose scratch has `bytes`
+int launched();                               // SIDCO_OK, or SIDCO_ERR_HIP with the text of the last launch's error
+
 }  // namespace sidco
 #endif

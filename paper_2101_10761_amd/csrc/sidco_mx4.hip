@@ -1,0 +1,479 @@
+// 4-bit microscaled numbers: a gradient's exchange with error feedback, matrices along both axes, and their products.
+//
+// A block is 32 neighbours x_i of a row.  With e = floor(log2 max|x_i|) its exponent byte is max(e - 2, -127) + 127, and its
+// codes are x_i / 2^(byte - 127) rounded to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (ties to the even code, 6 beyond it).
+// In the bits of an fp32 magnitude the byte is the exponent field less two, at least 0; a field of 255 (an infinity or a NaN
+// in the block) is kept as the byte 255, and the block then stands for NaN.  The division is by a power of two and therefore
+// exact; the rounding is the conversion instruction's.
+#include "sidco_dense.h"
+#include "sidco_product.h"
+
+namespace sidco {
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4h __attribute__((ext_vector_type(4), aligned(2)));
+
+struct F32 {
+    typedef float T;
+    static __device__ __forceinline__ float widen(T x) { return x; }
+    static __device__ __forceinline__ T narrow(float x) { return x; }
+};
+struct F16 {
+    typedef _Float16 T;
+    static __device__ __forceinline__ float widen(T x) { return (float)x; }
+    static __device__ __forceinline__ T narrow(float x) { return (T)x; }
+};
+struct Bf16 {
+    typedef __bf16 T;
+    static __device__ __forceinline__ float widen(T x) { return (float)x; }
+    static __device__ __forceinline__ T narrow(float x) { return (T)x; }
+};
+
+template <class E>
+__device__ __forceinline__ void load8(const typename E::T* p, float x[8])
+{
+    if constexpr (sizeof(typename E::T) == 4) {
+        const f4 a = *(const f4*)p, b = *(const f4*)(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+    } else {
+        const u4 a = *(const u4h*)p;
+        typedef typename E::T t8 __attribute__((ext_vector_type(8)));
+        const t8 v = __builtin_bit_cast(t8, a);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = E::widen(v[i]);
+    }
+}
+
+template <class E>
+__device__ __forceinline__ void store8(typename E::T* p, const float x[8])
+{
+    if constexpr (sizeof(typename E::T) == 4) {
+        *(f4*)p = f4{x[0], x[1], x[2], x[3]};
+        *(f4*)(p + 4) = f4{x[4], x[5], x[6], x[7]};
+    } else {
+        typedef typename E::T t8 __attribute__((ext_vector_type(8)));
+        t8 v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = E::narrow(x[i]);
+        *(u4h*)p = __builtin_bit_cast(u4, v);
+    }
+}
+
+// n < 8 elements, zeros after them
+template <class E>
+__device__ __forceinline__ void load_few(const typename E::T* p, int64_t n, float x[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < n ? E::widen(p[i]) : 0.0f;
+}
+
+template <class E>
+__device__ __forceinline__ void store_few(typename E::T* p, int64_t n, const float x[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) p[i] = E::narrow(x[i]);
+}
+
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+__device__ __forceinline__ uint32_t largest8(const float x[8])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = larger(m, magnitude(x[i]));
+    return m;
+}
+
+// the largest over the four lanes of a quad
+__device__ __forceinline__ uint32_t largest_of_quad(uint32_t m)
+{
+    m = larger(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 0xf, 0xf, true));  // lanes 1 0 3 2
+    return larger(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 0xf, 0xf, true));  // lanes 2 3 0 1
+}
+
+// exponent byte of a block whose largest magnitude has these bits
+__device__ __forceinline__ uint32_t exponent_byte(uint32_t top)
+{
+    const uint32_t e = top >> 23;
+    return e == 255 ? 255 : (e > 2 ? e - 2 : 0);
+}
+
+// 1 / 2^(byte - 127); byte <= 252
+__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254 - byte) << 23); }
+// 2^(byte - 127); NaN for 255
+__device__ __forceinline__ float scale_of(uint32_t byte)
+{
+    return __uint_as_float(byte == 0 ? 0x00400000u : (byte == 255 ? 0x7fc00000u : byte << 23));
+}
+
+// the codes of 8 neighbours, the first in the lowest bits
+__device__ __forceinline__ uint32_t encode8(const float x[8], uint32_t byte)
+{
+    const float inv = inverse_scale(byte);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0] * inv, x[1] * inv, 1.0f, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2] * inv, x[3] * inv, 1.0f, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4] * inv, x[5] * inv, 1.0f, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6] * inv, x[7] * inv, 1.0f, 3);
+    return byte == 255 ? 0 : c;
+}
+
+// what 8 codes stand for, times the scale's power of two
+__device__ __forceinline__ void decode8(uint32_t c, float scale, float x[8])
+{
+    const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
+    const v2f d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3);
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = d.x, x[5] = d.y, x[6] = e.x, x[7] = e.y;
+}
+
+constexpr int kFlat = 256;  // threads of the kernels of flat vectors
+
+// A lane has 8 neighbours, a quad of lanes a block.  acc = g + r; the residual keeps what the codes do not hold, and all of
+// acc where the block stands for NaN.
+template <class E, bool Residual>
+__global__ __launch_bounds__(kFlat) void k_mx4_compress(const typename E::T* __restrict__ grad, float* __restrict__ residual, int64_t d,
+                                                        uint32_t* __restrict__ codes, uint8_t* __restrict__ scales, int64_t groups)
+{
+    for (int64_t i = (int64_t)blockIdx.x * kFlat + threadIdx.x; i < groups; i += (int64_t)gridDim.x * kFlat) {
+        const int64_t j = i * 8, left = d - j;
+        float x[8], r[8];
+        if (left >= 8) {
+            load8<E>(grad + j, x);
+            if (Residual) load8<F32>(residual + j, r);
+        } else {
+            load_few<E>(grad + j, left, x);
+            if (Residual) load_few<F32>(residual + j, left, r);
+        }
+        if (Residual) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] += r[k];
+        }
+        const uint32_t byte = exponent_byte(largest_of_quad(largest8(x)));
+        const uint32_t c = encode8(x, byte);
+        codes[i] = c;
+        if ((threadIdx.x & 3) == 0) scales[i >> 2] = (uint8_t)byte;
+        if (Residual) {
+            decode8(c, byte == 255 ? 1.0f : scale_of(byte), r);  // 255: codes of zeros, nothing is taken from acc
+#pragma unroll
+            for (int k = 0; k < 8; ++k) r[k] = x[k] - r[k];
+            if (left >= 8)
+                store8<F32>(residual + j, r);
+            else
+                store_few<F32>(residual + j, left, r);
+        }
+    }
+}
+
+template <bool Accumulate>
+__global__ __launch_bounds__(kFlat) void k_mx4_aggregate(const uint8_t* __restrict__ codes, int64_t code_stride,
+                                                         const uint8_t* __restrict__ scales, int64_t scale_stride, int workers,
+                                                         int64_t d, float scale, float* __restrict__ dense, int64_t groups)
+{
+    for (int64_t i = (int64_t)blockIdx.x * kFlat + threadIdx.x; i < groups; i += (int64_t)gridDim.x * kFlat) {
+        const int64_t j = i * 8, left = d - j;
+        float sum[8] = {};
+#pragma unroll 4
+        for (int w = 0; w < workers; ++w) {
+            const uint32_t c = *(const uint32_t*)(codes + w * code_stride + i * 4);
+            const uint32_t byte = scales[w * scale_stride + (i >> 2)];
+            float x[8];
+            decode8(c, scale_of(byte), x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] += byte == 255 ? scale_of(255) : x[k];
+        }
+        float old[8];
+        if (Accumulate) {
+            if (left >= 8)
+                load8<F32>(dense + j, old);
+            else
+                load_few<F32>(dense + j, left, old);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[k] = Accumulate ? fmaf(scale, sum[k], old[k]) : scale * sum[k];
+        if (left >= 8)
+            store8<F32>(dense + j, sum);
+        else
+            store_few<F32>(dense + j, left, sum);
+    }
+}
+
+// ---- matrices ----
+
+constexpr int kSide = 128;       // a block quantises kSide x kSide elements
+constexpr int kQuant = 512;
+
+// Along the rows a quad of lanes has a block as above.  Along the columns a lane has one: it reads 32 rows of its column
+// from LDS.  Its four neighbours' codes follow each other in the transposed row, so a quad of lanes takes one column's four
+// blocks; the columns of a block of 32 rows are kept in LDS with their bits 4 and 5 changed by the block's number, so that
+// the quad's lanes read different banks.
+template <class E, bool Along, bool Across>
+__global__ __launch_bounds__(kQuant) void k_mx4_quantize(const typename E::T* __restrict__ x, int64_t rows, int64_t cols, int64_t ldx,
+                                                         uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                                         uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t,
+                                                           uint32_t across_x)
+{
+    typedef typename E::T T;
+    __shared__ __align__(16) T tile[Across ? kSide * kSide : 1];
+    const int64_t r0 = (int64_t)(blockIdx.x / across_x) * kSide, c0 = (int64_t)(blockIdx.x % across_x) * kSide;
+    const int64_t pitch = mx4_padded(cols) / 2, pitch_t = mx4_padded(rows) / 2;
+    const bool along = Along && c0 < pitch * 2, across = Across && r0 < pitch_t * 2;
+#pragma unroll
+    for (int k = 0; k < kSide * kSide / 8 / kQuant; ++k) {
+        const int g = k * kQuant + threadIdx.x, r = g / (kSide / 8), c = g % (kSide / 8) * 8;
+        const int64_t row = r0 + r, left = row < rows ? cols - (c0 + c) : 0;
+        const T* p = x + row * ldx + c0 + c;
+        float v[8];
+        if (left >= 8)
+            load8<E>(p, v);
+        else
+            load_few<E>(p, left, v);
+        if (along) {
+            const uint32_t byte = exponent_byte(largest_of_quad(largest8(v)));
+            const uint32_t code = encode8(v, byte);
+            if (row < rows) {
+                *(uint32_t*)(codes + row * pitch + (c0 + c) / 2) = code;
+                if ((threadIdx.x & 3) == 0) scales[row * (pitch / 16) + (c0 + c) / kMxBlock] = (uint8_t)byte;
+            }
+        }
+        if (Across) store8<E>(&tile[r * kSide + (c ^ (r / 32 * 16))], v);
+    }
+    if (!Across) return;
+    __syncthreads();
+    const int c = threadIdx.x / 4, b = threadIdx.x % 4;
+    float v[32];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        v[i] = E::widen(tile[(b * 32 + i) * kSide + (c ^ (b * 16))]);
+        top = larger(top, magnitude(v[i]));
+    }
+    if (!across || c0 + c >= cols) return;
+    const uint32_t byte = exponent_byte(top);
+    const u4 code = {encode8(v, byte), encode8(v + 8, byte), encode8(v + 16, byte), encode8(v + 24, byte)};
+    *(u4*)(codes_t + (c0 + c) * pitch_t + r0 / 2 + b * 16) = code;
+    scales_t[(c0 + c) * (pitch_t / 16) + r0 / kMxBlock + b] = (uint8_t)byte;
+}
+
+template <class E>
+__global__ __launch_bounds__(kFlat) void k_mx4_dequantize(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                          int64_t rows, int64_t cols, typename E::T* __restrict__ out, int64_t ldo)
+{
+    const int64_t pitch = mx4_padded(cols) / 2;
+    const int64_t j = ((int64_t)blockIdx.x * kFlat + threadIdx.x) * 8, left = cols - j;
+    if (left <= 0) return;
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+        const uint32_t byte = scales[row * (pitch / 16) + j / kMxBlock];
+        float v[8];
+        decode8(*(const uint32_t*)(codes + row * pitch + j / 2), scale_of(byte), v);
+        if (byte == 255) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = scale_of(255);
+        }
+        if (left >= 8)
+            store8<E>(out + row * ldo + j, v);
+        else
+            store_few<E>(out + row * ldo + j, left, v);
+    }
+}
+
+// ---- products ----
+
+template <class E>
+__device__ __forceinline__ void store_product(const Mx4Product& p, int64_t m, int64_t n, const v4f& acc)
+{
+    typedef typename E::T T;
+    if (m >= p.m || n >= p.n) return;
+    T* c = (T*)p.c + m * p.ldc + n;
+    typedef T t4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    if (n + 4 <= p.n) {
+        t4 v;
+        if (p.accumulate) {
+            const t4 old = *(const t4*)c;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = E::narrow(fmaf(p.alpha, acc[i], E::widen(old[i])));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = E::narrow(p.alpha * acc[i]);
+        }
+        *(t4*)c = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < p.n) c[i] = E::narrow(p.accumulate ? fmaf(p.alpha, acc[i], E::widen(c[i])) : p.alpha * acc[i]);
+    }
+}
+
+template <class E, class Tl>
+__global__ __launch_bounds__(Tl::kThreads) void k_mx4_product(Mx4Product p, uint32_t tm, uint32_t tn, int bm, int bn)
+{
+    __shared__ __align__(1024) char lds[Tl::kLds];
+    uint32_t i, j;
+    tile_of(xcd_run(blockIdx.x, tm * tn), tm, tn, i, j);
+    const uint32_t pitch = (uint32_t)(mx4_padded(p.k) / 2);
+    const Rows a = {p.a, p.a_scales, (uint32_t)p.m, pitch}, b = {p.b, p.b_scales, (uint32_t)p.n, pitch};
+    Tl t;
+    t.clear();
+    t.run(a, b, i * bm, j * bn, pitch / kLine, lds);
+    t.each([&](uint32_t m, uint32_t n, const v4f& acc) { store_product<E>(p, (int64_t)i * bm + m, (int64_t)j * bn + n, acc); });
+}
+
+// Few rows of A: the time is that of reading B once.  A block has 16 rows of B; its 8 waves take lines in turn, straight to
+// registers, and add up in LDS.
+constexpr int kFewWaves = 8;
+template <class E, int Mt>
+__global__ __launch_bounds__(64 * kFewWaves) void k_mx4_few(Mx4Product p)
+{
+    __shared__ v4f part[kFewWaves][Mt][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int64_t pitch = mx4_padded(p.k) / 2;
+    const int64_t nb = n0 + r < p.n ? n0 + r : p.n - 1;
+    const uint8_t *b = p.b + nb * pitch + q * 16, *bs = p.b_scales + nb * (pitch / 16) + q;
+    const uint8_t *a[Mt], *as[Mt];
+    v4f acc[Mt];
+#pragma unroll
+    for (int i = 0; i < Mt; ++i) {
+        const int64_t m = i * 16 + r < p.m ? i * 16 + r : p.m - 1;
+        a[i] = p.a + m * pitch + q * 16;
+        as[i] = p.a_scales + m * (pitch / 16) + q;
+        acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+#pragma unroll 2
+    for (int64_t k = (int64_t)wave * kLine; k < pitch; k += kFewWaves * kLine) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const v4i fb = *(const v4i*)(b + k + h * 64);
+            const int sb = bs[k / 16 + h * 4];
+#pragma unroll
+            for (int i = 0; i < Mt; ++i)
+                acc[i] = Mx4Core::mul(fb, *(const v4i*)(a[i] + k + h * 64), acc[i], sb, as[i][k / 16 + h * 4]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < Mt; ++i) part[wave][i][lane] = acc[i];
+    __syncthreads();
+    for (int i = wave; i < Mt; i += kFewWaves) {
+        v4f sum = part[0][i][lane];
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) sum += part[w][i][lane];
+        store_product<E>(p, i * 16 + r, n0 + 4 * q, sum);
+    }
+}
+
+template <class Tl>
+struct Shape {
+    typedef Tl Is;
+};
+
+template <class F>
+void by_type(int type, const F& f)
+{
+    if (type == kGradF32)
+        f(F32());
+    else if (type == kGradF16)
+        f(F16());
+    else
+        f(Bf16());
+}
+
+uint32_t flat_blocks(int64_t groups)
+{
+    const int64_t b = (groups + kFlat - 1) / kFlat;
+    return (uint32_t)(b < 8192 ? b : 8192);
+}
+
+}  // namespace
+
+void launch_mx4_compress(const void* grad, int type, float* residual, int64_t d, uint8_t* codes, uint8_t* scales, hipStream_t s)
+{
+    const int64_t groups = mx4_padded(d) / 8;
+    by_type(type, [&](auto e) {
+        typedef decltype(e) E;
+        if (residual)
+            k_mx4_compress<E, true><<<flat_blocks(groups), kFlat, 0, s>>>((const typename E::T*)grad, residual, d, (uint32_t*)codes,
+                                                                          scales, groups);
+        else
+            k_mx4_compress<E, false><<<flat_blocks(groups), kFlat, 0, s>>>((const typename E::T*)grad, residual, d, (uint32_t*)codes,
+                                                                           scales, groups);
+    });
+}
+
+void launch_mx4_aggregate(const uint8_t* codes, int64_t code_stride, const uint8_t* scales, int64_t scale_stride, int workers,
+                          int64_t d, float scale, bool accumulate, float* dense, hipStream_t s)
+{
+    const int64_t groups = (d + 7) / 8;
+    if (accumulate)
+        k_mx4_aggregate<true><<<flat_blocks(groups), kFlat, 0, s>>>(codes, code_stride, scales, scale_stride, workers, d, scale, dense,
+                                                                    groups);
+    else
+        k_mx4_aggregate<false><<<flat_blocks(groups), kFlat, 0, s>>>(codes, code_stride, scales, scale_stride, workers, d, scale,
+                                                                     dense, groups);
+}
+
+void launch_mx4_quantize(const void* x, int type, int64_t rows, int64_t cols, int64_t ldx, uint8_t* codes, uint8_t* scales,
+                         uint8_t* codes_t, uint8_t* scales_t, hipStream_t s)
+{
+    const uint32_t gx = (uint32_t)((codes ? mx4_padded(cols) : cols + kSide - 1) / kSide);
+    const uint32_t grid = gx * (uint32_t)((codes_t ? mx4_padded(rows) : rows + kSide - 1) / kSide);
+    by_type(type, [&](auto e) {
+        typedef decltype(e) E;
+        const typename E::T* p = (const typename E::T*)x;
+        if (codes && codes_t)
+            k_mx4_quantize<E, true, true><<<grid, kQuant, 0, s>>>(p, rows, cols, ldx, codes, scales, codes_t, scales_t, gx);
+        else if (codes)
+            k_mx4_quantize<E, true, false><<<grid, kQuant, 0, s>>>(p, rows, cols, ldx, codes, scales, codes_t, scales_t, gx);
+        else
+            k_mx4_quantize<E, false, true><<<grid, kQuant, 0, s>>>(p, rows, cols, ldx, codes, scales, codes_t, scales_t, gx);
+    });
+}
+
+void launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* out, int type, int64_t ldo,
+                           hipStream_t s)
+{
+    const dim3 grid((uint32_t)((cols + 8 * kFlat - 1) / (8 * kFlat)), (uint32_t)(rows < 32768 ? rows : 32768));
+    by_type(type, [&](auto e) {
+        typedef decltype(e) E;
+        k_mx4_dequantize<E><<<grid, kFlat, 0, s>>>(codes, scales, rows, cols, (typename E::T*)out, ldo);
+    });
+}
+
+void launch_mx4_product(const Mx4Product& p, hipStream_t s)
+{
+    auto go = [&](auto e, auto t, int bm, int bn) {
+        typedef decltype(e) E;
+        typedef typename decltype(t)::Is Tl;
+        const uint32_t tm = (uint32_t)((p.m + bm - 1) / bm), tn = (uint32_t)((p.n + bn - 1) / bn);
+        k_mx4_product<E, Tl><<<tm * tn, Tl::kThreads, 0, s>>>(p, tm, tn, bm, bn);
+    };
+    auto tiles = [&](int64_t b) { return ((p.m + b - 1) / b) * ((p.n + b - 1) / b); };
+    by_type(p.type, [&](auto e) {
+        if (tiles(256) >= 256)
+            go(e, Shape<Tile<Mx4Core, 256, 256, 2, 4, 2>>(), 256, 256);
+        else if (tiles(128) >= 200)
+            go(e, Shape<Tile<Mx4Core, 128, 128, 2, 2, 3>>(), 128, 128);
+        else
+            go(e, Shape<Tile<Mx4Core, 64, 64, 2, 2, 4>>(), 64, 64);
+    });
+}
+
+void launch_mx4_few(const Mx4Product& p, hipStream_t s)
+{
+    const uint32_t grid = (uint32_t)((p.n + 15) / 16);
+    by_type(p.type, [&](auto e) {
+        typedef decltype(e) E;
+        if (p.m <= 16)
+            k_mx4_few<E, 1><<<grid, 64 * kFewWaves, 0, s>>>(p);
+        else if (p.m <= 32)
+            k_mx4_few<E, 2><<<grid, 64 * kFewWaves, 0, s>>>(p);
+        else
+            k_mx4_few<E, 4><<<grid, 64 * kFewWaves, 0, s>>>(p);
+    });
+}
+
+}  // namespace sidco
