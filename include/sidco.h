@@ -555,6 +555,65 @@ int sidco_mx4_linear(void *stream, const void *x, int x_dtype, int64_t rows, int
                      const uint8_t *w_scales, int64_t n, float alpha, int accumulate, void *c, int c_dtype, int64_t ldc);
 size_t sidco_workspace_bytes_mx4_linear(int64_t rows, int64_t k);
 
+/* ---- the orthogonalised update --------------------------------------------------
+ *
+ * A matrix u is scaled to X = u / (|u|_F + eps) and moved `steps` times by X <- aX +
+ * (bG + cG^2) X with G = X X^T (X^T X for a tall matrix: the result is the same),
+ * which takes every singular value s to as + bs^3 + cs^5.  The default values
+ * bring them near 1 in 5 steps.  The coefficients have to keep singular values
+ * below 4 on the way; a matrix of zeros stays one, and a NaN or an infinity in u
+ * makes its matrix NaN.
+ *
+ * precision: SIDCO_NS_HALF multiplies operands of 11 bits (for matrices of random
+ * numbers the result is within about 2e-3 of the exact one, in the 2-norm),
+ * SIDCO_NS_FULL of 22 bits (1e-6, at about three times the time); sums are fp32
+ * either way.  Directions that u lacks altogether hold what the roundings left
+ * there, a^steps times: for a matrix of rank one up to 0.1 of the result with
+ * HALF, 1e-4 with FULL.  SIDCO_NS_BY_TYPE takes FULL where the result is fp32 and
+ * HALF where it has 16 bits.
+ * Results are deterministic.  Matrices of a batch have the same shape, and rows,
+ * cols <= 2^21, batch <= 65535.                                               */
+#define SIDCO_NS_BY_TYPE 0
+#define SIDCO_NS_HALF    1
+#define SIDCO_NS_FULL    2
+
+typedef struct sidco_newton_schulz {
+    int   steps;     /* 1 .. 100                  */
+    float a, b, c;   /* of aX + bGX + cG^2X       */
+    float eps;       /* >= 0                      */
+    int   precision; /* SIDCO_NS_*                */
+} sidco_newton_schulz;
+
+/* 5 steps of 3.4445, -4.7750, 2.0315 with eps 1e-7 and SIDCO_NS_BY_TYPE.       */
+void sidco_newton_schulz_default(sidco_newton_schulz *opt);
+
+/* Host helper: bytes of workspace that a call for `batch` matrices needs whose
+ * result has `out_dtype`; opt may be NULL (the default values).  0 for invalid
+ * arguments.                                                                  */
+size_t sidco_workspace_bytes_orthogonalize(int batch, int64_t rows, int64_t cols, int out_dtype, const sidco_newton_schulz *opt);
+
+/*
+ * out = the orthogonalised x, for `batch` matrices of rows x cols: row strides ldx,
+ * ldo >= cols and strides from matrix to matrix x_stride, out_stride >= rows * the
+ * row stride, all in elements.  out may be x with the same type and strides (any
+ * other overlap is not allowed).  opt may be NULL.
+ */
+int sidco_orthogonalize(void *stream, const void *x, int x_dtype, int64_t ldx, int64_t x_stride, int batch, int64_t rows,
+                        int64_t cols, const sidco_newton_schulz *opt, void *out, int out_dtype, int64_t ldo, int64_t out_stride);
+
+/*
+ * One optimiser step of `batch` contiguous rows x cols weights, one after the
+ * other, as their gradients and momenta are:
+ *   momentum = mu momentum + grad                       (fp32)
+ *   u        = grad + mu momentum (nesterov = 1), momentum (nesterov = 0)
+ *   weight   = (1 - lr weight_decay) weight - lr scale orthogonalised(u)
+ * in fp32, the weight rounded once to its type.  With SIDCO_NS_BY_TYPE the weight's
+ * type decides the precision.  opt may be NULL.  None of the three may overlap.
+ */
+int sidco_muon_step(void *stream, const void *grad, int grad_dtype, float *momentum, void *weight, int weight_dtype, int batch,
+                    int64_t rows, int64_t cols, float lr, float mu, int nesterov, float weight_decay, float scale,
+                    const sidco_newton_schulz *opt);
+
 /* Text for an error code; the HIP error string of the last SIDCO_ERR_HIP.     */
 const char *sidco_strerror(int code);
 const char *sidco_last_hip_error(void);

@@ -30,6 +30,7 @@ EXPORTS = [
     "sidco_get_profile", "sidco_strerror", "sidco_last_hip_error", "sidco_version", "sidco_shutdown",
     "sidco_mx4_code_bytes", "sidco_mx4_scale_bytes", "sidco_mx4_compress", "sidco_mx4_aggregate", "sidco_mx4_quantize",
     "sidco_mx4_dequantize", "sidco_mx4_matmul", "sidco_mx4_linear", "sidco_workspace_bytes_mx4_linear",
+    "sidco_newton_schulz_default", "sidco_workspace_bytes_orthogonalize", "sidco_orthogonalize", "sidco_muon_step",
 ]
 
 
@@ -44,6 +45,18 @@ class Diag(C.Structure):
         ("stages", C.c_int32),
         ("status", C.c_uint32),
         ("reserved", C.c_uint32),
+    ]
+
+
+class NewtonSchulz(C.Structure):
+    """Mirror of struct sidco_newton_schulz."""
+    _fields_ = [
+        ("steps", C.c_int),
+        ("a", C.c_float),
+        ("b", C.c_float),
+        ("c", C.c_float),
+        ("eps", C.c_float),
+        ("precision", C.c_int),
     ]
 
 
@@ -197,6 +210,16 @@ def load() -> C.CDLL:
     lib.sidco_mx4_linear.restype = C.c_int
     lib.sidco_workspace_bytes_mx4_linear.argtypes = [i64, i64]
     lib.sidco_workspace_bytes_mx4_linear.restype = C.c_size_t
+    nsp = C.POINTER(NewtonSchulz)
+    lib.sidco_newton_schulz_default.argtypes = [nsp]
+    lib.sidco_newton_schulz_default.restype = None
+    lib.sidco_workspace_bytes_orthogonalize.argtypes = [C.c_int, i64, i64, C.c_int, nsp]
+    lib.sidco_workspace_bytes_orthogonalize.restype = C.c_size_t
+    lib.sidco_orthogonalize.argtypes = [vp, vp, C.c_int, i64, i64, C.c_int, i64, i64, nsp, vp, C.c_int, i64, i64]
+    lib.sidco_orthogonalize.restype = C.c_int
+    lib.sidco_muon_step.argtypes = [vp, vp, C.c_int, f32p, vp, C.c_int, C.c_int, i64, i64, C.c_float, C.c_float, C.c_int, C.c_float,
+                                    C.c_float, nsp]
+    lib.sidco_muon_step.restype = C.c_int
     lib.sidco_strerror.argtypes = [C.c_int]
     lib.sidco_strerror.restype = C.c_char_p
     lib.sidco_last_hip_error.argtypes = []
@@ -796,6 +819,68 @@ def sidco_mx4_linear(x, w_codes, w_scales, out, alpha: float = 1.0, accumulate: 
     _check_packed(w_codes, w_scales, n, k, "the weight's")
     _check(load().sidco_mx4_linear(_stream_handle(stream), _ptr(x), x_code, rows, k, ldx, _ptr(w_codes), _ptr(w_scales), n, alpha,
                                    int(accumulate), _ptr(out), code, ld), "sidco_mx4_linear")
+
+
+# ---- the orthogonalised update ----
+
+NS_BY_TYPE, NS_HALF, NS_FULL = 0, 1, 2
+
+
+def sidco_newton_schulz_default() -> NewtonSchulz:
+    opt = NewtonSchulz()
+    load().sidco_newton_schulz_default(C.byref(opt))
+    return opt
+
+
+def _newton_schulz(steps, coef, eps, precision):
+    a, b, c = coef
+    return NewtonSchulz(steps, a, b, c, eps, precision)
+
+
+def sidco_workspace_bytes_orthogonalize(batch: int, rows: int, cols: int, out_dtype: int, precision: int = NS_BY_TYPE) -> int:
+    opt = sidco_newton_schulz_default()
+    opt.precision = precision
+    return int(load().sidco_workspace_bytes_orthogonalize(batch, rows, cols, out_dtype, C.byref(opt)))
+
+
+def _batch(x, name):
+    """(element code, row stride, matrix stride, batch, rows, cols) of a matrix or a batch of them."""
+    if x.dim() == 2:
+        x = x[None]
+    code, ld = _matrix(x, name, 3)
+    batch, rows, cols = x.shape
+    stride = x.stride(0) if batch > 1 else rows * ld
+    return code, ld, stride, batch, rows, cols
+
+
+def sidco_orthogonalize(x, out, steps: int = 5, coef=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, precision: int = NS_BY_TYPE,
+                        stream=None) -> None:
+    """out = the matrix x, or each of a batch, near the closest one with orthonormal rows or columns."""
+    code, ld, stride, batch, rows, cols = _batch(x, "x")
+    out_code, ldo, out_stride, *shape = _batch(out, "out")
+    if shape != [batch, rows, cols]:
+        raise ValueError("out must have x's shape")
+    opt = _newton_schulz(steps, coef, eps, precision)
+    _check(load().sidco_orthogonalize(_stream_handle(stream), _ptr(x), code, ld, stride, batch, rows, cols, C.byref(opt), _ptr(out),
+                                      out_code, ldo, out_stride), "sidco_orthogonalize")
+
+
+def sidco_muon_step(grad, momentum, weight, lr: float, mu: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
+                    scale: float = 1.0, steps: int = 5, coef=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
+                    precision: int = NS_BY_TYPE, stream=None) -> None:
+    """Momentum (float32), its orthogonalisation and the weights' update, in place, for a matrix or a batch of them; all
+    three contiguous."""
+    torch = _torch or _import_torch()
+    code, _, _, batch, rows, cols = _batch(grad, "grad")
+    w_code, *_ = _batch(weight, "weight")
+    if weight.shape != grad.shape or momentum.shape != grad.shape:
+        raise ValueError("grad, momentum and weight must have the same shape")
+    _check_tensor(grad, grad.dtype, "grad")
+    _check_tensor(momentum, torch.float32, "momentum")
+    _check_tensor(weight, weight.dtype, "weight")
+    opt = _newton_schulz(steps, coef, eps, precision)
+    _check(load().sidco_muon_step(_stream_handle(stream), _ptr(grad), code, _ptr(momentum), _ptr(weight), w_code, batch, rows, cols, lr,
+                                  mu, int(nesterov), weight_decay, scale, C.byref(opt)), "sidco_muon_step")
 
 
 def sidco_version() -> int:

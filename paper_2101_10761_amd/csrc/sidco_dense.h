@@ -37,5 +37,27 @@ void launch_mx4_product(const Mx4Product& p, hipStream_t s);
 constexpr int kFewRows = 64;  // rows of A up to which launch_mx4_few serves
 void launch_mx4_few(const Mx4Product& p, hipStream_t s);
 
+// A batch of matrices orthogonalised, out of x or of the momentum that x moves, into out or into the weights there
+struct OrthoCall {
+    const void* x;
+    int x_type;
+    int64_t ldx, x_stride;
+    float* momentum;  // NULL: x itself
+    float mu;
+    bool nesterov;
+    int batch;
+    int64_t rows, cols;
+    int steps;
+    float a, b, c, eps;
+    bool full;        // operands of 22 bits instead of 11
+    void* out;
+    int out_type;
+    int64_t ldo, out_stride;
+    bool update;      // out = keep * out + gain * result
+    float keep, gain;
+};
+size_t ortho_scratch(int batch, int64_t rows, int64_t cols, bool full);
+void launch_orthogonalize(const OrthoCall& q, char* scratch, hipStream_t s);
+
 }  // namespace sidco
 #endif

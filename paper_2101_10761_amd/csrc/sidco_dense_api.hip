@@ -33,6 +33,44 @@ int check_result(const void* c, int c_dtype, int64_t n, int64_t ldc, float alpha
     return aligned_type(c, c_dtype) ? SIDCO_OK : SIDCO_ERR_ALIGN;
 }
 
+constexpr int64_t kMaxSide = 1 << 21;  // of a matrix that is orthogonalised
+constexpr sidco_newton_schulz kNewtonSchulz = {5, 3.4445f, -4.7750f, 2.0315f, 1e-7f, SIDCO_NS_BY_TYPE};
+
+int check_newton_schulz(const sidco_newton_schulz& o)
+{
+    if (o.steps < 1 || o.steps > 100) return SIDCO_ERR_STAGES;
+    if (!isfinite(o.a) || !isfinite(o.b) || !isfinite(o.c) || !(o.eps >= 0.0f) || !isfinite(o.eps)) return SIDCO_ERR_ARG;
+    if (o.precision != SIDCO_NS_BY_TYPE && o.precision != SIDCO_NS_HALF && o.precision != SIDCO_NS_FULL) return SIDCO_ERR_ARG;
+    return SIDCO_OK;
+}
+
+int check_batch(int batch, int64_t rows, int64_t cols)
+{
+    if (batch < 1 || batch > 65535 || rows < 1 || rows > kMaxSide || cols < 1 || cols > kMaxSide) return SIDCO_ERR_SIZE;
+    // a tile's place in the batch has 31 bits
+    const int64_t tiles = ((rows + 63) / 64) * ((cols + 63) / 64);
+    return tiles <= (int64_t)INT32_MAX / batch ? SIDCO_OK : SIDCO_ERR_SIZE;
+}
+
+bool full_precision(const sidco_newton_schulz& o, int out_dtype)
+{
+    return o.precision == SIDCO_NS_FULL || (o.precision == SIDCO_NS_BY_TYPE && out_dtype == SIDCO_GRAD_F32);
+}
+
+int orthogonalize(void* stream, OrthoCall& q, const sidco_newton_schulz& o, int out_dtype)
+{
+    q.steps = o.steps;
+    q.a = o.a;
+    q.b = o.b;
+    q.c = o.c;
+    q.eps = o.eps;
+    q.full = full_precision(o, out_dtype);
+    StreamScratch ws(stream, ortho_scratch(q.batch, q.rows, q.cols, q.full));
+    if (ws.rc != SIDCO_OK) return ws.rc;
+    launch_orthogonalize(q, ws.data, (hipStream_t)stream);
+    return launched();
+}
+
 }  // namespace
 
 extern "C" {
@@ -147,6 +185,78 @@ int sidco_mx4_linear(void* stream, const void* x, int x_dtype, int64_t rows, int
     else
         launch_mx4_product(p, (hipStream_t)stream);
     return launched();
+}
+
+void sidco_newton_schulz_default(sidco_newton_schulz* opt)
+{
+    if (opt) *opt = kNewtonSchulz;
+}
+
+size_t sidco_workspace_bytes_orthogonalize(int batch, int64_t rows, int64_t cols, int out_dtype, const sidco_newton_schulz* opt)
+{
+    const sidco_newton_schulz o = opt ? *opt : kNewtonSchulz;
+    if (check_batch(batch, rows, cols) != SIDCO_OK || !element_type(out_dtype) || check_newton_schulz(o) != SIDCO_OK) return 0;
+    return workspace_with_scratch(ortho_scratch(batch, rows, cols, full_precision(o, out_dtype)));
+}
+
+int sidco_orthogonalize(void* stream, const void* x, int x_dtype, int64_t ldx, int64_t x_stride, int batch, int64_t rows, int64_t cols,
+                        const sidco_newton_schulz* opt, void* out, int out_dtype, int64_t ldo, int64_t out_stride)
+{
+    if (!x || !out) return SIDCO_ERR_NULL;
+    if (!element_type(x_dtype) || !element_type(out_dtype)) return SIDCO_ERR_ARG;
+    if (int rc = check_batch(batch, rows, cols)) return rc;
+    if (ldx < cols || ldo < cols || ldx > kMaxRows || ldo > kMaxRows) return SIDCO_ERR_SIZE;
+    if (batch > 1 && (x_stride < rows * ldx || out_stride < rows * ldo)) return SIDCO_ERR_SIZE;
+    if (!aligned_type(x, x_dtype) || !aligned_type(out, out_dtype)) return SIDCO_ERR_ALIGN;
+    const sidco_newton_schulz o = opt ? *opt : kNewtonSchulz;
+    if (int rc = check_newton_schulz(o)) return rc;
+    OrthoCall q = {};
+    q.x = x;
+    q.x_type = type_of(x_dtype);
+    q.ldx = ldx;
+    q.x_stride = x_stride;
+    q.batch = batch;
+    q.rows = rows;
+    q.cols = cols;
+    q.out = out;
+    q.out_type = type_of(out_dtype);
+    q.ldo = ldo;
+    q.out_stride = out_stride;
+    return orthogonalize(stream, q, o, out_dtype);
+}
+
+int sidco_muon_step(void* stream, const void* grad, int grad_dtype, float* momentum, void* weight, int weight_dtype, int batch,
+                    int64_t rows, int64_t cols, float lr, float mu, int nesterov, float weight_decay, float scale,
+                    const sidco_newton_schulz* opt)
+{
+    if (!grad || !momentum || !weight) return SIDCO_ERR_NULL;
+    if (!element_type(grad_dtype) || !element_type(weight_dtype)) return SIDCO_ERR_ARG;
+    if (int rc = check_batch(batch, rows, cols)) return rc;
+    if (!isfinite(lr) || !isfinite(mu) || !isfinite(weight_decay) || !isfinite(scale) || (nesterov != 0 && nesterov != 1))
+        return SIDCO_ERR_ARG;
+    if (!aligned_type(grad, grad_dtype) || !aligned(momentum, 4) || !aligned_type(weight, weight_dtype)) return SIDCO_ERR_ALIGN;
+    if (grad == (const void*)momentum || grad == weight || (void*)momentum == weight) return SIDCO_ERR_ARG;
+    const sidco_newton_schulz o = opt ? *opt : kNewtonSchulz;
+    if (int rc = check_newton_schulz(o)) return rc;
+    OrthoCall q = {};
+    q.x = grad;
+    q.x_type = type_of(grad_dtype);
+    q.ldx = cols;
+    q.x_stride = rows * cols;
+    q.momentum = momentum;
+    q.mu = mu;
+    q.nesterov = nesterov != 0;
+    q.batch = batch;
+    q.rows = rows;
+    q.cols = cols;
+    q.out = weight;
+    q.out_type = type_of(weight_dtype);
+    q.ldo = cols;
+    q.out_stride = rows * cols;
+    q.update = true;
+    q.keep = 1.0f - lr * weight_decay;
+    q.gain = -lr * scale;
+    return orthogonalize(stream, q, o, weight_dtype);
 }
 
 }  // extern "C"
