@@ -310,7 +310,7 @@ __device__ __forceinline__ void store_product(const Mx4Product& p, int64_t m, in
 }
 
 template <class E, class Tl>
-__global__ __launch_bounds__(Tl::kThreads) void k_mx4_product(Mx4Product p, uint32_t tm, uint32_t tn, int bm, int bn)
+__global__ __launch_bounds__(Tl::kThreads) void k_mx4_product(Mx4Product p, uint32_t tm, uint32_t tn)
 {
     __shared__ __align__(1024) char lds[Tl::kLds];
     uint32_t i, j;
@@ -319,8 +319,14 @@ __global__ __launch_bounds__(Tl::kThreads) void k_mx4_product(Mx4Product p, uint
     const Rows a = {p.a, p.a_scales, (uint32_t)p.m, pitch}, b = {p.b, p.b_scales, (uint32_t)p.n, pitch};
     Tl t;
     t.clear();
-    t.run(a, b, i * bm, j * bn, pitch / kLine, lds);
-    t.each([&](uint32_t m, uint32_t n, const v4f& acc) { store_product<E>(p, (int64_t)i * bm + m, (int64_t)j * bn + n, acc); });
+    t.run(a, b, i * Tl::kM, j * Tl::kN, lds);
+    t.each([&](uint32_t m, uint32_t n, const v4f& acc) { store_product<E>(p, (int64_t)i * Tl::kM + m, (int64_t)j * Tl::kN + n, acc); });
+}
+
+__device__ __forceinline__ v4f multiply16(const v4i& a, const v4i& b, const v4f& c, int sa, int sb)
+{
+    const v8i wa = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wb = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, c, 4, 4, 0, sa, 0, sb);  // 4: e2m1
 }
 
 // Few rows of A: the time is that of reading B once.  A block has 16 rows of B; its 8 waves take lines in turn, straight to
@@ -344,7 +350,6 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_mx4_few(Mx4Product p)
         as[i] = p.a_scales + m * (pitch / 16) + q;
         acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
-#pragma unroll 2
     for (int64_t k = (int64_t)wave * kLine; k < pitch; k += kFewWaves * kLine) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -352,7 +357,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_mx4_few(Mx4Product p)
             const int sb = bs[k / 16 + h * 4];
 #pragma unroll
             for (int i = 0; i < Mt; ++i)
-                acc[i] = Mx4Core::mul(fb, *(const v4i*)(a[i] + k + h * 64), acc[i], sb, as[i][k / 16 + h * 4]);
+                acc[i] = multiply16(fb, *(const v4i*)(a[i] + k + h * 64), acc[i], sb, as[i][k / 16 + h * 4]);
         }
     }
 #pragma unroll
@@ -445,20 +450,20 @@ void launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t 
 
 void launch_mx4_product(const Mx4Product& p, hipStream_t s)
 {
-    auto go = [&](auto e, auto t, int bm, int bn) {
+    auto go = [&](auto e, auto t) {
         typedef decltype(e) E;
         typedef typename decltype(t)::Is Tl;
-        const uint32_t tm = (uint32_t)((p.m + bm - 1) / bm), tn = (uint32_t)((p.n + bn - 1) / bn);
-        k_mx4_product<E, Tl><<<tm * tn, Tl::kThreads, 0, s>>>(p, tm, tn, bm, bn);
+        const uint32_t tm = (uint32_t)((p.m + Tl::kM - 1) / Tl::kM), tn = (uint32_t)((p.n + Tl::kN - 1) / Tl::kN);
+        k_mx4_product<E, Tl><<<tm * tn, Tl::kThreads, 0, s>>>(p, tm, tn);
     };
     auto tiles = [&](int64_t b) { return ((p.m + b - 1) / b) * ((p.n + b - 1) / b); };
     by_type(p.type, [&](auto e) {
         if (tiles(256) >= 256)
-            go(e, Shape<Tile<Mx4Core, 256, 256, 2, 4, 2>>(), 256, 256);
+            go(e, Shape<Tile<Mx4Core, 256, 256, 2, 2, 2, 2>>());
         else if (tiles(128) >= 200)
-            go(e, Shape<Tile<Mx4Core, 128, 128, 2, 2, 3>>(), 128, 128);
+            go(e, Shape<Tile<Mx4Core, 128, 128, 2, 2, 2, 2>>());
         else
-            go(e, Shape<Tile<Mx4Core, 64, 64, 2, 2, 4>>(), 64, 64);
+            go(e, Shape<Tile<Mx4Core, 64, 64, 2, 2, 2, 4>>());
     });
 }
 

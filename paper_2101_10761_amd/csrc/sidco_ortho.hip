@@ -198,13 +198,12 @@ template <class Tl, bool Full>
 __device__ __forceinline__ void products(Tl& t, const Plane& a, const Plane& b, int64_t z, uint32_t ra, uint32_t rb, uint32_t m0, uint32_t n0,
                                          char* lds)
 {
-    const uint32_t steps = (uint32_t)a.pitch * 2 / kLine;
     t.clear();
     if (Full) {  // the small ones first
-        t.run(rows_of(a, z, ra, true), rows_of(b, z, rb), m0, n0, steps, lds);
-        t.run(rows_of(a, z, ra), rows_of(b, z, rb, true), m0, n0, steps, lds);
+        t.run(rows_of(a, z, ra, true), rows_of(b, z, rb), m0, n0, lds);
+        t.run(rows_of(a, z, ra), rows_of(b, z, rb, true), m0, n0, lds);
     }
-    t.run(rows_of(a, z, ra), rows_of(b, z, rb), m0, n0, steps, lds);
+    t.run(rows_of(a, z, ra), rows_of(b, z, rb), m0, n0, lds);
 }
 
 struct Poly {
@@ -251,7 +250,6 @@ __global__ __launch_bounds__(Tl::kThreads) void k_symmetric(Plane x, Plane out, 
 // What the last product goes to: the result, or weights that move by it.
 struct Result {
     void* out;
-    int type;
     bool tall;          // it is X transposed
     bool update;
     float keep, gain;   // out = keep * out + gain * X
@@ -282,8 +280,8 @@ __device__ __forceinline__ void finish4(const Result& o, int64_t z, int64_t r, i
     }
 }
 
-// X' = P X: X' and its transpose, or with Last the result.
-template <class Tl, int BM, int BN, bool Full, bool Last>
+// X' = P X: X' and its transpose, or with Last the result, of element type T.
+template <class Tl, int B, bool Full, bool Last, class T>
 __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plane x2, Plane xt2, uint32_t m, uint32_t n, uint32_t tm, uint32_t tn,
                                                         float back, Result o)
 {
@@ -293,29 +291,20 @@ __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plan
     uint32_t i, j;
     tile_of(w % (tm * tn), tm, tn, i, j);
     Tl t;
-    products<Tl, Full>(t, pm, xt, z, m, n, i * BM, j * BN, lds);
-    t.each([&](uint32_t r, uint32_t c, v4f v) {
-        r += i * BM, c += j * BN;
-        v *= back;
-        if (Last) {
-            int64_t row = r, col = c;
-            if (o.tall) {
-                v = turn(v);
-                row = c + (threadIdx.x & 3);
-                col = r & ~3u;
-            }
-            if (o.type == kGradF32)
-                finish4<float>(o, z, row, col, v);
-            else if (o.type == kGradF16)
-                finish4<_Float16>(o, z, row, col, v);
-            else
-                finish4<__bf16>(o, z, row, col, v);
-        } else {
+    products<Tl, Full>(t, pm, xt, z, m, n, i * B, j * B, lds);
+    if (!Last) {
+        t.each([&](uint32_t r, uint32_t c, v4f v) {
+            r += i * B, c += j * B;
+            v *= back;
             put4<Full>(x2, z, m, n, r, c, v);
             v = turn(v);
             put4<Full>(xt2, z, n, m, c + (threadIdx.x & 3), r & ~3u, v);
-        }
-    });
+        });
+    } else if (o.tall) {
+        t.each([&](uint32_t r, uint32_t c, v4f v) { finish4<T>(o, z, j * B + c + (threadIdx.x & 3), (i * B + r) & ~3u, turn(v * back)); });
+    } else {
+        t.each([&](uint32_t r, uint32_t c, v4f v) { finish4<T>(o, z, i * B + r, j * B + c, v * back); });
+    }
 }
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -396,19 +385,27 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
         k_symmetric<Sym, kS, Full, true><<<tri * batch, Sym::kThreads, 0, s>>>(g, pm, (uint32_t)m, tri, poly);
         const uint32_t tm = (uint32_t)((m + kA - 1) / kA), tn = (uint32_t)((n + kA - 1) / kA);
         if (last) {
-            const Result o = {q.out, q.out_type, tall, q.update, q.keep, q.gain, q.ldo, q.out_stride, q.rows, q.cols};
-            k_apply<App, kA, kA, Full, true>
-                <<<tm * tn * batch, App::kThreads, 0, s>>>(pm, xt0, x1, xt1, (uint32_t)m, (uint32_t)n, tm, tn, 1.0f / (kScaleX * poly.scale), o);
+            const Result o = {q.out, tall, q.update, q.keep, q.gain, q.ldo, q.out_stride, q.rows, q.cols};
+            auto finish = [&](auto type) {
+                k_apply<App, kA, Full, true, typename decltype(type)::T>
+                    <<<tm * tn * batch, App::kThreads, 0, s>>>(pm, xt0, x1, xt1, (uint32_t)m, (uint32_t)n, tm, tn, 1.0f / (kScaleX * poly.scale), o);
+            };
+            if (q.out_type == kGradF32)
+                finish(Elem<kGradF32>());
+            else if (q.out_type == kGradF16)
+                finish(Elem<kGradF16>());
+            else
+                finish(Elem<kGradBf16>());
         } else {
-            k_apply<App, kA, kA, Full, false>
+            k_apply<App, kA, Full, false, float>
                 <<<tm * tn * batch, App::kThreads, 0, s>>>(pm, xt0, x1, xt1, (uint32_t)m, (uint32_t)n, tm, tn, 1.0f / poly.scale, none);
         }
     };
     const int64_t t256 = tiles(m, n, 256) * q.batch, t128 = tiles(m, n, 128) * q.batch;
     const int64_t s256 = tiles(m, m, 256) * q.batch / 2, s128 = tiles(m, m, 128) * q.batch / 2;
-    const Square<Tile<HalfCore, 256, 256, 2, 4, 2>, 256> q256;
-    const Square<Tile<HalfCore, 128, 128, 2, 2, 3>, 128> q128;
-    const Square<Tile<HalfCore, 64, 64, 2, 2, 6>, 64> q64;
+    const Square<Tile<HalfCore, 256, 256, 2, 2, 2, 2>, 256> q256;
+    const Square<Tile<HalfCore, 128, 128, 2, 2, 2, 2>, 128> q128;
+    const Square<Tile<HalfCore, 64, 64, 2, 2, 2, 6>, 64> q64;
     for (int k = 0; k < q.steps; ++k) {
         const bool last = k + 1 == q.steps;
         const Plane &x0 = x[k & 1], &xt0 = xt[k & 1], &x1 = x[~k & 1], &xt1 = xt[~k & 1];

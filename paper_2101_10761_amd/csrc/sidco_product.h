@@ -1,12 +1,13 @@
 // Tile product C = A B^T on the matrix cores, shared by the 4-bit products and by the Newton-Schulz products.
 //
-// Both operands are stored by rows along the contraction, and a step takes one 128-byte line of every row of the tile:
-// 64 half-precision numbers, or 256 4-bit codes with the 8 exponents of their blocks.  Both kinds keep a lane's share of a
-// matrix instruction at 16 bytes and the instruction at 16 cycles, so that one data path serves them.
+// Both operands are stored by rows along the contraction, in pieces of 16 bytes: 8 half-precision numbers, or a block of 32
+// 4-bit codes.  A matrix instruction takes four pieces of 16 rows of each operand in 16 cycles for either kind, so that one
+// data path serves both.  A stage is one or two such fours, 64 or 128 bytes of every row of the tile, and for 4-bit codes the
+// exponents of these blocks.
 //
-// The lines go from memory to LDS without passing through registers (each lane names its own 16 bytes of memory, LDS is
-// written in the order of the lanes).  A row of LDS is a line and rows follow each other, so equal columns of the 16 rows that
-// an instruction reads would sit in the same banks; piece c of row r is therefore kept at place c ^ (r % 8), by choosing
+// Stages go from memory to LDS without passing through registers (each lane names its own 16 bytes of memory, LDS is written
+// in the order of the lanes).  Rows follow each other in LDS, so the same piece of the 16 rows that an instruction reads
+// would sit in few banks; piece c of row r is therefore kept at place c ^ (r % 8) of 8, or c ^ (r / 2 % 4) of 4, by choosing
 // which piece a lane fetches.
 #ifndef SIDCO_PRODUCT_H
 #define SIDCO_PRODUCT_H
@@ -22,7 +23,7 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 typedef _Float16 v4h __attribute__((ext_vector_type(4)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
-constexpr int kLine = 128;  // bytes of a row that one step takes
+constexpr int kLine = 128;  // a row's bytes are a multiple of this
 
 // One operand: rows of `pitch` bytes, a multiple of kLine and less than 2^24, padded with zeros; for 4-bit codes also the exponents, a byte for
 // each block, pitch / 16 bytes a row.
@@ -43,20 +44,20 @@ __device__ __forceinline__ v4i resource(const void* base, uint32_t bytes)
                __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
 }
 
-// Each lane's Bytes at `offset` (its own) + `at` (the wave's) of the operand go to LDS, lane by lane from `l` on.  The load
-// names no register that it writes.  It is written out because the compiler, which cannot tell the stages of LDS apart, waits
-// for every load made so far before the next read of LDS; wait_loads says what is waited for instead.
-template <int Bytes>
+// Each lane's Bytes at `offset` (its own) + `at` (the wave's) of the operand go to LDS, lane by lane from `l` + More on.
+// The load names no register that it writes.  It is written out because the compiler, which cannot tell the stages of LDS
+// apart, waits for every load made so far before the next read of LDS; wait_loads says what is waited for instead.
+template <int Bytes, int More>
 __device__ __forceinline__ void to_lds(const v4i& from, uint32_t offset, uint32_t at, char* l)
 {
     static_assert(Bytes == 16 || Bytes == 4, "what the load takes");
-    const uint32_t place = (uint32_t)(uintptr_t)(lds_char*)l;
+    const uint32_t to = (uint32_t)(uintptr_t)(lds_char*)l;
     if constexpr (Bytes == 16)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(place), "v"(offset), "s"(from), "s"(at)
-                     : "memory");
+        asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(offset), "s"(from), "s"(at), "i"(More)
+                     : "memory", "scc");
     else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(place), "v"(offset), "s"(from), "s"(at)
-                     : "memory");
+        asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(offset), "s"(from), "s"(at), "i"(More)
+                     : "memory", "scc");
 }
 
 // Waits until at most N of this wave's loads are under way and its own LDS reads have arrived.
@@ -95,44 +96,60 @@ __device__ __forceinline__ void tile_of_triangle(uint32_t t, uint32_t& i, uint32
     j = t - r * (r + 1) / 2;
 }
 
-// What an instruction multiplies: 16 rows by 16 rows over half a line.
+// What an instruction multiplies: 16 rows by 16 rows over four pieces, lane l holding piece l / 16 of row l % 16.
+//
+// The instructions are written out because the sums have to stay where they are: with 64 tiles of them, all of a wave's 256
+// accumulation registers, the compiler's own choice of registers moved half of them about in every step.  The waits that it
+// would insert for them are written out too: settle() before instructions whose operands may just have been written by
+// another kind of instruction, and rest() before the sums are read.  Nothing may move the sums between the two (the compiler
+// would do it without a wait), which the one loop around all products sees to, and a test of the generated code.
 struct HalfCore {
     static constexpr bool kScaled = false;
-    static __device__ __forceinline__ v4f mul(const v4i& a, const v4i& b, const v4f& c, int, int)
+    static __device__ __forceinline__ void mul(const v4i& a, const v4i& b, v4f& c, int, int)
     {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+        asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
     }
 };
 
 struct Mx4Core {
     static constexpr bool kScaled = true;
-    static __device__ __forceinline__ v4f mul(const v4i& a, const v4i& b, const v4f& c, int sa, int sb)
+    static __device__ __forceinline__ void mul(const v4i& a, const v4i& b, v4f& c, int sa, int sb)  // 4: e2m1
     {
-        const v8i wa = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wb = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, c, 4, 4, 0, sa, 0, sb);  // 4: e2m1
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4"
+                     : "+a"(c)
+                     : "v"(a), "v"(b), "v"(sa), "v"(sb));
     }
 };
 
-// A block's tile: BM x BN by WM x WN waves, `Stages` lines deep in LDS.
-template <class Core, int BM, int BN, int WM, int WN, int Stages>
+__device__ __forceinline__ void settle() { asm volatile("s_nop 3" ::: "memory"); }
+__device__ __forceinline__ void rest() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+
+// A block's tile: BM x BN by WM x WN waves, `Stages` stages of `Fours` four pieces in LDS.
+template <class Core, int BM, int BN, int WM, int WN, int Fours, int Stages>
 struct Tile {
+    static constexpr int kM = BM, kN = BN;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int kMt = BM / WM / 16, kNt = BN / WN / 16;  // instructions' tiles of a wave
-    static constexpr int kScaleBytes = Core::kScaled ? 8 * (BM + BN) : 0;
-    static constexpr int kStage = (BM + BN) * kLine + kScaleBytes;
+    static constexpr int kSeg = 64 * Fours;                       // bytes of a row in a stage
+    static constexpr int kExps = 4 * Fours;                       // and exponents
+    // a stage: exponents of A's and of B's rows, A's rows, B's rows
+    static constexpr int kAtA = Core::kScaled ? (BM + BN) * kExps : 0, kAtB = kAtA + BM * kSeg, kStage = kAtB + BN * kSeg;
     static constexpr int kLds = Stages * kStage;
-    static constexpr int kLoadsA = BM / 8 / kWaves, kLoadsB = BN / 8 / kWaves;      // 8 rows a load
-    static constexpr int kLoadsS = Core::kScaled ? (BM + BN) / 32 / kWaves : 0;     // 32 rows' exponents a load
+    static constexpr int kRowsLoad = 1024 / kSeg, kRowsExps = 256 / kExps;  // rows that a load of 16 or of 4 bytes a lane takes
+    static constexpr int kLoadsA = BM / kRowsLoad / kWaves, kLoadsB = BN / kRowsLoad / kWaves;
+    static constexpr int kLoadsS = Core::kScaled ? (BM + BN) / kRowsExps / kWaves : 0;
     static constexpr int kLoads = kLoadsA + kLoadsB + kLoadsS;
     static_assert(BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "whole instructions");
-    static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0, "whole loads");
-    static_assert(!Core::kScaled || ((BM % 32 == 0) && (BM + BN) % (32 * kWaves) == 0), "whole loads of exponents");
-    static_assert(kLds <= 160 * 1024, "LDS of a CU");
+    static_assert(BM % (kRowsLoad * kWaves) == 0 && BN % (kRowsLoad * kWaves) == 0, "whole loads");
+    static_assert(!Core::kScaled || (BM % kRowsExps == 0 && (BM + BN) % (kRowsExps * kWaves) == 0), "whole loads of exponents");
+    static_assert(Fours == 1 || Fours == 2, "pieces of a line");
+    static_assert(Stages >= 2 && kLds <= 160 * 1024, "LDS of a CU");
 
     v4f acc[kMt][kNt];
     v4i from_a, from_b, from_sa, from_sb;
     uint32_t src[kLoadsA + kLoadsB];  // this lane's 16 bytes of each load's rows
     uint32_t ssrc[kLoadsS + 1];
+    uint32_t fours;                   // of the rows
     int wave, lane;
 
     __device__ __forceinline__ void clear()
@@ -143,6 +160,11 @@ struct Tile {
             for (int j = 0; j < kNt; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
+    static __device__ __forceinline__ int place(int row, int piece)
+    {
+        return Fours == 2 ? piece ^ (row & 7) : piece ^ (row >> 1 & 3);
+    }
+
     // Rows past the operand's end read its last row: their products are not stored.
     __device__ __forceinline__ void aim(const Rows& a, const Rows& b, uint32_t m0, uint32_t n0)
     {
@@ -151,11 +173,11 @@ struct Tile {
         const uint32_t ra = a.rows - m0 < BM ? a.rows - m0 : BM, rb = b.rows - n0 < BN ? b.rows - n0 : BN;
         from_a = resource((const char*)a.data + (size_t)m0 * a.pitch, ra * a.pitch);
         from_b = resource((const char*)b.data + (size_t)n0 * b.pitch, rb * b.pitch);
-        const uint32_t r = lane >> 3, c = (lane & 7) ^ r;
+        const int r = lane / (4 * Fours), c = place(r, lane % (4 * Fours));  // a load's first row is a multiple of 8
 #pragma unroll
         for (int k = 0; k < kLoadsA + kLoadsB; ++k) {
             const bool first = k < kLoadsA;
-            uint32_t row = (uint32_t)((first ? k : k - kLoadsA) * kWaves + wave) * 8 + r;
+            const uint32_t row = (uint32_t)((first ? k : k - kLoadsA) * kWaves + wave) * kRowsLoad + r;
             const uint32_t last = (first ? ra : rb) - 1;
             src[k] = (row < last ? row : last) * (first ? a.pitch : b.pitch) + c * 16;
         }
@@ -164,81 +186,136 @@ struct Tile {
             from_sb = resource((const char*)b.scales + (size_t)n0 * (b.pitch / 16), rb * (b.pitch / 16));
 #pragma unroll
             for (int k = 0; k < kLoadsS; ++k) {
-                const uint32_t at = (uint32_t)(k * kWaves + wave) * 32;  // row of the tile, B's after A's
-                const uint32_t row = (at < BM ? at : at - BM) + (lane >> 1), last = (at < BM ? ra : rb) - 1;
-                ssrc[k] = (row < last ? row : last) * ((at < BM ? a.pitch : b.pitch) / 16) + (lane & 1) * 4;
+                const uint32_t at = (uint32_t)(k * kWaves + wave) * kRowsExps;  // row of the tile, B's after A's
+                const uint32_t row = (at < BM ? at : at - BM) + lane / Fours, last = (at < BM ? ra : rb) - 1;
+                ssrc[k] = (row < last ? row : last) * ((at < BM ? a.pitch : b.pitch) / 16) + lane % Fours * 4;
             }
         }
+        fours = a.pitch / 64;
     }
 
-    // line t of every row
-    __device__ __forceinline__ void fetch(uint32_t t, char* stage)
+    // Load k of stage number u; one that the operands do not have is out of range for the load, which then fetches nothing.
+    template <int K>
+    __device__ __forceinline__ void fetch(uint32_t u, char* stage) const
     {
-#pragma unroll
-        for (int k = 0; k < kLoadsA + kLoadsB; ++k) {
-            const int at = k < kLoadsA ? (k * kWaves + wave) * 1024 : BM * kLine + ((k - kLoadsA) * kWaves + wave) * 1024;
-            to_lds<16>(k < kLoadsA ? from_a : from_b, src[k], t * kLine, stage + at);
-        }
-#pragma unroll
-        for (int k = 0; k < kLoadsS; ++k) {
-            const int at = k * kWaves + wave;
-            to_lds<4>(at * 32 < BM ? from_sa : from_sb, ssrc[k], t * 8, stage + (BM + BN) * kLine + at * 256);
+        constexpr int kS = K - kLoadsA - kLoadsB;
+        if constexpr (kS < 0) {
+            constexpr bool kFirst = K < kLoadsA;
+            constexpr int kAt = kFirst ? kAtA + K * kWaves * 1024 : kAtB + (K - kLoadsA) * kWaves * 1024;
+            v4i from = kFirst ? from_a : from_b;
+            from[2] = u * Fours < fours ? from[2] : 0;
+            to_lds<16, kAt>(from, src[K], u * kSeg, stage + wave * 1024);
+        } else {
+            v4i from = (kS * kWaves + wave) * kRowsExps < BM ? from_sa : from_sb;
+            from[2] = u * Fours < fours ? from[2] : 0;
+            to_lds<4, kS * kWaves * 256>(from, ssrc[kS], u * kExps, stage + wave * 256);
         }
     }
-
-    __device__ __forceinline__ void multiply(const char* stage)
+    template <int From, int To>
+    __device__ __forceinline__ void fetch_range(uint32_t u, char* stage) const
     {
-        const int wm = wave / WN, wn = wave % WN;
-        const int r = lane & 15, q = lane >> 4;
-        const char* pa = stage + (wm * (BM / WM) + r) * kLine;
-        const char* pb = stage + BM * kLine + (wn * (BN / WN) + r) * kLine;
-        const char* ps = stage + (BM + BN) * kLine;
-        uint2 sa[Core::kScaled ? kMt : 1], sb[Core::kScaled ? kNt : 1];
-        if (Core::kScaled) {
-#pragma unroll
-            for (int i = 0; i < kMt; ++i) sa[i] = *(const uint2*)(ps + (wm * (BM / WM) + i * 16 + r) * 8);
-#pragma unroll
-            for (int j = 0; j < kNt; ++j) sb[j] = *(const uint2*)(ps + BM * 8 + (wn * (BN / WN) + j * 16 + r) * 8);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int piece = ((h * 4 + q) ^ (r & 7)) * 16;
-            v4i fa[kMt], fb[kNt];
-#pragma unroll
-            for (int j = 0; j < kNt; ++j) fb[j] = *(const v4i*)(pb + j * 16 * kLine + piece);
-#pragma unroll
-            for (int i = 0; i < kMt; ++i) fa[i] = *(const v4i*)(pa + i * 16 * kLine + piece);
-#pragma unroll
-            for (int i = 0; i < kMt; ++i)
-#pragma unroll
-                for (int j = 0; j < kNt; ++j)
-                    acc[i][j] = Core::mul(fb[j], fa[i], acc[i][j], Core::kScaled ? (int)((h ? sb[j].y : sb[j].x) >> (8 * q)) : 0,
-                                          Core::kScaled ? (int)((h ? sa[i].y : sa[i].x) >> (8 * q)) : 0);
+        if constexpr (From < To) {
+            fetch<From>(u, stage);
+            fetch_range<From + 1, To>(u, stage);
         }
     }
 
-    // Adds the products over `steps` lines.  Every wave of the block calls it; LDS is free again when the next one fetches.
-    __device__ __forceinline__ void run(const Rows& a, const Rows& b, uint32_t m0, uint32_t n0, uint32_t steps, char* lds)
+    // What a wave holds of four pieces: its rows' and their exponents.
+    struct Part {
+        v4i a[kMt], b[kNt];
+        int sa[Core::kScaled ? kMt : 1], sb[Core::kScaled ? kNt : 1];
+    };
+
+    __device__ __forceinline__ void read_a(Part& p, const char* stage, int h, int i) const
+    {
+        const int r = lane & 15, row = wave / WN * (BM / WM) + r, c = 4 * h + (lane >> 4);
+        p.a[i] = *(const v4i*)(stage + row * kSeg + place(r, c) * 16 + (kAtA + i * 16 * kSeg));
+        if (Core::kScaled) p.sa[i] = *(const uint8_t*)(stage + row * kExps + c + i * 16 * kExps);
+    }
+    __device__ __forceinline__ void read_b(Part& p, const char* stage, int h, int j) const
+    {
+        const int r = lane & 15, row = wave % WN * (BN / WN) + r, c = 4 * h + (lane >> 4);
+        p.b[j] = *(const v4i*)(stage + row * kSeg + place(r, c) * 16 + (kAtB + j * 16 * kSeg));
+        if (Core::kScaled) p.sb[j] = *(const uint8_t*)(stage + row * kExps + c + (BM + j * 16) * kExps);
+    }
+    // reads in the order in which the products want them: a's first row, all of b, the rest of a
+    __device__ __forceinline__ void read(Part& p, const char* stage, int h, int n) const
+    {
+        if (n == 0)
+            read_a(p, stage, h, 0);
+        else if (n <= kNt)
+            read_b(p, stage, h, n - 1);
+        else
+            read_a(p, stage, h, n - kNt);
+    }
+
+    // The products of p with the reads of the next four pieces (number h of `stage`) between them, and with Fetch the loads of
+    // stage number u to `to`.  A product keeps the matrix unit for 16 cycles and its wave, which is alone on its SIMD, issues
+    // something every 4: up to three other instructions go between two products for nothing, a bunch of them stops the unit.
+    // So each product is followed by at most one read or load, and the reads come first, for the barrier waits for them.
+    template <bool Read, bool Fetch, int N = 0>
+    __device__ __forceinline__ void multiply(const Part& p, Part& next, const char* stage, int h, uint32_t u, char* to)
+    {
+        if constexpr (N < kMt * kNt) {
+            constexpr int i = N / kNt, j = N % kNt, kAll = kMt * kNt, kReads = kMt + kNt, kEvery = kAll >= 64 ? 3 : 1;
+            static_assert(kReads * kEvery <= kAll || kAll < 64, "a product for each read");
+            if (N == 0) settle();
+            Core::mul(p.b[j], p.a[i], acc[i][j], Core::kScaled ? p.sb[j] : 0, Core::kScaled ? p.sa[i] : 0);
+            if (Read && kAll >= 64 && N % kEvery == 0 && N / kEvery < kReads) read(next, stage, h, N / kEvery);
+            if (Read && kAll < 64) {
+#pragma unroll
+                for (int n = N * kReads / kAll; n < (N + 1) * kReads / kAll; ++n) read(next, stage, h, n);
+            }
+            if constexpr (Fetch && kAll >= 64) {
+                static_assert(kLoads * 3 <= kAll + 2, "a product for each load");
+                if constexpr (N % 3 == 1 && N / 3 < kLoads) fetch<N / 3>(u, to);
+            } else if constexpr (Fetch) {
+                fetch_range<N * kLoads / kAll, (N + 1) * kLoads / kAll>(u, to);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply<Read, Fetch, N + 1>(p, next, stage, h, u, to);
+        }
+    }
+
+    // Adds the products over the rows' whole length.  Every wave of the block calls it; LDS is free again when the next one
+    // fetches.  While four pieces are multiplied the next four are read from LDS into other registers.  Once every wave has
+    // read the last of a stage its place is free, and the stage after it has to be there: one barrier a stage.
+    __device__ __forceinline__ void run(const Rows& a, const Rows& b, uint32_t m0, uint32_t n0, char* lds)
     {
         aim(a, b, m0, n0);
         __syncthreads();  // the stages may still be read for what was computed before
 #pragma unroll
-        for (int s = 0; s < Stages - 1; ++s)
-            if ((uint32_t)s < steps) fetch(s, lds + s * kStage);
-        int at = 0;
-        for (uint32_t t = 0; t < steps; ++t) {
-            // step t's lines are there once the later steps' alone are under way, and once every wave says so
-            if (t + Stages - 2 < steps)
-                wait_loads<(Stages - 2) * kLoads>();
-            else
-                wait_loads<0>();
+        for (int s = 0; s < Stages; ++s) fetch_range<0, kLoads>(s, lds + s * kStage);
+        wait_loads<(Stages - 1) * kLoads>();
+        __builtin_amdgcn_s_barrier();
+        Part p0, p1;
+#pragma unroll
+        for (int n = 0; n < kMt + kNt; ++n) read(p0, lds, 0, n);
+        char *stage = lds, *const end = lds + kLds;
+        auto turn = [&](const Part& p, Part& next, uint32_t u) {
+            wait_loads<(Stages - 2) * kLoads>();
             __builtin_amdgcn_s_barrier();
-            int next = at + Stages - 1;
-            next = next >= Stages ? next - Stages : next;
-            if (t + Stages - 1 < steps) fetch(t + Stages - 1, lds + next * kStage);
-            multiply(lds + at * kStage);
-            at = at + 1 == Stages ? 0 : at + 1;
-        }
+            char* to = stage;
+            stage = stage + kStage == end ? lds : stage + kStage;
+            multiply<true, true>(p, next, stage, 0, u + Stages, to);
+        };
+        // Rows are whole lines: an even number of fours.  The last turn reads what follows the last stage, which nothing uses;
+        // a loop without an end of its own leaves the sums in their registers.
+        uint32_t u = 0, f = 0;
+        do {
+            if (Fours == 2)
+                multiply<true, false>(p0, p1, stage, 1, 0, nullptr);
+            else
+                turn(p0, p1, u++);
+            turn(p1, p0, u++);
+            f += 2;
+        } while (f < fours);
+        wait_loads<0>();
+        rest();
+#pragma unroll
+        for (int i = 0; i < kMt; ++i)
+#pragma unroll
+            for (int j = 0; j < kNt; ++j) asm volatile("" : "+a"(acc[i][j]));  // not read before this point
     }
 
     // f(row, column, 4 values): C's row and the first of four neighbouring columns, relative to the tile.
