@@ -147,46 +147,39 @@ __global__ __launch_bounds__(256) void k_start(Start<T> p, float eps, Plane natu
 
 // ---- the products ----
 
-// Four lanes with four columns of their row each come to hold four rows of one column each.
-__device__ __forceinline__ v4f turn(v4f v)
-{
-    const int t = threadIdx.x & 3;
-    auto swap1 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xb1, 0xf, 0xf, true)); };
-    auto swap2 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x4e, 0xf, 0xf, true)); };
-#pragma unroll
-    for (int i = 0; i < 4; i += 2) {
-        const float got = swap1(t & 1 ? v[i] : v[i + 1]);
-        if (t & 1)
-            v[i] = got;
-        else
-            v[i + 1] = got;
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const float got = swap2(t & 2 ? v[i] : v[i + 2]);
-        if (t & 2)
-            v[i] = got;
-        else
-            v[i + 2] = got;
-    }
-    return v;
-}
-
-// four neighbours of row r from column c on, a multiple of 4; columns from `cols` to the pitch are padding
-template <bool Full>
-__device__ __forceinline__ void put4(const Plane& o, int64_t z, uint32_t rows, uint32_t cols, uint32_t r, uint32_t c, v4f v)
+// Eight neighbours of row r from column c on, a multiple of 8; columns from `cols` on are padding, to 64, and zero.
+__device__ __forceinline__ void put8(const Plane& o, int64_t z, uint32_t rows, uint32_t cols, uint32_t r, uint32_t c, v8h v, bool low)
 {
     if (r >= rows || c >= (uint32_t)o.pitch) return;
-    v4h h, l;
+    if (c + 8 > cols) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float x = c + i < cols ? v[i] : 0.0f;
-        h[i] = (_Float16)x;
-        l[i] = (_Float16)(x - (float)h[i]);
+        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? v[i] : (_Float16)0.0f;
     }
-    _Float16* p = o.at + z * o.stride + (int64_t)r * o.pitch + c;
-    *(v4h*)p = h;
-    if (Full) *(v4h*)(p + o.low) = l;
+    *(v8h*)(o.at + z * o.stride + (low ? o.low : 0) + (int64_t)r * o.pitch + c) = v;
+}
+
+// What a half leaves of v.
+__device__ __forceinline__ v4f rest_of(const v4f& v)
+{
+    v4f r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = v[i] - (float)(_Float16)v[i];
+    return r;
+}
+
+// The tile at (m0, n0) of a rows x cols matrix to `o`, or with Turn its transpose; value() as in Tile::out.
+template <bool Turn, bool Full, class Tl, class Value>
+__device__ __forceinline__ void put_tile(Tl& t, char* lds, const Plane& o, int64_t z, uint32_t rows, uint32_t cols, uint32_t m0,
+                                         uint32_t n0, const Value& value)
+{
+    auto at = [&](uint32_t r, uint32_t c, const v4f& v) -> v4f { return value(m0 + r, n0 + c, v); };
+    auto store = [&](bool low) {
+        return [&, low](uint32_t r, uint32_t c, const v8h& v) {
+            put8(o, z, Turn ? cols : rows, Turn ? rows : cols, (Turn ? n0 : m0) + r, (Turn ? m0 : n0) + c, v, low);
+        };
+    };
+    t.template out<_Float16, Turn>(lds, at, store(false));
+    if (Full) t.template out<_Float16, Turn>(lds, [&](uint32_t r, uint32_t c, const v4f& v) { return rest_of(at(r, c, v)); }, store(true));
 }
 
 __device__ __forceinline__ Rows rows_of(const Plane& o, int64_t z, uint32_t rows, bool low = false)
@@ -221,30 +214,24 @@ __global__ __launch_bounds__(Tl::kThreads) void k_symmetric(Plane x, Plane out, 
     tile_of_triangle(w % tiles, i, j);
     Tl t;
     products<Tl, Full>(t, x, x, z, m, m, i * B, j * B, lds);
-    t.each([&](uint32_t r, uint32_t c, v4f v) {
-        r += i * B, c += j * B;
-        if (Second) {
-            v4f g = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (r < m && c < (uint32_t)x.pitch) {
-                const _Float16* q = x.at + z * x.stride + (int64_t)r * x.pitch + c;
-                const v4h h = *(const v4h*)q;
-                v4h l = {0, 0, 0, 0};
-                if (Full) l = *(const v4h*)(q + x.low);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) g[k] = (float)h[k] + (float)l[k];
-            }
+    __syncthreads();
+    auto value = [&](uint32_t r, uint32_t c, const v4f& v) -> v4f {
+        if (!Second) return v * (1.0f / kScaleX);
+        v4f w = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (r < m && c < (uint32_t)x.pitch) {
+            const _Float16* g = x.at + z * x.stride + (int64_t)r * x.pitch + c;
+            const v4h h = *(const v4h*)g;
+            v4h l = {0, 0, 0, 0};
+            if (Full) l = *(const v4h*)(g + x.low);
             const float c2 = p.c * p.scale / (kScaleX * kScaleX), c1 = p.b * p.scale / kScaleX;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = fmaf(c2, v[k], fmaf(c1, g[k], r == c + k ? p.a * p.scale : 0.0f));
-        } else {
-            v *= 1.0f / kScaleX;
+            for (int k = 0; k < 4; ++k)
+                w[k] = fmaf(c2, v[k], fmaf(c1, (float)h[k] + (float)l[k], r == c + k ? p.a * p.scale : 0.0f));
         }
-        put4<Full>(out, z, m, m, r, c, v);
-        if (i != j) {
-            v = turn(v);
-            put4<Full>(out, z, m, m, c + (threadIdx.x & 3), r & ~3u, v);
-        }
-    });
+        return w;
+    };
+    put_tile<false, Full>(t, lds, out, z, m, m, i * B, j * B, value);
+    if (i != j) put_tile<true, Full>(t, lds, out, z, m, m, i * B, j * B, value);
 }
 
 // What the last product goes to: the result, or weights that move by it.
@@ -292,18 +279,17 @@ __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plan
     tile_of(w % (tm * tn), tm, tn, i, j);
     Tl t;
     products<Tl, Full>(t, pm, xt, z, m, n, i * B, j * B, lds);
+    __syncthreads();
+    auto value = [&](uint32_t, uint32_t, const v4f& v) -> v4f { return v * back; };
     if (!Last) {
-        t.each([&](uint32_t r, uint32_t c, v4f v) {
-            r += i * B, c += j * B;
-            v *= back;
-            put4<Full>(x2, z, m, n, r, c, v);
-            v = turn(v);
-            put4<Full>(xt2, z, n, m, c + (threadIdx.x & 3), r & ~3u, v);
-        });
+        put_tile<false, Full>(t, lds, x2, z, m, n, i * B, j * B, value);
+        put_tile<true, Full>(t, lds, xt2, z, m, n, i * B, j * B, value);
     } else if (o.tall) {
-        t.each([&](uint32_t r, uint32_t c, v4f v) { finish4<T>(o, z, j * B + c + (threadIdx.x & 3), (i * B + r) & ~3u, turn(v * back)); });
+        t.each([&](uint32_t r, uint32_t c, const v4f& v) {
+            finish4<T>(o, z, j * B + c + (threadIdx.x & 3), (i * B + r) & ~3u, Tl::turned(v * back));
+        });
     } else {
-        t.each([&](uint32_t r, uint32_t c, v4f v) { finish4<T>(o, z, i * B + r, j * B + c, v * back); });
+        t.each([&](uint32_t r, uint32_t c, const v4f& v) { finish4<T>(o, z, i * B + r, j * B + c, v * back); });
     }
 }
 

@@ -160,6 +160,15 @@ struct Tile {
             for (int j = 0; j < kNt; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
+    // The sums are in their registers here; nothing computed from them comes from before.
+    __device__ __forceinline__ void hold()
+    {
+#pragma unroll
+        for (int i = 0; i < kMt; ++i)
+#pragma unroll
+            for (int j = 0; j < kNt; ++j) asm volatile("" : "+a"(acc[i][j]));
+    }
+
     static __device__ __forceinline__ int place(int row, int piece)
     {
         return Fours == 2 ? piece ^ (row & 7) : piece ^ (row >> 1 & 3);
@@ -312,10 +321,7 @@ struct Tile {
         } while (f < fours);
         wait_loads<0>();
         rest();
-#pragma unroll
-        for (int i = 0; i < kMt; ++i)
-#pragma unroll
-            for (int j = 0; j < kNt; ++j) asm volatile("" : "+a"(acc[i][j]));  // not read before this point
+        hold();
     }
 
     // f(row, column, 4 values): C's row and the first of four neighbouring columns, relative to the tile.
@@ -328,6 +334,78 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < kNt; ++j)
                 f((uint32_t)(wm * (BM / WM) + i * 16 + (lane & 15)), (uint32_t)(wn * (BN / WN) + j * 16 + 4 * (lane >> 4)), acc[i][j]);
+    }
+
+    // ---- by way of LDS ----
+    //
+    // A lane holds four neighbouring columns; halves stored like that touch 16 rows with 32 bytes each.  So a wave puts 16 rows (or columns, for the transpose) of its tile at a time into LDS, as S, and reads them
+    // back in 16 bytes a lane along the row.
+
+    static constexpr int pad(int bytes) { return bytes + 16; }
+    template <class S>
+    static constexpr int out_bytes()  // of LDS for each wave
+    {
+        return 16 * pad((kNt > kMt ? kNt : kMt) * 16 * (int)sizeof(S));
+    }
+
+    // Four lanes with four columns of their row each come to hold four rows of one column each.
+    static __device__ __forceinline__ v4f turned(v4f v)
+    {
+        const int t = threadIdx.x & 3;
+        auto swap1 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xb1, 0xf, 0xf, true)); };
+        auto swap2 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x4e, 0xf, 0xf, true)); };
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            const float got = swap1(t & 1 ? v[i] : v[i + 1]);
+            v[i] = t & 1 ? got : v[i];
+            v[i + 1] = t & 1 ? v[i + 1] : got;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float got = swap2(t & 2 ? v[i] : v[i + 2]);
+            v[i] = t & 2 ? got : v[i];
+            v[i + 2] = t & 2 ? v[i + 2] : got;
+        }
+        return v;
+    }
+
+    // value(row, column, sums) gives the four values of C's row from a column on; store(row, column, 16 bytes of S) takes
+    // neighbours of a row - with Turn of a column: row and column are C's, exchanged.  All relative to the tile.  Every wave
+    // of the block calls it, after a barrier since run(); `lds` has out_bytes<S>() for each wave.
+    template <class S, bool Turn, class Value, class Store>
+    __device__ __forceinline__ void out(char* lds, const Value& value, const Store& store)
+    {
+        hold();  // what an earlier way out has computed of them is not kept
+        constexpr int kStrips = Turn ? kNt : kMt, kTiles = Turn ? kMt : kNt, kPitch = pad(kTiles * 16 * (int)sizeof(S));
+        constexpr int kPer = 16 / (int)sizeof(S), kLanes = kTiles * 16 / kPer;  // lanes of a row
+        static_assert(16 * kLanes % 64 == 0, "whole waves");
+        typedef S s4 __attribute__((ext_vector_type(4)));
+        typedef S sv __attribute__((ext_vector_type(kPer)));
+        char* mine = lds + wave * out_bytes<S>();
+        const int r = lane & 15, q = lane >> 4;
+        const int row0 = wave / WN * (BM / WM), col0 = wave % WN * (BN / WN);
+#pragma unroll
+        for (int x = 0; x < kStrips; ++x) {
+#pragma unroll
+            for (int y = 0; y < kTiles; ++y) {
+                const int i = Turn ? y : x, j = Turn ? x : y;
+                v4f v = value((uint32_t)(row0 + i * 16 + r), (uint32_t)(col0 + j * 16 + 4 * q), acc[i][j]);
+                if (Turn) v = turned(v);
+                const s4 w = {(S)v[0], (S)v[1], (S)v[2], (S)v[3]};
+                if (Turn)
+                    *(s4*)(mine + (4 * q + (r & 3)) * kPitch + (y * 16 + (r & ~3)) * (int)sizeof(S)) = w;
+                else
+                    *(s4*)(mine + r * kPitch + (y * 16 + 4 * q) * (int)sizeof(S)) = w;
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int k = 0; k < 16 * kLanes / 64; ++k) {
+                const int at = k * 64 + lane, row = at / kLanes, col = at % kLanes * kPer;
+                store((uint32_t)((Turn ? col0 : row0) + x * 16 + row), (uint32_t)((Turn ? row0 : col0) + col),
+                      *(const sv*)(mine + row * kPitch + col * (int)sizeof(S)));
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
     }
 };
 
