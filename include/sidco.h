@@ -561,7 +561,7 @@ size_t sidco_workspace_bytes_mx4_linear(int64_t rows, int64_t k);
  * (bG + cG^2) X with G = X X^T (X^T X for a tall matrix: the result is the same),
  * which takes every singular value s to as + bs^3 + cs^5.  The default values
  * bring them near 1 in 5 steps.  The coefficients have to keep singular values
- * below 4 on the way; a matrix of zeros stays one, and a NaN or an infinity in u
+ * below 1.5 on the way; a matrix of zeros stays one, and a NaN or an infinity in u
  * makes its matrix NaN.
  *
  * precision: SIDCO_NS_HALF multiplies operands of 11 bits (for matrices of random

@@ -456,11 +456,13 @@ void launch_mx4_product(const Mx4Product& p, hipStream_t s)
         const uint32_t tm = (uint32_t)((p.m + Tl::kM - 1) / Tl::kM), tn = (uint32_t)((p.n + Tl::kN - 1) / Tl::kN);
         k_mx4_product<E, Tl><<<tm * tn, Tl::kThreads, 0, s>>>(p, tm, tn);
     };
-    auto tiles = [&](int64_t b) { return ((p.m + b - 1) / b) * ((p.n + b - 1) / b); };
+    const int pick = best_tile([&](int64_t b) { return ((p.m + b - 1) / b) * ((p.n + b - 1) / b); }, mx4_padded(p.k) / 2 / kLine);
     by_type(p.type, [&](auto e) {
-        if (tiles(256) >= 256)
+        if (pick == 0)
             go(e, Shape<Tile<Mx4Core, 256, 256, 2, 2, 2, 2>>());
-        else if (tiles(128) >= 200)
+        else if (pick == 1)
+            go(e, Shape<Tile<Mx4Core, 192, 192, 2, 2, 2, 3>>());
+        else if (pick == 2)
             go(e, Shape<Tile<Mx4Core, 128, 128, 2, 2, 2, 2>>());
         else
             go(e, Shape<Tile<Mx4Core, 64, 64, 2, 2, 2, 4>>());

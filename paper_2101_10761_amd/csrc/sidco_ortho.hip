@@ -12,6 +12,8 @@
 // X's relative error of 2^-12 an element, about 1.5e-3 (2-norm) reaches the result, less than a result in bf16 loses; halves
 // are used where it has 16 bits.  For a result in 32 bits each operand is a pair of halves, the second one what the first
 // leaves, 22 bits together, and a product is three: high high + low high + high low.
+#include <type_traits>
+
 #include "sidco_dense.h"
 #include "sidco_product.h"
 
@@ -199,39 +201,44 @@ __device__ __forceinline__ void products(Tl& t, const Plane& a, const Plane& b, 
     t.run(rows_of(a, z, ra), rows_of(b, z, rb), m0, n0, lds);
 }
 
-struct Poly {
-    float a, b, c, scale;  // of P; scale: what P is kept times
+// A product of two symmetric matrices that commute, A B^T = A B: symmetric too.  out = p2 A B + p1 B + p0 I, all with the
+// scales of their planes in the factors; p1 = p0 = 0 for a plain product.
+struct Symmetric {
+    Plane a, b, out;
+    float p2, p1, p0;
 };
 
-// G = X X^T, or with Second P = aI + bG + cG^2; `x` is X or G, `out` G or P, both m x m.
-template <class Tl, int B, bool Full, bool Second>
-__global__ __launch_bounds__(Tl::kThreads) void k_symmetric(Plane x, Plane out, uint32_t m, uint32_t tiles, Poly p)
+// One or two of them of the same size.  Tiles on and below the diagonal are computed and mirrored.
+template <class Tl, bool Full, bool Poly>
+__global__ __launch_bounds__(Tl::kThreads) void k_symmetric(Symmetric first, Symmetric second, uint32_t m, uint32_t tiles, uint32_t each)
 {
+    constexpr int B = Tl::kM;
     __shared__ __align__(1024) char lds[Tl::kLds];
-    const uint32_t w = xcd_run(blockIdx.x, gridDim.x);
+    uint32_t w = xcd_run(blockIdx.x, gridDim.x);
+    const Symmetric& p = w < each ? first : second;
+    w = w < each ? w : w - each;
     const int64_t z = w / tiles;
     uint32_t i, j;
     tile_of_triangle(w % tiles, i, j);
     Tl t;
-    products<Tl, Full>(t, x, x, z, m, m, i * B, j * B, lds);
+    products<Tl, Full>(t, p.a, p.b, z, m, m, i * B, j * B, lds);
     __syncthreads();
+    const float p2 = p.p2, p1 = p.p1, p0 = p.p0;
     auto value = [&](uint32_t r, uint32_t c, const v4f& v) -> v4f {
-        if (!Second) return v * (1.0f / kScaleX);
+        if (!Poly) return v * p2;
         v4f w = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (r < m && c < (uint32_t)x.pitch) {
-            const _Float16* g = x.at + z * x.stride + (int64_t)r * x.pitch + c;
+        if (r < m && c < (uint32_t)p.b.pitch) {
+            const _Float16* g = p.b.at + z * p.b.stride + (int64_t)r * p.b.pitch + c;
             const v4h h = *(const v4h*)g;
             v4h l = {0, 0, 0, 0};
-            if (Full) l = *(const v4h*)(g + x.low);
-            const float c2 = p.c * p.scale / (kScaleX * kScaleX), c1 = p.b * p.scale / kScaleX;
+            if (Full) l = *(const v4h*)(g + p.b.low);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                w[k] = fmaf(c2, v[k], fmaf(c1, (float)h[k] + (float)l[k], r == c + k ? p.a * p.scale : 0.0f));
+            for (int k = 0; k < 4; ++k) w[k] = fmaf(p2, v[k], fmaf(p1, (float)h[k] + (float)l[k], r == c + k ? p0 : 0.0f));
         }
         return w;
     };
-    put_tile<false, Full>(t, lds, out, z, m, m, i * B, j * B, value);
-    if (i != j) put_tile<true, Full>(t, lds, out, z, m, m, i * B, j * B, value);
+    put_tile<false, Full>(t, lds, p.out, z, m, m, i * B, j * B, value);
+    if (i != j) put_tile<true, Full>(t, lds, p.out, z, m, m, i * B, j * B, value);
 }
 
 // What the last product goes to: the result, or weights that move by it.
@@ -267,11 +274,12 @@ __device__ __forceinline__ void finish4(const Result& o, int64_t z, int64_t r, i
     }
 }
 
-// X' = P X: X' and its transpose, or with Last the result, of element type T.
-template <class Tl, int B, bool Full, bool Last, class T>
+// X' = Q X: X' and its transpose, or with Last the result, of element type T.
+template <class Tl, bool Full, bool Last, class T>
 __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plane x2, Plane xt2, uint32_t m, uint32_t n, uint32_t tm, uint32_t tn,
                                                         float back, Result o)
 {
+    constexpr int B = Tl::kM;
     __shared__ __align__(1024) char lds[Tl::kLds];
     const uint32_t w = xcd_run(blockIdx.x, gridDim.x);
     const int64_t z = w / (tm * tn);
@@ -295,11 +303,12 @@ __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plan
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-// The workspace of a batch: partial sums, then X, X^T, both once more, G and P of every matrix.
+// The workspace of a batch: partial sums, then X, X^T and both once more, and the symmetric matrices, of every matrix.
+constexpr int kSmall = 7;  // G, G', P, P', T, Q, Q'
 struct Layout {
     int64_t m, n, mp, np;
     int planes, parts;
-    size_t part_bytes, x, g, total;  // halves of one X (or X^T) and one G of a matrix, all planes of them
+    size_t part_bytes, total;
     Layout(int batch, int64_t rows, int64_t cols, bool full)
     {
         m = rows < cols ? rows : cols;
@@ -310,18 +319,49 @@ struct Layout {
         const int64_t want = (rows * cols + 16 * kNormBlock - 1) / (16 * kNormBlock);
         parts = (int)(want < 512 ? want : 512);
         part_bytes = (size_t)up((int64_t)batch * parts * (int64_t)sizeof(double), 256);
-        x = (size_t)(m * np) * planes;
-        g = (size_t)(m * mp) * planes;
-        const size_t xt = (size_t)(n * mp) * planes;
-        total = part_bytes + (size_t)batch * 2 * (2 * up((int64_t)x, 128) + 2 * up((int64_t)xt, 128) + 2 * up((int64_t)g, 128));
+        const int64_t halves = 2 * plane(m, np) + 2 * plane(n, mp) + kSmall * plane(m, mp);
+        total = part_bytes + (size_t)batch * halves * sizeof(_Float16);
     }
+    int64_t plane(int64_t height, int64_t pitch) const { return up(height * pitch * planes, 128); }
 };
 
-template <class Tl, int B>
-struct Square {
+template <class Tl>
+struct Shape {
     typedef Tl Is;
-    static constexpr int kSide = B;
 };
+
+// f(a tile's type) for the tile of kTileCosts[pick]
+template <class F>
+void by_tile(int pick, const F& f)
+{
+    if (pick == 0)
+        f(Shape<Tile<HalfCore, 256, 256, 2, 2, 2, 2>>());
+    else if (pick == 1)
+        f(Shape<Tile<HalfCore, 192, 192, 2, 2, 2, 3>>());
+    else if (pick == 2)
+        f(Shape<Tile<HalfCore, 128, 128, 2, 2, 2, 2>>());
+    else
+        f(Shape<Tile<HalfCore, 64, 64, 2, 2, 2, 4>>());
+}
+
+// How many steps share a pass over X.  Steps after the first of a group know their G without X: P and G commute, so that
+// (PX)(PX)^T = P G P, and the group's X is Q X with Q the product of its P.  In products of m x m x m operations, symmetric ones
+// counting half, and with n = r m, a step of its own costs 3r + 1 and one that joins a group 4.  What rounding leaves in G where
+// it should be small grows by a^2 with every step of a group, as the error of X itself does by a; with a = 3.4445, errors of
+// groups of 2 in halves are those of single steps (1e-3 to 3e-3 for spectra from flat to 1/k; of 3 up to 6e-3), of 3 with 22 bits
+// too (3e-7 to 6e-6; of 5 without bound).  A launch counts 4 us against 6e14 operations a second.
+int group_of(const OrthoCall& q, int64_t m, int64_t n, bool full)
+{
+    const double r = (double)n / (double)m, unit = (double)q.batch * (double)m * (double)m * (double)m * (full ? 3.0 : 1.0) / 6e8;
+    int best = 1;
+    double least = 0.0;
+    for (int g = 1; g <= (full ? 3 : 2) && g <= q.steps; ++g) {
+        const int groups = (q.steps + g - 1) / g, joined = q.steps - groups;
+        const double t = (groups * (3 * r + 1) + joined * 4) * unit + (groups * 3 + joined * 4) * 4.0;
+        if (g == 1 || t < least) least = t, best = g;
+    }
+    return best;
+}
 
 template <bool Full>
 void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
@@ -331,15 +371,15 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
     const int64_t m = l.m, n = l.n;
     const bool tall = q.rows > q.cols;
     _Float16* at = (_Float16*)(ws + l.part_bytes);
-    auto plane = [&](int64_t rows, int64_t pitch) {
-        const int64_t each = up(rows * pitch * l.planes, 128);
-        Plane p = {at, pitch, rows * pitch, each};
+    auto plane = [&](int64_t height, int64_t pitch) {
+        const int64_t each = l.plane(height, pitch);
+        Plane p = {at, pitch, height * pitch, each};
         at += each * q.batch;
         return p;
     };
-    Plane x[2], xt[2];
-    for (int i = 0; i < 2; ++i) x[i] = plane(m, l.np), xt[i] = plane(n, l.mp);
-    const Plane g = plane(m, l.mp), pm = plane(m, l.mp);
+    Plane x[2], xt[2], g[2], pm[2], qm[2];
+    for (int i = 0; i < 2; ++i) x[i] = plane(m, l.np), xt[i] = plane(n, l.mp), g[i] = plane(m, l.mp), pm[i] = plane(m, l.mp), qm[i] = plane(m, l.mp);
+    const Plane tm = plane(m, l.mp);
 
     auto start = [&](auto type) {
         typedef typename decltype(type)::T T;
@@ -355,56 +395,82 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
     else
         start(Elem<kGradBf16>());
 
-    // P's entries are at most |a| + 1.5 |b| + 2.25 |c| while singular values stay below 1.22
-    int e = 0;
-    (void)frexpf(32768.0f / (fabsf(q.a) + 1.5f * fabsf(q.b) + 2.25f * fabsf(q.c) + 1e-30f), &e);
-    e = e - 1 < 14 ? e - 1 : 14;
-    const Poly poly = {q.a, q.b, q.c, ldexpf(1.0f, e)};
-    const Result none = {};
-    auto tiles = [&](int64_t rows, int64_t cols, int64_t side) { return ((rows + side - 1) / side) * ((cols + side - 1) / side); };
-    auto run = [&](auto sym, auto app, const Plane& x0, const Plane& xt0, const Plane& x1, const Plane& xt1, bool last) {
-        typedef typename decltype(sym)::Is Sym;
-        typedef typename decltype(app)::Is App;
-        constexpr int kS = decltype(sym)::kSide, kA = decltype(app)::kSide;
-        const uint32_t side = (uint32_t)((m + kS - 1) / kS), tri = side * (side + 1) / 2;
-        k_symmetric<Sym, kS, Full, false><<<tri * batch, Sym::kThreads, 0, s>>>(x0, g, (uint32_t)m, tri, poly);
-        k_symmetric<Sym, kS, Full, true><<<tri * batch, Sym::kThreads, 0, s>>>(g, pm, (uint32_t)m, tri, poly);
-        const uint32_t tm = (uint32_t)((m + kA - 1) / kA), tn = (uint32_t)((n + kA - 1) / kA);
-        if (last) {
-            const Result o = {q.out, tall, q.update, q.keep, q.gain, q.ldo, q.out_stride, q.rows, q.cols};
-            auto finish = [&](auto type) {
-                k_apply<App, kA, Full, true, typename decltype(type)::T>
-                    <<<tm * tn * batch, App::kThreads, 0, s>>>(pm, xt0, x1, xt1, (uint32_t)m, (uint32_t)n, tm, tn, 1.0f / (kScaleX * poly.scale), o);
-            };
-            if (q.out_type == kGradF32)
-                finish(Elem<kGradF32>());
-            else if (q.out_type == kGradF16)
-                finish(Elem<kGradF16>());
-            else
-                finish(Elem<kGradBf16>());
-        } else {
-            k_apply<App, kA, Full, false, float>
-                <<<tm * tn * batch, App::kThreads, 0, s>>>(pm, xt0, x1, xt1, (uint32_t)m, (uint32_t)n, tm, tn, 1.0f / poly.scale, none);
-        }
+    // Scales: the largest powers of two that leave room for the largest element of P = a + bx + cx^2 over the squares x of
+    // singular values up to 1.5, of Q's products of it and of T = P G.
+    float top = fmaxf(fabsf(q.a), fabsf(q.a + 2.25f * q.b + 5.0625f * q.c));
+    if (q.c != 0.0f && -q.b / (2 * q.c) > 0.0f && -q.b / (2 * q.c) < 2.25f) top = fmaxf(top, fabsf(q.a - q.b * q.b / (4 * q.c)));
+    auto scale = [](float bound) {
+        int e = 0;
+        (void)frexpf(32768.0f / fmaxf(bound, 1.0f), &e);
+        return ldexpf(1.0f, e - 1 > -10 ? e - 1 : -10);
     };
-    const int64_t t256 = tiles(m, n, 256) * q.batch, t128 = tiles(m, n, 128) * q.batch;
-    const int64_t s256 = tiles(m, m, 256) * q.batch / 2, s128 = tiles(m, m, 128) * q.batch / 2;
-    const Square<Tile<HalfCore, 256, 256, 2, 2, 2, 2>, 256> q256;
-    const Square<Tile<HalfCore, 128, 128, 2, 2, 2, 2>, 128> q128;
-    const Square<Tile<HalfCore, 64, 64, 2, 2, 2, 6>, 64> q64;
-    for (int k = 0; k < q.steps; ++k) {
-        const bool last = k + 1 == q.steps;
-        const Plane &x0 = x[k & 1], &xt0 = xt[k & 1], &x1 = x[~k & 1], &xt1 = xt[~k & 1];
-        if (s256 >= 200)
-            run(q256, q256, x0, xt0, x1, xt1, last);
-        else if (s128 >= 100 && t256 >= 200)
-            run(q128, q256, x0, xt0, x1, xt1, last);
-        else if (s128 >= 100)
-            run(q128, q128, x0, xt0, x1, xt1, last);
-        else if (t128 >= 200)
-            run(q64, q128, x0, xt0, x1, xt1, last);
-        else
-            run(q64, q64, x0, xt0, x1, xt1, last);
+    const float sx = kScaleX, sp = scale(top), st = scale(2.25f * top);
+
+    const int64_t segments = Full ? 3 : 1;
+    auto triangle = [](int64_t side, int64_t b) { const int64_t k = (side + b - 1) / b; return k * (k + 1) / 2; };
+    auto symmetric = [&](auto poly, int jobs, const Symmetric& a, const Symmetric& b) {
+        const int pick = best_tile([&](int64_t side) { return triangle(m, side) * q.batch * jobs; }, a.a.pitch * 2 / kLine * segments);
+        by_tile(pick, [&](auto shape) {
+            typedef typename decltype(shape)::Is Tl;
+            const uint32_t tri = (uint32_t)triangle(m, Tl::kM), each = tri * batch;
+            k_symmetric<Tl, Full, decltype(poly)::value><<<each * jobs, Tl::kThreads, 0, s>>>(a, b, (uint32_t)m, tri, each);
+        });
+    };
+    auto product = [](const Plane& a, float sa, const Plane& b, float sb, const Plane& o, float so) -> Symmetric {
+        return {a, b, o, so / (sa * sb), 0.0f, 0.0f};
+    };
+    auto poly = [&](const Plane& gm, const Plane& o) -> Symmetric { return {gm, gm, o, q.c * sp / (sx * sx), q.b * sp / sx, q.a * sp}; };
+    const int apply_pick = best_tile([&](int64_t b) { return ((m + b - 1) / b) * ((n + b - 1) / b) * q.batch; }, l.mp * 2 / kLine * segments);
+    auto apply = [&](const Plane& by, float sb, int from, bool last) {
+        by_tile(apply_pick, [&](auto shape) {
+            typedef typename decltype(shape)::Is Tl;
+            const uint32_t ti = (uint32_t)((m + Tl::kM - 1) / Tl::kM), tj = (uint32_t)((n + Tl::kN - 1) / Tl::kN);
+            const Result o = {q.out, tall, q.update, q.keep, q.gain, q.ldo, q.out_stride, q.rows, q.cols};
+            auto go = [&](auto kernel, float back) {
+                kernel<<<ti * tj * batch, Tl::kThreads, 0, s>>>(by, xt[from], x[1 - from], xt[1 - from], (uint32_t)m, (uint32_t)n, ti, tj, back, o);
+            };
+            if (!last)
+                go(k_apply<Tl, Full, false, float>, 1.0f / sb);
+            else if (q.out_type == kGradF32)
+                go(k_apply<Tl, Full, true, float>, 1.0f / (sx * sb));
+            else if (q.out_type == kGradF16)
+                go(k_apply<Tl, Full, true, _Float16>, 1.0f / (sx * sb));
+            else
+                go(k_apply<Tl, Full, true, __bf16>, 1.0f / (sx * sb));
+        });
+    };
+    const std::true_type with_poly;
+    const std::false_type plain;
+    const int group = group_of(q, m, n, Full);
+    for (int done = 0, from = 0; done < q.steps; from = 1 - from) {
+        const int steps = q.steps - done < group ? q.steps - done : group;
+        const Symmetric gram = product(x[from], sx, x[from], sx, g[0], sx);
+        symmetric(plain, 1, gram, gram);
+        symmetric(with_poly, 1, poly(g[0], pm[0]), gram);
+        Plane by = pm[0];
+        float sb = sp, grown = top;
+        for (int k = 1; k < steps; ++k) {
+            const int now = k & 1, was = 1 - now;
+            // T = P G (with it the Q of the step before, which waits for the same P), G = T P, P of it
+            const Symmetric t = product(pm[was], sp, g[was], sx, tm, st);
+            if (k > 1) {
+                const Symmetric grow = product(pm[was], sp, by, sb, qm[was], scale(grown * top));
+                symmetric(plain, 2, t, grow);
+                by = qm[was], sb = scale(grown *= top);
+            } else {
+                symmetric(plain, 1, t, t);
+            }
+            const Symmetric next = product(tm, st, pm[was], sp, g[now], sx);
+            symmetric(plain, 1, next, next);
+            symmetric(with_poly, 1, poly(g[now], pm[now]), next);
+            if (k + 1 == steps) {
+                const Symmetric grow = product(pm[now], sp, by, sb, qm[now], scale(grown * top));
+                symmetric(plain, 1, grow, grow);
+                by = qm[now], sb = scale(grown *= top);
+            }
+        }
+        done += steps;
+        apply(by, sb, from, done == q.steps);
     }
 }
 

@@ -409,5 +409,34 @@ struct Tile {
     }
 };
 
+// ---- which tile ----
+//
+// A product's time is the rounds of its tiles, `slots` at a time, by what a line of the rows takes in each and what a tile
+// takes besides (its first loads, its stores).  Measured, us: see DESIGN.  Large tiles read less for an operation, small ones
+// leave less of the last round empty.
+struct TileCost {
+    int side;
+    float alone, line, fixed;  // a line of 128 bytes where a CU has one tile, or as many as it takes; a tile's rest
+    int per_cu;
+};
+constexpr TileCost kTileCosts[] = {{256, 1.67f, 1.67f, 8.0f, 1}, {192, 1.0f, 1.0f, 6.0f, 1}, {128, 0.5f, 0.88f, 5.0f, 2}, {64, 0.17f, 0.30f, 4.0f, 2}};
+constexpr int kCus = 256;
+
+// count(side): tiles of the whole launch.  Returns an index of kTileCosts.
+template <class Count>
+inline int best_tile(const Count& count, int64_t lines)
+{
+    int best = 0;
+    double least = 0.0;
+    for (int i = 0; i < 4; ++i) {
+        const TileCost& c = kTileCosts[i];
+        const int64_t n = count(c.side), slots = (int64_t)kCus * c.per_cu, rounds = n / slots, left = n % slots;
+        double t = (double)rounds * (lines * c.line + c.fixed);
+        if (left) t += lines * (left <= kCus ? c.alone : c.line) + c.fixed;
+        if (i == 0 || t < least) least = t, best = i;
+    }
+    return best;
+}
+
 }  // namespace sidco
 #endif
