@@ -313,14 +313,37 @@ template <class E, class Tl>
 __global__ __launch_bounds__(Tl::kThreads) void k_mx4_product(Mx4Product p, uint32_t tm, uint32_t tn)
 {
     __shared__ __align__(1024) char lds[Tl::kLds];
-    uint32_t i, j;
-    tile_of(xcd_run(blockIdx.x, tm * tn), tm, tn, i, j);
     const uint32_t pitch = (uint32_t)(mx4_padded(p.k) / 2);
     const Rows a = {p.a, p.a_scales, (uint32_t)p.m, pitch}, b = {p.b, p.b_scales, (uint32_t)p.n, pitch};
     Tl t;
-    t.clear();
-    t.run(a, b, i * Tl::kM, j * Tl::kN, lds);
-    t.each([&](uint32_t m, uint32_t n, const v4f& acc) { store_product<E>(p, (int64_t)i * Tl::kM + m, (int64_t)j * Tl::kN + n, acc); });
+    auto place = [&](uint32_t tile, uint32_t& m0, uint32_t& n0) {
+        uint32_t i, j;
+        tile_of(xcd_run(tile, tm * tn), tm, tn, i, j);
+        m0 = i * Tl::kM;
+        n0 = j * Tl::kN;
+    };
+    t.template run<1>(
+        tm * tn, pitch, lds,
+        [&](uint32_t tile, int) {
+            uint32_t m0, n0;
+            place(tile, m0, n0);
+            t.take(a, b, m0, n0);
+        },
+        [&](uint32_t tile) {
+            uint32_t m0, n0;
+            place(tile, m0, n0);
+            if (m0 + Tl::kM <= p.m && n0 + Tl::kN <= p.n && !p.accumulate) {
+                typedef typename E::T T;
+                typedef T t4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+                T* c = (T*)p.c + (int64_t)m0 * p.ldc + n0;
+                t.each([&](uint32_t m, uint32_t n, const v4f& v) {
+                    *(t4*)(c + (int64_t)m * p.ldc + n) = t4{E::narrow(p.alpha * v[0]), E::narrow(p.alpha * v[1]), E::narrow(p.alpha * v[2]),
+                                                            E::narrow(p.alpha * v[3])};
+                });
+            } else {
+                t.each([&](uint32_t m, uint32_t n, const v4f& v) { store_product<E>(p, (int64_t)m0 + m, (int64_t)n0 + n, v); });
+            }
+        });
 }
 
 __device__ __forceinline__ v4f multiply16(const v4i& a, const v4i& b, const v4f& c, int sa, int sb)
@@ -450,13 +473,13 @@ void launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t 
 
 void launch_mx4_product(const Mx4Product& p, hipStream_t s)
 {
+    const int pick = best_tile([&](int64_t b) { return ((p.m + b - 1) / b) * ((p.n + b - 1) / b); }, mx4_padded(p.k) / 2 / kLine);
     auto go = [&](auto e, auto t) {
         typedef decltype(e) E;
         typedef typename decltype(t)::Is Tl;
         const uint32_t tm = (uint32_t)((p.m + Tl::kM - 1) / Tl::kM), tn = (uint32_t)((p.n + Tl::kN - 1) / Tl::kN);
-        k_mx4_product<E, Tl><<<tm * tn, Tl::kThreads, 0, s>>>(p, tm, tn);
+        k_mx4_product<E, Tl><<<tile_blocks(pick, (int64_t)tm * tn), Tl::kThreads, 0, s>>>(p, tm, tn);
     };
-    const int pick = best_tile([&](int64_t b) { return ((p.m + b - 1) / b) * ((p.n + b - 1) / b); }, mx4_padded(p.k) / 2 / kLine);
     by_type(p.type, [&](auto e) {
         if (pick == 0)
             go(e, Shape<Tile<Mx4Core, 256, 256, 2, 2, 2, 2>>());

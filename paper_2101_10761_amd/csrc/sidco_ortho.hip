@@ -189,16 +189,17 @@ __device__ __forceinline__ Rows rows_of(const Plane& o, int64_t z, uint32_t rows
     return {o.at + z * o.stride + (low ? o.low : 0), nullptr, rows, (uint32_t)o.pitch * 2};
 }
 
-template <class Tl, bool Full>
-__device__ __forceinline__ void products(Tl& t, const Plane& a, const Plane& b, int64_t z, uint32_t ra, uint32_t rb, uint32_t m0, uint32_t n0,
-                                         char* lds)
+// Operands of the terms of a product: with pairs of halves the small ones first.
+template <bool Full, class Tl>
+__device__ __forceinline__ void take(Tl& t, int term, const Plane& a, const Plane& b, int64_t z, uint32_t ra, uint32_t rb, uint32_t m0, uint32_t n0)
 {
-    t.clear();
-    if (Full) {  // the small ones first
-        t.run(rows_of(a, z, ra, true), rows_of(b, z, rb), m0, n0, lds);
-        t.run(rows_of(a, z, ra), rows_of(b, z, rb, true), m0, n0, lds);
-    }
-    t.run(rows_of(a, z, ra), rows_of(b, z, rb), m0, n0, lds);
+    t.take(rows_of(a, z, ra, Full && term == 0), rows_of(b, z, rb, Full && term == 1), m0, n0);
+}
+
+template <class Tl>
+constexpr int lds_of()
+{
+    return Tl::kLds + Tl::kWaves * Tl::template out_bytes<_Float16>();
 }
 
 // A product of two symmetric matrices that commute, A B^T = A B: symmetric too.  out = p2 A B + p1 B + p0 I, all with the
@@ -210,35 +211,52 @@ struct Symmetric {
 
 // One or two of them of the same size.  Tiles on and below the diagonal are computed and mirrored.
 template <class Tl, bool Full, bool Poly>
-__global__ __launch_bounds__(Tl::kThreads) void k_symmetric(Symmetric first, Symmetric second, uint32_t m, uint32_t tiles, uint32_t each)
+__global__ __launch_bounds__(Tl::kThreads) void k_symmetric(Symmetric first, Symmetric second, uint32_t m, uint32_t tiles, uint32_t each,
+                                                            uint32_t total)
 {
     constexpr int B = Tl::kM;
-    __shared__ __align__(1024) char lds[Tl::kLds];
-    uint32_t w = xcd_run(blockIdx.x, gridDim.x);
-    const Symmetric& p = w < each ? first : second;
-    w = w < each ? w : w - each;
-    const int64_t z = w / tiles;
-    uint32_t i, j;
-    tile_of_triangle(w % tiles, i, j);
-    Tl t;
-    products<Tl, Full>(t, p.a, p.b, z, m, m, i * B, j * B, lds);
-    __syncthreads();
-    const float p2 = p.p2, p1 = p.p1, p0 = p.p0;
-    auto value = [&](uint32_t r, uint32_t c, const v4f& v) -> v4f {
-        if (!Poly) return v * p2;
-        v4f w = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (r < m && c < (uint32_t)p.b.pitch) {
-            const _Float16* g = p.b.at + z * p.b.stride + (int64_t)r * p.b.pitch + c;
-            const v4h h = *(const v4h*)g;
-            v4h l = {0, 0, 0, 0};
-            if (Full) l = *(const v4h*)(g + p.b.low);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = fmaf(p2, v[k], fmaf(p1, (float)h[k] + (float)l[k], r == c + k ? p0 : 0.0f));
-        }
-        return w;
+    __shared__ __align__(1024) char lds[lds_of<Tl>()];
+    struct Place {
+        bool second;
+        int64_t z;
+        uint32_t m0, n0;
     };
-    put_tile<false, Full>(t, lds, p.out, z, m, m, i * B, j * B, value);
-    if (i != j) put_tile<true, Full>(t, lds, p.out, z, m, m, i * B, j * B, value);
+    auto place = [&](uint32_t tile) -> Place {
+        uint32_t w = xcd_run(tile, total), i, j;
+        const bool other = w >= each;
+        if (other) w -= each;
+        tile_of_triangle(w % tiles, i, j);
+        return {other, w / tiles, i * B, j * B};
+    };
+    Tl t;
+    t.template run<Full ? 3 : 1>(
+        total, (uint32_t)first.a.pitch * 2, lds,
+        [&](uint32_t tile, int term) {
+            const Place at = place(tile);
+            const Symmetric& p = at.second ? second : first;
+            take<Full>(t, term, p.a, p.b, at.z, m, m, at.m0, at.n0);
+        },
+        [&](uint32_t tile) {
+            const Place at = place(tile);
+            const Symmetric& p = at.second ? second : first;
+            const Plane g = p.b;
+            const float p2 = p.p2, p1 = p.p1, p0 = p.p0;
+            auto value = [&](uint32_t r, uint32_t c, const v4f& v) -> v4f {
+                if (!Poly) return v * p2;
+                v4f w = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (r < m && c < (uint32_t)g.pitch) {
+                    const _Float16* q = g.at + at.z * g.stride + (int64_t)r * g.pitch + c;
+                    const v4h h = *(const v4h*)q;
+                    v4h l = {0, 0, 0, 0};
+                    if (Full) l = *(const v4h*)(q + g.low);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[k] = fmaf(p2, v[k], fmaf(p1, (float)h[k] + (float)l[k], r == c + k ? p0 : 0.0f));
+                }
+                return w;
+            };
+            put_tile<false, Full>(t, lds + Tl::kLds, p.out, at.z, m, m, at.m0, at.n0, value);
+            if (at.m0 != at.n0) put_tile<true, Full>(t, lds + Tl::kLds, p.out, at.z, m, m, at.m0, at.n0, value);
+        });
 }
 
 // What the last product goes to: the result, or weights that move by it.
@@ -277,28 +295,41 @@ __device__ __forceinline__ void finish4(const Result& o, int64_t z, int64_t r, i
 // X' = Q X: X' and its transpose, or with Last the result, of element type T.
 template <class Tl, bool Full, bool Last, class T>
 __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plane x2, Plane xt2, uint32_t m, uint32_t n, uint32_t tm, uint32_t tn,
-                                                        float back, Result o)
+                                                        uint32_t total, float back, Result o)
 {
     constexpr int B = Tl::kM;
-    __shared__ __align__(1024) char lds[Tl::kLds];
-    const uint32_t w = xcd_run(blockIdx.x, gridDim.x);
-    const int64_t z = w / (tm * tn);
-    uint32_t i, j;
-    tile_of(w % (tm * tn), tm, tn, i, j);
+    __shared__ __align__(1024) char lds[lds_of<Tl>()];
+    struct Place {
+        int64_t z;
+        uint32_t m0, n0;
+    };
+    auto place = [&](uint32_t tile) -> Place {
+        const uint32_t w = xcd_run(tile, total);
+        uint32_t i, j;
+        tile_of(w % (tm * tn), tm, tn, i, j);
+        return {w / (tm * tn), i * B, j * B};
+    };
     Tl t;
-    products<Tl, Full>(t, pm, xt, z, m, n, i * B, j * B, lds);
-    __syncthreads();
-    auto value = [&](uint32_t, uint32_t, const v4f& v) -> v4f { return v * back; };
-    if (!Last) {
-        put_tile<false, Full>(t, lds, x2, z, m, n, i * B, j * B, value);
-        put_tile<true, Full>(t, lds, xt2, z, m, n, i * B, j * B, value);
-    } else if (o.tall) {
-        t.each([&](uint32_t r, uint32_t c, const v4f& v) {
-            finish4<T>(o, z, j * B + c + (threadIdx.x & 3), (i * B + r) & ~3u, Tl::turned(v * back));
+    t.template run<Full ? 3 : 1>(
+        total, (uint32_t)pm.pitch * 2, lds,
+        [&](uint32_t tile, int term) {
+            const Place at = place(tile);
+            take<Full>(t, term, pm, xt, at.z, m, n, at.m0, at.n0);
+        },
+        [&](uint32_t tile) {
+            const Place at = place(tile);
+            auto value = [&](uint32_t, uint32_t, const v4f& v) -> v4f { return v * back; };
+            if (!Last) {
+                put_tile<false, Full>(t, lds + Tl::kLds, x2, at.z, m, n, at.m0, at.n0, value);
+                put_tile<true, Full>(t, lds + Tl::kLds, xt2, at.z, m, n, at.m0, at.n0, value);
+            } else if (o.tall) {
+                t.each([&](uint32_t r, uint32_t c, const v4f& v) {
+                    finish4<T>(o, at.z, at.n0 + c + (threadIdx.x & 3), (at.m0 + r) & ~3u, Tl::turned(v * back));
+                });
+            } else {
+                t.each([&](uint32_t r, uint32_t c, const v4f& v) { finish4<T>(o, at.z, at.m0 + r, at.n0 + c, v * back); });
+            }
         });
-    } else {
-        t.each([&](uint32_t r, uint32_t c, const v4f& v) { finish4<T>(o, z, i * B + r, j * B + c, v * back); });
-    }
 }
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -413,7 +444,8 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
         by_tile(pick, [&](auto shape) {
             typedef typename decltype(shape)::Is Tl;
             const uint32_t tri = (uint32_t)triangle(m, Tl::kM), each = tri * batch;
-            k_symmetric<Tl, Full, decltype(poly)::value><<<each * jobs, Tl::kThreads, 0, s>>>(a, b, (uint32_t)m, tri, each);
+            k_symmetric<Tl, Full, decltype(poly)::value>
+                <<<tile_blocks(pick, each * jobs), Tl::kThreads, 0, s>>>(a, b, (uint32_t)m, tri, each, each * jobs);
         });
     };
     auto product = [](const Plane& a, float sa, const Plane& b, float sb, const Plane& o, float so) -> Symmetric {
@@ -427,7 +459,9 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
             const uint32_t ti = (uint32_t)((m + Tl::kM - 1) / Tl::kM), tj = (uint32_t)((n + Tl::kN - 1) / Tl::kN);
             const Result o = {q.out, tall, q.update, q.keep, q.gain, q.ldo, q.out_stride, q.rows, q.cols};
             auto go = [&](auto kernel, float back) {
-                kernel<<<ti * tj * batch, Tl::kThreads, 0, s>>>(by, xt[from], x[1 - from], xt[1 - from], (uint32_t)m, (uint32_t)n, ti, tj, back, o);
+                const uint32_t total = ti * tj * batch;
+                kernel<<<tile_blocks(apply_pick, total), Tl::kThreads, 0, s>>>(by, xt[from], x[1 - from], xt[1 - from], (uint32_t)m, (uint32_t)n, ti, tj,
+                                                                              total, back, o);
             };
             if (!last)
                 go(k_apply<Tl, Full, false, float>, 1.0f / sb);

@@ -146,7 +146,7 @@ struct Tile {
     static_assert(Stages >= 2 && kLds <= 160 * 1024, "LDS of a CU");
 
     v4f acc[kMt][kNt];
-    v4i from_a, from_b, from_sa, from_sb;
+    v4i from_a, from_b, from_s[kLoadsS + 1];
     uint32_t src[kLoadsA + kLoadsB];  // this lane's 16 bytes of each load's rows
     uint32_t ssrc[kLoadsS + 1];
     uint32_t fours;                   // of the rows
@@ -174,36 +174,44 @@ struct Tile {
         return Fours == 2 ? piece ^ (row & 7) : piece ^ (row >> 1 & 3);
     }
 
-    // Rows past the operand's end read its last row: their products are not stored.
-    __device__ __forceinline__ void aim(const Rows& a, const Rows& b, uint32_t m0, uint32_t n0)
+    // The lanes' places in a stage, the same for every tile.
+    __device__ __forceinline__ void aim(uint32_t pitch)
     {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        fours = pitch / 64;
+        const int r = lane / (4 * Fours), c = place(r, lane % (4 * Fours));  // a load's first row is a multiple of 8
+#pragma unroll
+        for (int k = 0; k < kLoadsA + kLoadsB; ++k)
+            src[k] = (uint32_t)(((k < kLoadsA ? k : k - kLoadsA) * kWaves + wave) * kRowsLoad + r) * pitch + c * 16;
+#pragma unroll
+        for (int k = 0; k < kLoadsS; ++k) {
+            const uint32_t at = (uint32_t)(k * kWaves + wave) * kRowsExps;  // row of the tile, B's after A's
+            ssrc[k] = ((at < BM ? at : at - BM) + lane / Fours) * (pitch / 16) + lane % Fours * 4;
+        }
+    }
+
+    // The tile whose stages are fetched from now on.  Rows past the operand's end are out of range: zeros come for them.
+    __device__ __forceinline__ void take(const Rows& a, const Rows& b, uint32_t m0, uint32_t n0)
+    {
         const uint32_t ra = a.rows - m0 < BM ? a.rows - m0 : BM, rb = b.rows - n0 < BN ? b.rows - n0 : BN;
         from_a = resource((const char*)a.data + (size_t)m0 * a.pitch, ra * a.pitch);
         from_b = resource((const char*)b.data + (size_t)n0 * b.pitch, rb * b.pitch);
-        const int r = lane / (4 * Fours), c = place(r, lane % (4 * Fours));  // a load's first row is a multiple of 8
 #pragma unroll
-        for (int k = 0; k < kLoadsA + kLoadsB; ++k) {
-            const bool first = k < kLoadsA;
-            const uint32_t row = (uint32_t)((first ? k : k - kLoadsA) * kWaves + wave) * kRowsLoad + r;
-            const uint32_t last = (first ? ra : rb) - 1;
-            src[k] = (row < last ? row : last) * (first ? a.pitch : b.pitch) + c * 16;
+        for (int k = 0; k < kLoadsS; ++k) {
+            const bool first = (k * kWaves + wave) * kRowsExps < BM;
+            const uint32_t exps = (first ? a.pitch : b.pitch) / 16;
+            from_s[k] = resource((const char*)(first ? a.scales : b.scales) + (size_t)(first ? m0 : n0) * exps, (first ? ra : rb) * exps);
         }
-        if (Core::kScaled) {
-            from_sa = resource((const char*)a.scales + (size_t)m0 * (a.pitch / 16), ra * (a.pitch / 16));
-            from_sb = resource((const char*)b.scales + (size_t)n0 * (b.pitch / 16), rb * (b.pitch / 16));
+    }
+    __device__ __forceinline__ void take_nothing()
+    {
+        from_a[2] = from_b[2] = 0;
 #pragma unroll
-            for (int k = 0; k < kLoadsS; ++k) {
-                const uint32_t at = (uint32_t)(k * kWaves + wave) * kRowsExps;  // row of the tile, B's after A's
-                const uint32_t row = (at < BM ? at : at - BM) + lane / Fours, last = (at < BM ? ra : rb) - 1;
-                ssrc[k] = (row < last ? row : last) * ((at < BM ? a.pitch : b.pitch) / 16) + lane % Fours * 4;
-            }
-        }
-        fours = a.pitch / 64;
+        for (int k = 0; k < kLoadsS; ++k) from_s[k][2] = 0;
     }
 
-    // Load k of stage number u; one that the operands do not have is out of range for the load, which then fetches nothing.
+    // Load k of stage number u of the tile taken.
     template <int K>
     __device__ __forceinline__ void fetch(uint32_t u, char* stage) const
     {
@@ -211,13 +219,9 @@ struct Tile {
         if constexpr (kS < 0) {
             constexpr bool kFirst = K < kLoadsA;
             constexpr int kAt = kFirst ? kAtA + K * kWaves * 1024 : kAtB + (K - kLoadsA) * kWaves * 1024;
-            v4i from = kFirst ? from_a : from_b;
-            from[2] = u * Fours < fours ? from[2] : 0;
-            to_lds<16, kAt>(from, src[K], u * kSeg, stage + wave * 1024);
+            to_lds<16, kAt>(kFirst ? from_a : from_b, src[K], u * kSeg, stage + wave * 1024);
         } else {
-            v4i from = (kS * kWaves + wave) * kRowsExps < BM ? from_sa : from_sb;
-            from[2] = u * Fours < fours ? from[2] : 0;
-            to_lds<4, kS * kWaves * 256>(from, ssrc[kS], u * kExps, stage + wave * 256);
+            to_lds<4, kS * kWaves * 256>(from_s[kS], ssrc[kS], u * kExps, stage + wave * 256);
         }
     }
     template <int From, int To>
@@ -286,54 +290,86 @@ struct Tile {
         }
     }
 
-    // Adds the products over the rows' whole length.  Every wave of the block calls it; LDS is free again when the next one
-    // fetches.  While four pieces are multiplied the next four are read from LDS into other registers.  Once every wave has
-    // read the last of a stage its place is free, and the stage after it has to be there: one barrier a stage.
-    __device__ __forceinline__ void run(const Rows& a, const Rows& b, uint32_t m0, uint32_t n0, char* lds)
+    // Works tile after tile of this block's: number blockIdx.x, gridDim.x after that and so on below `tiles`.  A tile's sum is
+    // over `Terms` products of operands with the same pitch:
+    //   operands(tile, term) takes them (take)
+    //   finish(tile)         is called with the sums
+    // While four pieces are multiplied the next four are read from LDS into other registers.  Once every wave has read the last
+    // of a stage its place is free, and the stage after it has to be there: one barrier a stage.  The stages of all tiles are
+    // one sequence: the next tile's are under way while this one's sums go out.
+    template <int Terms, class Operands, class Finish>
+    __device__ __forceinline__ void run(uint32_t tiles, uint32_t pitch, char* lds, const Operands& operands, const Finish& finish)
     {
-        aim(a, b, m0, n0);
-        __syncthreads();  // the stages may still be read for what was computed before
+        aim(pitch);
+        const uint32_t stages = fours / Fours;
+        uint32_t coming = blockIdx.x, u = 0;  // the tile, term and stage fetched next
+        int term = 0;
+        operands(coming, term);
+        auto advance = [&] {
+            if (++u < stages) return;
+            u = 0;
+            if (++term == Terms) term = 0, coming += gridDim.x;
+            if (coming < tiles)
+                operands(coming, term);
+            else
+                take_nothing();
+        };
 #pragma unroll
-        for (int s = 0; s < Stages; ++s) fetch_range<0, kLoads>(s, lds + s * kStage);
+        for (int s = 0; s < Stages; ++s) {
+            fetch_range<0, kLoads>(u, lds + s * kStage);
+            advance();
+        }
         wait_loads<(Stages - 1) * kLoads>();
         __builtin_amdgcn_s_barrier();
         Part p0, p1;
 #pragma unroll
         for (int n = 0; n < kMt + kNt; ++n) read(p0, lds, 0, n);
         char *stage = lds, *const end = lds + kLds;
-        auto turn = [&](const Part& p, Part& next, uint32_t u) {
-            wait_loads<(Stages - 2) * kLoads>();
+        auto turn = [&](const Part& p, Part& next, uint32_t all) {
+            if (Stages > 2 && !all)
+                wait_loads<(Stages - 2) * kLoads>();
+            else
+                wait_loads<0>();
             __builtin_amdgcn_s_barrier();
             char* to = stage;
             stage = stage + kStage == end ? lds : stage + kStage;
-            multiply<true, true>(p, next, stage, 0, u + Stages, to);
+            multiply<true, true>(p, next, stage, 0, u, to);
+            advance();
         };
-        // Rows are whole lines: an even number of fours.  The last turn reads what follows the last stage, which nothing uses;
-        // a loop without an end of its own leaves the sums in their registers.
-        uint32_t u = 0, f = 0;
-        do {
-            if (Fours == 2)
-                multiply<true, false>(p0, p1, stage, 1, 0, nullptr);
-            else
-                turn(p0, p1, u++);
-            turn(p1, p0, u++);
-            f += 2;
-        } while (f < fours);
+        for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+            clear();
+            hold();
+            // Rows are whole lines: an even number of fours.  The last turn of all reads what follows the last stage, which
+            // nothing uses.  The first turn waits for everything: stores of the tile before may be counted among the loads.
+            uint32_t f = 0, fresh = 1;
+            do {
+                if (Fours == 2)
+                    multiply<true, false>(p0, p1, stage, 1, 0, nullptr);
+                else
+                    turn(p0, p1, fresh);
+                turn(p1, p0, fresh);
+                fresh = 0;
+                asm volatile("" : "+s"(fresh));  // a copy of the loop for its first turn would move the sums
+                f += 2;
+            } while (f < Terms * fours);
+            rest();
+            hold();
+            finish(tile);
+        }
         wait_loads<0>();
-        rest();
-        hold();
     }
 
     // f(row, column, 4 values): C's row and the first of four neighbouring columns, relative to the tile.
     template <class F>
     __device__ __forceinline__ void each(const F& f) const
     {
-        const int wm = wave / WN, wn = wave % WN;
+        uint32_t row = wave / WN * (BM / WM) + (lane & 15), col = wave % WN * (BN / WN) + 4 * (lane >> 4);
 #pragma unroll
-        for (int i = 0; i < kMt; ++i)
+        for (int i = 0; i < kMt; ++i) {
+            asm volatile("" : "+v"(row), "+v"(col));  // addresses of later rows are not kept from here on
 #pragma unroll
-            for (int j = 0; j < kNt; ++j)
-                f((uint32_t)(wm * (BM / WM) + i * 16 + (lane & 15)), (uint32_t)(wn * (BN / WN) + j * 16 + 4 * (lane >> 4)), acc[i][j]);
+            for (int j = 0; j < kNt; ++j) f(row + i * 16, col + j * 16, acc[i][j]);
+        }
     }
 
     // ---- by way of LDS ----
@@ -343,7 +379,7 @@ struct Tile {
 
     static constexpr int pad(int bytes) { return bytes + 16; }
     template <class S>
-    static constexpr int out_bytes()  // of LDS for each wave
+    static constexpr int out_bytes()  // of LDS for each wave, besides the stages
     {
         return 16 * pad((kNt > kMt ? kNt : kMt) * 16 * (int)sizeof(S));
     }
@@ -370,8 +406,8 @@ struct Tile {
     }
 
     // value(row, column, sums) gives the four values of C's row from a column on; store(row, column, 16 bytes of S) takes
-    // neighbours of a row - with Turn of a column: row and column are C's, exchanged.  All relative to the tile.  Every wave
-    // of the block calls it, after a barrier since run(); `lds` has out_bytes<S>() for each wave.
+    // neighbours of a row - with Turn of a column: row and column are C's, exchanged.  All relative to the tile.  `lds`
+    // has out_bytes<S>() for each wave.
     template <class S, bool Turn, class Value, class Store>
     __device__ __forceinline__ void out(char* lds, const Value& value, const Store& store)
     {
@@ -383,9 +419,10 @@ struct Tile {
         typedef S sv __attribute__((ext_vector_type(kPer)));
         char* mine = lds + wave * out_bytes<S>();
         const int r = lane & 15, q = lane >> 4;
-        const int row0 = wave / WN * (BM / WM), col0 = wave % WN * (BN / WN);
+        uint32_t row0 = wave / WN * (BM / WM), col0 = wave % WN * (BN / WN);
 #pragma unroll
         for (int x = 0; x < kStrips; ++x) {
+            asm volatile("" : "+v"(row0), "+v"(col0));  // addresses of later strips are not kept from here on
 #pragma unroll
             for (int y = 0; y < kTiles; ++y) {
                 const int i = Turn ? y : x, j = Turn ? x : y;
@@ -423,6 +460,13 @@ constexpr TileCost kTileCosts[] = {{256, 1.67f, 1.67f, 8.0f, 1}, {192, 1.0f, 1.0
 constexpr int kCus = 256;
 
 // count(side): tiles of the whole launch.  Returns an index of kTileCosts.
+// Blocks of a launch of that many tiles: each works one after the other.
+inline uint32_t tile_blocks(int pick, int64_t tiles)
+{
+    const int64_t most = (int64_t)kCus * kTileCosts[pick].per_cu;
+    return (uint32_t)(tiles < most ? tiles : most);
+}
+
 template <class Count>
 inline int best_tile(const Count& count, int64_t lines)
 {
