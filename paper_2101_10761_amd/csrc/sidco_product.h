@@ -448,25 +448,21 @@ struct Tile {
 
 // ---- which tile ----
 //
-// A product's time is the rounds of its tiles, `slots` at a time, by what a line of the rows takes in each and what a tile
-// takes besides (its first loads, its stores).  Measured, us: see DESIGN.  Large tiles read less for an operation, small ones
-// leave less of the last round empty.
+// A product's time is the rounds of its tiles by what a line of the rows takes in each, and what a round and the launch take
+// besides (first loads, stores).  Large tiles read less for an operation, small ones leave less of the last round empty and
+// are done sooner where there are few.  Measured on 4-bit products with one tile for all, us, tiles of 256, 192, 128, 64:
+//   8192 x 8192 x 8192 258 313 356 605; 4096 x 4096 x 25088 185 234 270 506; 4096 x 25088 x 4096 (fp32) 281 308 392 718;
+//   3000 x 3000 x 4096 35.4 27.7 39.2 46.2; 2048 x 2048 x 2048 23.1 17.9 12.1 14.7; 1024 x 1024 x 1024 16.8 12.3 8.9 8.7;
+//   700 x 1500 x 6000 39.7 29.0 20.5 16.4; 6000 x 1500 x 700 18.0 15.0 15.0 15.5; 100 x 4096 x 4096 30.3 22.5 14.1 9.1.
 struct TileCost {
-    int side;
-    float alone, line, fixed;  // a line of 128 bytes where a CU has one tile, or as many as it takes; a tile's rest
-    int per_cu;
+    int side, per_cu;
+    float alone, line;    // us a line of 128 bytes, one tile to a CU or per_cu of them
+    float round, launch;  // us besides
 };
-constexpr TileCost kTileCosts[] = {{256, 1.67f, 1.67f, 8.0f, 1}, {192, 1.0f, 1.0f, 6.0f, 1}, {128, 0.5f, 0.88f, 5.0f, 2}, {64, 0.17f, 0.30f, 4.0f, 2}};
+constexpr TileCost kTileCosts[] = {{256, 1, 1.55f, 1.75f, 7.0f, 10.0f}, {192, 1, 1.05f, 1.10f, 6.0f, 8.0f}, {128, 2, 0.80f, 1.25f, 2.5f, 5.5f}, {64, 2, 0.25f, 0.58f, 2.0f, 4.5f}};
 constexpr int kCus = 256;
 
 // count(side): tiles of the whole launch.  Returns an index of kTileCosts.
-// Blocks of a launch of that many tiles: each works one after the other.
-inline uint32_t tile_blocks(int pick, int64_t tiles)
-{
-    const int64_t most = (int64_t)kCus * kTileCosts[pick].per_cu;
-    return (uint32_t)(tiles < most ? tiles : most);
-}
-
 template <class Count>
 inline int best_tile(const Count& count, int64_t lines)
 {
@@ -474,12 +470,19 @@ inline int best_tile(const Count& count, int64_t lines)
     double least = 0.0;
     for (int i = 0; i < 4; ++i) {
         const TileCost& c = kTileCosts[i];
-        const int64_t n = count(c.side), slots = (int64_t)kCus * c.per_cu, rounds = n / slots, left = n % slots;
-        double t = (double)rounds * (lines * c.line + c.fixed);
-        if (left) t += lines * (left <= kCus ? c.alone : c.line) + c.fixed;
+        const int64_t n = count(c.side), slots = (int64_t)kCus * c.per_cu, left = n % slots;
+        double t = c.launch + (double)(n / slots) * (lines * c.line + c.round);
+        if (left) t += lines * (left <= kCus ? c.alone : c.line) + c.round;
         if (i == 0 || t < least) least = t, best = i;
     }
     return best;
+}
+
+// Blocks of a launch of that many tiles: each works one after the other.
+inline uint32_t tile_blocks(int pick, int64_t tiles)
+{
+    const int64_t most = (int64_t)kCus * kTileCosts[pick].per_cu;
+    return (uint32_t)(tiles < most ? tiles : most);
 }
 
 }  // namespace sidco
