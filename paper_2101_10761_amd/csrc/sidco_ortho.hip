@@ -38,6 +38,18 @@ struct Elem<kGradBf16> {
     typedef __bf16 T;
 };
 
+// f(Elem) for an element type
+template <class F>
+void by_element(int type, const F& f)
+{
+    if (type == kGradF32)
+        f(Elem<kGradF32>());
+    else if (type == kGradF16)
+        f(Elem<kGradF16>());
+    else
+        f(Elem<kGradBf16>());
+}
+
 // ---- the start: momentum, norm, X and its transpose ----
 
 // Sum over the block; the result is thread 0's.
@@ -292,6 +304,14 @@ __device__ __forceinline__ void finish4(const Result& o, int64_t z, int64_t r, i
     }
 }
 
+template <class T>
+__device__ __forceinline__ void finish1(const Result& o, int64_t z, int64_t r, int64_t c, float v)
+{
+    if (r >= o.rows || c >= o.cols) return;
+    T* p = (T*)o.out + z * o.stride + r * o.ld + c;
+    *p = (T)(o.update ? fmaf(o.gain, v, o.keep * (float)*p) : v);
+}
+
 // X' = Q X: X' and its transpose, or with Last the result, of element type T.
 template <class Tl, bool Full, bool Last, class T>
 __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plane x2, Plane xt2, uint32_t m, uint32_t n, uint32_t tm, uint32_t tn,
@@ -330,6 +350,302 @@ __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plan
                 t.each([&](uint32_t r, uint32_t c, const v4f& v) { finish4<T>(o, at.z, at.m0 + r, at.n0 + c, v * back); });
             }
         });
+}
+
+// ---- a matrix in one block ----
+//
+// With m <= 64 and X^T in LDS one block does everything, all steps in one launch; the launches of the kernels above, 2 and 15
+// for 5 steps, take longer than their work at this size.  X^T is kept by rows of 64 (m padded with zeros), so that
+//   G = X X^T  reads its operands down the columns, with the transposing read of LDS, each wave a part of X's length,
+//   X <- P X   reads rows and writes them in place: a row of X^T depends on that row alone, and each wave has its own.
+// G stays fp32 between the two and P is a pair of halves whatever X is, both being small; G's parts are added up in the order of the waves.  16-byte pieces c of row r are kept at place
+// c ^ (r % 8) of a row of halves and c ^ (r % 16) of a row of floats.
+constexpr int kOneWaves = 8, kOneSide = 64;
+
+struct One {
+    const void* x;
+    int64_t ldx, x_stride;
+    float* momentum;
+    float mu;
+    bool nesterov;
+    int rows, cols, m, n;
+    int steps;
+    float a, b, c, eps, sp;
+    int out_type;
+    Result o;
+};
+
+__device__ __forceinline__ v4h highs(const v4f& v) { return v4h{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]}; }
+
+__device__ __forceinline__ v4f mul16(const v8h& a, const v8h& b, const v4f& c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+template <bool Full>
+__device__ __forceinline__ v4f mul16(const v8h (&a)[2], const v8h (&b)[2], v4f c)
+{
+    if (Full) {
+        c = mul16(a[1], b[0], c);
+        c = mul16(a[0], b[1], c);
+    }
+    return mul16(a[0], b[0], c);
+}
+
+// a pair of halves times a pair, or with Full false times the high half alone
+template <bool Full>
+__device__ __forceinline__ v4f mul16_pair(const v8h (&a)[2], const v8h (&b)[2], v4f c)
+{
+    c = mul16(a[1], b[0], c);
+    if (Full) c = mul16(a[0], b[1], c);
+    return mul16(a[0], b[0], c);
+}
+
+// Cap: rows of X^T that LDS has room for
+template <class T, int Cap, bool Full>
+__global__ __launch_bounds__(64 * kOneWaves) void k_one(One p)
+{
+    constexpr int kPlanes = Full ? 2 : 1, kRow = kOneSide * 2, kPlane = Cap * kRow;
+    __shared__ __align__(16) char xt[kPlanes * kPlane];
+    __shared__ __align__(16) char gp[kOneSide * kOneSide * 4];  // G in floats, then P in halves
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    auto down = [](char* at) {  // four rows of a column
+        return __builtin_bit_cast(v4h, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)at));
+    };
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
+    const int64_t z = blockIdx.x;
+    const int np = (p.n + 31) & ~31;
+    // bytes from a row's start: piece of 16 bytes `c` of row `row` of halves; column `e`, a multiple of 4, of a row of floats
+    auto piece = [](int row, int c) { return row * kRow + ((c ^ (row & 7)) << 4); };
+    auto place = [](int row, int e) { return row * kOneSide * 4 + (((e >> 2) ^ (row & 15)) << 4); };
+
+    // Momentum, norm and X^T: four neighbours of a row of X^T at a time, lanes along the rows in memory, all in registers until
+    // the norm is known.  Loads go out in batches: one after the other each would take a memory's latency.
+    constexpr int kGroups = Cap / 32, kBatch = 6;  // of 4 elements a lane
+    double* sums = (double*)gp;
+    double sum = 0.0;
+    const bool tall = p.o.tall;
+    const T* x = (const T*)p.x + z * p.x_stride;
+    float* momentum = p.momentum ? p.momentum + z * p.rows * p.cols : nullptr;
+    auto group = [&](int g, int& row, int& m0) {
+        g = g * kOneWaves + wave;
+        row = tall ? g * 4 + q : g / 4 * 16 + r;
+        m0 = tall ? r * 4 : g % 4 * 16 + q * 4;
+    };
+    v4f u[kGroups];
+#pragma unroll
+    for (int b = 0; b < kGroups; b += kBatch) {
+        v4f old[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch && b + k < kGroups; ++k) {
+            int row, m0;
+            group(b + k, row, m0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at_r = tall ? row : m0 + i, at_c = tall ? m0 + i : row;
+                const bool in = row < p.n && m0 + i < p.m;
+                u[b + k][i] = in ? (float)x[at_r * p.ldx + at_c] : 0.0f;
+                old[k][i] = in && momentum ? momentum[(int64_t)at_r * p.cols + at_c] : 0.0f;
+            }
+        }
+        if (momentum) {
+#pragma unroll
+            for (int k = 0; k < kBatch && b + k < kGroups; ++k) {
+                int row, m0;
+                group(b + k, row, m0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float moved = fmaf(p.mu, old[k][i], u[b + k][i]);
+                    if (row < p.n && m0 + i < p.m) momentum[(int64_t)(tall ? row : m0 + i) * p.cols + (tall ? m0 + i : row)] = moved;
+                    u[b + k][i] = p.nesterov ? fmaf(p.mu, moved, u[b + k][i]) : moved;
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch && b + k < kGroups; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += (double)u[b + k][i] * (double)u[b + k][i];
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    sum = block_sum(sum, sums);
+    if (threadIdx.x == 0) sums[kOneWaves] = (double)kScaleX / (sqrt(sum) + (double)p.eps);
+    __syncthreads();
+    const double inverse = sums[kOneWaves];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        int row, m0;
+        group(g, row, m0);
+        if (row >= np) continue;
+        v4f v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (float)((double)u[g][i] * inverse);
+        char* at = xt + piece(row, m0 >> 3) + (m0 & 4) * 2;
+        *(v4h*)at = highs(v);
+        if (Full) *(v4h*)(at + kPlane) = highs(rest_of(v));
+    }
+    __syncthreads();
+
+    for (int step = 0; step < p.steps; ++step) {
+        // G: waves 0 to 3 have five of the ten tiles on and below the diagonal, 4 to 7 the others; each takes every fourth 32 rows
+        v4f part[5] = {};
+        const int half = wave >> 2, share = wave & 3;
+        for (int k = share * 32; k < np; k += 128) {
+            v8h f[4][2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int h = 0; h < kPlanes; ++h) {
+                    const int row = k + 8 * q + (r >> 2), e = 16 * i + 4 * (r & 3);
+                    char* at = xt + h * kPlane + (e & 4) * 2;
+                    const v4h lo = down(at + piece(row, e >> 3));
+                    const v4h hi = down(at + piece(row + 4, e >> 3));
+                    f[i][h] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                }
+            if (half == 0) {
+                part[0] = mul16<Full>(f[0], f[0], part[0]);
+                part[1] = mul16<Full>(f[1], f[0], part[1]);
+                part[2] = mul16<Full>(f[1], f[1], part[2]);
+                part[3] = mul16<Full>(f[3], f[0], part[3]);
+                part[4] = mul16<Full>(f[3], f[1], part[4]);
+            } else {
+                part[0] = mul16<Full>(f[2], f[0], part[0]);
+                part[1] = mul16<Full>(f[2], f[1], part[1]);
+                part[2] = mul16<Full>(f[2], f[2], part[2]);
+                part[3] = mul16<Full>(f[3], f[2], part[3]);
+                part[4] = mul16<Full>(f[3], f[3], part[4]);
+            }
+        }
+        for (int turn = 0; turn < 4; ++turn) {
+            if (share == turn) {
+#pragma unroll
+                for (int t = 0; t < 5; ++t) {
+                    const int i = half ? (t < 3 ? 2 : 3) : (t == 0 ? 0 : (t < 3 ? 1 : 3)), j = half ? (t < 3 ? t : t - 1) : (t < 2 ? 0 : t == 2 ? 1 : t - 3);
+                    // element (16 i + 4 q + e, 16 j + r), and by symmetry
+                    v4f* at = (v4f*)(gp + place(16 * j + r, 16 * i + 4 * q));
+                    v4f v = part[t];
+                    if (turn > 0) v += *at;
+                    if (turn == 3) {
+                        v *= 1.0f / (kScaleX * kScaleX);
+                        if (i != j) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int row = 16 * i + 4 * q + e, col = 16 * j + r;
+                                *(float*)(gp + place(row, col & ~3) + (col & 3) * 4) = v[e];
+                            }
+                        }
+                    }
+                    *at = v;
+                }
+            }
+            __syncthreads();
+        }
+        // P: a wave has two neighbouring tiles of a row of them
+        v4f pv[2];
+        {
+            auto operand = [&](int tile, int k, v8h (&f)[2]) {
+                const v4f a = *(const v4f*)(gp + place(16 * tile + r, k + 8 * q)), b = *(const v4f*)(gp + place(16 * tile + r, k + 8 * q + 4));
+                const v4f va = a * kScaleX, vb = b * kScaleX;
+                f[0] = __builtin_shufflevector(highs(va), highs(vb), 0, 1, 2, 3, 4, 5, 6, 7);
+                f[1] = __builtin_shufflevector(highs(rest_of(va)), highs(rest_of(vb)), 0, 1, 2, 3, 4, 5, 6, 7);
+            };
+            const int i = wave >> 1;
+            pv[0] = pv[1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < kOneSide; k += 32) {
+                v8h fi[2], fj[2];
+                operand(i, k, fi);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    operand(2 * (wave & 1) + t, k, fj);
+                    pv[t] = mul16<true>(fi, fj, pv[t]);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int j = 2 * (wave & 1) + t;
+                const v4f g = *(const v4f*)(gp + place(16 * j + r, 16 * i + 4 * q));
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    pv[t][e] = p.sp * fmaf(p.c / (kScaleX * kScaleX), pv[t][e], fmaf(p.b, g[e], 16 * i + 4 * q + e == 16 * j + r ? p.a : 0.0f));
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int i = wave >> 1, j = 2 * (wave & 1) + t;  // stored by symmetry, four neighbours of row 16 j + r
+            char* at = gp + piece(16 * j + r, 2 * i + (q >> 1)) + (q & 1) * 8;
+            *(v4h*)at = highs(pv[t]);
+            *(v4h*)(at + kOneSide * kRow) = highs(rest_of(pv[t]));
+        }
+        __syncthreads();
+        // X <- P X
+        v8h pf[4][2][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) pf[i][k][h] = *(const v8h*)(gp + h * kOneSide * kRow + piece(16 * i + r, 4 * k + q));
+        const bool last = step + 1 == p.steps;
+        for (int n0 = wave * 16; n0 < np; n0 += kOneWaves * 16) {
+            v8h f[2][2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int h = 0; h < kPlanes; ++h) f[k][h] = *(const v8h*)(xt + h * kPlane + piece(n0 + r, 4 * k + q));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+                v = mul16_pair<Full>(pf[i][0], f[0], v);
+                v = mul16_pair<Full>(pf[i][1], f[1], v);
+                if (!last) {
+                    v *= 1.0f / p.sp;
+                    char* at = xt + piece(n0 + r, 2 * i + (q >> 1)) + (q & 1) * 8;
+                    *(v4h*)at = highs(v);
+                    if (Full) *(v4h*)(at + kPlane) = highs(rest_of(v));
+                    continue;
+                }
+                v *= 1.0f / (kScaleX * p.sp);
+                const int row = n0 + r, col = 16 * i + 4 * q;  // of X^T
+                if (tall) {
+                    if (p.out_type == kGradF32)
+                        finish4<float>(p.o, z, row, col, v);
+                    else if (p.out_type == kGradF16)
+                        finish4<_Float16>(p.o, z, row, col, v);
+                    else
+                        finish4<__bf16>(p.o, z, row, col, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (p.out_type == kGradF32)
+                            finish1<float>(p.o, z, col + e, row, v[e]);
+                        else if (p.out_type == kGradF16)
+                            finish1<_Float16>(p.o, z, col + e, row, v[e]);
+                        else
+                            finish1<__bf16>(p.o, z, col + e, row, v[e]);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Whether k_one has room, and its launch.
+template <bool Full>
+bool one_block(const OrthoCall& q, float sp, hipStream_t s)
+{
+    const int64_t m = q.rows < q.cols ? q.rows : q.cols, n = q.rows < q.cols ? q.cols : q.rows;
+    constexpr int kMost = Full ? 576 : 768, kFew = 128;  // the 160 KB of LDS, less 16 KB for G, or the registers; and less for little ones
+    if (m > kOneSide || n > kMost) return false;
+    const Result o = {q.out, q.rows > q.cols, q.update, q.keep, q.gain, q.ldo, q.out_stride, q.rows, q.cols};
+    const One p = {q.x, q.ldx, q.x_stride, q.momentum, q.mu, q.nesterov, (int)q.rows, (int)q.cols, (int)m, (int)n,
+                   q.steps, q.a, q.b, q.c, q.eps, sp, q.out_type, o};
+    by_element(q.x_type, [&](auto type) {
+        typedef typename decltype(type)::T T;
+        if (n <= kFew)
+            k_one<T, kFew, Full><<<(uint32_t)q.batch, 64 * kOneWaves, 0, s>>>(p);
+        else
+            k_one<T, kMost, Full><<<(uint32_t)q.batch, 64 * kOneWaves, 0, s>>>(p);
+    });
+    return true;
 }
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -397,6 +713,19 @@ int group_of(const OrthoCall& q, int64_t m, int64_t n, bool full)
 template <bool Full>
 void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
 {
+    // Scales: the largest powers of two that leave room for the largest element of P = a + bx + cx^2 over the squares x of
+    // singular values up to 1.5, of Q's products of it and of T = P G.
+    float top = fmaxf(fabsf(q.a), fabsf(q.a + 2.25f * q.b + 5.0625f * q.c));
+    if (q.c != 0.0f && -q.b / (2 * q.c) > 0.0f && -q.b / (2 * q.c) < 2.25f) top = fmaxf(top, fabsf(q.a - q.b * q.b / (4 * q.c)));
+    auto scale = [](float bound) {
+        int e = 0;
+        (void)frexpf(32768.0f / fmaxf(bound, 1.0f), &e);
+        return ldexpf(1.0f, e - 1 > -10 ? e - 1 : -10);
+    };
+    const float sx = kScaleX, sp = scale(top), st = scale(2.25f * top);
+
+    if (one_block<Full>(q, sp, s)) return;
+
     const Layout l(q.batch, q.rows, q.cols, Full);
     const uint32_t batch = (uint32_t)q.batch;
     const int64_t m = l.m, n = l.n;
@@ -412,30 +741,13 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
     for (int i = 0; i < 2; ++i) x[i] = plane(m, l.np), xt[i] = plane(n, l.mp), g[i] = plane(m, l.mp), pm[i] = plane(m, l.mp), qm[i] = plane(m, l.mp);
     const Plane tm = plane(m, l.mp);
 
-    auto start = [&](auto type) {
+    by_element(q.x_type, [&](auto type) {
         typedef typename decltype(type)::T T;
         const Start<T> p = {(const T*)q.x, q.ldx, q.x_stride, q.momentum, q.mu, q.nesterov, q.rows, q.cols, (double*)ws, l.parts};
         k_norm<T><<<dim3((uint32_t)l.parts, batch), kNormBlock, 0, s>>>(p);
         const dim3 grid((uint32_t)((q.cols + 63) / 64), (uint32_t)((q.rows + 63) / 64), batch);
         k_start<T, Full><<<grid, 256, 0, s>>>(p, q.eps, tall ? xt[0] : x[0], tall ? x[0] : xt[0]);
-    };
-    if (q.x_type == kGradF32)
-        start(Elem<kGradF32>());
-    else if (q.x_type == kGradF16)
-        start(Elem<kGradF16>());
-    else
-        start(Elem<kGradBf16>());
-
-    // Scales: the largest powers of two that leave room for the largest element of P = a + bx + cx^2 over the squares x of
-    // singular values up to 1.5, of Q's products of it and of T = P G.
-    float top = fmaxf(fabsf(q.a), fabsf(q.a + 2.25f * q.b + 5.0625f * q.c));
-    if (q.c != 0.0f && -q.b / (2 * q.c) > 0.0f && -q.b / (2 * q.c) < 2.25f) top = fmaxf(top, fabsf(q.a - q.b * q.b / (4 * q.c)));
-    auto scale = [](float bound) {
-        int e = 0;
-        (void)frexpf(32768.0f / fmaxf(bound, 1.0f), &e);
-        return ldexpf(1.0f, e - 1 > -10 ? e - 1 : -10);
-    };
-    const float sx = kScaleX, sp = scale(top), st = scale(2.25f * top);
+    });
 
     const int64_t segments = Full ? 3 : 1;
     auto triangle = [](int64_t side, int64_t b) { const int64_t k = (side + b - 1) / b; return k * (k + 1) / 2; };

@@ -273,7 +273,7 @@ struct Tile {
             constexpr int i = N / kNt, j = N % kNt, kAll = kMt * kNt, kReads = kMt + kNt, kEvery = kAll >= 64 ? 3 : 1;
             static_assert(kReads * kEvery <= kAll || kAll < 64, "a product for each read");
             if (N == 0) settle();
-            Core::mul(p.b[j], p.a[i], acc[i][j], Core::kScaled ? p.sb[j] : 0, Core::kScaled ? p.sa[i] : 0);
+            Core::mul(p.b[j], p.a[i], acc[i][j], p.sb[Core::kScaled ? j : 0], p.sa[Core::kScaled ? i : 0]);
             if (Read && kAll >= 64 && N % kEvery == 0 && N / kEvery < kReads) read(next, stage, h, N / kEvery);
             if (Read && kAll < 64) {
 #pragma unroll
