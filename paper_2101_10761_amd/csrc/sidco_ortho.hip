@@ -12,6 +12,8 @@
 // X's relative error of 2^-12 an element, about 1.5e-3 (2-norm) reaches the result, less than a result in bf16 loses; halves
 // are used where it has 16 bits.  For a result in 32 bits each operand is a pair of halves, the second one what the first
 // leaves, 22 bits together, and a product is three: high high + low high + high low.
+#include <math.h>
+
 #include <type_traits>
 
 #include "sidco_dense.h"
@@ -66,6 +68,30 @@ __device__ __forceinline__ double block_sum(double v, double* lds)
     return t;
 }
 
+// Eight neighbours, in words of the element's own alignment: a row may start anywhere.
+template <class T>
+__device__ __forceinline__ void load8(const T* p, float v[8])
+{
+    if constexpr (sizeof(T) == 4) {
+        typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+        const f4 a = *(const f4*)p, b = *(const f4*)(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    } else {
+        typedef T t8 __attribute__((ext_vector_type(8), aligned(2)));
+        const t8 a = *(const t8*)p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
+    }
+}
+
+__device__ __forceinline__ void store8(float* p, const float v[8])
+{
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+    *(f4*)p = f4{v[0], v[1], v[2], v[3]};
+    *(f4*)(p + 4) = f4{v[4], v[5], v[6], v[7]};
+}
+
 template <class T>
 struct Start {
     const T* x;        // the matrix, or the gradient
@@ -78,35 +104,73 @@ struct Start {
     int parts;
 };
 
-// u from the gradient and the momentum that k_norm has moved
+// u from the gradient and the momentum that k_norm has moved: n of 8 neighbours, zeros after them
 template <class T>
-__device__ __forceinline__ float update_of(const Start<T>& p, int64_t z, int64_t r, int64_t c)
+__device__ __forceinline__ void update8(const Start<T>& p, int64_t z, int64_t r, int64_t c, int64_t n, float u[8])
 {
-    const float g = (float)p.x[z * p.stride + r * p.ld + c];
-    if (!p.momentum) return g;
-    const float m = p.momentum[(z * p.rows + r) * p.cols + c];
-    return p.nesterov ? fmaf(p.mu, m, g) : m;
+    const T* x = p.x + z * p.stride + r * p.ld + c;
+    const float* m = p.momentum ? p.momentum + (z * p.rows + r) * p.cols + c : nullptr;
+    if (n >= 8) {
+        load8(x, u);
+        if (m) {
+            float old[8];
+            load8(m, old);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = p.nesterov ? fmaf(p.mu, old[i], u[i]) : old[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            u[i] = i < n ? (float)x[i] : 0.0f;
+            if (m && i < n) u[i] = p.nesterov ? fmaf(p.mu, m[i], u[i]) : m[i];
+        }
+    }
 }
 
+// Moves the momentum and adds up u^2.  A block takes rows, of a matrix without gaps pieces of kNormRow elements, in turn.
+constexpr int kNormRow = 16 * kNormBlock;
 template <class T>
 __global__ __launch_bounds__(kNormBlock) void k_norm(Start<T> p)
 {
     __shared__ double lds[kNormBlock / 64];
-    const int64_t z = blockIdx.y;
+    const int64_t z = blockIdx.y, all = p.rows * p.cols;
+    const bool whole = p.ld == p.cols;
+    const int64_t rows = whole ? (all + kNormRow - 1) / kNormRow : p.rows;
     double sum = 0.0;
-    const int64_t n = p.rows * p.cols;
-    for (int64_t i = (int64_t)blockIdx.x * kNormBlock + threadIdx.x; i < n; i += (int64_t)gridDim.x * kNormBlock) {
-        const int64_t r = i / p.cols, c = i - r * p.cols;
-        float u;
-        if (p.momentum) {
-            float* m = p.momentum + z * n + i;
-            const float g = (float)p.x[z * p.stride + r * p.ld + c], moved = fmaf(p.mu, *m, g);
-            *m = moved;
-            u = p.nesterov ? fmaf(p.mu, moved, g) : moved;
-        } else {
-            u = (float)p.x[z * p.stride + r * p.ld + c];
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const int64_t len = whole ? (all - r * kNormRow < kNormRow ? all - r * kNormRow : kNormRow) : p.cols;
+        const T* x = p.x + z * p.stride + r * (whole ? kNormRow : p.ld);
+        float* m = p.momentum ? p.momentum + z * all + r * (whole ? kNormRow : p.cols) : nullptr;
+#pragma unroll 2
+        for (int64_t c = threadIdx.x * 8; c < len; c += 8 * kNormBlock) {
+            float u[8];
+            if (c + 8 <= len) {
+                load8(x + c, u);
+                if (m) {
+                    float moved[8];
+                    load8(m + c, moved);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        moved[i] = fmaf(p.mu, moved[i], u[i]);
+                        u[i] = p.nesterov ? fmaf(p.mu, moved[i], u[i]) : moved[i];
+                    }
+                    store8(m + c, moved);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool in = c + i < len;
+                    u[i] = in ? (float)x[c + i] : 0.0f;
+                    if (m && in) {
+                        const float moved = fmaf(p.mu, m[c + i], u[i]);
+                        m[c + i] = moved;
+                        u[i] = p.nesterov ? fmaf(p.mu, moved, u[i]) : moved;
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += (double)u[i] * (double)u[i];
         }
-        sum += (double)u * (double)u;
     }
     sum = block_sum(sum, lds);
     if (threadIdx.x == 0) p.part[z * p.parts + blockIdx.x] = sum;
@@ -119,12 +183,17 @@ struct Plane {
 };
 
 template <bool Full>
-__device__ __forceinline__ void put(const Plane& o, int64_t z, int64_t r, int64_t c, float v)
+__device__ __forceinline__ void put8(const Plane& o, int64_t z, int64_t r, int64_t c, const float v[8])
 {
     _Float16* p = o.at + z * o.stride + r * o.pitch + c;
-    const _Float16 h = (_Float16)v;
-    *p = h;
-    if (Full) p[o.low] = (_Float16)(v - (float)h);
+    v8h h, l;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        h[i] = (_Float16)v[i];
+        l[i] = (_Float16)(v[i] - (float)h[i]);
+    }
+    *(v8h*)p = h;
+    if (Full) *(v8h*)(p + o.low) = l;
 }
 
 // 64 x 64 elements a block: rows go to `natural`, and through LDS to `turned`, the padding of both as zeros.
@@ -137,25 +206,42 @@ __global__ __launch_bounds__(256) void k_start(Start<T> p, float eps, Plane natu
     const int64_t z = blockIdx.z;
     double sum = 0.0;
     for (int i = threadIdx.x; i < p.parts; i += 256) sum += p.part[z * p.parts + i];
+    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
+    const int row = threadIdx.x >> 3, col = (threadIdx.x & 7) * 8;
+    float u[2][8];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int64_t r = r0 + k * 32 + row, c = c0 + col;
+        update8(p, z, r, c, r < p.rows ? p.cols - c : 0, u[k]);
+    }
     sum = block_sum(sum, lds);
     if (threadIdx.x == 0) inverse = (double)kScaleX / (sqrt(sum) + (double)eps);
     __syncthreads();
-    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const double inv = inverse;
-#pragma unroll 4
-    for (int k = 0; k < 16; ++k) {
-        const int64_t r = r0 + k * 4 + wave, c = c0 + lane;
-        float v = 0.0f;
-        if (r < p.rows && c < p.cols) v = (float)((double)update_of(p, z, r, c) * inv);
-        tile[k * 4 + wave][lane] = v;
-        if (r < p.rows) put<Full>(natural, z, r, c, v);
+    const double inv = inverse > 1e300 ? 1e300 : inverse;  // zeros stay zeros without eps too; a NaN stays one
+    const bool plain = inv > 1e-30 && inv < 1e30;  // else the factor or the elements are not of fp32's range
+    const float f = (float)inv;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (plain) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[k][i] *= f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[k][i] = (float)((double)u[k][i] * inv);
+        }
+        const int64_t r = r0 + k * 32 + row;
+        if (r < p.rows) put8<Full>(natural, z, r, c0 + col, u[k]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) tile[k * 32 + row][col + i] = u[k][i];
     }
     __syncthreads();
-#pragma unroll 4
-    for (int k = 0; k < 16; ++k) {
-        const int64_t r = c0 + k * 4 + wave, c = r0 + lane;
-        if (r < p.cols) put<Full>(turned, z, r, c, tile[lane][k * 4 + wave]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c = k * 32 + row;
+        if (c0 + c >= p.cols) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[k][i] = tile[col + i][c];
+        put8<Full>(turned, z, c0 + c, r0 + col, u[k]);
     }
 }
 
@@ -193,7 +279,7 @@ __device__ __forceinline__ void put_tile(Tl& t, char* lds, const Plane& o, int64
         };
     };
     t.template out<_Float16, Turn>(lds, at, store(false));
-    if (Full) t.template out<_Float16, Turn>(lds, [&](uint32_t r, uint32_t c, const v4f& v) { return rest_of(at(r, c, v)); }, store(true));
+    if (Full) t.template out<_Float16, Turn>(lds, [&](uint32_t r, uint32_t c, const v4f& v) { return rest_of(rounded(at(r, c, v))); }, store(true));
 }
 
 __device__ __forceinline__ Rows rows_of(const Plane& o, int64_t z, uint32_t rows, bool low = false)
@@ -344,7 +430,7 @@ __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plan
                 put_tile<true, Full>(t, lds + Tl::kLds, xt2, at.z, m, n, at.m0, at.n0, value);
             } else if (o.tall) {
                 t.each([&](uint32_t r, uint32_t c, const v4f& v) {
-                    finish4<T>(o, at.z, at.n0 + c + (threadIdx.x & 3), (at.m0 + r) & ~3u, Tl::turned(v * back));
+                    finish4<T>(o, at.z, at.n0 + c + (threadIdx.x & 3), (at.m0 + r) & ~3u, turned(v * back));
                 });
             } else {
                 t.each([&](uint32_t r, uint32_t c, const v4f& v) { finish4<T>(o, at.z, at.m0 + r, at.n0 + c, v * back); });
@@ -356,10 +442,9 @@ __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plan
 //
 // With m <= 64 and X^T in LDS one block does everything, all steps in one launch; the launches of the kernels above, 2 and 15
 // for 5 steps, take longer than their work at this size.  X^T is kept by rows of 64 (m padded with zeros), so that
-//   G = X X^T  reads its operands down the columns, with the transposing read of LDS, each wave a part of X's length,
+//   G = X X^T  reads its operands down the columns, with the transposing read of LDS,
 //   X <- P X   reads rows and writes them in place: a row of X^T depends on that row alone, and each wave has its own.
-// G stays fp32 between the two and P is a pair of halves whatever X is, both being small; G's parts are added up in the order of the waves.  16-byte pieces c of row r are kept at place
-// c ^ (r % 8) of a row of halves and c ^ (r % 16) of a row of floats.
+// G and P, being small, are pairs of halves whatever X is.  16-byte piece c of row r is kept at place c ^ (r % 8).
 constexpr int kOneWaves = 8, kOneSide = 64;
 
 struct One {
@@ -404,7 +489,7 @@ __global__ __launch_bounds__(64 * kOneWaves) void k_one(One p)
 {
     constexpr int kPlanes = Full ? 2 : 1, kRow = kOneSide * 2, kPlane = Cap * kRow;
     __shared__ __align__(16) char xt[kPlanes * kPlane];
-    __shared__ __align__(16) char gp[kOneSide * kOneSide * 4];  // G in floats, then P in halves
+    __shared__ __align__(16) char gp[2 * kOneSide * kRow];  // G, then P, as pairs of halves
     typedef short v4s __attribute__((ext_vector_type(4)));
     auto down = [](char* at) {  // four rows of a column
         return __builtin_bit_cast(v4h, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)at));
@@ -412,70 +497,94 @@ __global__ __launch_bounds__(64 * kOneWaves) void k_one(One p)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
     const int64_t z = blockIdx.x;
     const int np = (p.n + 31) & ~31;
-    // bytes from a row's start: piece of 16 bytes `c` of row `row` of halves; column `e`, a multiple of 4, of a row of floats
-    auto piece = [](int row, int c) { return row * kRow + ((c ^ (row & 7)) << 4); };
-    auto place = [](int row, int e) { return row * kOneSide * 4 + (((e >> 2) ^ (row & 15)) << 4); };
+    auto piece = [](int row, int c) { return row * kRow + ((c ^ (row & 7)) << 4); };  // where 16 bytes of a row are
 
     // Momentum, norm and X^T: four neighbours of a row of X^T at a time, lanes along the rows in memory, all in registers until
     // the norm is known.  Loads go out in batches: one after the other each would take a memory's latency.
     constexpr int kGroups = Cap / 32, kBatch = 6;  // of 4 elements a lane
     double* sums = (double*)gp;
-    double sum = 0.0;
+    float top = 0.0f;
     const bool tall = p.o.tall;
     const T* x = (const T*)p.x + z * p.x_stride;
     float* momentum = p.momentum ? p.momentum + z * p.rows * p.cols : nullptr;
-    auto group = [&](int g, int& row, int& m0) {
-        g = g * kOneWaves + wave;
-        row = tall ? g * 4 + q : g / 4 * 16 + r;
-        m0 = tall ? r * 4 : g % 4 * 16 + q * 4;
-    };
+    // Group g has row row0 + 32 g of X^T (tall: of the matrix; else its column), elements m0 to m0 + 3.
+    const int row0 = tall ? wave * 4 + q : wave / 4 * 16 + r, m0 = tall ? r * 4 : wave % 4 * 16 + q * 4;
+    int xs[4], ms[4];  // element offsets; an element that there is not is read at another's place
+    bool in[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        in[i] = m0 + i < p.m;
+        const int m = in[i] ? m0 + i : p.m - 1;
+        xs[i] = tall ? m : m * (int)p.ldx;
+        ms[i] = tall ? m : m * p.cols;
+    }
     v4f u[kGroups];
 #pragma unroll
     for (int b = 0; b < kGroups; b += kBatch) {
+        T new_x[kBatch][4];
         v4f old[kBatch];
 #pragma unroll
         for (int k = 0; k < kBatch && b + k < kGroups; ++k) {
-            int row, m0;
-            group(b + k, row, m0);
+            int row = row0 + 32 * (b + k);
+            row = row < p.n ? row : p.n - 1;
+            const int xr = tall ? row * (int)p.ldx : row, mr = tall ? row * p.cols : row;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int at_r = tall ? row : m0 + i, at_c = tall ? m0 + i : row;
-                const bool in = row < p.n && m0 + i < p.m;
-                u[b + k][i] = in ? (float)x[at_r * p.ldx + at_c] : 0.0f;
-                old[k][i] = in && momentum ? momentum[(int64_t)at_r * p.cols + at_c] : 0.0f;
+                new_x[k][i] = x[xr + xs[i]];
+                if (momentum) old[k][i] = momentum[mr + ms[i]];
             }
         }
-        if (momentum) {
 #pragma unroll
-            for (int k = 0; k < kBatch && b + k < kGroups; ++k) {
-                int row, m0;
-                group(b + k, row, m0);
+        for (int k = 0; k < kBatch && b + k < kGroups; ++k) {
+            const int row = row0 + 32 * (b + k);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float moved = fmaf(p.mu, old[k][i], u[b + k][i]);
-                    if (row < p.n && m0 + i < p.m) momentum[(int64_t)(tall ? row : m0 + i) * p.cols + (tall ? m0 + i : row)] = moved;
-                    u[b + k][i] = p.nesterov ? fmaf(p.mu, moved, u[b + k][i]) : moved;
+            for (int i = 0; i < 4; ++i) {
+                const bool there = in[i] && row < p.n;
+                float v = (float)new_x[k][i];
+                if (momentum) {
+                    const float moved = fmaf(p.mu, old[k][i], v);
+                    if (there) momentum[(tall ? row * p.cols : row) + ms[i]] = moved;
+                    v = p.nesterov ? fmaf(p.mu, moved, v) : moved;
                 }
+                v = there ? v : 0.0f;
+                u[b + k][i] = v;
+                top = fmaxf(top, fabsf(v));
             }
         }
-#pragma unroll
-        for (int k = 0; k < kBatch && b + k < kGroups; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum += (double)u[b + k][i] * (double)u[b + k][i];
         __builtin_amdgcn_sched_barrier(0);
     }
-    sum = block_sum(sum, sums);
-    if (threadIdx.x == 0) sums[kOneWaves] = (double)kScaleX / (sqrt(sum) + (double)p.eps);
+    // The norm from elements over a power of two near the largest, which keeps their squares in fp32's range.
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+    if (lane == 0) ((float*)sums)[wave] = top;
     __syncthreads();
-    const double inverse = sums[kOneWaves];
+#pragma unroll
+    for (int w = 0; w < kOneWaves; ++w) top = fmaxf(top, ((float*)sums)[w]);
+    __syncthreads();
+    int e = 0;
+    (void)frexpf(top, &e);
+    const float down_to = top > 0.0f && top < INFINITY ? ldexpf(1.0f, e > 126 ? -126 : (e < -126 ? 126 : -e)) : 1.0f;
+    v4f squares = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-        int row, m0;
-        group(g, row, m0);
+        u[g] *= down_to;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) squares[i] = fmaf(u[g][i], u[g][i], squares[i]);
+    }
+    double sum = (double)squares[0] + (double)squares[1] + (double)squares[2] + (double)squares[3];
+    sum = block_sum(sum, sums);
+    if (threadIdx.x == 0) sums[kOneWaves] = (double)kScaleX / (sqrt(sum) + (double)p.eps * (double)down_to);
+    __syncthreads();
+    // zeros alone may ask for more than the largest number; a NaN stays one
+    const float inverse = sums[kOneWaves] > 3e38 ? 3e38f : (float)sums[kOneWaves];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        const int row = row0 + 32 * g;
         if (row >= np) continue;
         v4f v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (float)((double)u[g][i] * inverse);
+        for (int i = 0; i < 4; ++i) v[i] = u[g][i] * inverse;
+        v = rounded(v);
         char* at = xt + piece(row, m0 >> 3) + (m0 & 4) * 2;
         *(v4h*)at = highs(v);
         if (Full) *(v4h*)(at + kPlane) = highs(rest_of(v));
@@ -483,97 +592,79 @@ __global__ __launch_bounds__(64 * kOneWaves) void k_one(One p)
     __syncthreads();
 
     for (int step = 0; step < p.steps; ++step) {
-        // G: waves 0 to 3 have five of the ten tiles on and below the diagonal, 4 to 7 the others; each takes every fourth 32 rows
-        v4f part[5] = {};
-        const int half = wave >> 2, share = wave & 3;
-        for (int k = share * 32; k < np; k += 128) {
-            v8h f[4][2];
+        // G: a wave has one of the six tiles below the diagonal, or two of the four on it, over all of X's length
+        v4f v2[2] = {};
+        const bool on = wave >= 6;
+        const int ti = on ? 2 * (wave - 6) : (wave < 1 ? 1 : wave < 3 ? 2 : 3), tj = on ? ti + 1 : (wave < 1 ? 0 : wave < 3 ? wave - 1 : wave - 3);
+        auto operands = [&](int k, v8h (&f)[2][2]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int h = 0; h < kPlanes; ++h) {
-                    const int row = k + 8 * q + (r >> 2), e = 16 * i + 4 * (r & 3);
+                    const int row = k + 8 * q + (r >> 2), e = 16 * (i ? tj : ti) + 4 * (r & 3);
                     char* at = xt + h * kPlane + (e & 4) * 2;
-                    const v4h lo = down(at + piece(row, e >> 3));
-                    const v4h hi = down(at + piece(row + 4, e >> 3));
+                    const v4h lo = down(at + piece(row, e >> 3)), hi = down(at + piece(row + 4, e >> 3));
                     f[i][h] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                 }
-            if (half == 0) {
-                part[0] = mul16<Full>(f[0], f[0], part[0]);
-                part[1] = mul16<Full>(f[1], f[0], part[1]);
-                part[2] = mul16<Full>(f[1], f[1], part[2]);
-                part[3] = mul16<Full>(f[3], f[0], part[3]);
-                part[4] = mul16<Full>(f[3], f[1], part[4]);
+        };
+        auto products = [&](const v8h (&f)[2][2]) {
+            if (on) {
+                v2[0] = mul16<Full>(f[0], f[0], v2[0]);
+                v2[1] = mul16<Full>(f[1], f[1], v2[1]);
             } else {
-                part[0] = mul16<Full>(f[2], f[0], part[0]);
-                part[1] = mul16<Full>(f[2], f[1], part[1]);
-                part[2] = mul16<Full>(f[2], f[2], part[2]);
-                part[3] = mul16<Full>(f[3], f[2], part[3]);
-                part[4] = mul16<Full>(f[3], f[3], part[4]);
+                v2[0] = mul16<Full>(f[0], f[1], v2[0]);
             }
+        };
+        v8h fa[2][2], fb[2][2];  // the next operands are read while these are multiplied
+        operands(0, fa);
+        for (int k = 0; k < np; k += 64) {
+            if (k + 32 < np) operands(k + 32, fb);
+            products(fa);
+            if (k + 64 < np) operands(k + 64, fa);
+            if (k + 32 < np) products(fb);
         }
-        for (int turn = 0; turn < 4; ++turn) {
-            if (share == turn) {
+        // four neighbours of a row of G or P, from element (row, col) on
+        auto store4 = [&](int row, int col, v4f v) {
+            v = rounded(v);
+            char* at = gp + piece(row, col >> 3) + (col & 4) * 2;
+            *(v4h*)at = highs(v);
+            *(v4h*)(at + kOneSide * kRow) = highs(rest_of(v));
+        };
 #pragma unroll
-                for (int t = 0; t < 5; ++t) {
-                    const int i = half ? (t < 3 ? 2 : 3) : (t == 0 ? 0 : (t < 3 ? 1 : 3)), j = half ? (t < 3 ? t : t - 1) : (t < 2 ? 0 : t == 2 ? 1 : t - 3);
-                    // element (16 i + 4 q + e, 16 j + r), and by symmetry
-                    v4f* at = (v4f*)(gp + place(16 * j + r, 16 * i + 4 * q));
-                    v4f v = part[t];
-                    if (turn > 0) v += *at;
-                    if (turn == 3) {
-                        v *= 1.0f / (kScaleX * kScaleX);
-                        if (i != j) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int row = 16 * i + 4 * q + e, col = 16 * j + r;
-                                *(float*)(gp + place(row, col & ~3) + (col & 3) * 4) = v[e];
-                            }
-                        }
-                    }
-                    *at = v;
-                }
-            }
-            __syncthreads();
+        for (int t = 0; t < 2; ++t) {
+            if (t && !on) break;
+            const int i = t ? tj : ti, j = on ? i : tj;  // v[e] is element (16 i + 4 q + e, 16 j + r): by symmetry a row's neighbours
+            const v4f v = v2[t] * (1.0f / kScaleX);
+            store4(16 * j + r, 16 * i + 4 * q, v);
+            if (i != j) store4(16 * i + 4 * q + (r & 3), 16 * j + (r & ~3), turned(v));
         }
+        __syncthreads();
         // P: a wave has two neighbouring tiles of a row of them
-        v4f pv[2];
-        {
-            auto operand = [&](int tile, int k, v8h (&f)[2]) {
-                const v4f a = *(const v4f*)(gp + place(16 * tile + r, k + 8 * q)), b = *(const v4f*)(gp + place(16 * tile + r, k + 8 * q + 4));
-                const v4f va = a * kScaleX, vb = b * kScaleX;
-                f[0] = __builtin_shufflevector(highs(va), highs(vb), 0, 1, 2, 3, 4, 5, 6, 7);
-                f[1] = __builtin_shufflevector(highs(rest_of(va)), highs(rest_of(vb)), 0, 1, 2, 3, 4, 5, 6, 7);
-            };
-            const int i = wave >> 1;
-            pv[0] = pv[1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        v4f pv[2] = {};
+        const int pi = wave >> 1, pj = 2 * (wave & 1);
 #pragma unroll
-            for (int k = 0; k < kOneSide; k += 32) {
-                v8h fi[2], fj[2];
-                operand(i, k, fi);
+        for (int k = 0; k < 2; ++k) {
+            v8h f[3][2];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    operand(2 * (wave & 1) + t, k, fj);
-                    pv[t] = mul16<true>(fi, fj, pv[t]);
-                }
-            }
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int j = 2 * (wave & 1) + t;
-                const v4f g = *(const v4f*)(gp + place(16 * j + r, 16 * i + 4 * q));
+                for (int t = 0; t < 3; ++t)
+                    f[t][h] = *(const v8h*)(gp + h * kOneSide * kRow + piece(16 * (t == 0 ? pi : pj + t - 1) + r, 4 * k + q));
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    pv[t][e] = p.sp * fmaf(p.c / (kScaleX * kScaleX), pv[t][e], fmaf(p.b, g[e], 16 * i + 4 * q + e == 16 * j + r ? p.a : 0.0f));
-            }
+            for (int t = 0; t < 2; ++t) pv[t] = mul16<true>(f[0], f[1 + t], pv[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int row = 16 * (pj + t) + r, col = 16 * pi + 4 * q;
+            const char* at = gp + piece(row, col >> 3) + (col & 4) * 2;
+            const v4h gh = *(const v4h*)at, gl = *(const v4h*)(at + kOneSide * kRow);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                pv[t][e] = p.sp * fmaf(p.c / (kScaleX * kScaleX), pv[t][e], fmaf(p.b / kScaleX, (float)gh[e] + (float)gl[e], col + e == row ? p.a : 0.0f));
         }
         __syncthreads();
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int i = wave >> 1, j = 2 * (wave & 1) + t;  // stored by symmetry, four neighbours of row 16 j + r
-            char* at = gp + piece(16 * j + r, 2 * i + (q >> 1)) + (q & 1) * 8;
-            *(v4h*)at = highs(pv[t]);
-            *(v4h*)(at + kOneSide * kRow) = highs(rest_of(pv[t]));
-        }
+        for (int t = 0; t < 2; ++t) store4(16 * (pj + t) + r, 16 * pi + 4 * q, pv[t]);
         __syncthreads();
         // X <- P X
         v8h pf[4][2][2];
@@ -584,19 +675,28 @@ __global__ __launch_bounds__(64 * kOneWaves) void k_one(One p)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) pf[i][k][h] = *(const v8h*)(gp + h * kOneSide * kRow + piece(16 * i + r, 4 * k + q));
         const bool last = step + 1 == p.steps;
+        auto rows_at = [&](int n0, v8h (&f)[2][2]) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int h = 0; h < kPlanes; ++h) f[k][h] = *(const v8h*)(xt + h * kPlane + piece(n0 + r, 4 * k + q));
+        };
+        v8h ahead[2][2];
+        if (wave * 16 < np) rows_at(wave * 16, ahead);
         for (int n0 = wave * 16; n0 < np; n0 += kOneWaves * 16) {
             v8h f[2][2];
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int h = 0; h < kPlanes; ++h) f[k][h] = *(const v8h*)(xt + h * kPlane + piece(n0 + r, 4 * k + q));
+                for (int h = 0; h < kPlanes; ++h) f[k][h] = ahead[k][h];
+            if (n0 + kOneWaves * 16 < np) rows_at(n0 + kOneWaves * 16, ahead);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
                 v = mul16_pair<Full>(pf[i][0], f[0], v);
                 v = mul16_pair<Full>(pf[i][1], f[1], v);
                 if (!last) {
-                    v *= 1.0f / p.sp;
+                    v = rounded(v * (1.0f / p.sp));
                     char* at = xt + piece(n0 + r, 2 * i + (q >> 1)) + (q & 1) * 8;
                     *(v4h*)at = highs(v);
                     if (Full) *(v4h*)(at + kPlane) = highs(rest_of(v));
@@ -634,7 +734,7 @@ bool one_block(const OrthoCall& q, float sp, hipStream_t s)
 {
     const int64_t m = q.rows < q.cols ? q.rows : q.cols, n = q.rows < q.cols ? q.cols : q.rows;
     constexpr int kMost = Full ? 576 : 768, kFew = 128;  // the 160 KB of LDS, less 16 KB for G, or the registers; and less for little ones
-    if (m > kOneSide || n > kMost) return false;
+    if (m > kOneSide || n > kMost || q.ldx > (1 << 20)) return false;  // offsets of 32 bits within a matrix
     const Result o = {q.out, q.rows > q.cols, q.update, q.keep, q.gain, q.ldo, q.out_stride, q.rows, q.cols};
     const One p = {q.x, q.ldx, q.x_stride, q.momentum, q.mu, q.nesterov, (int)q.rows, (int)q.cols, (int)m, (int)n,
                    q.steps, q.a, q.b, q.c, q.eps, sp, q.out_type, o};
@@ -663,8 +763,8 @@ struct Layout {
         mp = up(m, 64);
         np = up(n, 64);
         planes = full ? 2 : 1;
-        const int64_t want = (rows * cols + 16 * kNormBlock - 1) / (16 * kNormBlock);
-        parts = (int)(want < 512 ? want : 512);
+        const int64_t want = (rows * cols + kNormRow - 1) / kNormRow;
+        parts = (int)(want < 1024 ? want : 1024);
         part_bytes = (size_t)up((int64_t)batch * parts * (int64_t)sizeof(double), 256);
         const int64_t halves = 2 * plane(m, np) + 2 * plane(n, mp) + kSmall * plane(m, mp);
         total = part_bytes + (size_t)batch * halves * sizeof(_Float16);

@@ -96,6 +96,40 @@ __device__ __forceinline__ void tile_of_triangle(uint32_t t, uint32_t& i, uint32
     j = t - r * (r + 1) / 2;
 }
 
+    // Four lanes with four columns of their row each come to hold four rows of one column each.
+    __device__ __forceinline__ v4f turned(v4f v)
+    {
+        const int t = threadIdx.x & 3;
+        auto swap1 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xb1, 0xf, 0xf, true)); };
+        auto swap2 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x4e, 0xf, 0xf, true)); };
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            const float got = swap1(t & 1 ? v[i] : v[i + 1]);
+            v[i] = t & 1 ? got : v[i];
+            v[i + 1] = t & 1 ? v[i + 1] : got;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float got = swap2(t & 2 ? v[i] : v[i + 2]);
+            v[i] = t & 2 ? got : v[i];
+            v[i + 2] = t & 2 ? v[i + 2] : got;
+        }
+        return v;
+    }
+
+// The values as rounded to fp32.  A product rounded to fp32 and then to half is otherwise rounded once, by an instruction that
+// does both, in one place and not in another: the half and what it leaves of the value would belong to different halves.
+__device__ __forceinline__ v4f rounded(v4f v)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x = v[i];
+        asm("" : "+v"(x));
+        v[i] = x;
+    }
+    return v;
+}
+
 // What an instruction multiplies: 16 rows by 16 rows over four pieces, lane l holding piece l / 16 of row l % 16.
 //
 // The instructions are written out because the sums have to stay where they are: with 64 tiles of them, all of a wave's 256
@@ -384,27 +418,6 @@ struct Tile {
         return 16 * pad((kNt > kMt ? kNt : kMt) * 16 * (int)sizeof(S));
     }
 
-    // Four lanes with four columns of their row each come to hold four rows of one column each.
-    static __device__ __forceinline__ v4f turned(v4f v)
-    {
-        const int t = threadIdx.x & 3;
-        auto swap1 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xb1, 0xf, 0xf, true)); };
-        auto swap2 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x4e, 0xf, 0xf, true)); };
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-            const float got = swap1(t & 1 ? v[i] : v[i + 1]);
-            v[i] = t & 1 ? got : v[i];
-            v[i + 1] = t & 1 ? v[i + 1] : got;
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float got = swap2(t & 2 ? v[i] : v[i + 2]);
-            v[i] = t & 2 ? got : v[i];
-            v[i + 2] = t & 2 ? v[i + 2] : got;
-        }
-        return v;
-    }
-
     // value(row, column, sums) gives the four values of C's row from a column on; store(row, column, 16 bytes of S) takes
     // neighbours of a row - with Turn of a column: row and column are C's, exchanged.  All relative to the tile.  `lds`
     // has out_bytes<S>() for each wave.
@@ -426,7 +439,7 @@ struct Tile {
 #pragma unroll
             for (int y = 0; y < kTiles; ++y) {
                 const int i = Turn ? y : x, j = Turn ? x : y;
-                v4f v = value((uint32_t)(row0 + i * 16 + r), (uint32_t)(col0 + j * 16 + 4 * q), acc[i][j]);
+                v4f v = rounded(value((uint32_t)(row0 + i * 16 + r), (uint32_t)(col0 + j * 16 + 4 * q), acc[i][j]));
                 if (Turn) v = turned(v);
                 const s4 w = {(S)v[0], (S)v[1], (S)v[2], (S)v[3]};
                 if (Turn)
