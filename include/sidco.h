@@ -548,8 +548,9 @@ int sidco_mx4_matmul(void *stream, const uint8_t *a_codes, const uint8_t *a_scal
 /*
  * A layer with a 4-bit weight on rows as they come: x (rows x k of `x_dtype`, row
  * stride ldx) is quantised along its rows and multiplied with the n x k weight, c =
- * alpha x^ W^T (+ c) as in sidco_mx4_matmul.  From one row on.  Uses the stream's
- * workspace: sidco_workspace_bytes_mx4_linear(rows, k).
+ * alpha x^ W^T (+ c) as in sidco_mx4_matmul.  From one row on; c must not overlap x.
+ * Uses the stream's workspace, of sidco_workspace_bytes_mx4_linear(rows, k), unless
+ * there are few rows (one launch then does both).
  */
 int sidco_mx4_linear(void *stream, const void *x, int x_dtype, int64_t rows, int64_t k, int64_t ldx, const uint8_t *w_codes,
                      const uint8_t *w_scales, int64_t n, float alpha, int accumulate, void *c, int c_dtype, int64_t ldc);

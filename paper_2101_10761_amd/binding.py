@@ -724,25 +724,41 @@ def sidco_workspace_bytes_mx4_linear(rows: int, k: int) -> int:
     return int(load().sidco_workspace_bytes_mx4_linear(rows, k))
 
 
-def _check_packed(codes, scales, rows, cols, name):
+_types = None  # torch's element types as the C ABI numbers them
+
+
+def _element_types():
+    global _types
     torch = _torch or _import_torch()
-    padded = (cols + 255) // 256
-    _check_tensor(codes, torch.uint8, name + " codes", rows * padded * 128)
-    _check_tensor(scales, torch.uint8, name + " scales", rows * padded * 8)
+    _types = {torch.float32: GRAD_F32, torch.float16: GRAD_F16, torch.bfloat16: GRAD_BF16}
+    return _types
+
+
+def _check_packed(codes, scales, rows, cols, name):
+    """The addresses of packed buffers that hold rows x cols numbers."""
+    torch = _torch or _import_torch()
+    lines = rows * ((cols + 255) // 256)
+    for t, least in ((codes, 128 * lines), (scales, 8 * lines)):
+        if not isinstance(t, torch.Tensor) or t.dtype is not torch.uint8 or not t.is_cuda or not t.is_contiguous():
+            raise TypeError(f"{name} codes and scales must be contiguous CUDA tensors of dtype torch.uint8")
+        if t.numel() < least:
+            raise ValueError(f"{name} codes or scales have {t.numel()} bytes, need {least}")
+    return codes.data_ptr(), scales.data_ptr()
 
 
 def _matrix(x, name, dims=2):
     """Element code and row stride of a CUDA matrix (or batch of them) whose rows are contiguous."""
     torch = _torch or _import_torch()
-    codes = {torch.float32: GRAD_F32, torch.float16: GRAD_F16, torch.bfloat16: GRAD_BF16}
-    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != dims or x.dtype not in codes:
+    code = (_types or _element_types()).get(x.dtype) if isinstance(x, torch.Tensor) else None
+    if code is None or not x.is_cuda or x.dim() != dims:
         raise TypeError(f"{name} must be a CUDA tensor of {dims} dimensions and dtype float32, float16 or bfloat16")
-    code = codes[x.dtype]
     rows, cols = x.shape[-2:]
-    if cols > 1 and x.stride(-1) != 1:
+    *_, ld, step = x.stride()
+    if step != 1 and cols > 1:
         raise TypeError(f"{name} must have contiguous rows")
-    ld = x.stride(-2) if rows > 1 else cols
-    if ld < cols:
+    if rows <= 1:
+        ld = cols
+    elif ld < cols:
         raise ValueError(f"{name}'s rows overlap")
     return code, ld
 
@@ -755,9 +771,10 @@ def sidco_mx4_compress(grad, residual, codes, scales, stream=None) -> None:
     _check_tensor(grad, grad.dtype, "grad")
     if residual is not None:
         _check_tensor(residual, torch.float32, "residual", d)
-    _check_packed(codes, scales, 1, d, "the gradient's")
-    _check(load().sidco_mx4_compress(_stream_handle(stream), _ptr(grad), code, _ptr(residual), d, _ptr(codes), _ptr(scales)),
-           "sidco_mx4_compress")
+    c, e = _check_packed(codes, scales, 1, d, "the gradient's")
+    rc = load().sidco_mx4_compress(_stream_handle(stream), grad.data_ptr(), code, _ptr(residual), d, c, e)
+    if rc:
+        raise SidcoError(rc, "sidco_mx4_compress")
 
 
 def sidco_mx4_aggregate(codes, scales, dense, scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
@@ -767,12 +784,16 @@ def sidco_mx4_aggregate(codes, scales, dense, scale: float = 1.0, accumulate: bo
     _check_tensor(dense, torch.float32, "dense", 1)
     if codes.dim() != 2 or scales.dim() != 2 or codes.shape[0] != scales.shape[0]:
         raise ValueError("codes and scales must have a row for each worker")
-    workers = codes.shape[0]
-    _check_packed(codes, scales, 1, 1, "the workers'")
-    if codes.shape[1] < (d + 255) // 256 * 128 or scales.shape[1] < (d + 255) // 256 * 8:
+    workers, code_stride = codes.shape
+    scale_stride = scales.shape[1]
+    c, e = _check_packed(codes, scales, 1, 1, "the workers'")
+    lines = (d + 255) // 256
+    if code_stride < lines * 128 or scale_stride < lines * 8:
         raise ValueError("codes or scales are shorter than dense")
-    _check(load().sidco_mx4_aggregate(_stream_handle(stream), _ptr(codes), codes.shape[1], _ptr(scales), scales.shape[1], workers,
-                                      d, scale, int(accumulate), _ptr(dense)), "sidco_mx4_aggregate")
+    rc = load().sidco_mx4_aggregate(_stream_handle(stream), c, code_stride, e, scale_stride, workers, d, scale, 1 if accumulate else 0,
+                                    dense.data_ptr())
+    if rc:
+        raise SidcoError(rc, "sidco_mx4_aggregate")
 
 
 def sidco_mx4_quantize(x, codes, scales, codes_t=None, scales_t=None, stream=None) -> None:
@@ -813,12 +834,14 @@ def sidco_mx4_linear(x, w_codes, w_scales, out, alpha: float = 1.0, accumulate: 
     x_code, ldx = _matrix(x, "x")
     code, ld = _matrix(out, "out")
     rows, k = x.shape
-    if out.shape[0] != rows:
+    out_rows, n = out.shape
+    if out_rows != rows:
         raise ValueError("out must have a row for each of x's")
-    n = out.shape[1]
-    _check_packed(w_codes, w_scales, n, k, "the weight's")
-    _check(load().sidco_mx4_linear(_stream_handle(stream), _ptr(x), x_code, rows, k, ldx, _ptr(w_codes), _ptr(w_scales), n, alpha,
-                                   int(accumulate), _ptr(out), code, ld), "sidco_mx4_linear")
+    w, e = _check_packed(w_codes, w_scales, n, k, "the weight's")
+    rc = load().sidco_mx4_linear(_stream_handle(stream), x.data_ptr(), x_code, rows, k, ldx, w, e, n, alpha, 1 if accumulate else 0,
+                                 out.data_ptr(), code, ld)
+    if rc:
+        raise SidcoError(rc, "sidco_mx4_linear")
 
 
 # ---- the orthogonalised update ----

@@ -174,6 +174,11 @@ int sidco_mx4_linear(void* stream, const void* x, int x_dtype, int64_t rows, int
     if (((rows + 63) / 64) * ((n + 63) / 64) > (int64_t)INT32_MAX) return SIDCO_ERR_SIZE;
     if (!aligned_type(x, x_dtype)) return SIDCO_ERR_ALIGN;
     if (int rc = check_result(c, c_dtype, n, ldc, alpha, accumulate)) return rc;
+    if (few_takes_x(rows, n, k)) {
+        const Mx4Product p = {nullptr, nullptr, w_codes, w_scales, rows, n, k, alpha, accumulate != 0, c, type_of(c_dtype), ldc};
+        launch_mx4_few_x(p, x, type_of(x_dtype), ldx, (hipStream_t)stream);
+        return launched();
+    }
     StreamScratch ws(stream, (size_t)(code_bytes(rows, k) + scale_bytes(rows, k)));
     if (ws.rc != SIDCO_OK) return ws.rc;
     uint8_t* codes = (uint8_t*)ws.data;

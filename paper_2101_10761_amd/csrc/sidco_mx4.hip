@@ -353,35 +353,71 @@ __device__ __forceinline__ v4f multiply16(const v4i& a, const v4i& b, const v4f&
 }
 
 // Few rows of A: the time is that of reading B once.  A block has 16 rows of B; its 8 waves take lines in turn, straight to
-// registers, and add up in LDS.
+// registers, the next line under way while one is multiplied, and add up in LDS.  A comes in blocks, or (X other than Packed) as
+// it is: then each block quantises all of it into LDS while its first lines are under way.
 constexpr int kFewWaves = 8;
-template <class E, int Mt>
-__global__ __launch_bounds__(64 * kFewWaves) void k_mx4_few(Mx4Product p)
+struct Packed {
+    typedef uint8_t T;
+};
+
+template <class E, class X, int Mt>
+__global__ __launch_bounds__(64 * kFewWaves) void k_mx4_few(Mx4Product p, const typename X::T* __restrict__ x, int64_t ldx)
 {
+    constexpr bool kPacked = sizeof(typename X::T) == 1;
+    constexpr int kRowPad = 16;  // bytes after a row of codes, so that 16 rows' pieces are in different banks
     __shared__ v4f part[kFewWaves][Mt][64];
+    __shared__ __align__(16) uint8_t codes[kPacked ? 16 : kFewElements / 2 + Mt * 16 * kRowPad], exps[kPacked ? 1 : kFewElements / kMxBlock];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
     const int64_t pitch = mx4_padded(p.k) / 2;
     const int64_t nb = n0 + r < p.n ? n0 + r : p.n - 1;
     const uint8_t *b = p.b + nb * pitch + q * 16, *bs = p.b_scales + nb * (pitch / 16) + q;
+    v4i fb[2], next[2];
+    int sb[2], snext[2];
+    auto fetch = [&](int64_t k, v4i (&f)[2], int (&sc)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f[h] = *(const v4i*)(b + k + h * 64);
+            sc[h] = bs[k / 16 + h * 4];
+        }
+    };
+    const int64_t step = kFewWaves * kLine;
+    int64_t k = (int64_t)wave * kLine;
+    if (k < pitch) fetch(k, fb, sb);
+    if constexpr (!kPacked) {
+        const int row_groups = (int)(pitch / 4), groups = (int)p.m * row_groups;  // of 8 elements; whole quads of lanes
+        for (int g = threadIdx.x; g < groups; g += 64 * kFewWaves) {
+            const int row = g / row_groups, at = g - row * row_groups, left = (int)p.k - at * 8;
+            const typename X::T* from = x + row * ldx + at * 8;
+            float v[8];
+            if (left >= 8)
+                load8<X>(from, v);
+            else
+                load_few<X>(from, left, v);
+            const uint32_t byte = exponent_byte(largest_of_quad(largest8(v)));
+            *(uint32_t*)(codes + row * (pitch + kRowPad) + at * 4) = encode8(v, byte);
+            if ((at & 3) == 0) exps[row * (pitch / 16) + (at >> 2)] = (uint8_t)byte;
+        }
+        __syncthreads();
+    }
     const uint8_t *a[Mt], *as[Mt];
     v4f acc[Mt];
 #pragma unroll
     for (int i = 0; i < Mt; ++i) {
         const int64_t m = i * 16 + r < p.m ? i * 16 + r : p.m - 1;
-        a[i] = p.a + m * pitch + q * 16;
-        as[i] = p.a_scales + m * (pitch / 16) + q;
+        a[i] = (kPacked ? p.a + m * pitch : codes + m * (pitch + kRowPad)) + q * 16;
+        as[i] = (kPacked ? p.a_scales : exps) + m * (pitch / 16) + q;
         acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    for (int64_t k = (int64_t)wave * kLine; k < pitch; k += kFewWaves * kLine) {
+    for (; k < pitch; k += step) {
+        if (k + step < pitch) fetch(k + step, next, snext);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const v4i fb = *(const v4i*)(b + k + h * 64);
-            const int sb = bs[k / 16 + h * 4];
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < Mt; ++i)
-                acc[i] = multiply16(fb, *(const v4i*)(a[i] + k + h * 64), acc[i], sb, as[i][k / 16 + h * 4]);
-        }
+                acc[i] = multiply16(fb[h], *(const v4i*)(a[i] + k + h * 64), acc[i], sb[h], as[i][k / 16 + h * 4]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) fb[h] = next[h], sb[h] = snext[h];
     }
 #pragma unroll
     for (int i = 0; i < Mt; ++i) part[wave][i][lane] = acc[i];
@@ -492,17 +528,30 @@ void launch_mx4_product(const Mx4Product& p, hipStream_t s)
     });
 }
 
-void launch_mx4_few(const Mx4Product& p, hipStream_t s)
+namespace {
+template <class X>
+void few(const Mx4Product& p, const typename X::T* x, int64_t ldx, hipStream_t s)
 {
     const uint32_t grid = (uint32_t)((p.n + 15) / 16);
     by_type(p.type, [&](auto e) {
         typedef decltype(e) E;
         if (p.m <= 16)
-            k_mx4_few<E, 1><<<grid, 64 * kFewWaves, 0, s>>>(p);
+            k_mx4_few<E, X, 1><<<grid, 64 * kFewWaves, 0, s>>>(p, x, ldx);
         else if (p.m <= 32)
-            k_mx4_few<E, 2><<<grid, 64 * kFewWaves, 0, s>>>(p);
-        else
-            k_mx4_few<E, 4><<<grid, 64 * kFewWaves, 0, s>>>(p);
+            k_mx4_few<E, X, 2><<<grid, 64 * kFewWaves, 0, s>>>(p, x, ldx);
+        else if constexpr (sizeof(typename X::T) == 1)
+            k_mx4_few<E, X, 4><<<grid, 64 * kFewWaves, 0, s>>>(p, x, ldx);
+    });
+}
+}  // namespace
+
+void launch_mx4_few(const Mx4Product& p, hipStream_t s) { few<Packed>(p, nullptr, 0, s); }
+
+void launch_mx4_few_x(const Mx4Product& p, const void* x, int type, int64_t ldx, hipStream_t s)
+{
+    by_type(type, [&](auto t) {
+        typedef decltype(t) X;
+        few<X>(p, (const typename X::T*)x, ldx, s);
     });
 }
 
