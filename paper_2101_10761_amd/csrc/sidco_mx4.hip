@@ -21,13 +21,30 @@ struct F32 {
     static __device__ __forceinline__ float widen(T x) { return x; }
     static __device__ __forceinline__ T narrow(float x) { return x; }
 };
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+
 struct F16 {
     typedef _Float16 T;
+    // fp32 bits of the magnitude that a 16-bit one has, and two neighbours' codes over `scale` into byte Sel
+    static __device__ __forceinline__ uint32_t widen_bits(uint32_t m) { return __float_as_uint((float)__builtin_bit_cast(_Float16, (unsigned short)m)); }
+    template <int Sel>
+    static __device__ __forceinline__ uint32_t encode2(uint32_t c, uint32_t two, float scale)
+    {
+        typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(v2h, two), scale, Sel);
+    }
     static __device__ __forceinline__ float widen(T x) { return (float)x; }
     static __device__ __forceinline__ T narrow(float x) { return (T)x; }
 };
 struct Bf16 {
     typedef __bf16 T;
+    static __device__ __forceinline__ uint32_t widen_bits(uint32_t m) { return m << 16; }
+    template <int Sel>
+    static __device__ __forceinline__ uint32_t encode2(uint32_t c, uint32_t two, float scale)
+    {
+        typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(v2b, two), scale, Sel);
+    }
     static __device__ __forceinline__ float widen(T x) { return (float)x; }
     static __device__ __forceinline__ T narrow(float x) { return (T)x; }
 };
@@ -124,6 +141,22 @@ __device__ __forceinline__ uint32_t encode8(const float x[8], uint32_t byte)
     return byte == 255 ? 0 : c;
 }
 
+// The same for elements of 16 bits, which stay as they are, two to a register: a magnitude's order is that of its bits, and the
+// conversion takes pairs and divides by the scale itself.
+__device__ __forceinline__ us2 magnitudes(uint32_t two) { return __builtin_bit_cast(us2, two & 0x7fff7fffu); }
+__device__ __forceinline__ us2 larger2(us2 a, us2 b) { return __builtin_elementwise_max(a, b); }
+
+template <class E>
+__device__ __forceinline__ uint32_t encode_pairs(uint32_t a, uint32_t b, uint32_t d, uint32_t e, uint32_t byte)
+{
+    const float scale = scale_of(byte);
+    uint32_t c = E::template encode2<0>(0, a, scale);
+    c = E::template encode2<1>(c, b, scale);
+    c = E::template encode2<2>(c, d, scale);
+    c = E::template encode2<3>(c, e, scale);
+    return byte == 255 ? 0 : c;
+}
+
 // what 8 codes stand for, times the scale's power of two
 __device__ __forceinline__ void decode8(uint32_t c, float scale, float x[8])
 {
@@ -208,17 +241,19 @@ __global__ __launch_bounds__(kFlat) void k_mx4_aggregate(const uint8_t* __restri
 constexpr int kSide = 128;       // a block quantises kSide x kSide elements
 constexpr int kQuant = 512;
 
-// Along the rows a quad of lanes has a block as above.  Along the columns a lane has one: it reads 32 rows of its column
-// from LDS.  Its four neighbours' codes follow each other in the transposed row, so a quad of lanes takes one column's four
-// blocks; the columns of a block of 32 rows are kept in LDS with their bits 4 and 5 changed by the block's number, so that
-// the quad's lanes read different banks.
+// Along the rows a quad of lanes has a block as above.  Along the columns a lane reads its column from LDS: 32 rows of one of
+// fp32 elements, 16 of two neighbouring ones of 16 bits, two lanes then having a block.  The blocks' codes follow each other
+// in the transposed row, so neighbouring lanes take the blocks of one column; their rows' columns are kept with bits 4 to 6
+// changed by the block's number, so that the lanes read different banks.
 template <class E, bool Along, bool Across>
 __global__ __launch_bounds__(kQuant) void k_mx4_quantize(const typename E::T* __restrict__ x, int64_t rows, int64_t cols, int64_t ldx,
-                                                         uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                                                         uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t,
+                                                           uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                                           uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t,
                                                            uint32_t across_x)
 {
     typedef typename E::T T;
+    constexpr bool kHalf = sizeof(T) == 2;
+    constexpr int kTurn = kHalf ? 16 : 32;  // rows whose columns are kept alike
     __shared__ __align__(16) T tile[Across ? kSide * kSide : 1];
     const int64_t r0 = (int64_t)(blockIdx.x / across_x) * kSide, c0 = (int64_t)(blockIdx.x % across_x) * kSide;
     const int64_t pitch = mx4_padded(cols) / 2, pitch_t = mx4_padded(rows) / 2;
@@ -228,36 +263,76 @@ __global__ __launch_bounds__(kQuant) void k_mx4_quantize(const typename E::T* __
         const int g = k * kQuant + threadIdx.x, r = g / (kSide / 8), c = g % (kSide / 8) * 8;
         const int64_t row = r0 + r, left = row < rows ? cols - (c0 + c) : 0;
         const T* p = x + row * ldx + c0 + c;
-        float v[8];
-        if (left >= 8)
-            load8<E>(p, v);
-        else
-            load_few<E>(p, left, v);
-        if (along) {
-            const uint32_t byte = exponent_byte(largest_of_quad(largest8(v)));
-            const uint32_t code = encode8(v, byte);
-            if (row < rows) {
-                *(uint32_t*)(codes + row * pitch + (c0 + c) / 2) = code;
-                if ((threadIdx.x & 3) == 0) scales[row * (pitch / 16) + (c0 + c) / kMxBlock] = (uint8_t)byte;
+        T* to = &tile[Across ? r * kSide + (c ^ (r / kTurn * 16)) : 0];
+        uint32_t byte, code;
+        if constexpr (kHalf) {
+            u4 v = {0, 0, 0, 0};
+            if (left >= 8) {
+                v = *(const u4h*)p;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < left) v[i / 2] |= (uint32_t)__builtin_bit_cast(unsigned short, p[i]) << (16 * (i % 2));
             }
+            const us2 m = larger2(larger2(magnitudes(v[0]), magnitudes(v[1])), larger2(magnitudes(v[2]), magnitudes(v[3])));
+            byte = exponent_byte(largest_of_quad(E::widen_bits(larger(m[0], m[1]))));
+            code = encode_pairs<E>(v[0], v[1], v[2], v[3], byte);
+            if (Across) *(u4*)to = v;
+        } else {
+            float v[8];
+            if (left >= 8)
+                load8<E>(p, v);
+            else
+                load_few<E>(p, left, v);
+            byte = exponent_byte(largest_of_quad(largest8(v)));
+            code = encode8(v, byte);
+            if (Across) store8<E>(to, v);
         }
-        if (Across) store8<E>(&tile[r * kSide + (c ^ (r / 32 * 16))], v);
+        if (along && row < rows) {
+            *(uint32_t*)(codes + row * pitch + (c0 + c) / 2) = code;
+            if ((threadIdx.x & 3) == 0) scales[row * (pitch / 16) + (c0 + c) / kMxBlock] = (uint8_t)byte;
+        }
     }
     if (!Across) return;
     __syncthreads();
-    const int c = threadIdx.x / 4, b = threadIdx.x % 4;
-    float v[32];
-    uint32_t top = 0;
+    if constexpr (kHalf) {
+        const int c = threadIdx.x / 8 * 2, h = threadIdx.x % 8;  // columns c and c + 1, rows 16 h to 16 h + 15
+        uint32_t v[16];
+        us2 top = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        v[i] = E::widen(tile[(b * 32 + i) * kSide + (c ^ (b * 16))]);
-        top = larger(top, magnitude(v[i]));
+        for (int i = 0; i < 16; ++i) {
+            v[i] = *(const uint32_t*)&tile[(h * 16 + i) * kSide + (c ^ (h * 16))];
+            top = larger2(top, magnitudes(v[i]));
+        }
+        const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, top), 0xb1, 0xf, 0xf, true);  // lanes 1 0 3 2
+        top = larger2(top, __builtin_bit_cast(us2, other));
+        if (!across) return;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (c0 + c + j >= cols) break;
+            const uint32_t byte = exponent_byte(E::widen_bits(top[j])), pick = j ? 0x07060302u : 0x05040100u;
+            uint32_t two[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) two[i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], pick);
+            uint2 code = {encode_pairs<E>(two[0], two[1], two[2], two[3], byte), encode_pairs<E>(two[4], two[5], two[6], two[7], byte)};
+            *(uint2*)(codes_t + (c0 + c + j) * pitch_t + r0 / 2 + h * 8) = code;
+            if ((h & 1) == 0) scales_t[(c0 + c + j) * (pitch_t / 16) + r0 / kMxBlock + h / 2] = (uint8_t)byte;
+        }
+    } else {
+        const int c = threadIdx.x / 4, b = threadIdx.x % 4;
+        float v[32];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            v[i] = tile[(b * 32 + i) * kSide + (c ^ (b * 16))];
+            top = larger(top, magnitude(v[i]));
+        }
+        if (!across || c0 + c >= cols) return;
+        const uint32_t byte = exponent_byte(top);
+        const u4 code = {encode8(v, byte), encode8(v + 8, byte), encode8(v + 16, byte), encode8(v + 24, byte)};
+        *(u4*)(codes_t + (c0 + c) * pitch_t + r0 / 2 + b * 16) = code;
+        scales_t[(c0 + c) * (pitch_t / 16) + r0 / kMxBlock + b] = (uint8_t)byte;
     }
-    if (!across || c0 + c >= cols) return;
-    const uint32_t byte = exponent_byte(top);
-    const u4 code = {encode8(v, byte), encode8(v + 8, byte), encode8(v + 16, byte), encode8(v + 24, byte)};
-    *(u4*)(codes_t + (c0 + c) * pitch_t + r0 / 2 + b * 16) = code;
-    scales_t[(c0 + c) * (pitch_t / 16) + r0 / kMxBlock + b] = (uint8_t)byte;
 }
 
 template <class E>
@@ -310,7 +385,7 @@ __device__ __forceinline__ void store_product(const Mx4Product& p, int64_t m, in
 }
 
 template <class E, class Tl>
-__global__ __launch_bounds__(Tl::kThreads) void k_mx4_product(Mx4Product p, uint32_t tm, uint32_t tn)
+__global__ __launch_bounds__(Tl::kThreads) void k_mx4_product(Mx4Product p, uint32_t tm, uint32_t tn, uint32_t from)
 {
     __shared__ __align__(1024) char lds[Tl::kLds];
     const uint32_t pitch = (uint32_t)(mx4_padded(p.k) / 2);
@@ -320,7 +395,7 @@ __global__ __launch_bounds__(Tl::kThreads) void k_mx4_product(Mx4Product p, uint
         uint32_t i, j;
         tile_of(xcd_run(tile, tm * tn), tm, tn, i, j);
         m0 = i * Tl::kM;
-        n0 = j * Tl::kN;
+        n0 = from + j * Tl::kN;
     };
     t.template run<1>(
         tm * tn, pitch, lds,
@@ -509,23 +584,27 @@ void launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t 
 
 void launch_mx4_product(const Mx4Product& p, hipStream_t s)
 {
-    const int pick = best_tile([&](int64_t b) { return ((p.m + b - 1) / b) * ((p.n + b - 1) / b); }, mx4_padded(p.k) / 2 / kLine);
-    auto go = [&](auto e, auto t) {
-        typedef decltype(e) E;
-        typedef typename decltype(t)::Is Tl;
-        const uint32_t tm = (uint32_t)((p.m + Tl::kM - 1) / Tl::kM), tn = (uint32_t)((p.n + Tl::kN - 1) / Tl::kN);
-        k_mx4_product<E, Tl><<<tile_blocks(pick, (int64_t)tm * tn), Tl::kThreads, 0, s>>>(p, tm, tn);
+    auto part = [&](int pick, int64_t from, int64_t columns) {
+        auto go = [&](auto e, auto t) {
+            typedef decltype(e) E;
+            typedef typename decltype(t)::Is Tl;
+            const uint32_t tm = (uint32_t)((p.m + Tl::kM - 1) / Tl::kM), tn = (uint32_t)((columns + Tl::kN - 1) / Tl::kN);
+            k_mx4_product<E, Tl><<<tile_blocks(pick, (int64_t)tm * tn), Tl::kThreads, 0, s>>>(p, tm, tn, (uint32_t)from);
+        };
+        by_type(p.type, [&](auto e) {
+            if (pick == 0)
+                go(e, Shape<Tile<Mx4Core, 256, 256, 2, 2, 2, 2>>());
+            else if (pick == 1)
+                go(e, Shape<Tile<Mx4Core, 192, 192, 2, 2, 2, 3>>());
+            else if (pick == 2)
+                go(e, Shape<Tile<Mx4Core, 128, 128, 2, 2, 2, 2>>());
+            else
+                go(e, Shape<Tile<Mx4Core, 64, 64, 2, 2, 2, 4>>());
+        });
     };
-    by_type(p.type, [&](auto e) {
-        if (pick == 0)
-            go(e, Shape<Tile<Mx4Core, 256, 256, 2, 2, 2, 2>>());
-        else if (pick == 1)
-            go(e, Shape<Tile<Mx4Core, 192, 192, 2, 2, 2, 3>>());
-        else if (pick == 2)
-            go(e, Shape<Tile<Mx4Core, 128, 128, 2, 2, 2, 2>>());
-        else
-            go(e, Shape<Tile<Mx4Core, 64, 64, 2, 2, 2, 4>>());
-    });
+    const TilePlan plan = plan_tiles(p.m, p.n, 1, mx4_padded(p.k) / 2 / kLine);
+    part(plan.pick, 0, plan.columns);
+    if (plan.columns < p.n) part(plan.rest_pick, plan.columns, p.n - plan.columns);
 }
 
 namespace {

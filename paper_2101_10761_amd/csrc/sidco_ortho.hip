@@ -7,11 +7,13 @@
 // the diagonal and mirrored.  With a in P's diagonal the last product needs no second operand in its epilogue, and the largest
 // term of the sum is not rounded twice.
 //
-// Operands are halves; sums, the norm and the update are fp32 or more.  Singular values stay below 4, so X and G are kept
-// times 2^14 and P times a power of two that follows from a, b, c: entries far below the largest one keep their 11 bits.  Of
-// X's relative error of 2^-12 an element, about 1.5e-3 (2-norm) reaches the result, less than a result in bf16 loses; halves
-// are used where it has 16 bits.  For a result in 32 bits each operand is a pair of halves, the second one what the first
-// leaves, 22 bits together, and a product is three: high high + low high + high low.
+// Steps go in groups (see group_of): within one the next G is P G P, and X moves once, by the product of the P.
+//
+// Operands are halves; sums, the norm and the update are fp32 or more.  Singular values stay below 1.5, so X and G are kept
+// times 2^14 and P and its products times powers of two that follow from a, b, c: entries far below the largest one keep their
+// 11 bits.  Of X's relative error of 2^-12 an element, about 1.5e-3 (2-norm) reaches the result, less than a result in bf16
+// loses; halves are used where it has 16 bits.  For a result in 32 bits each operand is a pair of halves, the second one what
+// the first leaves, 22 bits together, and a product is three: low high + high low + high high.
 #include <math.h>
 
 #include <type_traits>
@@ -401,7 +403,7 @@ __device__ __forceinline__ void finish1(const Result& o, int64_t z, int64_t r, i
 // X' = Q X: X' and its transpose, or with Last the result, of element type T.
 template <class Tl, bool Full, bool Last, class T>
 __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plane x2, Plane xt2, uint32_t m, uint32_t n, uint32_t tm, uint32_t tn,
-                                                        uint32_t total, float back, Result o)
+                                                        uint32_t total, uint32_t from, float back, Result o)
 {
     constexpr int B = Tl::kM;
     __shared__ __align__(1024) char lds[lds_of<Tl>()];
@@ -413,7 +415,7 @@ __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plan
         const uint32_t w = xcd_run(tile, total);
         uint32_t i, j;
         tile_of(w % (tm * tn), tm, tn, i, j);
-        return {w / (tm * tn), i * B, j * B};
+        return {w / (tm * tn), i * B, from + j * B};
     };
     Tl t;
     t.template run<Full ? 3 : 1>(
@@ -864,16 +866,16 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
         return {a, b, o, so / (sa * sb), 0.0f, 0.0f};
     };
     auto poly = [&](const Plane& gm, const Plane& o) -> Symmetric { return {gm, gm, o, q.c * sp / (sx * sx), q.b * sp / sx, q.a * sp}; };
-    const int apply_pick = best_tile([&](int64_t b) { return ((m + b - 1) / b) * ((n + b - 1) / b) * q.batch; }, l.mp * 2 / kLine * segments);
-    auto apply = [&](const Plane& by, float sb, int from, bool last) {
-        by_tile(apply_pick, [&](auto shape) {
+    const TilePlan plan = plan_tiles(m, n, q.batch, l.mp * 2 / kLine * segments);
+    auto apply_part = [&](int pick, int64_t first, int64_t columns, const Plane& by, float sb, int from, bool last) {
+        by_tile(pick, [&](auto shape) {
             typedef typename decltype(shape)::Is Tl;
-            const uint32_t ti = (uint32_t)((m + Tl::kM - 1) / Tl::kM), tj = (uint32_t)((n + Tl::kN - 1) / Tl::kN);
+            const uint32_t ti = (uint32_t)((m + Tl::kM - 1) / Tl::kM), tj = (uint32_t)((columns + Tl::kN - 1) / Tl::kN);
             const Result o = {q.out, tall, q.update, q.keep, q.gain, q.ldo, q.out_stride, q.rows, q.cols};
             auto go = [&](auto kernel, float back) {
                 const uint32_t total = ti * tj * batch;
-                kernel<<<tile_blocks(apply_pick, total), Tl::kThreads, 0, s>>>(by, xt[from], x[1 - from], xt[1 - from], (uint32_t)m, (uint32_t)n, ti, tj,
-                                                                              total, back, o);
+                kernel<<<tile_blocks(pick, total), Tl::kThreads, 0, s>>>(by, xt[from], x[1 - from], xt[1 - from], (uint32_t)m, (uint32_t)n, ti, tj,
+                                                                        total, (uint32_t)first, back, o);
             };
             if (!last)
                 go(k_apply<Tl, Full, false, float>, 1.0f / sb);
@@ -884,6 +886,10 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
             else
                 go(k_apply<Tl, Full, true, __bf16>, 1.0f / (sx * sb));
         });
+    };
+    auto apply = [&](const Plane& by, float sb, int from, bool last) {
+        apply_part(plan.pick, 0, plan.columns, by, sb, from, last);
+        if (plan.columns < n) apply_part(plan.rest_pick, plan.columns, n - plan.columns, by, sb, from, last);
     };
     const std::true_type with_poly;
     const std::false_type plain;

@@ -475,20 +475,50 @@ struct TileCost {
 constexpr TileCost kTileCosts[] = {{256, 1, 1.55f, 1.75f, 7.0f, 10.0f}, {192, 1, 1.05f, 1.10f, 6.0f, 8.0f}, {128, 2, 0.80f, 1.25f, 2.5f, 5.5f}, {64, 2, 0.25f, 0.58f, 2.0f, 4.5f}};
 constexpr int kCus = 256;
 
+inline double tile_time(int pick, int64_t tiles, int64_t lines)
+{
+    const TileCost& c = kTileCosts[pick];
+    const int64_t slots = (int64_t)kCus * c.per_cu, left = tiles % slots;
+    double t = c.launch + (double)(tiles / slots) * (lines * c.line + c.round);
+    if (left) t += lines * (left <= kCus ? c.alone : c.line) + c.round;
+    return t;
+}
+
 // count(side): tiles of the whole launch.  Returns an index of kTileCosts.
 template <class Count>
-inline int best_tile(const Count& count, int64_t lines)
+inline int best_tile(const Count& count, int64_t lines, double* time = nullptr)
 {
     int best = 0;
     double least = 0.0;
     for (int i = 0; i < 4; ++i) {
-        const TileCost& c = kTileCosts[i];
-        const int64_t n = count(c.side), slots = (int64_t)kCus * c.per_cu, left = n % slots;
-        double t = c.launch + (double)(n / slots) * (lines * c.line + c.round);
-        if (left) t += lines * (left <= kCus ? c.alone : c.line) + c.round;
+        const double t = tile_time(i, count(kTileCosts[i].side), lines);
         if (i == 0 || t < least) least = t, best = i;
     }
+    if (time) *time = least;
     return best;
+}
+
+// A batch of m x n products in one launch or two: the first n columns in as many large tiles as fill whole rounds, and the rest
+// in tiles of its own.  4096 x 25088 in tiles of 256 is 6.1 rounds, done in 7.
+struct TilePlan {
+    int pick, rest_pick;
+    int64_t columns;  // of the first launch
+};
+inline TilePlan plan_tiles(int64_t m, int64_t n, int64_t batch, int64_t lines)
+{
+    auto tiles = [&](int64_t cols, int64_t side) { return (m + side - 1) / side * ((cols + side - 1) / side) * batch; };
+    double least = 0.0;
+    TilePlan plan = {best_tile([&](int64_t side) { return tiles(n, side); }, lines, &least), 0, n};
+    for (int i = 0; i < 2; ++i) {
+        const int64_t side = kTileCosts[i].side, strip = (m + side - 1) / side * batch, slots = (int64_t)kCus * kTileCosts[i].per_cu;
+        const int64_t columns = tiles(n, side) / slots * slots / strip * side;
+        if (columns <= 0 || columns >= n) continue;
+        double rest = 0.0;
+        const int rest_pick = best_tile([&](int64_t s) { return tiles(n - columns, s); }, lines, &rest);
+        const double t = tile_time(i, tiles(columns, side), lines) + rest;
+        if (t < least) least = t, plan = {i, rest_pick, columns};
+    }
+    return plan;
 }
 
 // Blocks of a launch of that many tiles: each works one after the other.
