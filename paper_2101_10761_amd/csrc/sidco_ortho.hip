@@ -341,19 +341,23 @@ __global__ __launch_bounds__(Tl::kThreads) void k_symmetric(Symmetric first, Sym
             const Symmetric& p = at.second ? second : first;
             const Plane g = p.b;
             const float p2 = p.p2, p1 = p.p1, p0 = p.p0;
-            auto value = [&](uint32_t r, uint32_t c, const v4f& v) -> v4f {
-                if (!Poly) return v * p2;
-                v4f w = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (r < m && c < (uint32_t)g.pitch) {
-                    const _Float16* q = g.at + at.z * g.stride + (int64_t)r * g.pitch + c;
-                    const v4h h = *(const v4h*)q;
-                    v4h l = {0, 0, 0, 0};
-                    if (Full) l = *(const v4h*)(q + g.low);
+            if (Poly) {  // in place: G is read once, and a tile off the diagonal goes out twice
+                t.become([&](uint32_t r, uint32_t c, const v4f& v) -> v4f {
+                    r += at.m0;
+                    c += at.n0;
+                    v4f w = {0.0f, 0.0f, 0.0f, 0.0f};
+                    if (r < m && c < (uint32_t)g.pitch) {
+                        const _Float16* q = g.at + at.z * g.stride + (int64_t)r * g.pitch + c;
+                        const v4h h = *(const v4h*)q;
+                        v4h l = {0, 0, 0, 0};
+                        if (Full) l = *(const v4h*)(q + g.low);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) w[k] = fmaf(p2, v[k], fmaf(p1, (float)h[k] + (float)l[k], r == c + k ? p0 : 0.0f));
-                }
-                return w;
-            };
+                        for (int k = 0; k < 4; ++k) w[k] = fmaf(p2, v[k], fmaf(p1, (float)h[k] + (float)l[k], r == c + k ? p0 : 0.0f));
+                    }
+                    return w;
+                });
+            }
+            auto value = [&](uint32_t, uint32_t, const v4f& v) -> v4f { return Poly ? v : v * p2; };
             put_tile<false, Full>(t, lds + Tl::kLds, p.out, at.z, m, m, at.m0, at.n0, value);
             if (at.m0 != at.n0) put_tile<true, Full>(t, lds + Tl::kLds, p.out, at.z, m, m, at.m0, at.n0, value);
         });

@@ -406,6 +406,19 @@ struct Tile {
         }
     }
 
+    // The sums become f(row, column, sums).
+    template <class F>
+    __device__ __forceinline__ void become(const F& f)
+    {
+        uint32_t row = wave / WN * (BM / WM) + (lane & 15), col = wave % WN * (BN / WN) + 4 * (lane >> 4);
+#pragma unroll
+        for (int i = 0; i < kMt; ++i) {
+            asm volatile("" : "+v"(row), "+v"(col));  // addresses of later rows are not kept from here on
+#pragma unroll
+            for (int j = 0; j < kNt; ++j) acc[i][j] = f(row + i * 16, col + j * 16, acc[i][j]);
+        }
+    }
+
     // ---- by way of LDS ----
     //
     // A lane holds four neighbouring columns; halves stored like that touch 16 rows with 32 bytes each.  So a wave puts 16 rows (or columns, for the transpose) of its tile at a time into LDS, as S, and reads them
