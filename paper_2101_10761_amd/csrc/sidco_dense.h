@@ -34,17 +34,9 @@ struct Mx4Product {
     int64_t ldc;
 };
 void launch_mx4_product(const Mx4Product& p, hipStream_t s);
-constexpr int kFewRows = 64;  // rows of A up to which launch_mx4_few serves
-void launch_mx4_few(const Mx4Product& p, hipStream_t s);
-// The same with rows of A as they are, which every block of 16 rows of B quantises on its own into LDS.  Two launches and this
-// one, us: 1 row, 4096 x 4096 10.9 and 6.7; 20 rows, 10000 x 1500 11.3 and 11.1, where the two meet.
-void launch_mx4_few_x(const Mx4Product& p, const void* x, int type, int64_t ldx, hipStream_t s);
-constexpr int kFewElements = 65536;  // of A, padding included, that LDS has room for
-inline bool few_takes_x(int64_t m, int64_t n, int64_t k)
-{
-    const int64_t all = m * mx4_padded(k);
-    return m <= 32 && all <= kFewElements && all / 4096 * ((n + 15) / 16) <= 20 * 256;
-}
+// The same with rows of A as they are, quantised on the way: where mx4_takes_x(m, n, k).
+bool mx4_takes_x(int64_t m, int64_t n, int64_t k);
+void launch_mx4_product_x(const Mx4Product& p, const void* x, int type, int64_t ldx, hipStream_t s);
 
 // A batch of matrices orthogonalised, out of x or of the momentum that x moves, into out or into the weights there
 struct OrthoCall {

@@ -150,10 +150,7 @@ int sidco_mx4_matmul(void* stream, const uint8_t* a_codes, const uint8_t* a_scal
     if (int rc = check_result(c, c_dtype, n, ldc, alpha, accumulate)) return rc;
     if (((m + 63) / 64) * ((n + 63) / 64) > (int64_t)INT32_MAX) return SIDCO_ERR_SIZE;
     const Mx4Product p = {a_codes, a_scales, b_codes, b_scales, m, n, k, alpha, accumulate != 0, c, type_of(c_dtype), ldc};
-    if (m <= kFewRows)
-        launch_mx4_few(p, (hipStream_t)stream);
-    else
-        launch_mx4_product(p, (hipStream_t)stream);
+    launch_mx4_product(p, (hipStream_t)stream);
     return launched();
 }
 
@@ -174,9 +171,9 @@ int sidco_mx4_linear(void* stream, const void* x, int x_dtype, int64_t rows, int
     if (((rows + 63) / 64) * ((n + 63) / 64) > (int64_t)INT32_MAX) return SIDCO_ERR_SIZE;
     if (!aligned_type(x, x_dtype)) return SIDCO_ERR_ALIGN;
     if (int rc = check_result(c, c_dtype, n, ldc, alpha, accumulate)) return rc;
-    if (few_takes_x(rows, n, k)) {
+    if (mx4_takes_x(rows, n, k)) {
         const Mx4Product p = {nullptr, nullptr, w_codes, w_scales, rows, n, k, alpha, accumulate != 0, c, type_of(c_dtype), ldc};
-        launch_mx4_few_x(p, x, type_of(x_dtype), ldx, (hipStream_t)stream);
+        launch_mx4_product_x(p, x, type_of(x_dtype), ldx, (hipStream_t)stream);
         return launched();
     }
     StreamScratch ws(stream, (size_t)(code_bytes(rows, k) + scale_bytes(rows, k)));
@@ -185,10 +182,7 @@ int sidco_mx4_linear(void* stream, const void* x, int x_dtype, int64_t rows, int
     uint8_t* scales = codes + code_bytes(rows, k);
     launch_mx4_quantize(x, type_of(x_dtype), rows, k, ldx, codes, scales, nullptr, nullptr, (hipStream_t)stream);
     const Mx4Product p = {codes, scales, w_codes, w_scales, rows, n, k, alpha, accumulate != 0, c, type_of(c_dtype), ldc};
-    if (rows <= kFewRows)
-        launch_mx4_few(p, (hipStream_t)stream);
-    else
-        launch_mx4_product(p, (hipStream_t)stream);
+    launch_mx4_product(p, (hipStream_t)stream);
     return launched();
 }
 

@@ -168,7 +168,9 @@ __device__ __forceinline__ void decode8(uint32_t c, float scale, float x[8])
 constexpr int kFlat = 256;  // threads of the kernels of flat vectors
 
 // A lane has 8 neighbours, a quad of lanes a block.  acc = g + r; the residual keeps what the codes do not hold, and all of
-// acc where the block stands for NaN.
+// acc where the block stands for NaN.  Bound by memory: one pass, and the block's largest magnitude goes round its quad in
+// registers, so that LDS and a second look at the data are not needed.  138.4 M elements, gradient in bf16 with a residual:
+// 270 us for 1.46 GB, 5.4 TB/s (a plain copy reaches 5.0); 270 thousand of fp32: 2.9 us, a launch.
 template <class E, bool Residual>
 __global__ __launch_bounds__(kFlat) void k_mx4_compress(const typename E::T* __restrict__ grad, float* __restrict__ residual, int64_t d,
                                                         uint32_t* __restrict__ codes, uint8_t* __restrict__ scales, int64_t groups)
@@ -203,6 +205,9 @@ __global__ __launch_bounds__(kFlat) void k_mx4_compress(const typename E::T* __r
     }
 }
 
+// dense (+)= scale * the sum over the workers, in their order and in fp32: one thread adds all of an element, and the result is
+// the same in every run.  Bound by memory: codes are read once, the dense vector is written once.  Four workers' loads are
+// under way together (eight were no faster).  138.4 M elements of 8 workers: 252 us for 1.14 GB, 4.5 TB/s.
 template <bool Accumulate>
 __global__ __launch_bounds__(kFlat) void k_mx4_aggregate(const uint8_t* __restrict__ codes, int64_t code_stride,
                                                          const uint8_t* __restrict__ scales, int64_t scale_stride, int workers,
@@ -244,7 +249,11 @@ constexpr int kQuant = 512;
 // Along the rows a quad of lanes has a block as above.  Along the columns a lane reads its column from LDS: 32 rows of one of
 // fp32 elements, 16 of two neighbouring ones of 16 bits, two lanes then having a block.  The blocks' codes follow each other
 // in the transposed row, so neighbouring lanes take the blocks of one column; their rows' columns are kept with bits 4 to 6
-// changed by the block's number, so that the lanes read different banks.
+// changed by the block's number, so that the lanes read different banks.  x is read once for both.  Bound by memory, and more
+// so by the short pieces (64 bytes of 128 rows and of 128 columns) that a square tile writes: bf16, both directions,
+// 4096 x 25088 81 us for 315 MB, 3.9 TB/s; 16384 x 4096 61 us for 206 MB, 3.4 TB/s.  Tiles given to the XCDs in runs make whole
+// lines of the pieces in L2 (81 to 79 us) but leave the codes elsewhere for whoever reads them next (64 us, and 6 us on two
+// reads): not done.  Two loads in flight ahead of the first use cost registers and time (61 to 65 us).
 template <class E, bool Along, bool Across>
 __global__ __launch_bounds__(kQuant) void k_mx4_quantize(const typename E::T* __restrict__ x, int64_t rows, int64_t cols, int64_t ldx,
                                                            uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
@@ -335,6 +344,8 @@ __global__ __launch_bounds__(kQuant) void k_mx4_quantize(const typename E::T* __
     }
 }
 
+// A lane has 8 neighbours of a row; a block of 2048 columns takes rows in turn.  Bound by memory: 16384 x 4096 to bf16 39 us for
+// 170 MB, 4.4 TB/s; 26 us where the codes are still in the caches.
 template <class E>
 __global__ __launch_bounds__(kFlat) void k_mx4_dequantize(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                           int64_t rows, int64_t cols, typename E::T* __restrict__ out, int64_t ldo)
@@ -384,6 +395,11 @@ __device__ __forceinline__ void store_product(const Mx4Product& p, int64_t m, in
     }
 }
 
+// Many rows on both sides: the matrix cores' time.  The instruction multiplies codes under their blocks' exponents and adds in
+// fp32, so codes go from memory to it as they are; alpha and the old C are the epilogue's.  4096 x 4096 x 25088 (rows, columns,
+// contraction) 190 us, 4.4 PFLOP/s; 4096 x 25088 x 4096 to bf16 256 + 19 us in two launches, 3.1, and 25088 columns to fp32
+// 281 + 20 us, 2.8, where every 32 lines of a tile end with its stores; 8192 cubed 258 us, 4.3.  The matrix units are busy
+// two thirds of the time and the clock falls under their load.
 template <class E, class Tl>
 __global__ __launch_bounds__(Tl::kThreads) void k_mx4_product(Mx4Product p, uint32_t tm, uint32_t tn, uint32_t from)
 {
@@ -429,8 +445,11 @@ __device__ __forceinline__ v4f multiply16(const v4i& a, const v4i& b, const v4f&
 
 // Few rows of A: the time is that of reading B once.  A block has 16 rows of B; its 8 waves take lines in turn, straight to
 // registers, the next line under way while one is multiplied, and add up in LDS.  A comes in blocks, or (X other than Packed) as
-// it is: then each block quantises all of it into LDS while its first lines are under way.
+// it is: then each block quantises all of it into LDS while its first lines are under way, which a launch less pays for while A
+// has few elements.  1 x 4096 by 4096 x 4096: 5.0 us (8.9 MB, 1.8 TB/s: a launch's start, one trip to memory for each of two
+// lines, a sum).
 constexpr int kFewWaves = 8;
+constexpr int kFewElements = 65536;  // of A, padding included, that LDS has room for
 struct Packed {
     typedef uint8_t T;
 };
@@ -582,8 +601,67 @@ void launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t 
     });
 }
 
+namespace {
+
+// Rows that k_mx4_few serves, two instructions' worth.
+constexpr int kFewRows = 32;
+
+// Times, us, for the choice between k_mx4_few and a tile of 64 rows, which leaves most of itself empty but has its operands
+// under way ahead.  The first spreads a row of B over 8 waves and is better where rows are long and few, the second where there
+// are many.  Measured, us, few / tiles, 1, 16 and 32 rows:
+//   4096 x 25088 12.9 18.8 29.1 / 32.0 33.4 40.2; 4096 x 16384 11.1 16.8 23.9 / 22.6 23.8 27.1; 8192 x 8192 12.3 17.3 24.4 /
+//   13.9 14.3 16.2; 25088 x 4096 17.2 27.5 39.8 / 14.3 15.7 17.9; 16384 x 16384 35.6 58.1 86.9 / 25.0 27.1 31.1;
+// with 64 rows 45.8 / 53.7 for the first of these, 38.0 / 35.2 and 38.8 / 20.7 for the next.  A as it is costs each block its
+// quantisation, a launch of its own 3 us; one launch / two, 1, 4 and 16 rows:
+//   4096 x 4096 8.9 8.4 11.3 / 11.6 11.2 11.0; 10000 x 4096 9.1 12.0 22.4 / 11.9 11.7 12.2; 16384 x 16384 34.9 45.4 / 27.9 28.1;
+//   10000 x 1500 8.7 8.3 10.1 / 11.0 10.5 11.1, with 20 rows 11.5 / 10.9, with 32 16.4 / 10.8.
+struct FewTimes {
+    float few, few_x, tiles;
+};
+FewTimes few_times(int64_t m, int64_t n, int64_t k)
+{
+    const float blocks = (float)((n + 15) / 16) / kCus, rounds = blocks > 1.0f ? blocks : 1.0f;
+    const int64_t lines = mx4_padded(k) / 2 / kLine;
+    const float few = 4.0f + rounds * (float)lines / kFewWaves * (0.9f + 0.04f * (float)m);
+    return {few, few + rounds * (0.3f + 0.22f * (float)(m * mx4_padded(k)) / 4096.0f), (float)tile_time(3, (n + 63) / 64, lines)};
+}
+
+template <class X>
+void few(const Mx4Product& p, const typename X::T* x, int64_t ldx, hipStream_t s)
+{
+    const uint32_t grid = (uint32_t)((p.n + 15) / 16);
+    by_type(p.type, [&](auto e) {
+        typedef decltype(e) E;
+        if (p.m <= 16)
+            k_mx4_few<E, X, 1><<<grid, 64 * kFewWaves, 0, s>>>(p, x, ldx);
+        else
+            k_mx4_few<E, X, 2><<<grid, 64 * kFewWaves, 0, s>>>(p, x, ldx);
+    });
+}
+
+}  // namespace
+
+bool mx4_takes_x(int64_t m, int64_t n, int64_t k)
+{
+    if (m > kFewRows || m * mx4_padded(k) > kFewElements) return false;
+    const FewTimes t = few_times(m, n, k);
+    return t.few_x <= 3.0f + (t.few < t.tiles ? t.few : t.tiles);
+}
+
+void launch_mx4_product_x(const Mx4Product& p, const void* x, int type, int64_t ldx, hipStream_t s)
+{
+    by_type(type, [&](auto t) {
+        typedef decltype(t) X;
+        few<X>(p, (const typename X::T*)x, ldx, s);
+    });
+}
+
 void launch_mx4_product(const Mx4Product& p, hipStream_t s)
 {
+    if (p.m <= kFewRows) {
+        const FewTimes t = few_times(p.m, p.n, p.k);
+        if (t.few <= t.tiles) return few<Packed>(p, nullptr, 0, s);
+    }
     auto part = [&](int pick, int64_t from, int64_t columns) {
         auto go = [&](auto e, auto t) {
             typedef decltype(e) E;
@@ -605,33 +683,6 @@ void launch_mx4_product(const Mx4Product& p, hipStream_t s)
     const TilePlan plan = plan_tiles(p.m, p.n, 1, mx4_padded(p.k) / 2 / kLine);
     part(plan.pick, 0, plan.columns);
     if (plan.columns < p.n) part(plan.rest_pick, plan.columns, p.n - plan.columns);
-}
-
-namespace {
-template <class X>
-void few(const Mx4Product& p, const typename X::T* x, int64_t ldx, hipStream_t s)
-{
-    const uint32_t grid = (uint32_t)((p.n + 15) / 16);
-    by_type(p.type, [&](auto e) {
-        typedef decltype(e) E;
-        if (p.m <= 16)
-            k_mx4_few<E, X, 1><<<grid, 64 * kFewWaves, 0, s>>>(p, x, ldx);
-        else if (p.m <= 32)
-            k_mx4_few<E, X, 2><<<grid, 64 * kFewWaves, 0, s>>>(p, x, ldx);
-        else if constexpr (sizeof(typename X::T) == 1)
-            k_mx4_few<E, X, 4><<<grid, 64 * kFewWaves, 0, s>>>(p, x, ldx);
-    });
-}
-}  // namespace
-
-void launch_mx4_few(const Mx4Product& p, hipStream_t s) { few<Packed>(p, nullptr, 0, s); }
-
-void launch_mx4_few_x(const Mx4Product& p, const void* x, int type, int64_t ldx, hipStream_t s)
-{
-    by_type(type, [&](auto t) {
-        typedef decltype(t) X;
-        few<X>(p, (const typename X::T*)x, ldx, s);
-    });
 }
 
 }  // namespace sidco

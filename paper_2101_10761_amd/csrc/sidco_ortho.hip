@@ -129,7 +129,9 @@ __device__ __forceinline__ void update8(const Start<T>& p, int64_t z, int64_t r,
     }
 }
 
-// Moves the momentum and adds up u^2.  A block takes rows, of a matrix without gaps pieces of kNormRow elements, in turn.
+// Moves the momentum and adds up u^2, in 64 bits.  A block takes rows, of a matrix without gaps pieces of kNormRow elements, in
+// turn; its sum has a place of its own, so that the total does not depend on which block ends first.  Bound by memory:
+// 4096 x 25088, gradient in fp16, 168 us for 1.03 GB, 6.1 TB/s; four of 1500 x 6000 in fp32 76 us for 432 MB, 5.7 TB/s.
 constexpr int kNormRow = 16 * kNormBlock;
 template <class T>
 __global__ __launch_bounds__(kNormBlock) void k_norm(Start<T> p)
@@ -198,7 +200,9 @@ __device__ __forceinline__ void put8(const Plane& o, int64_t z, int64_t r, int64
     if (Full) *(v8h*)(p + o.low) = l;
 }
 
-// 64 x 64 elements a block: rows go to `natural`, and through LDS to `turned`, the padding of both as zeros.
+// 64 x 64 elements a block: rows go to `natural`, and through LDS to `turned`, the padding of both as zeros.  X is kept both
+// ways so that every product reads whole lines along its contraction.  Bound by memory: 4096 x 25088 with momentum 215 us for
+// 1.03 GB, 4.8 TB/s; four of 1500 x 6000, pairs of halves, 110 us for 576 MB, 5.2 TB/s.
 template <class T, bool Full>
 __global__ __launch_bounds__(256) void k_start(Start<T> p, float eps, Plane natural, Plane turned)
 {
@@ -309,7 +313,10 @@ struct Symmetric {
     float p2, p1, p0;
 };
 
-// One or two of them of the same size.  Tiles on and below the diagonal are computed and mirrored.
+// One or two of them of the same size.  Tiles on and below the diagonal are computed and mirrored: half the operations, and a
+// second way out through LDS.  Bound by the matrix cores and by how 253 tiles meet 256 CUs: m = 4096 in halves 80 us a product
+// (6.9e10 operations, 0.86 PFLOP/s), 84 with the polynomial; four of m = 1500, three products of halves each, 82 and 94 us
+// (4.1e10, 0.5: 144 tiles); six of m = 256, 5.6 us, a launch.
 template <class Tl, bool Full, bool Poly>
 __global__ __launch_bounds__(Tl::kThreads) void k_symmetric(Symmetric first, Symmetric second, uint32_t m, uint32_t tiles, uint32_t each,
                                                             uint32_t total)
@@ -404,7 +411,9 @@ __device__ __forceinline__ void finish1(const Result& o, int64_t z, int64_t r, i
     *p = (T)(o.update ? fmaf(o.gain, v, o.keep * (float)*p) : v);
 }
 
-// X' = Q X: X' and its transpose, or with Last the result, of element type T.
+// X' = Q X: X' and its transpose, or with Last the result, of element type T.  Bound by the matrix cores: m = 4096, n = 25088 in
+// halves 751 + 35 us in two launches, 1.07 PFLOP/s (a large library product of the type reaches 1.35); four of 1500 x 6000 in
+// pairs of halves 378 + 71 and 336 + 71 us, 0.72 and 0.80.
 template <class Tl, bool Full, bool Last, class T>
 __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plane x2, Plane xt2, uint32_t m, uint32_t n, uint32_t tm, uint32_t tn,
                                                         uint32_t total, uint32_t from, float back, Result o)
@@ -447,7 +456,9 @@ __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plan
 // ---- a matrix in one block ----
 //
 // With m <= 64 and X^T in LDS one block does everything, all steps in one launch; the launches of the kernels above, 2 and 15
-// for 5 steps, take longer than their work at this size.  X^T is kept by rows of 64 (m padded with zeros), so that
+// for 5 steps, take longer than their work at this size, 5 us and more each.  Bound by the chain of reads, products and
+// barriers of a step, and a matrix has one CU: 64 x 576 in 32 bits, momentum and weights with it, 61 us, of which 7 to 9 a step
+// and the rest the start and the end.  X^T is kept by rows of 64 (m padded with zeros), so that
 //   G = X X^T  reads its operands down the columns, with the transposing read of LDS,
 //   X <- P X   reads rows and writes them in place: a row of X^T depends on that row alone, and each wave has its own.
 // G and P, being small, are pairs of halves whatever X is.  16-byte piece c of row r is kept at place c ^ (r % 8).
@@ -734,7 +745,8 @@ __global__ __launch_bounds__(64 * kOneWaves) void k_one(One p)
     }
 }
 
-// Whether k_one has room, and its launch.
+// Whether k_one has room, and its launch.  Where it has, it is faster at every batch; us, 64 x 576 here / 65 x 576 there, batches
+// of 3, 64 and 1024: 52 53 233 / 129 199 985, in halves 43 44 174 / 84 118 555; and 64 x 128 20 21 80 / 65 x 128 107 112 591.
 template <bool Full>
 bool one_block(const OrthoCall& q, float sp, hipStream_t s)
 {

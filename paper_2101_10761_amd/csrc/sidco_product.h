@@ -421,8 +421,8 @@ struct Tile {
 
     // ---- by way of LDS ----
     //
-    // A lane holds four neighbouring columns; halves stored like that touch 16 rows with 32 bytes each.  So a wave puts 16 rows (or columns, for the transpose) of its tile at a time into LDS, as S, and reads them
-    // back in 16 bytes a lane along the row.
+    // A lane holds four neighbouring columns; halves stored like that touch 16 rows with 32 bytes each.  So a wave puts 16 rows
+    // (or columns, for the transpose) of its tile at a time into LDS, as S, and reads them back in 16 bytes a lane along the row.
 
     static constexpr int pad(int bytes) { return bytes + 16; }
     template <class S>

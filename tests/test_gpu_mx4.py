@@ -259,6 +259,25 @@ def test_layer_on_rows_as_they_come(rows, n, k, dtype):
     np.testing.assert_array_equal(_host(narrow), _host((out * 0.5).to(narrow.dtype)))
 
 
+# few rows against many or few, long or short rows: both kernels that serve them, a layer in one launch and in two
+@pytest.mark.parametrize("m,n,k", [(1, 40_001, 700), (7, 600, 5000), (16, 300, 9000), (17, 30_003, 600), (31, 9000, 1500), (32, 70, 4000),
+                                   (33, 4100, 300)])
+def test_few_rows(m, n, k):
+    torch, sidco = _torch(), _sidco()
+    rng = np.random.default_rng(m + n + k)
+    a, b = _whole(rng, m, k, 0), _whole(rng, n, k, 0)  # multiples of 1/4, at most 36 a product: exact up to 2^24 / 144 columns
+    want = a.astype(np.float32) @ b.astype(np.float32).T
+    out = torch.full((m + 1, n + 3), 7.0, dtype=torch.float32, device="cuda")
+    sidco.sidco_mx4_matmul(*_upload(a), *_upload(b), k, out[:m, 1:n + 1])
+    np.testing.assert_array_equal(_host(out[:m, 1:n + 1]), want)
+    pb = _upload(b)
+    layer = torch.full((m, n), 0.25, dtype=torch.float32, device="cuda")
+    sidco.sidco_mx4_linear(_dev(a.astype(np.float32), "bfloat16"), *pb, layer, alpha=-2.0, accumulate=True)
+    np.testing.assert_array_equal(_host(layer), 0.25 - 2.0 * want)
+    out[:m, 1:n + 1] = 7.0
+    assert bool((out == 7.0).all()), "written outside the result"
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 40, 300), (20, 40, 300), (200, 100, 600), (600, 600, 300)])
 def test_blocks_that_stand_for_nan(m, n, k):
     """A row with such a block gives NaN in its whole row or column of the product and nowhere else."""
