@@ -455,7 +455,7 @@ __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plan
 
 // ---- a matrix in one block ----
 //
-// With m <= 64 and X^T in LDS one block does everything, all steps in one launch; the launches of the kernels above, 2 and 15
+// With m <= 64 and X^T in LDS one block does everything, all steps in one launch; the launches of the kernels above, 2 and 17
 // for 5 steps, take longer than their work at this size, 5 us and more each.  Bound by the chain of reads, products and
 // barriers of a step, and a matrix has one CU: 64 x 576 in 32 bits, momentum and weights with it, 61 us, of which 7 to 9 a step
 // and the rest the start and the end.  X^T is kept by rows of 64 (m padded with zeros), so that
