@@ -565,13 +565,18 @@ size_t sidco_workspace_bytes_mx4_linear(int64_t rows, int64_t k);
  * below 1.5 on the way; a matrix of zeros stays one, and a NaN or an infinity in u
  * makes its matrix NaN.
  *
- * precision: SIDCO_NS_HALF multiplies operands of 11 bits (for matrices of random
- * numbers the result is within about 2e-3 of the exact one, in the 2-norm),
- * SIDCO_NS_FULL of 22 bits (1e-6, at about three times the time); sums are fp32
- * either way.  Directions that u lacks altogether hold what the roundings left
- * there, a^steps times: for a matrix of rank one up to 0.1 of the result with
- * HALF, 1e-4 with FULL.  SIDCO_NS_BY_TYPE takes FULL where the result is fp32 and
- * HALF where it has 16 bits.
+ * precision: SIDCO_NS_FULL multiplies operands of 22 bits, SIDCO_NS_HALF of 11,
+ * at about a third of the operations; sums are fp32 either way.  How far a result
+ * of 5 steps with the default coefficients is from the exact one, in the 2-norm,
+ * depends on u's singular values: what a rounding leaves in directions in which u
+ * has little or nothing is multiplied by up to a in each step after it.
+ *                 alike   like 1/k   like 1/k^2, or 32 alone   rank one
+ *     FULL        1e-6    2e-6       1.5e-5                    7e-5
+ *     HALF        2e-3    3e-3       2.5e-2                    0.15
+ * SIDCO_NS_BY_TYPE takes as much as the result's type shows: FULL for fp32 and
+ * fp16; for bf16, whose own rounding is 1.7e-3, HALF in the last step and FULL in
+ * those before it (4e-4 to 8e-4, 1.4e-3 at rank one), or FULL in all if a, b and c
+ * move some singular value by more than a factor of 4.
  * Results are deterministic.  Matrices of a batch have the same shape, and rows,
  * cols <= 2^21, batch <= 65535.                                               */
 #define SIDCO_NS_BY_TYPE 0

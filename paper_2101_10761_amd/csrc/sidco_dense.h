@@ -50,14 +50,14 @@ struct OrthoCall {
     int64_t rows, cols;
     int steps;
     float a, b, c, eps;
-    bool full;        // operands of 22 bits instead of 11
+    int paired;       // steps from the first on whose operands have 22 bits; the others' have 11
     void* out;
     int out_type;
     int64_t ldo, out_stride;
     bool update;      // out = keep * out + gain * result
     float keep, gain;
 };
-size_t ortho_scratch(int batch, int64_t rows, int64_t cols, bool full);
+size_t ortho_scratch(const OrthoCall& q);  // of x, ldx and out it needs nothing
 void launch_orthogonalize(const OrthoCall& q, char* scratch, hipStream_t s);
 
 }  // namespace sidco

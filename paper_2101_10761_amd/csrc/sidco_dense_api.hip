@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include "sidco_dense.h"
+#include "sidco_ortho_plan.h"
 
 using namespace sidco;
 
@@ -52,20 +53,27 @@ int check_batch(int batch, int64_t rows, int64_t cols)
     return tiles <= (int64_t)INT32_MAX / batch ? SIDCO_OK : SIDCO_ERR_SIZE;
 }
 
-bool full_precision(const sidco_newton_schulz& o, int out_dtype)
+int paired_steps(const sidco_newton_schulz& o, int out_dtype)
 {
-    return o.precision == SIDCO_NS_FULL || (o.precision == SIDCO_NS_BY_TYPE && out_dtype == SIDCO_GRAD_F32);
+    if (o.precision == SIDCO_NS_FULL) return o.steps;
+    if (o.precision == SIDCO_NS_HALF) return 0;
+    return ortho_paired(o.steps, o.a, o.b, o.c, type_of(out_dtype) == kGradBf16);
 }
 
-int orthogonalize(void* stream, OrthoCall& q, const sidco_newton_schulz& o, int out_dtype)
+void take_options(OrthoCall& q, const sidco_newton_schulz& o, int out_dtype)
 {
     q.steps = o.steps;
     q.a = o.a;
     q.b = o.b;
     q.c = o.c;
     q.eps = o.eps;
-    q.full = full_precision(o, out_dtype);
-    StreamScratch ws(stream, ortho_scratch(q.batch, q.rows, q.cols, q.full));
+    q.paired = paired_steps(o, out_dtype);
+}
+
+int orthogonalize(void* stream, OrthoCall& q, const sidco_newton_schulz& o, int out_dtype)
+{
+    take_options(q, o, out_dtype);
+    StreamScratch ws(stream, ortho_scratch(q));
     if (ws.rc != SIDCO_OK) return ws.rc;
     launch_orthogonalize(q, ws.data, (hipStream_t)stream);
     return launched();
@@ -195,7 +203,12 @@ size_t sidco_workspace_bytes_orthogonalize(int batch, int64_t rows, int64_t cols
 {
     const sidco_newton_schulz o = opt ? *opt : kNewtonSchulz;
     if (check_batch(batch, rows, cols) != SIDCO_OK || !element_type(out_dtype) || check_newton_schulz(o) != SIDCO_OK) return 0;
-    return workspace_with_scratch(ortho_scratch(batch, rows, cols, full_precision(o, out_dtype)));
+    OrthoCall q = {};
+    q.batch = batch;
+    q.rows = rows;
+    q.cols = cols;
+    take_options(q, o, out_dtype);
+    return workspace_with_scratch(ortho_scratch(q));
 }
 
 int sidco_orthogonalize(void* stream, const void* x, int x_dtype, int64_t ldx, int64_t x_stride, int batch, int64_t rows, int64_t cols,

@@ -7,18 +7,23 @@
 // the diagonal and mirrored.  With a in P's diagonal the last product needs no second operand in its epilogue, and the largest
 // term of the sum is not rounded twice.
 //
-// Steps go in groups (see group_of): within one the next G is P G P, and X moves once, by the product of the P.
+// Steps go in groups (sidco_ortho_plan.h): within one the next G is P G P, and X moves once, by the product of the P.
 //
 // Operands are halves; sums, the norm and the update are fp32 or more.  Singular values stay below 1.5, so X and G are kept
 // times 2^14 and P and its products times powers of two that follow from a, b, c: entries far below the largest one keep their
-// 11 bits.  Of X's relative error of 2^-12 an element, about 1.5e-3 (2-norm) reaches the result, less than a result in bf16
-// loses; halves are used where it has 16 bits.  For a result in 32 bits each operand is a pair of halves, the second one what
-// the first leaves, 22 bits together, and a product is three: low high + high low + high high.
+// 11 bits.  Or each operand is a pair of halves, the second one what the first leaves, 22 bits together, and a product is three:
+// low high + high low + high high.  Which of the two is decided step by step: what a rounding leaves in directions in which u has
+// little or nothing is multiplied by up to a in every step after it, so that halves from the first step on cost a result 1e-3
+// where the singular values are alike, but 1.6e-2 to 2.4e-2 where they fall off like 1/k^2 or exp(-k/10) or 32 of them are all there
+// are, and 0.15 at rank one (a = 3.4445, five steps).  With pairs in all steps but the last it is 4e-4 to 8e-4, 1.4e-3 at rank
+// one, less than a result in bf16 loses by its own rounding (1.7e-3; together 1.7e-3 to 1.8e-3 and 2.4e-3): that is what such a
+// result takes.  Results in fp32 and fp16 take pairs throughout (5e-7 to 1.3e-5; 6.5e-5).
 #include <math.h>
 
 #include <type_traits>
 
 #include "sidco_dense.h"
+#include "sidco_ortho_plan.h"
 #include "sidco_product.h"
 
 namespace sidco {
@@ -183,7 +188,7 @@ __global__ __launch_bounds__(kNormBlock) void k_norm(Start<T> p)
 // Where X and X^T of one matrix after the other lie: rows of `pitch` halves, the low halves `low` after the high ones.
 struct Plane {
     _Float16* at;
-    int64_t pitch, low, stride;
+    int64_t pitch, low, stride;  // low 0: there are none
 };
 
 template <bool Full>
@@ -285,7 +290,7 @@ __device__ __forceinline__ void put_tile(Tl& t, char* lds, const Plane& o, int64
         };
     };
     t.template out<_Float16, Turn>(lds, at, store(false));
-    if (Full) t.template out<_Float16, Turn>(lds, [&](uint32_t r, uint32_t c, const v4f& v) { return rest_of(rounded(at(r, c, v))); }, store(true));
+    if (Full && o.low) t.template out<_Float16, Turn>(lds, [&](uint32_t r, uint32_t c, const v4f& v) { return rest_of(rounded(at(r, c, v))); }, store(true));
 }
 
 __device__ __forceinline__ Rows rows_of(const Plane& o, int64_t z, uint32_t rows, bool low = false)
@@ -772,22 +777,26 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 constexpr int kSmall = 7;  // G, G', P, P', T, Q, Q'
 struct Layout {
     int64_t m, n, mp, np;
-    int planes, parts;
+    OrthoGroups groups;
+    int planes, planes2;  // of X and the symmetric matrices; of the second X, which takes turns with the first
+    int parts;
     size_t part_bytes, total;
-    Layout(int batch, int64_t rows, int64_t cols, bool full)
+    explicit Layout(const OrthoCall& q)
     {
-        m = rows < cols ? rows : cols;
-        n = rows < cols ? cols : rows;
+        m = q.rows < q.cols ? q.rows : q.cols;
+        n = q.rows < q.cols ? q.cols : q.rows;
         mp = up(m, 64);
         np = up(n, 64);
-        planes = full ? 2 : 1;
-        const int64_t want = (rows * cols + kNormRow - 1) / kNormRow;
+        groups = ortho_groups(q.batch, m, n, q.steps, q.paired);
+        planes = q.paired > 0 ? 2 : 1;
+        planes2 = q.paired > groups.paired ? 2 : 1;  // one group of steps in pairs leaves an X for halves, or the result
+        const int64_t want = (q.rows * q.cols + kNormRow - 1) / kNormRow;
         parts = (int)(want < 1024 ? want : 1024);
-        part_bytes = (size_t)up((int64_t)batch * parts * (int64_t)sizeof(double), 256);
-        const int64_t halves = 2 * plane(m, np) + 2 * plane(n, mp) + kSmall * plane(m, mp);
-        total = part_bytes + (size_t)batch * halves * sizeof(_Float16);
+        part_bytes = (size_t)up((int64_t)q.batch * parts * (int64_t)sizeof(double), 256);
+        const int64_t halves = plane(m, np, planes) + plane(n, mp, planes) + plane(m, np, planes2) + plane(n, mp, planes2) + kSmall * plane(m, mp, planes);
+        total = part_bytes + (size_t)q.batch * halves * sizeof(_Float16);
     }
-    int64_t plane(int64_t height, int64_t pitch) const { return up(height * pitch * planes, 128); }
+    static int64_t plane(int64_t height, int64_t pitch, int count) { return up(height * pitch * count, 128); }
 };
 
 template <class Tl>
@@ -809,32 +818,10 @@ void by_tile(int pick, const F& f)
         f(Shape<Tile<HalfCore, 64, 64, 2, 2, 2, 4>>());
 }
 
-// How many steps share a pass over X.  Steps after the first of a group know their G without X: P and G commute, so that
-// (PX)(PX)^T = P G P, and the group's X is Q X with Q the product of its P.  In products of m x m x m operations, symmetric ones
-// counting half, and with n = r m, a step of its own costs 3r + 1 and one that joins a group 4.  What rounding leaves in G where
-// it should be small grows by a^2 with every step of a group, as the error of X itself does by a; with a = 3.4445, errors of
-// groups of 2 in halves are those of single steps (1e-3 to 3e-3 for spectra from flat to 1/k; of 3 up to 6e-3), of 3 with 22 bits
-// too (3e-7 to 6e-6; of 5 without bound).  A launch counts 4 us against 6e14 operations a second.
-int group_of(const OrthoCall& q, int64_t m, int64_t n, bool full)
-{
-    const double r = (double)n / (double)m, unit = (double)q.batch * (double)m * (double)m * (double)m * (full ? 3.0 : 1.0) / 6e8;
-    int best = 1;
-    double least = 0.0;
-    for (int g = 1; g <= (full ? 3 : 2) && g <= q.steps; ++g) {
-        const int groups = (q.steps + g - 1) / g, joined = q.steps - groups;
-        const double t = (groups * (3 * r + 1) + joined * 4) * unit + (groups * 3 + joined * 4) * 4.0;
-        if (g == 1 || t < least) least = t, best = g;
-    }
-    return best;
-}
-
-template <bool Full>
 void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
 {
-    // Scales: the largest powers of two that leave room for the largest element of P = a + bx + cx^2 over the squares x of
-    // singular values up to 1.5, of Q's products of it and of T = P G.
-    float top = fmaxf(fabsf(q.a), fabsf(q.a + 2.25f * q.b + 5.0625f * q.c));
-    if (q.c != 0.0f && -q.b / (2 * q.c) > 0.0f && -q.b / (2 * q.c) < 2.25f) top = fmaxf(top, fabsf(q.a - q.b * q.b / (4 * q.c)));
+    // Scales: the largest powers of two that leave room for the largest element of P, of Q's products of it and of T = P G.
+    const float top = ortho_growth(q.a, q.b, q.c);
     auto scale = [](float bound) {
         int e = 0;
         (void)frexpf(32768.0f / fmaxf(bound, 1.0f), &e);
@@ -842,76 +829,82 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
     };
     const float sx = kScaleX, sp = scale(top), st = scale(2.25f * top);
 
-    if (one_block<Full>(q, sp, s)) return;
+    if (q.paired > 0 ? one_block<true>(q, sp, s) : one_block<false>(q, sp, s)) return;
 
-    const Layout l(q.batch, q.rows, q.cols, Full);
+    const Layout l(q);
     const uint32_t batch = (uint32_t)q.batch;
     const int64_t m = l.m, n = l.n;
     const bool tall = q.rows > q.cols;
     _Float16* at = (_Float16*)(ws + l.part_bytes);
-    auto plane = [&](int64_t height, int64_t pitch) {
-        const int64_t each = l.plane(height, pitch);
-        Plane p = {at, pitch, height * pitch, each};
+    auto plane = [&](int64_t height, int64_t pitch, int count) {
+        const int64_t each = l.plane(height, pitch, count);
+        Plane p = {at, pitch, count == 2 ? height * pitch : 0, each};
         at += each * q.batch;
         return p;
     };
     Plane x[2], xt[2], g[2], pm[2], qm[2];
-    for (int i = 0; i < 2; ++i) x[i] = plane(m, l.np), xt[i] = plane(n, l.mp), g[i] = plane(m, l.mp), pm[i] = plane(m, l.mp), qm[i] = plane(m, l.mp);
-    const Plane tm = plane(m, l.mp);
+    for (int i = 0; i < 2; ++i) {
+        x[i] = plane(m, l.np, i ? l.planes2 : l.planes);
+        xt[i] = plane(n, l.mp, i ? l.planes2 : l.planes);
+        g[i] = plane(m, l.mp, l.planes);
+        pm[i] = plane(m, l.mp, l.planes);
+        qm[i] = plane(m, l.mp, l.planes);
+    }
+    const Plane tm = plane(m, l.mp, l.planes);
 
     by_element(q.x_type, [&](auto type) {
         typedef typename decltype(type)::T T;
         const Start<T> p = {(const T*)q.x, q.ldx, q.x_stride, q.momentum, q.mu, q.nesterov, q.rows, q.cols, (double*)ws, l.parts};
         k_norm<T><<<dim3((uint32_t)l.parts, batch), kNormBlock, 0, s>>>(p);
         const dim3 grid((uint32_t)((q.cols + 63) / 64), (uint32_t)((q.rows + 63) / 64), batch);
-        k_start<T, Full><<<grid, 256, 0, s>>>(p, q.eps, tall ? xt[0] : x[0], tall ? x[0] : xt[0]);
+        if (q.paired > 0)
+            k_start<T, true><<<grid, 256, 0, s>>>(p, q.eps, tall ? xt[0] : x[0], tall ? x[0] : xt[0]);
+        else
+            k_start<T, false><<<grid, 256, 0, s>>>(p, q.eps, tall ? xt[0] : x[0], tall ? x[0] : xt[0]);
     });
 
-    const int64_t segments = Full ? 3 : 1;
     auto triangle = [](int64_t side, int64_t b) { const int64_t k = (side + b - 1) / b; return k * (k + 1) / 2; };
-    auto symmetric = [&](auto poly, int jobs, const Symmetric& a, const Symmetric& b) {
-        const int pick = best_tile([&](int64_t side) { return triangle(m, side) * q.batch * jobs; }, a.a.pitch * 2 / kLine * segments);
-        by_tile(pick, [&](auto shape) {
-            typedef typename decltype(shape)::Is Tl;
-            const uint32_t tri = (uint32_t)triangle(m, Tl::kM), each = tri * batch;
-            k_symmetric<Tl, Full, decltype(poly)::value>
-                <<<tile_blocks(pick, each * jobs), Tl::kThreads, 0, s>>>(a, b, (uint32_t)m, tri, each, each * jobs);
-        });
-    };
     auto product = [](const Plane& a, float sa, const Plane& b, float sb, const Plane& o, float so) -> Symmetric {
         return {a, b, o, so / (sa * sb), 0.0f, 0.0f};
     };
     auto poly = [&](const Plane& gm, const Plane& o) -> Symmetric { return {gm, gm, o, q.c * sp / (sx * sx), q.b * sp / sx, q.a * sp}; };
-    const TilePlan plan = plan_tiles(m, n, q.batch, l.mp * 2 / kLine * segments);
-    auto apply_part = [&](int pick, int64_t first, int64_t columns, const Plane& by, float sb, int from, bool last) {
-        by_tile(pick, [&](auto shape) {
-            typedef typename decltype(shape)::Is Tl;
-            const uint32_t ti = (uint32_t)((m + Tl::kM - 1) / Tl::kM), tj = (uint32_t)((columns + Tl::kN - 1) / Tl::kN);
-            const Result o = {q.out, tall, q.update, q.keep, q.gain, q.ldo, q.out_stride, q.rows, q.cols};
-            auto go = [&](auto kernel, float back) {
-                const uint32_t total = ti * tj * batch;
-                kernel<<<tile_blocks(pick, total), Tl::kThreads, 0, s>>>(by, xt[from], x[1 - from], xt[1 - from], (uint32_t)m, (uint32_t)n, ti, tj,
-                                                                        total, (uint32_t)first, back, o);
-            };
-            if (!last)
-                go(k_apply<Tl, Full, false, float>, 1.0f / sb);
-            else if (q.out_type == kGradF32)
-                go(k_apply<Tl, Full, true, float>, 1.0f / (sx * sb));
-            else if (q.out_type == kGradF16)
-                go(k_apply<Tl, Full, true, _Float16>, 1.0f / (sx * sb));
-            else
-                go(k_apply<Tl, Full, true, __bf16>, 1.0f / (sx * sb));
-        });
-    };
-    auto apply = [&](const Plane& by, float sb, int from, bool last) {
-        apply_part(plan.pick, 0, plan.columns, by, sb, from, last);
-        if (plan.columns < n) apply_part(plan.rest_pick, plan.columns, n - plan.columns, by, sb, from, last);
-    };
     const std::true_type with_poly;
     const std::false_type plain;
-    const int group = group_of(q, m, n, Full);
-    for (int done = 0, from = 0; done < q.steps; from = 1 - from) {
-        const int steps = q.steps - done < group ? q.steps - done : group;
+    // `steps` steps from x[from], in pairs of halves or halves; what comes out is the result, or an X with or without low halves
+    auto pass = [&](auto pairs, int steps, int from, bool last, bool low) {
+        constexpr bool Full = decltype(pairs)::value;
+        const int64_t segments = Full ? 3 : 1;
+        auto symmetric = [&](auto poly, int jobs, const Symmetric& a, const Symmetric& b) {
+            const int pick = best_tile([&](int64_t side) { return triangle(m, side) * q.batch * jobs; }, a.a.pitch * 2 / kLine * segments);
+            by_tile(pick, [&](auto shape) {
+                typedef typename decltype(shape)::Is Tl;
+                const uint32_t tri = (uint32_t)triangle(m, Tl::kM), each = tri * batch;
+                k_symmetric<Tl, Full, decltype(poly)::value>
+                    <<<tile_blocks(pick, each * jobs), Tl::kThreads, 0, s>>>(a, b, (uint32_t)m, tri, each, each * jobs);
+            });
+        };
+        auto apply_part = [&](int pick, int64_t first, int64_t columns, const Plane& by, float sb) {
+            Plane to = x[1 - from], to_t = xt[1 - from];
+            if (!low) to.low = to_t.low = 0;
+            by_tile(pick, [&](auto shape) {
+                typedef typename decltype(shape)::Is Tl;
+                const uint32_t ti = (uint32_t)((m + Tl::kM - 1) / Tl::kM), tj = (uint32_t)((columns + Tl::kN - 1) / Tl::kN);
+                const Result o = {q.out, tall, q.update, q.keep, q.gain, q.ldo, q.out_stride, q.rows, q.cols};
+                auto go = [&](auto kernel, float back) {
+                    const uint32_t total = ti * tj * batch;
+                    kernel<<<tile_blocks(pick, total), Tl::kThreads, 0, s>>>(by, xt[from], to, to_t, (uint32_t)m, (uint32_t)n, ti, tj, total,
+                                                                            (uint32_t)first, back, o);
+                };
+                if (!last)
+                    go(k_apply<Tl, Full, false, float>, 1.0f / sb);
+                else if (q.out_type == kGradF32)
+                    go(k_apply<Tl, Full, true, float>, 1.0f / (sx * sb));
+                else if (q.out_type == kGradF16)
+                    go(k_apply<Tl, Full, true, _Float16>, 1.0f / (sx * sb));
+                else
+                    go(k_apply<Tl, Full, true, __bf16>, 1.0f / (sx * sb));
+            });
+        };
         const Symmetric gram = product(x[from], sx, x[from], sx, g[0], sx);
         symmetric(plain, 1, gram, gram);
         symmetric(with_poly, 1, poly(g[0], pm[0]), gram);
@@ -937,21 +930,26 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
                 by = qm[now], sb = scale(grown *= top);
             }
         }
+        const TilePlan plan = plan_tiles(m, n, q.batch, l.mp * 2 / kLine * segments);
+        apply_part(plan.pick, 0, plan.columns, by, sb);
+        if (plan.columns < n) apply_part(plan.rest_pick, plan.columns, n - plan.columns, by, sb);
+    };
+    for (int done = 0, from = 0; done < q.steps; from = 1 - from) {
+        const bool pairs = done < q.paired;
+        const int left = (pairs ? q.paired : q.steps) - done, most = pairs ? l.groups.paired : l.groups.halves;
+        const int steps = left < most ? left : most;
         done += steps;
-        apply(by, sb, from, done == q.steps);
+        if (pairs)
+            pass(std::true_type(), steps, from, done == q.steps, done < q.paired);
+        else
+            pass(std::false_type(), steps, from, done == q.steps, false);
     }
 }
 
 }  // namespace
 
-size_t ortho_scratch(int batch, int64_t rows, int64_t cols, bool full) { return Layout(batch, rows, cols, full).total; }
+size_t ortho_scratch(const OrthoCall& q) { return Layout(q).total; }
 
-void launch_orthogonalize(const OrthoCall& q, char* scratch, hipStream_t s)
-{
-    if (q.full)
-        orthogonalize<true>(q, scratch, s);
-    else
-        orthogonalize<false>(q, scratch, s);
-}
+void launch_orthogonalize(const OrthoCall& q, char* scratch, hipStream_t s) { orthogonalize(q, scratch, s); }
 
 }  // namespace sidco
