@@ -19,10 +19,11 @@
  * outputs are valid once the stream reaches that point.  The library never
  * spins on the device, and an enqueueing call synchronises with the host in
  * one case only: when the stream's workspace has to grow (first use, or a
- * longer vector than before), it is freed and allocated again, which waits for
- * the device.  sidco_reserve moves that out of the enqueueing calls, and
- * sidco_compress_static never allocates at all.  (sidco_controller_compress also
- * reads one counter back on every Q-th call; that is its contract.)
+ * longer vector or larger matrices than before), it is freed and allocated again,
+ * which waits for the device.  sidco_reserve moves that out of the enqueueing
+ * calls, and sidco_compress_static never allocates at all.
+ * (sidco_controller_compress also reads one counter back on every Q-th call; that
+ * is its contract.)
  *
  * Results are deterministic for a given history of calls on a workspace: the
  * same inputs at the same places after the same previous calls give the same
@@ -51,8 +52,13 @@
  * Workspaces.  The library keeps one workspace per (device, stream), so calls
  * on different streams do not share state and may overlap; calls on one stream
  * are ordered by the stream.  A caller-provided workspace (sidco_set_workspace)
- * replaces them all on its device: calls that use it must not overlap.  The
- * diagnostics calls that take a stream (sidco_read_diag, sidco_fit_result, ...)
+ * replaces them all on its device: calls that use it must not overlap.  A graph
+ * that calls were captured into holds the workspace's address: reserve the most
+ * that calls on the stream need before capturing.  The dense operators' calls
+ * (sidco_mx4_*, sidco_orthogonalize, sidco_muon_step) work behind what the
+ * sparsifier's keep, or in memory of their own where the stream's workspace has
+ * no room: they never grow it, and leave the diagnostics, the scatter flag and the
+ * controller as they are.  The diagnostics calls that take a stream (sidco_read_diag, sidco_fit_result, ...)
  * report the last call made on that stream.
  */
 #ifndef SIDCO_H

@@ -50,6 +50,8 @@ struct WsCtx {
     void* ws = nullptr;        // workspace in use
     size_t ws_bytes = 0;
     bool ws_owned = false;
+    void* dense = nullptr;     // scratch of the dense calls that have no room behind the workspace's head
+    size_t dense_bytes = 0;
     hipEvent_t ev[kMaxKernels + 1] = {};
     bool ev_made = false;
     int prof_n = 0;            // kernels of the last profiled call
@@ -174,6 +176,31 @@ int ensure_workspace(WsCtx& c, size_t need)
     return SIDCO_OK;
 }
 
+// Scratch of a dense call, behind the head of the workspace if that is large enough (sidco_reserve, or a vector's), else of its
+// own: the workspace does not grow for it, because its head is what scatter_check, the diagnostics and the controller read
+// later, and graphs that a sparsifier call was captured into hold its address.
+int ensure_dense(WsCtx& c, size_t bytes, char** out)
+{
+    if (c.ws && c.ws_bytes >= head_bytes() + bytes) {
+        *out = (char*)c.ws + head_bytes();
+        return SIDCO_OK;
+    }
+    if (c.ws && !c.ws_owned) return SIDCO_ERR_WORKSPACE;  // caller-provided and too small
+    if (c.dense_bytes < bytes) {
+        hipError_t e = c.dense ? hipFree(c.dense) : hipSuccess;  // waits for work that still uses it
+        c.dense = nullptr;
+        c.dense_bytes = 0;
+        if (e != hipSuccess) return hip_fail(e, "hipFree(workspace)");
+        void* p = nullptr;
+        e = hipMalloc(&p, bytes);
+        if (e != hipSuccess) return hip_fail(e, "hipMalloc(workspace)");
+        c.dense = p;
+        c.dense_bytes = bytes;
+    }
+    *out = (char*)c.dense;
+    return SIDCO_OK;
+}
+
 // Launch geometry of a sweep (see WaveTiles): `base` is the vector whose lines the tiles sit on, NULL if its alignment
 // does not matter.  `turn_rows`: see kTurnRows.
 template <typename P>
@@ -266,6 +293,7 @@ int static_ws(WsCtx** out)
 void free_ws(WsCtx& c)
 {
     if (c.ws && c.ws_owned) (void)hipFree(c.ws);
+    if (c.dense) (void)hipFree(c.dense);
     if (c.ev_made)
         for (int i = 0; i <= kMaxKernels; ++i) (void)hipEventDestroy(c.ev[i]);
     for (auto* img : c.batch_images) delete img;
@@ -641,8 +669,7 @@ StreamScratch::StreamScratch(void* stream, size_t bytes) : rc(SIDCO_OK), data(nu
     g_mu.lock();
     WsCtx* c = nullptr;
     rc = pick_ws(stream, true, &c);
-    if (rc == SIDCO_OK) rc = ensure_workspace(*c, head_bytes() + bytes);
-    if (rc == SIDCO_OK) data = (char*)c->ws + head_bytes();
+    if (rc == SIDCO_OK) rc = ensure_dense(*c, bytes, &data);
 }
 
 StreamScratch::~StreamScratch() { g_mu.unlock(); }

@@ -406,9 +406,9 @@ void launch_gather(const Params& p, hipStream_t s);
 
 // ---- what the C ABI's other source files use of the one that keeps the workspaces ----
 
-// The workspace of `stream` behind its head, of at least `bytes` bytes and 256-byte aligned, for one call: no other call
-// enters the library while this lives.  rc is SIDCO_OK or the error to return.  What a call leaves there, later calls
-// may write over.
+// Scratch on `stream` of at least `bytes` bytes and 256-byte aligned, for one call: no other call enters the library while
+// this lives.  rc is SIDCO_OK or the error to return.  What a call leaves there, later calls may write over; what the
+// sparsifier's calls keep in the head of their workspace stays.
 class StreamScratch {
   public:
     StreamScratch(void* stream, size_t bytes);
