@@ -58,7 +58,7 @@ struct OrthoCall {
     float keep, gain;
 };
 size_t ortho_scratch(const OrthoCall& q);  // of x, ldx and out it needs nothing
-void launch_orthogonalize(const OrthoCall& q, char* scratch, hipStream_t s);
+void launch_orthogonalize(const OrthoCall& q, char* scratch, hipStream_t s);  // scratch may be NULL for ortho_one_block
 
 }  // namespace sidco
 #endif

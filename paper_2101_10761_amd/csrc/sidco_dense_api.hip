@@ -73,6 +73,10 @@ void take_options(OrthoCall& q, const sidco_newton_schulz& o, int out_dtype)
 int orthogonalize(void* stream, OrthoCall& q, const sidco_newton_schulz& o, int out_dtype)
 {
     take_options(q, o, out_dtype);
+    if (ortho_one_block(q.rows, q.cols, q.ldx, q.paired > 0)) {
+        launch_orthogonalize(q, nullptr, (hipStream_t)stream);
+        return launched();
+    }
     StreamScratch ws(stream, ortho_scratch(q));
     if (ws.rc != SIDCO_OK) return ws.rc;
     launch_orthogonalize(q, ws.data, (hipStream_t)stream);

@@ -467,7 +467,7 @@ __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plan
 //   G = X X^T  reads its operands down the columns, with the transposing read of LDS,
 //   X <- P X   reads rows and writes them in place: a row of X^T depends on that row alone, and each wave has its own.
 // G and P, being small, are pairs of halves whatever X is.  16-byte piece c of row r is kept at place c ^ (r % 8).
-constexpr int kOneWaves = 8, kOneSide = 64;
+constexpr int kOneWaves = 8;
 
 struct One {
     const void* x;
@@ -750,14 +750,13 @@ __global__ __launch_bounds__(64 * kOneWaves) void k_one(One p)
     }
 }
 
-// Whether k_one has room, and its launch.  Where it has, it is faster at every batch; us, 64 x 576 here / 65 x 576 there, batches
+// The launch of k_one.  Where it has room it is faster at every batch; us, 64 x 576 here / 65 x 576 there, batches
 // of 3, 64 and 1024: 52 53 233 / 129 199 985, in halves 43 44 174 / 84 118 555; and 64 x 128 20 21 80 / 65 x 128 107 112 591.
 template <bool Full>
-bool one_block(const OrthoCall& q, float sp, hipStream_t s)
+void one_block(const OrthoCall& q, float sp, hipStream_t s)
 {
     const int64_t m = q.rows < q.cols ? q.rows : q.cols, n = q.rows < q.cols ? q.cols : q.rows;
-    constexpr int kMost = Full ? 576 : 768, kFew = 128;  // the 160 KB of LDS, less 16 KB for G, or the registers; and less for little ones
-    if (m > kOneSide || n > kMost || q.ldx > (1 << 20)) return false;  // offsets of 32 bits within a matrix
+    constexpr int kMost = Full ? kOnePairs : kOneHalves, kFew = 128;  // less LDS for little ones
     const Result o = {q.out, q.rows > q.cols, q.update, q.keep, q.gain, q.ldo, q.out_stride, q.rows, q.cols};
     const One p = {q.x, q.ldx, q.x_stride, q.momentum, q.mu, q.nesterov, (int)q.rows, (int)q.cols, (int)m, (int)n,
                    q.steps, q.a, q.b, q.c, q.eps, sp, q.out_type, o};
@@ -768,7 +767,6 @@ bool one_block(const OrthoCall& q, float sp, hipStream_t s)
         else
             k_one<T, kMost, Full><<<(uint32_t)q.batch, 64 * kOneWaves, 0, s>>>(p);
     });
-    return true;
 }
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -829,7 +827,7 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
     };
     const float sx = kScaleX, sp = scale(top), st = scale(2.25f * top);
 
-    if (q.paired > 0 ? one_block<true>(q, sp, s) : one_block<false>(q, sp, s)) return;
+    if (ortho_one_block(q.rows, q.cols, q.ldx, q.paired > 0)) return q.paired > 0 ? one_block<true>(q, sp, s) : one_block<false>(q, sp, s);
 
     const Layout l(q);
     const uint32_t batch = (uint32_t)q.batch;

@@ -44,6 +44,15 @@ inline int ortho_group(int batch, int64_t m, int64_t n, int steps, bool pairs, i
     return best;
 }
 
+// Whether one block takes a matrix through all its steps, in LDS: 160 KB less 16 KB for G hold 576 rows of 64 pairs of halves;
+// of halves alone the registers have room for 768.  Offsets within the matrix have 32 bits there.
+constexpr int kOneSide = 64, kOnePairs = 576, kOneHalves = 768;
+inline bool ortho_one_block(int64_t rows, int64_t cols, int64_t ldx, bool pairs)
+{
+    const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    return m <= kOneSide && n <= (pairs ? kOnePairs : kOneHalves) && ldx <= (1 << 20);
+}
+
 struct OrthoGroups {
     int paired, halves;  // steps in a group of either kind; 0 where there is none
 };
