@@ -243,6 +243,10 @@ __global__ __launch_bounds__(kFlat) void k_mx4_aggregate(const uint8_t* __restri
 
 // ---- matrices ----
 
+// A launch's dimension has fewer than 2^32 threads: blocks of 512 beyond 2^20 go on in the next row of the grid.
+__device__ __forceinline__ uint32_t block_number() { return blockIdx.y * gridDim.x + blockIdx.x; }
+dim3 grid_of(uint32_t blocks) { return blocks <= 1u << 20 ? dim3(blocks) : dim3(1u << 20, (blocks - 1) / (1u << 20) + 1); }
+
 constexpr int kSide = 128;       // a block quantises kSide x kSide elements
 constexpr int kQuant = 512;
 
@@ -258,13 +262,15 @@ template <class E, bool Along, bool Across>
 __global__ __launch_bounds__(kQuant) void k_mx4_quantize(const typename E::T* __restrict__ x, int64_t rows, int64_t cols, int64_t ldx,
                                                            uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                                                            uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t,
-                                                           uint32_t across_x)
+                                                           uint32_t across_x, uint32_t blocks)
 {
     typedef typename E::T T;
     constexpr bool kHalf = sizeof(T) == 2;
     constexpr int kTurn = kHalf ? 16 : 32;  // rows whose columns are kept alike
     __shared__ __align__(16) T tile[Across ? kSide * kSide : 1];
-    const int64_t r0 = (int64_t)(blockIdx.x / across_x) * kSide, c0 = (int64_t)(blockIdx.x % across_x) * kSide;
+    const uint32_t block = block_number();
+    if (block >= blocks) return;
+    const int64_t r0 = (int64_t)(block / across_x) * kSide, c0 = (int64_t)(block % across_x) * kSide;
     const int64_t pitch = mx4_padded(cols) / 2, pitch_t = mx4_padded(rows) / 2;
     const bool along = Along && c0 < pitch * 2, across = Across && r0 < pitch_t * 2;
 #pragma unroll
@@ -462,7 +468,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_mx4_few(Mx4Product p, const 
     __shared__ v4f part[kFewWaves][Mt][64];
     __shared__ __align__(16) uint8_t codes[kPacked ? 16 : kFewElements / 2 + Mt * 16 * kRowPad], exps[kPacked ? 1 : kFewElements / kMxBlock];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int64_t n0 = (int64_t)block_number() * 16;
+    if (n0 >= p.n) return;
     const int64_t pitch = mx4_padded(p.k) / 2;
     const int64_t nb = n0 + r < p.n ? n0 + r : p.n - 1;
     const uint8_t *b = p.b + nb * pitch + q * 16, *bs = p.b_scales + nb * (pitch / 16) + q;
@@ -578,16 +585,17 @@ void launch_mx4_quantize(const void* x, int type, int64_t rows, int64_t cols, in
                          uint8_t* codes_t, uint8_t* scales_t, hipStream_t s)
 {
     const uint32_t gx = (uint32_t)((codes ? mx4_padded(cols) : cols + kSide - 1) / kSide);
-    const uint32_t grid = gx * (uint32_t)((codes_t ? mx4_padded(rows) : rows + kSide - 1) / kSide);
+    const uint32_t blocks = gx * (uint32_t)((codes_t ? mx4_padded(rows) : rows + kSide - 1) / kSide);
+    const dim3 grid = grid_of(blocks);
     by_type(type, [&](auto e) {
         typedef decltype(e) E;
         const typename E::T* p = (const typename E::T*)x;
         if (codes && codes_t)
-            k_mx4_quantize<E, true, true><<<grid, kQuant, 0, s>>>(p, rows, cols, ldx, codes, scales, codes_t, scales_t, gx);
+            k_mx4_quantize<E, true, true><<<grid, kQuant, 0, s>>>(p, rows, cols, ldx, codes, scales, codes_t, scales_t, gx, blocks);
         else if (codes)
-            k_mx4_quantize<E, true, false><<<grid, kQuant, 0, s>>>(p, rows, cols, ldx, codes, scales, codes_t, scales_t, gx);
+            k_mx4_quantize<E, true, false><<<grid, kQuant, 0, s>>>(p, rows, cols, ldx, codes, scales, codes_t, scales_t, gx, blocks);
         else
-            k_mx4_quantize<E, false, true><<<grid, kQuant, 0, s>>>(p, rows, cols, ldx, codes, scales, codes_t, scales_t, gx);
+            k_mx4_quantize<E, false, true><<<grid, kQuant, 0, s>>>(p, rows, cols, ldx, codes, scales, codes_t, scales_t, gx, blocks);
     });
 }
 
@@ -629,7 +637,7 @@ FewTimes few_times(int64_t m, int64_t n, int64_t k)
 template <class X>
 void few(const Mx4Product& p, const typename X::T* x, int64_t ldx, hipStream_t s)
 {
-    const uint32_t grid = (uint32_t)((p.n + 15) / 16);
+    const dim3 grid = grid_of((uint32_t)((p.n + 15) / 16));
     by_type(p.type, [&](auto e) {
         typedef decltype(e) E;
         if (p.m <= 16)
