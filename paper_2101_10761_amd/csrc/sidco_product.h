@@ -158,6 +158,22 @@ struct Mx4Core {
 __device__ __forceinline__ void settle() { asm volatile("s_nop 3" ::: "memory"); }
 __device__ __forceinline__ void rest() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
 
+// The stages that a block fetches, in order: `stages` of each of `terms` terms of tile after tile, `step` apart.  Behind the last
+// it stays at stage 0: the loads that are still made then are of a resource without bytes, whose range check subtracts the
+// stage's offset from its size, and only at 0 is that no number of bytes at all.
+struct Sequence {
+    uint32_t tile, u;
+    int term;
+    // Goes on; whether to another tile's or term's first stage, or (tile >= tiles) behind the last.
+    __host__ __device__ __forceinline__ bool next(uint32_t stages, int terms, uint32_t tiles, uint32_t step)
+    {
+        if (tile >= tiles || ++u < stages) return false;
+        u = 0;
+        if (++term == terms) term = 0, tile += step;
+        return true;
+    }
+};
+
 // A block's tile: BM x BN by WM x WN waves, `Stages` stages of `Fours` four pieces in LDS.
 template <class Core, int BM, int BN, int WM, int WN, int Fours, int Stages>
 struct Tile {
@@ -336,21 +352,18 @@ struct Tile {
     {
         aim(pitch);
         const uint32_t stages = fours / Fours;
-        uint32_t coming = blockIdx.x, u = 0;  // the tile, term and stage fetched next
-        int term = 0;
-        operands(coming, term);
+        Sequence coming = {blockIdx.x, 0, 0};  // what is fetched next
+        operands(coming.tile, coming.term);
         auto advance = [&] {
-            if (++u < stages) return;
-            u = 0;
-            if (++term == Terms) term = 0, coming += gridDim.x;
-            if (coming < tiles)
-                operands(coming, term);
+            if (!coming.next(stages, Terms, tiles, gridDim.x)) return;
+            if (coming.tile < tiles)
+                operands(coming.tile, coming.term);
             else
                 take_nothing();
         };
 #pragma unroll
         for (int s = 0; s < Stages; ++s) {
-            fetch_range<0, kLoads>(u, lds + s * kStage);
+            fetch_range<0, kLoads>(coming.u, lds + s * kStage);
             advance();
         }
         wait_loads<(Stages - 1) * kLoads>();
@@ -367,7 +380,7 @@ struct Tile {
             __builtin_amdgcn_s_barrier();
             char* to = stage;
             stage = stage + kStage == end ? lds : stage + kStage;
-            multiply<true, true>(p, next, stage, 0, u, to);
+            multiply<true, true>(p, next, stage, 0, coming.u, to);
             advance();
         };
         for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
