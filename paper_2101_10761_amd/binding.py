@@ -780,8 +780,10 @@ def sidco_mx4_compress(grad, residual, codes, scales, stream=None) -> None:
 def sidco_mx4_aggregate(codes, scales, dense, scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
     """dense (+)= scale * the sum of what the workers' blocks stand for; row w of codes and scales is worker w's."""
     torch = _torch or _import_torch()
-    d = dense.numel()
     _check_tensor(dense, torch.float32, "dense", 1)
+    d = dense.numel()
+    if not isinstance(codes, torch.Tensor) or not isinstance(scales, torch.Tensor):
+        raise TypeError("the workers' codes and scales must be contiguous CUDA tensors of dtype torch.uint8")
     if codes.dim() != 2 or scales.dim() != 2 or codes.shape[0] != scales.shape[0]:
         raise ValueError("codes and scales must have a row for each worker")
     workers, code_stride = codes.shape
@@ -868,6 +870,9 @@ def sidco_workspace_bytes_orthogonalize(batch: int, rows: int, cols: int, out_dt
 
 def _batch(x, name):
     """(element code, row stride, matrix stride, batch, rows, cols) of a matrix or a batch of them."""
+    torch = _torch or _import_torch()
+    if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3):
+        raise TypeError(f"{name} must be a CUDA tensor of 2 or 3 dimensions and dtype float32, float16 or bfloat16")
     if x.dim() == 2:
         x = x[None]
     code, ld = _matrix(x, name, 3)
@@ -896,10 +901,10 @@ def sidco_muon_step(grad, momentum, weight, lr: float, mu: float = 0.95, nestero
     torch = _torch or _import_torch()
     code, _, _, batch, rows, cols = _batch(grad, "grad")
     w_code, *_ = _batch(weight, "weight")
+    _check_tensor(momentum, torch.float32, "momentum")
     if weight.shape != grad.shape or momentum.shape != grad.shape:
         raise ValueError("grad, momentum and weight must have the same shape")
     _check_tensor(grad, grad.dtype, "grad")
-    _check_tensor(momentum, torch.float32, "momentum")
     _check_tensor(weight, weight.dtype, "weight")
     opt = _newton_schulz(steps, coef, eps, precision)
     _check(load().sidco_muon_step(_stream_handle(stream), _ptr(grad), code, _ptr(momentum), _ptr(weight), w_code, batch, rows, cols, lr,
