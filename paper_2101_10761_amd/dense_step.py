@@ -62,7 +62,11 @@ class Exchange4Bit:
         self.codes = torch.empty(workers, sidco.sidco_mx4_code_bytes(1, d), dtype=torch.uint8, device=device)
         self.scales = torch.empty(workers, sidco.sidco_mx4_scale_bytes(1, d), dtype=torch.uint8, device=device)
         self.residuals = torch.zeros(workers, d, device=device)
-        self.bytes = self.codes.shape[1] + self.scales.shape[1]
+
+    @property
+    def bytes(self) -> float:
+        """What one worker sends in a step."""
+        return self.codes.shape[1] + self.scales.shape[1]
 
     def send(self, worker: int, grad) -> None:
         sidco.sidco_mx4_compress(grad, self.residuals[worker], self.codes[worker], self.scales[worker])
@@ -82,11 +86,18 @@ class ExchangeSparse:
         self.val = torch.empty(workers, cap, device=device)
         self.count = torch.zeros(workers, dtype=torch.int32, device=device)
         self.eta = torch.zeros(workers, device=device)
-        self.bytes = int(8 * delta * d)
+        self.pairs, self.sends = torch.zeros(1, dtype=torch.int64, device=device), 0
+
+    @property
+    def bytes(self) -> float:
+        """What one worker has sent in a step on average: an index and a value for each pair that was selected."""
+        return 8 * int(self.pairs) / max(1, self.sends)
 
     def send(self, worker: int, grad) -> None:
         sidco.sidco_compress(grad, self.residuals[worker], self.delta, sidco.DIST_EXP, 2, self.idx[worker], self.val[worker],
                              self.count[worker:worker + 1], self.eta[worker:worker + 1])
+        self.pairs += self.count[worker:worker + 1]
+        self.sends += 1
 
     def average(self, out) -> None:
         out.zero_()
@@ -96,7 +107,8 @@ class ExchangeSparse:
 
 def train(exchange: str = "4bit", workers: int = 4, steps: int = 60, batch: int = 256, sizes=(384, 512, 96), lr: float = 0.02,
           delta: float = 0.05, seed: int = 0) -> dict:
-    """Trains and returns {"losses": [...], "answers": (largest difference of a single row's answer, its size), "bytes": ...}."""
+    """Trains and returns {"losses": [...], "answers": (largest difference of a single row's answer, its size), "bytes": of a worker's
+    message, "gradient_bytes": of the gradient in float32}."""
     import torch
     dev = torch.device("cuda")
     g = torch.Generator(device=dev).manual_seed(seed)
@@ -157,7 +169,7 @@ def main() -> None:
     for exchange in ("4bit", "sparse"):
         r = train(exchange, a.workers, a.steps)
         shown = ", ".join("%.4f" % r["losses"][i] for i in sorted({0, a.steps // 4, a.steps // 2, a.steps - 1}))
-        print(f"{exchange}: loss {shown}; {r['bytes']} of {r['gradient_bytes']} bytes a worker and step; "
+        print(f"{exchange}: loss {shown}; {r['bytes']:.0f} of {r['gradient_bytes']} bytes a worker and step; "
               f"a single row's answer within {r['answers'][0]:.2g} of {r['answers'][1]:.3g}", flush=True)
 
 
