@@ -679,13 +679,13 @@ void launch_mx4_product(const Mx4Product& p, hipStream_t s)
         };
         by_type(p.type, [&](auto e) {
             if (pick == 0)
-                go(e, Shape<Tile<Mx4Core, 256, 256, 2, 2, 2, 2>>());
+                go(e, Shape<Tile<Mx4Core, 256, 256, 2, 2, 2>>());
             else if (pick == 1)
-                go(e, Shape<Tile<Mx4Core, 192, 192, 2, 2, 2, 3>>());
+                go(e, Shape<Tile<Mx4Core, 192, 192, 2, 2, 3>>());
             else if (pick == 2)
-                go(e, Shape<Tile<Mx4Core, 128, 128, 2, 2, 2, 2>>());
+                go(e, Shape<Tile<Mx4Core, 128, 128, 2, 2, 2>>());
             else
-                go(e, Shape<Tile<Mx4Core, 64, 64, 2, 2, 2, 4>>());
+                go(e, Shape<Tile<Mx4Core, 64, 64, 2, 2, 4>>());
         });
     };
     const TilePlan plan = plan_tiles(p.m, p.n, 1, mx4_padded(p.k) / 2 / kLine);

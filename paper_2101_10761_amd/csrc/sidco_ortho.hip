@@ -807,13 +807,13 @@ template <class F>
 void by_tile(int pick, const F& f)
 {
     if (pick == 0)
-        f(Shape<Tile<HalfCore, 256, 256, 2, 2, 2, 2>>());
+        f(Shape<Tile<HalfCore, 256, 256, 2, 2, 2>>());
     else if (pick == 1)
-        f(Shape<Tile<HalfCore, 192, 192, 2, 2, 2, 3>>());
+        f(Shape<Tile<HalfCore, 192, 192, 2, 2, 3>>());
     else if (pick == 2)
-        f(Shape<Tile<HalfCore, 128, 128, 2, 2, 2, 2>>());
+        f(Shape<Tile<HalfCore, 128, 128, 2, 2, 2>>());
     else
-        f(Shape<Tile<HalfCore, 64, 64, 2, 2, 2, 4>>());
+        f(Shape<Tile<HalfCore, 64, 64, 2, 2, 4>>());
 }
 
 void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)

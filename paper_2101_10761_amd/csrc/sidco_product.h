@@ -2,13 +2,12 @@
 //
 // Both operands are stored by rows along the contraction, in pieces of 16 bytes: 8 half-precision numbers, or a block of 32
 // 4-bit codes.  A matrix instruction takes four pieces of 16 rows of each operand in 16 cycles for either kind, so that one
-// data path serves both.  A stage is one or two such fours, 64 or 128 bytes of every row of the tile, and for 4-bit codes the
+// data path serves both.  A stage is two such fours, a line of 128 bytes of every row of the tile, and for 4-bit codes the
 // exponents of these blocks.
 //
 // Stages go from memory to LDS without passing through registers (each lane names its own 16 bytes of memory, LDS is written
 // in the order of the lanes).  Rows follow each other in LDS, so the same piece of the 16 rows that an instruction reads
-// would sit in few banks; piece c of row r is therefore kept at place c ^ (r % 8) of 8, or c ^ (r / 2 % 4) of 4, by choosing
-// which piece a lane fetches.
+// would sit in few banks; piece c of row r is therefore kept at place c ^ (r % 8), by choosing which piece a lane fetches.
 #ifndef SIDCO_PRODUCT_H
 #define SIDCO_PRODUCT_H
 
@@ -96,26 +95,26 @@ __device__ __forceinline__ void tile_of_triangle(uint32_t t, uint32_t& i, uint32
     j = t - r * (r + 1) / 2;
 }
 
-    // Four lanes with four columns of their row each come to hold four rows of one column each.
-    __device__ __forceinline__ v4f turned(v4f v)
-    {
-        const int t = threadIdx.x & 3;
-        auto swap1 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xb1, 0xf, 0xf, true)); };
-        auto swap2 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x4e, 0xf, 0xf, true)); };
+// Four lanes with four columns of their row each come to hold four rows of one column each.
+__device__ __forceinline__ v4f turned(v4f v)
+{
+    const int t = threadIdx.x & 3;
+    auto swap1 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xb1, 0xf, 0xf, true)); };
+    auto swap2 = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x4e, 0xf, 0xf, true)); };
 #pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-            const float got = swap1(t & 1 ? v[i] : v[i + 1]);
-            v[i] = t & 1 ? got : v[i];
-            v[i + 1] = t & 1 ? v[i + 1] : got;
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float got = swap2(t & 2 ? v[i] : v[i + 2]);
-            v[i] = t & 2 ? got : v[i];
-            v[i + 2] = t & 2 ? v[i + 2] : got;
-        }
-        return v;
+    for (int i = 0; i < 4; i += 2) {
+        const float got = swap1(t & 1 ? v[i] : v[i + 1]);
+        v[i] = t & 1 ? got : v[i];
+        v[i + 1] = t & 1 ? v[i + 1] : got;
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float got = swap2(t & 2 ? v[i] : v[i + 2]);
+        v[i] = t & 2 ? got : v[i];
+        v[i + 2] = t & 2 ? v[i + 2] : got;
+    }
+    return v;
+}
 
 // The values as rounded to fp32.  A product rounded to fp32 and then to half is otherwise rounded once, by an instruction that
 // does both, in one place and not in another: the half and what it leaves of the value would belong to different halves.
@@ -174,14 +173,13 @@ struct Sequence {
     }
 };
 
-// A block's tile: BM x BN by WM x WN waves, `Stages` stages of `Fours` four pieces in LDS.
-template <class Core, int BM, int BN, int WM, int WN, int Fours, int Stages>
+// A block's tile: BM x BN by WM x WN waves, `Stages` stages in LDS.
+template <class Core, int BM, int BN, int WM, int WN, int Stages>
 struct Tile {
     static constexpr int kM = BM, kN = BN;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int kMt = BM / WM / 16, kNt = BN / WN / 16;  // instructions' tiles of a wave
-    static constexpr int kSeg = 64 * Fours;                       // bytes of a row in a stage
-    static constexpr int kExps = 4 * Fours;                       // and exponents
+    static constexpr int kSeg = kLine, kExps = kLine / 16;        // bytes of a row in a stage, and exponents
     // a stage: exponents of A's and of B's rows, A's rows, B's rows
     static constexpr int kAtA = Core::kScaled ? (BM + BN) * kExps : 0, kAtB = kAtA + BM * kSeg, kStage = kAtB + BN * kSeg;
     static constexpr int kLds = Stages * kStage;
@@ -192,14 +190,13 @@ struct Tile {
     static_assert(BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "whole instructions");
     static_assert(BM % (kRowsLoad * kWaves) == 0 && BN % (kRowsLoad * kWaves) == 0, "whole loads");
     static_assert(!Core::kScaled || (BM % kRowsExps == 0 && (BM + BN) % (kRowsExps * kWaves) == 0), "whole loads of exponents");
-    static_assert(Fours == 1 || Fours == 2, "pieces of a line");
     static_assert(Stages >= 2 && kLds <= 160 * 1024, "LDS of a CU");
 
     v4f acc[kMt][kNt];
     v4i from_a, from_b, from_s[kLoadsS + 1];
     uint32_t src[kLoadsA + kLoadsB];  // this lane's 16 bytes of each load's rows
     uint32_t ssrc[kLoadsS + 1];
-    uint32_t fours;                   // of the rows
+    uint32_t stages;                  // of the rows
     int wave, lane;
 
     __device__ __forceinline__ void clear()
@@ -221,7 +218,7 @@ struct Tile {
 
     static __device__ __forceinline__ int place(int row, int piece)
     {
-        return Fours == 2 ? piece ^ (row & 7) : piece ^ (row >> 1 & 3);
+        return piece ^ (row & 7);
     }
 
     // The lanes' places in a stage, the same for every tile.
@@ -229,15 +226,15 @@ struct Tile {
     {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        fours = pitch / 64;
-        const int r = lane / (4 * Fours), c = place(r, lane % (4 * Fours));  // a load's first row is a multiple of 8
+        stages = pitch / kLine;
+        const int r = lane / 8, c = place(r, lane % 8);  // a load's first row is a multiple of 8
 #pragma unroll
         for (int k = 0; k < kLoadsA + kLoadsB; ++k)
             src[k] = (uint32_t)(((k < kLoadsA ? k : k - kLoadsA) * kWaves + wave) * kRowsLoad + r) * pitch + c * 16;
 #pragma unroll
         for (int k = 0; k < kLoadsS; ++k) {
             const uint32_t at = (uint32_t)(k * kWaves + wave) * kRowsExps;  // row of the tile, B's after A's
-            ssrc[k] = ((at < BM ? at : at - BM) + lane / Fours) * (pitch / 16) + lane % Fours * 4;
+            ssrc[k] = ((at < BM ? at : at - BM) + lane / 2) * (pitch / 16) + lane % 2 * 4;
         }
     }
 
@@ -351,7 +348,6 @@ struct Tile {
     __device__ __forceinline__ void run(uint32_t tiles, uint32_t pitch, char* lds, const Operands& operands, const Finish& finish)
     {
         aim(pitch);
-        const uint32_t stages = fours / Fours;
         Sequence coming = {blockIdx.x, 0, 0};  // what is fetched next
         operands(coming.tile, coming.term);
         auto advance = [&] {
@@ -386,19 +382,15 @@ struct Tile {
         for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
             clear();
             hold();
-            // Rows are whole lines: an even number of fours.  The last turn of all reads what follows the last stage, which
-            // nothing uses.  The first turn waits for everything: stores of the tile before may be counted among the loads.
+            // The last turn of all reads what follows the last stage, which nothing uses.  The first turn waits for
+            // everything: stores of the tile before may be counted among the loads.
             uint32_t f = 0, fresh = 1;
             do {
-                if (Fours == 2)
-                    multiply<true, false>(p0, p1, stage, 1, 0, nullptr);
-                else
-                    turn(p0, p1, fresh);
+                multiply<true, false>(p0, p1, stage, 1, 0, nullptr);
                 turn(p1, p0, fresh);
                 fresh = 0;
                 asm volatile("" : "+s"(fresh));  // a copy of the loop for its first turn would move the sums
-                f += 2;
-            } while (f < Terms * fours);
+            } while (++f < Terms * stages);
             rest();
             hold();
             finish(tile);
