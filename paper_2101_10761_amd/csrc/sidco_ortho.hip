@@ -861,7 +861,6 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
             k_start<T, false><<<grid, 256, 0, s>>>(p, q.eps, tall ? xt[0] : x[0], tall ? x[0] : xt[0]);
     });
 
-    auto triangle = [](int64_t side, int64_t b) { const int64_t k = (side + b - 1) / b; return k * (k + 1) / 2; };
     auto product = [](const Plane& a, float sa, const Plane& b, float sb, const Plane& o, float so) -> Symmetric {
         return {a, b, o, so / (sa * sb), 0.0f, 0.0f};
     };
@@ -873,10 +872,10 @@ void orthogonalize(const OrthoCall& q, char* ws, hipStream_t s)
         constexpr bool Full = decltype(pairs)::value;
         const int64_t segments = Full ? 3 : 1;
         auto symmetric = [&](auto poly, int jobs, const Symmetric& a, const Symmetric& b) {
-            const int pick = best_tile([&](int64_t side) { return triangle(m, side) * q.batch * jobs; }, a.a.pitch * 2 / kLine * segments);
+            const int pick = best_triangle(m, (int64_t)q.batch * jobs, a.a.pitch * 2 / kLine * segments);
             by_tile(pick, [&](auto shape) {
                 typedef typename decltype(shape)::Is Tl;
-                const uint32_t tri = (uint32_t)triangle(m, Tl::kM), each = tri * batch;
+                const uint32_t tri = (uint32_t)triangle_tiles(m, Tl::kM), each = tri * batch;
                 k_symmetric<Tl, Full, decltype(poly)::value>
                     <<<tile_blocks(pick, each * jobs), Tl::kThreads, 0, s>>>(a, b, (uint32_t)m, tri, each, each * jobs);
             });

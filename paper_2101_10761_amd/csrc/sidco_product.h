@@ -516,6 +516,17 @@ inline int best_tile(const Count& count, int64_t lines, double* time = nullptr)
     return best;
 }
 
+// Tiles on and below the diagonal of an m x m matrix, and the tile for `count` such matrices.
+inline int64_t triangle_tiles(int64_t m, int64_t side)
+{
+    const int64_t k = (m + side - 1) / side;
+    return k * (k + 1) / 2;
+}
+inline int best_triangle(int64_t m, int64_t count, int64_t lines)
+{
+    return best_tile([&](int64_t side) { return triangle_tiles(m, side) * count; }, lines);
+}
+
 // A batch of m x n products in one launch or two: the first n columns in as many large tiles as fill whole rounds, and the rest
 // in tiles of its own.  4096 x 25088 in tiles of 256 is 6.1 rounds, done in 7.
 struct TilePlan {

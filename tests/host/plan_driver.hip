@@ -3,6 +3,7 @@
 #include <cstdio>
 #include <cstring>
 
+#include "sidco_ortho_plan.h"
 #include "sidco_product.h"
 
 using namespace sidco;
@@ -37,6 +38,23 @@ int main()
             int terms, depth;
             if (std::scanf("%u %d %u %u %u %d", &stages, &terms, &tiles, &blocks, &block, &depth) != 6) return 1;
             std::printf("%d\n", sequence(stages, terms, tiles, blocks, block, depth));
+        } else if (!std::strcmp(what, "plan")) {  // tile, columns and second tile of a batch of products
+            long m, n, batch, lines;
+            if (std::scanf("%ld %ld %ld %ld", &m, &n, &batch, &lines) != 4) return 1;
+            const TilePlan p = plan_tiles(m, n, batch, lines);
+            std::printf("%d %ld %d\n", p.pick, (long)p.columns, p.rest_pick);
+        } else if (!std::strcmp(what, "triangle")) {  // tile of `count` symmetric products
+            long m, count, lines;
+            if (std::scanf("%ld %ld %ld", &m, &count, &lines) != 3) return 1;
+            std::printf("%d\n", best_triangle(m, count, lines));
+        } else if (!std::strcmp(what, "steps")) {  // one block?, steps in pairs, steps in a group of either kind
+            long rows, cols;
+            int batch, steps, paired;
+            float a, b, c;
+            if (std::scanf("%d %ld %ld %d %d %f %f %f", &batch, &rows, &cols, &steps, &paired, &a, &b, &c) != 8) return 1;
+            if (paired < 0) paired = ortho_paired(steps, a, b, c, paired == -16);  // by the type: -16 bf16, -32 another
+            const OrthoGroups g = ortho_groups(batch, rows < cols ? rows : cols, rows < cols ? cols : rows, steps, paired);
+            std::printf("%d %d %d %d\n", ortho_one_block(rows, cols, cols, paired > 0), paired, g.paired, g.halves);
         } else {
             return 1;
         }
