@@ -58,8 +58,9 @@
  * (sidco_mx4_*, sidco_orthogonalize, sidco_muon_step) work behind what the
  * sparsifier's keep, or in memory of their own where the stream's workspace has
  * no room: they never grow it, and leave the diagnostics, the scatter flag and the
- * controller as they are.  The diagnostics calls that take a stream (sidco_read_diag, sidco_fit_result, ...)
- * report the last call made on that stream.
+ * controller as they are.  The diagnostics calls that take a stream
+ * (sidco_read_diag, sidco_fit_result, ...) report the last of the sparsifier's
+ * calls made on that stream.
  */
 #ifndef SIDCO_H
 #define SIDCO_H
@@ -506,8 +507,10 @@ int64_t sidco_mx4_scale_bytes(int64_t rows, int64_t cols);
  * Dense 4-bit compression of one worker's gradient with error feedback: acc = grad
  * + residual (rounded to fp32, as the residual holds it) becomes codes and
  * exponents, and residual = acc - what they stand for.  In a block that stands
- * for NaN the residual keeps acc.  residual may be NULL (memoryless); it must not
- * alias grad.  1 <= d <= 2^31-1.  Needs no workspace.
+ * for NaN the residual keeps acc, so an infinity stays there, and its block NaN,
+ * until the caller clears it: a step that is skipped for overflow, as with loss
+ * scaling, is not compressed, or the residual is put back.  residual may be NULL
+ * (memoryless); it must not alias grad.  1 <= d <= 2^31-1.  Needs no workspace.
  */
 int sidco_mx4_compress(void *stream, const void *grad, int grad_dtype, float *residual, int64_t d, uint8_t *codes,
                        uint8_t *scales);
@@ -555,8 +558,10 @@ int sidco_mx4_matmul(void *stream, const uint8_t *a_codes, const uint8_t *a_scal
  * A layer with a 4-bit weight on rows as they come: x (rows x k of `x_dtype`, row
  * stride ldx) is quantised along its rows and multiplied with the n x k weight, c =
  * alpha x^ W^T (+ c) as in sidco_mx4_matmul.  From one row on; c must not overlap x.
- * Uses the stream's workspace, of sidco_workspace_bytes_mx4_linear(rows, k), unless
- * there are few rows (one launch then does both).
+ * Uses the stream's workspace, of sidco_workspace_bytes_mx4_linear(rows, k) at most.
+ * Up to 32 rows of together up to 65536 elements (k rounded up to 256) are taken in
+ * one launch without it where the library expects that to be faster, by rows, n and
+ * k alone.
  */
 int sidco_mx4_linear(void *stream, const void *x, int x_dtype, int64_t rows, int64_t k, int64_t ldx, const uint8_t *w_codes,
                      const uint8_t *w_scales, int64_t n, float alpha, int accumulate, void *c, int c_dtype, int64_t ldc);

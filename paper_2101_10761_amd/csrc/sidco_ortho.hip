@@ -136,7 +136,7 @@ __device__ __forceinline__ void update8(const Start<T>& p, int64_t z, int64_t r,
 
 // Moves the momentum and adds up u^2, in 64 bits.  A block takes rows, of a matrix without gaps pieces of kNormRow elements, in
 // turn; its sum has a place of its own, so that the total does not depend on which block ends first.  Bound by memory:
-// 4096 x 25088, gradient in fp16, 168 us for 1.03 GB, 6.1 TB/s; four of 1500 x 6000 in fp32 76 us for 432 MB, 5.7 TB/s.
+// 4096 x 25088, gradient in bf16, 167 us for 1.03 GB, 6.2 TB/s; four of 1500 x 6000 in fp32 75 us for 432 MB, 5.8 TB/s.
 constexpr int kNormRow = 16 * kNormBlock;
 template <class T>
 __global__ __launch_bounds__(kNormBlock) void k_norm(Start<T> p)
@@ -206,8 +206,8 @@ __device__ __forceinline__ void put8(const Plane& o, int64_t z, int64_t r, int64
 }
 
 // 64 x 64 elements a block: rows go to `natural`, and through LDS to `turned`, the padding of both as zeros.  X is kept both
-// ways so that every product reads whole lines along its contraction.  Bound by memory: 4096 x 25088 with momentum 215 us for
-// 1.03 GB, 4.8 TB/s; four of 1500 x 6000, pairs of halves, 110 us for 576 MB, 5.2 TB/s.
+// ways so that every product reads whole lines along its contraction.  Bound by memory: 4096 x 25088 with momentum, pairs of
+// halves, 297 us for 1.44 GB, 4.8 TB/s; four of 1500 x 6000 112 us for 576 MB, 5.1 TB/s.
 template <class T, bool Full>
 __global__ __launch_bounds__(256) void k_start(Start<T> p, float eps, Plane natural, Plane turned)
 {
@@ -319,9 +319,10 @@ struct Symmetric {
 };
 
 // One or two of them of the same size.  Tiles on and below the diagonal are computed and mirrored: half the operations, and a
-// second way out through LDS.  Bound by the matrix cores and by how 253 tiles meet 256 CUs: m = 4096 in halves 80 us a product
-// (6.9e10 operations, 0.86 PFLOP/s), 84 with the polynomial; four of m = 1500, three products of halves each, 82 and 94 us
-// (4.1e10, 0.5: 144 tiles); six of m = 256, 5.6 us, a launch.
+// second way out through LDS.  Bound by the matrix cores and by how the tiles meet 256 CUs.  m = 4096 in 253 tiles: pairs of
+// halves, three products each, 204 us (2.1e11 operations, 1.0 PFLOP/s), 214 with the polynomial, 401 for two; G over n = 25088
+// 1132 us (1.1), in halves 368 us.  Four of m = 1500 in 144 tiles, pairs, 83 and 93 to 97 us (4.1e10, 0.5), two 143; G over n =
+// 6000 260 us (0.6).  Six of m = 256, pairs, 8 and 9.7 us, G over n = 2304 30 us.
 template <class Tl, bool Full, bool Poly>
 __global__ __launch_bounds__(Tl::kThreads) void k_symmetric(Symmetric first, Symmetric second, uint32_t m, uint32_t tiles, uint32_t each,
                                                             uint32_t total)
@@ -417,8 +418,8 @@ __device__ __forceinline__ void finish1(const Result& o, int64_t z, int64_t r, i
 }
 
 // X' = Q X: X' and its transpose, or with Last the result, of element type T.  Bound by the matrix cores: m = 4096, n = 25088 in
-// halves 751 + 35 us in two launches, 1.07 PFLOP/s (a large library product of the type reaches 1.35); four of 1500 x 6000 in
-// pairs of halves 378 + 71 and 336 + 71 us, 0.72 and 0.80.
+// halves 736 + 36 us in two launches, 1.09 PFLOP/s (a large library product of the type reaches 1.35), in pairs of halves 1873 +
+// 89 us, 1.29; four of 1500 x 6000 in pairs 375 + 72 us (X) and 336 + 73 us (weights), 0.72 and 0.79.
 template <class Tl, bool Full, bool Last, class T>
 __global__ __launch_bounds__(Tl::kThreads) void k_apply(Plane pm, Plane xt, Plane x2, Plane xt2, uint32_t m, uint32_t n, uint32_t tm, uint32_t tn,
                                                         uint32_t total, uint32_t from, float back, Result o)
