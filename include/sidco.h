@@ -605,9 +605,9 @@ typedef struct sidco_newton_schulz {
 void sidco_newton_schulz_default(sidco_newton_schulz *opt);
 
 /* Host helper: bytes of workspace that a call for `batch` matrices needs whose
- * result has `out_dtype`; opt may be NULL (the default values).  0 for invalid
- * arguments.  Matrices of up to 64 rows and 576 columns, or 64 columns and 576
- * rows, whose row stride ldx is at most 2^20 use none of it.                   */
+ * result has `out_dtype`, with the opt of that call; opt may be NULL (the default
+ * values).  0 for invalid arguments.  Matrices of up to 64 rows and 576 columns,
+ * or 64 columns and 576 rows, whose row stride ldx is at most 2^20 use none of it. */
 size_t sidco_workspace_bytes_orthogonalize(int batch, int64_t rows, int64_t cols, int out_dtype, const sidco_newton_schulz *opt);
 
 /*

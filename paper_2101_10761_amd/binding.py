@@ -862,9 +862,10 @@ def _newton_schulz(steps, coef, eps, precision):
     return NewtonSchulz(steps, a, b, c, eps, precision)
 
 
-def sidco_workspace_bytes_orthogonalize(batch: int, rows: int, cols: int, out_dtype: int, precision: int = NS_BY_TYPE) -> int:
-    opt = sidco_newton_schulz_default()
-    opt.precision = precision
+def sidco_workspace_bytes_orthogonalize(batch: int, rows: int, cols: int, out_dtype: int, precision: int = NS_BY_TYPE, steps: int = 5,
+                                        coef=(3.4445, -4.7750, 2.0315)) -> int:
+    """Of a call with these steps and coefficients, which decide the precision of a step and how many go together."""
+    opt = _newton_schulz(steps, coef, 1e-7, precision)
     return int(load().sidco_workspace_bytes_orthogonalize(batch, rows, cols, out_dtype, C.byref(opt)))
 
 
