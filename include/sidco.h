@@ -55,7 +55,8 @@
  * replaces them all on its device: calls that use it must not overlap.  A graph
  * that calls were captured into holds the workspace's address: reserve the most
  * that calls on the stream need before capturing.  The dense operators' calls
- * (sidco_mx4_*, sidco_orthogonalize, sidco_muon_step) work behind what the
+ * (sidco_mx4_*, sidco_orthogonalize, sidco_muon_step) and a language model's
+ * (sidco_embedding*, sidco_dropout, sidco_cross_entropy*) work behind what the
  * sparsifier's keep, or in memory of their own where the stream's workspace has
  * no room: they never grow it, and leave the diagnostics, the scatter flag and the
  * controller as they are.  The diagnostics calls that take a stream
@@ -631,6 +632,58 @@ int sidco_orthogonalize(void *stream, const void *x, int x_dtype, int64_t ldx, i
 int sidco_muon_step(void *stream, const void *grad, int grad_dtype, float *momentum, void *weight, int weight_dtype, int batch,
                     int64_t rows, int64_t cols, float lr, float mu, int nesterov, float weight_decay, float scale,
                     const sidco_newton_schulz *opt);
+
+/* ---- a language model's ends --------------------------------------------------
+ *
+ * Words (tokens, targets) are int32 or int64, SIDCO_WORD_*, contiguous.  A word
+ * outside [0, vocab) stands for padding.  Matrices have contiguous rows and row
+ * strides in elements, numbers of rows, columns and words and strides are at most
+ * 2^31-1; element types are SIDCO_GRAD_F32, _F16 and _BF16, and sums are fp32 whatever
+ * they are.  Results are deterministic.                                       */
+#define SIDCO_WORD_I32 0
+#define SIDCO_WORD_I64 1
+
+/*
+ * The lookup: out_i = scale * table[words_i] for n words, rounded once; zeros for
+ * padding.  table is vocab x dim with row stride ldt, out n x dim with row stride ldo.
+ * They must not overlap.  Needs no workspace.
+ */
+int sidco_embedding(void *stream, const void *table, int table_dtype, int64_t vocab, int64_t dim, int64_t ldt, const void *words,
+                    int word_type, int64_t n, float scale, void *out, int out_dtype, int64_t ldo);
+
+/*
+ * The table's gradient: table_grad_v = scale * the sum of grad_i over the places i with
+ * words_i = v, in an order that the words alone decide, zeros for words that do not occur
+ * (accumulate = 0), or that added to table_grad and rounded once, where rows of words that
+ * do not occur are not touched (accumulate = 1: several batches, or a table that is the
+ * decoder's weight too).  Padding has no gradient, whatever its row of grad holds.  grad is
+ * n x dim with row stride ldg, table_grad vocab x dim with row stride ldt.  Uses the
+ * stream's workspace, of sidco_workspace_bytes_embedding_grad(n, dim).
+ */
+int sidco_embedding_grad(void *stream, const void *grad, int grad_dtype, int64_t n, int64_t dim, int64_t ldg, const void *words,
+                         int word_type, int64_t vocab, float scale, int accumulate, void *table_grad, int table_dtype, int64_t ldt);
+size_t sidco_workspace_bytes_embedding_grad(int64_t n, int64_t dim);
+
+/*
+ * Dropout whose mask is a function of seed and place and is not stored: y = kept ? x *
+ * 65536 / (65536 - T) : 0, plus residual if there is one (not NULL; of y's type).  The
+ * backward pass is the same call on the gradient of y.
+ *
+ * Element (r, c) has number c % 8 of block offset + *device_offset + r * ceil(cols / 8) +
+ * c / 8 of the seed's sequence, and is kept where that number is at least T = floor(65536 p
+ * + 1/2), 0 <= p <= 1: p = 0 keeps all, p = 1 none.  Block b is Philox4x32-10 of the counter
+ * (b mod 2^32, b / 2^32, 0, 0) with the seed as its key, eight numbers of 16 bits, low halves
+ * of its words first.  A call takes sidco_dropout_blocks(rows, cols) blocks, which the next
+ * one adds to its offset; device_offset (device, 8-byte aligned, one number; NULL: 0) is read when
+ * the call runs, so that a captured call draws others with each replay if the caller moves it on.
+ *
+ * x and y are rows x cols with row strides ldx, ldy.  y may be x or residual with the same
+ * type and row stride; any other overlap is not allowed.  What is dropped is 0, an infinity
+ * or a NaN too.  Needs no workspace.
+ */
+int sidco_dropout(void *stream, const void *x, int x_dtype, int64_t rows, int64_t cols, int64_t ldx, double p, uint64_t seed,
+                  uint64_t offset, const uint64_t *device_offset, const void *residual, int64_t ldr, void *y, int y_dtype, int64_t ldy);
+int64_t sidco_dropout_blocks(int64_t rows, int64_t cols);
 
 /* Text for an error code; the HIP error string of the last SIDCO_ERR_HIP.     */
 const char *sidco_strerror(int code);

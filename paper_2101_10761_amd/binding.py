@@ -31,6 +31,7 @@ EXPORTS = [
     "sidco_mx4_code_bytes", "sidco_mx4_scale_bytes", "sidco_mx4_compress", "sidco_mx4_aggregate", "sidco_mx4_quantize",
     "sidco_mx4_dequantize", "sidco_mx4_matmul", "sidco_mx4_linear", "sidco_workspace_bytes_mx4_linear",
     "sidco_newton_schulz_default", "sidco_workspace_bytes_orthogonalize", "sidco_orthogonalize", "sidco_muon_step",
+    "sidco_embedding", "sidco_embedding_grad", "sidco_workspace_bytes_embedding_grad", "sidco_dropout", "sidco_dropout_blocks",
 ]
 
 
@@ -220,6 +221,16 @@ def load() -> C.CDLL:
     lib.sidco_muon_step.argtypes = [vp, vp, C.c_int, f32p, vp, C.c_int, C.c_int, i64, i64, C.c_float, C.c_float, C.c_int, C.c_float,
                                     C.c_float, nsp]
     lib.sidco_muon_step.restype = C.c_int
+    lib.sidco_embedding.argtypes = [vp, vp, C.c_int, i64, i64, i64, vp, C.c_int, i64, C.c_float, vp, C.c_int, i64]
+    lib.sidco_embedding.restype = C.c_int
+    lib.sidco_embedding_grad.argtypes = [vp, vp, C.c_int, i64, i64, i64, vp, C.c_int, i64, C.c_float, C.c_int, vp, C.c_int, i64]
+    lib.sidco_embedding_grad.restype = C.c_int
+    lib.sidco_workspace_bytes_embedding_grad.argtypes = [i64, i64]
+    lib.sidco_workspace_bytes_embedding_grad.restype = C.c_size_t
+    lib.sidco_dropout.argtypes = [vp, vp, C.c_int, i64, i64, i64, C.c_double, C.c_uint64, C.c_uint64, vp, vp, i64, vp, C.c_int, i64]
+    lib.sidco_dropout.restype = C.c_int
+    lib.sidco_dropout_blocks.argtypes = [i64, i64]
+    lib.sidco_dropout_blocks.restype = i64
     lib.sidco_strerror.argtypes = [C.c_int]
     lib.sidco_strerror.restype = C.c_char_p
     lib.sidco_last_hip_error.argtypes = []
@@ -910,6 +921,89 @@ def sidco_muon_step(grad, momentum, weight, lr: float, mu: float = 0.95, nestero
     opt = _newton_schulz(steps, coef, eps, precision)
     _check(load().sidco_muon_step(_stream_handle(stream), _ptr(grad), code, _ptr(momentum), _ptr(weight), w_code, batch, rows, cols, lr,
                                   mu, int(nesterov), weight_decay, scale, C.byref(opt)), "sidco_muon_step")
+
+
+# ---- a language model's ends ----
+
+WORD_I32, WORD_I64 = 0, 1
+
+_word_types = None  # torch's integer types as the C ABI numbers them
+
+
+def _words(words, name):
+    """Address, type and number of a contiguous CUDA tensor of words, of any shape."""
+    global _word_types
+    if _word_types is None:
+        torch = _torch or _import_torch()
+        _word_types = {torch.int32: WORD_I32, torch.int64: WORD_I64}
+    torch = _torch or _import_torch()
+    code = _word_types.get(words.dtype) if isinstance(words, torch.Tensor) else None
+    if code is None or not words.is_cuda or not words.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous CUDA tensor of dtype int32 or int64")
+    return words.data_ptr(), code, words.numel()
+
+
+def sidco_embedding(table, words, out, scale: float = 1.0, stream=None) -> None:
+    """out[i] = scale * table[words[i]], zeros where words[i] is no row of the table; out has a row for each word."""
+    code, ldt = _matrix(table, "table")
+    out_code, ldo = _matrix(out, "out")
+    w, word_type, n = _words(words, "words")
+    vocab, dim = table.shape
+    if out.shape[0] != n or out.shape[1] != dim:
+        raise ValueError("out must have a row of the table's length for each word")
+    rc = load().sidco_embedding(_stream_handle(stream), table.data_ptr(), code, vocab, dim, ldt, w, word_type, n, scale, out.data_ptr(),
+                                out_code, ldo)
+    if rc:
+        raise SidcoError(rc, "sidco_embedding")
+
+
+def sidco_workspace_bytes_embedding_grad(n: int, dim: int) -> int:
+    return int(load().sidco_workspace_bytes_embedding_grad(n, dim))
+
+
+def sidco_embedding_grad(grad, words, table_grad, scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
+    """table_grad[v] (+)= scale * the sum of grad's rows whose word is v."""
+    code, ldg = _matrix(grad, "grad")
+    table_code, ldt = _matrix(table_grad, "table_grad")
+    w, word_type, n = _words(words, "words")
+    vocab, dim = table_grad.shape
+    if grad.shape[0] != n or grad.shape[1] != dim:
+        raise ValueError("grad must have a row of the table's length for each word")
+    rc = load().sidco_embedding_grad(_stream_handle(stream), grad.data_ptr(), code, n, dim, ldg, w, word_type, vocab, scale,
+                                     1 if accumulate else 0, table_grad.data_ptr(), table_code, ldt)
+    if rc:
+        raise SidcoError(rc, "sidco_embedding_grad")
+
+
+def sidco_dropout_blocks(rows: int, cols: int) -> int:
+    n = load().sidco_dropout_blocks(rows, cols)
+    if n < 0:
+        raise SidcoError(int(n), "sidco_dropout_blocks")
+    return int(n)
+
+
+def sidco_dropout(x, out, p: float, seed: int, offset: int = 0, residual=None, device_offset=None, stream=None) -> None:
+    """out = x with elements dropped with probability p and the others scaled, plus residual (of out's type) if given.  seed and
+    offset (in blocks of the sequence) are taken modulo 2^64; device_offset, a CUDA tensor of one int64, is added to the
+    offset when the call runs."""
+    code, ldx = _matrix(x, "x")
+    out_code, ldo = _matrix(out, "out")
+    rows, cols = x.shape
+    if out.shape[0] != rows or out.shape[1] != cols:
+        raise ValueError("out must have x's shape")
+    ldr, torch = 0, _torch
+    if residual is not None:
+        res_code, ldr = _matrix(residual, "residual")
+        if res_code != out_code:
+            raise TypeError("residual must have out's dtype")
+        if residual.shape != out.shape:
+            raise ValueError("residual must have x's shape")
+    if device_offset is not None:
+        _check_tensor(device_offset, torch.int64, "device_offset", 1)
+    rc = load().sidco_dropout(_stream_handle(stream), x.data_ptr(), code, rows, cols, ldx, p, seed & 0xFFFFFFFFFFFFFFFF,
+                              offset & 0xFFFFFFFFFFFFFFFF, _ptr(device_offset), _ptr(residual), ldr, out.data_ptr(), out_code, ldo)
+    if rc:
+        raise SidcoError(rc, "sidco_dropout")
 
 
 def sidco_version() -> int:
