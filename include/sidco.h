@@ -685,6 +685,42 @@ int sidco_dropout(void *stream, const void *x, int x_dtype, int64_t rows, int64_
                   uint64_t offset, const uint64_t *device_offset, const void *residual, int64_t ldr, void *y, int y_dtype, int64_t ldy);
 int64_t sidco_dropout_blocks(int64_t rows, int64_t cols);
 
+/*
+ * Softmax cross entropy of n rows x against a vocabulary's weight w: with the logits l = x
+ * w^T (n x vocab, never kept), lse_i = log of the sum of exp(l_iv) over v, and loss_i = lse_i -
+ * l_i,t with t = targets_i; 0 where t is padding, whatever the row holds.  x is n x dim with
+ * row stride ldx, w vocab x dim with row stride ldw, both of `dtype`; loss and lse (device, n
+ * floats each; one of them may be NULL) must not overlap anything.  n <= 2^22, dim <= 2^21, and
+ * vocab / 64 times n / 64 or dim / 64, each rounded up, at most 2^31-1 (SIDCO_ERR_SIZE).
+ *
+ * Sums are fp32.  16-bit operands are multiplied exactly; fp32 ones as pairs of halves under a
+ * power of two for each matrix, 22 bits of its elements down to 2^-28 of its largest magnitude
+ * and 2^-39 of that below, and there an infinity counts as a NaN.  From one row on.  Uses the
+ * stream's workspace, of sidco_workspace_bytes_cross_entropy(n, dim, vocab, dtype) at most.
+ */
+int sidco_cross_entropy(void *stream, const void *x, const void *w, int dtype, int64_t n, int64_t dim, int64_t vocab, int64_t ldx, int64_t ldw,
+                        const void *targets, int word_type, float *loss, float *lse);
+size_t sidco_workspace_bytes_cross_entropy(int64_t n, int64_t dim, int64_t vocab, int dtype);
+
+/*
+ * Its gradient, from the lse that the call before it wrote for the same x, w and targets.
+ * With P_iv = loss_grad_i (exp(l_iv - lse_i) - [v = t]), rows of zeros where t is padding:
+ *   x_grad = P w                                        (dtype, row stride ldgx)
+ *   w_grad = P^T x (accumulate = 0) or w_grad + P^T x   (accumulate = 1)
+ *                                                       (dtype or SIDCO_GRAD_F32, row stride ldgw)
+ * Either may be NULL, not both.  loss_grad (device, n floats) is 1 / n for the gradient of the
+ * mean, times the loss scale if there is one; NULL stands for ones.  P is formed for one piece of
+ * the vocabulary at a time; it has 22 bits where the gradient it makes is fp32 and the operands are
+ * halves or fp32, 16 where they are bf16, and for a 16-bit gradient the operands' own, halves
+ * under a power of two.  Rows of x whose target is padding do not enter w_grad whatever they
+ * hold.  The gradients must not overlap x, w or each other.  Uses the stream's workspace, of
+ * sidco_workspace_bytes_cross_entropy_grad(n, dim, vocab, dtype, w_grad_dtype) at most.
+ */
+int sidco_cross_entropy_grad(void *stream, const void *x, const void *w, int dtype, int64_t n, int64_t dim, int64_t vocab, int64_t ldx,
+                             int64_t ldw, const void *targets, int word_type, const float *lse, const float *loss_grad, void *x_grad,
+                             int64_t ldgx, void *w_grad, int w_grad_dtype, int64_t ldgw, int accumulate);
+size_t sidco_workspace_bytes_cross_entropy_grad(int64_t n, int64_t dim, int64_t vocab, int dtype, int w_grad_dtype);
+
 /* Text for an error code; the HIP error string of the last SIDCO_ERR_HIP.     */
 const char *sidco_strerror(int code);
 const char *sidco_last_hip_error(void);

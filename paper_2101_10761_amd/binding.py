@@ -32,6 +32,7 @@ EXPORTS = [
     "sidco_mx4_dequantize", "sidco_mx4_matmul", "sidco_mx4_linear", "sidco_workspace_bytes_mx4_linear",
     "sidco_newton_schulz_default", "sidco_workspace_bytes_orthogonalize", "sidco_orthogonalize", "sidco_muon_step",
     "sidco_embedding", "sidco_embedding_grad", "sidco_workspace_bytes_embedding_grad", "sidco_dropout", "sidco_dropout_blocks",
+    "sidco_cross_entropy", "sidco_workspace_bytes_cross_entropy", "sidco_cross_entropy_grad", "sidco_workspace_bytes_cross_entropy_grad",
 ]
 
 
@@ -231,6 +232,15 @@ def load() -> C.CDLL:
     lib.sidco_dropout.restype = C.c_int
     lib.sidco_dropout_blocks.argtypes = [i64, i64]
     lib.sidco_dropout_blocks.restype = i64
+    lib.sidco_cross_entropy.argtypes = [vp, vp, vp, C.c_int, i64, i64, i64, i64, i64, vp, C.c_int, f32p, f32p]
+    lib.sidco_cross_entropy.restype = C.c_int
+    lib.sidco_workspace_bytes_cross_entropy.argtypes = [i64, i64, i64, C.c_int]
+    lib.sidco_workspace_bytes_cross_entropy.restype = C.c_size_t
+    lib.sidco_cross_entropy_grad.argtypes = [vp, vp, vp, C.c_int, i64, i64, i64, i64, i64, vp, C.c_int, f32p, f32p, vp, i64, vp, C.c_int, i64,
+                                             C.c_int]
+    lib.sidco_cross_entropy_grad.restype = C.c_int
+    lib.sidco_workspace_bytes_cross_entropy_grad.argtypes = [i64, i64, i64, C.c_int, C.c_int]
+    lib.sidco_workspace_bytes_cross_entropy_grad.restype = C.c_size_t
     lib.sidco_strerror.argtypes = [C.c_int]
     lib.sidco_strerror.restype = C.c_char_p
     lib.sidco_last_hip_error.argtypes = []
@@ -1004,6 +1014,67 @@ def sidco_dropout(x, out, p: float, seed: int, offset: int = 0, residual=None, d
                               offset & 0xFFFFFFFFFFFFFFFF, _ptr(device_offset), _ptr(residual), ldr, out.data_ptr(), out_code, ldo)
     if rc:
         raise SidcoError(rc, "sidco_dropout")
+
+
+def _logits(x, weight, targets):
+    """Arguments that both cross entropy calls begin with, and their sizes."""
+    code, ldx = _matrix(x, "x")
+    w_code, ldw = _matrix(weight, "weight")
+    if w_code != code:
+        raise TypeError("weight must have x's dtype")
+    w, word_type, n = _words(targets, "targets")
+    dim = x.shape[1]
+    if weight.shape[1] != dim or x.shape[0] != n:
+        raise ValueError("weight must have x's columns, and targets a word for each of its rows")
+    vocab = weight.shape[0]
+    return (x.data_ptr(), weight.data_ptr(), code, n, dim, vocab, ldx, ldw, w, word_type), n, dim, vocab, code
+
+
+def sidco_workspace_bytes_cross_entropy(n: int, dim: int, vocab: int, dtype: int) -> int:
+    return int(load().sidco_workspace_bytes_cross_entropy(n, dim, vocab, dtype))
+
+
+def sidco_cross_entropy(x, weight, targets, loss, lse, stream=None) -> None:
+    """loss[i] = lse[i] - (x weight^T)[i, targets[i]], lse[i] the logarithm of the row's sum of exponentials; either may be None."""
+    torch = _torch or _import_torch()
+    args, n, *_ = _logits(x, weight, targets)
+    for t, name in ((loss, "loss"), (lse, "lse")):
+        if t is not None:
+            _check_tensor(t, torch.float32, name, n)
+    rc = load().sidco_cross_entropy(_stream_handle(stream), *args, _ptr(loss), _ptr(lse))
+    if rc:
+        raise SidcoError(rc, "sidco_cross_entropy")
+
+
+def sidco_workspace_bytes_cross_entropy_grad(n: int, dim: int, vocab: int, dtype: int, weight_grad_dtype: int) -> int:
+    return int(load().sidco_workspace_bytes_cross_entropy_grad(n, dim, vocab, dtype, weight_grad_dtype))
+
+
+def sidco_cross_entropy_grad(x, weight, targets, lse, loss_grad, x_grad=None, weight_grad=None, accumulate: bool = False,
+                             stream=None) -> None:
+    """The gradients of the sum of loss_grad[i] * loss[i] (None: of the losses' sum) with respect to x, in its dtype, and weight, in its
+    dtype or float32, or with `accumulate` added to what weight_grad holds; either may be None.  lse is what sidco_cross_entropy
+    wrote."""
+    torch = _torch or _import_torch()
+    args, n, dim, vocab, code = _logits(x, weight, targets)
+    _check_tensor(lse, torch.float32, "lse", n)
+    if loss_grad is not None:
+        _check_tensor(loss_grad, torch.float32, "loss_grad", n)
+    ldgx = ldgw = w_code = 0
+    if x_grad is not None:
+        x_code, ldgx = _matrix(x_grad, "x_grad")
+        if x_code != code:
+            raise TypeError("x_grad must have x's dtype")
+        if x_grad.shape != x.shape:
+            raise ValueError("x_grad must have x's shape")
+    if weight_grad is not None:
+        w_code, ldgw = _matrix(weight_grad, "weight_grad")
+        if weight_grad.shape != weight.shape:
+            raise ValueError("weight_grad must have weight's shape")
+    rc = load().sidco_cross_entropy_grad(_stream_handle(stream), *args, lse.data_ptr(), _ptr(loss_grad), _ptr(x_grad), ldgx, _ptr(weight_grad),
+                                         w_code, ldgw, 1 if accumulate else 0)
+    if rc:
+        raise SidcoError(rc, "sidco_cross_entropy_grad")
 
 
 def sidco_version() -> int:

@@ -12,7 +12,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsidco.so")
 SOURCES = ["sidco_kernels.hip", "sidco_topk.hip", "sidco_dgc.hip", "sidco_api.hip", "sidco_mx4.hip",
-           "sidco_ortho.hip", "sidco_dense_api.hip", "sidco_embed.hip", "sidco_dropout.hip", "sidco_language_api.hip"]
+           "sidco_ortho.hip", "sidco_dense_api.hip", "sidco_embed.hip", "sidco_dropout.hip", "sidco_entropy.hip",
+           "sidco_language_api.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",

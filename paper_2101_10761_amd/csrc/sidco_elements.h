@@ -79,6 +79,16 @@ __device__ __forceinline__ uint32_t word_at(const void* words, int64_t i, uint32
     return w >= 0 && w < (I)vocab ? (uint32_t)w : vocab;
 }
 
+// The same where the type is not worth a kernel of its own.
+struct WordList {
+    const void* at;  // may be NULL
+    bool wide;
+    uint32_t vocab;
+    __device__ __forceinline__ uint32_t operator[](int64_t i) const { return wide ? word_at<int64_t>(at, i, vocab) : word_at<int32_t>(at, i, vocab); }
+    __device__ __forceinline__ bool none(int64_t i) const { return (*this)[i] == vocab; }
+    WordList from(int64_t i) const { return {(const char*)at + i * (wide ? 8 : 4), wide, vocab}; }
+};
+
 // f(an int32_t or int64_t) for the words' type
 template <class F>
 inline void by_word(const Words& w, const F& f)

@@ -1,0 +1,826 @@
+// Softmax cross entropy of rows x against a vocabulary's weight w, in pieces, without keeping the logits.
+//
+//   l = x w^T,  lse_i = log sum_v exp l_iv,  loss_i = lse_i - l_i,t,
+//   P_iv = g_i (exp(l_iv - lse_i) - [v = t_i]),  dx = P w,  dw = P^T x.
+//
+// The forward pass is one product whose tiles go out as the largest logit of each row and the sum of exponentials below it, in
+// powers of two; a second kernel joins the tiles' pairs.  The gradient forms the logits again, a piece of the vocabulary at a
+// time, and P leaves the product's registers both by rows of x and by words, for the two products that contract over words
+// and over rows: four products for the three that an arithmetic minimum takes, and no N x V array.
+//
+// Products are those of sidco_product.h and want both operands by rows along the contraction, in whole lines of 128 bytes.
+// 16-bit operands that lie like that are read where they are; others, and the transposes that the gradient needs, are laid out
+// in the workspace first.  fp32 operands become pairs of halves, 22 bits, under a power of two that brings the largest
+// magnitude of the matrix to 2^14 to 2^15, and a product is three: low high + high low + high high.  P is held in the
+// operands' 16 bits (its rounding, 2^-9 or 2^-12 of each element, is that of the gradient's own type, and dx and dw add many
+// of them up), times a power of two for halves, whose smallest numbers it would reach; for a gradient in fp32 it is a pair.
+#include <math.h>
+
+#include <algorithm>
+
+#include "sidco_elements.h"
+#include "sidco_product.h"
+
+namespace sidco {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr double kLn2 = 0.69314718055994530942;
+constexpr float kFar = 3.0e38f;  // stands for an infinite largest logit
+
+// How element types are multiplied: what operands are held in, and whether as pairs.
+struct ModeF32 {
+    typedef float T;
+    typedef _Float16 H;
+    typedef HalfCore Core;
+    static constexpr bool kPairs = true, kScaled = true;
+};
+struct ModeF16 {
+    typedef _Float16 T, H;
+    typedef HalfCore Core;
+    static constexpr bool kPairs = false, kScaled = true;
+};
+struct ModeBf16 {
+    typedef __bf16 T, H;
+    typedef Bf16Core Core;
+    static constexpr bool kPairs = false, kScaled = false;  // has fp32's range
+};
+
+template <class F>
+void by_mode(int type, const F& f)
+{
+    if (type == kGradF32)
+        f(ModeF32());
+    else if (type == kGradF16)
+        f(ModeF16());
+    else
+        f(ModeBf16());
+}
+
+// ---- scales ----
+
+// Powers of two: of x and w as they are laid out, and of P.
+struct Scales {
+    float x, w, p;
+};
+constexpr int kParts = 512;  // blocks of k_top, and partial results of each of the three
+
+// What brings a largest magnitude to 2^14 to 2^15; 1 for zeros.
+__device__ __forceinline__ float scale_of(float top)
+{
+    if (!(top > 0.0f)) return 1.0f;
+    int e = 0;
+    (void)frexpf(top, &e);
+    e = 15 - e;
+    return ldexpf(1.0f, e > 120 ? 120 : e);
+}
+
+template <class T>
+struct Source {
+    const T* at;
+    int64_t ld, rows, cols;
+    WordList words;  // rows of padding are left out; without an address none is
+};
+
+template <class T>
+__device__ __forceinline__ float top_of(const Source<T>& p)
+{
+    float top = 0.0f;
+    for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+        if (p.words.at && p.words.none(r)) continue;
+        for (int64_t c = threadIdx.x * 8; c < p.cols; c += 256 * 8) {
+            Eight<T> v;
+            v.load(p.at + r * p.ld + c, p.cols - c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float m = fabsf(v.get(i));
+                top = m < INFINITY && m > top ? m : top;
+            }
+        }
+    }
+    return top;
+}
+
+// Largest finite magnitudes of x, w and the rows' gradient, a partial result from each block.
+template <class T>
+__global__ __launch_bounds__(256) void k_top(Source<T> x, Source<T> w, Source<float> g, float* part)
+{
+    __shared__ float lds[4][3];
+    float top[3] = {0.0f, 0.0f, 0.0f};
+    if (x.at) top[0] = top_of(x);
+    if (w.at) top[1] = top_of(w);
+    if (g.at) top[2] = top_of(g);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+#pragma unroll
+        for (int s = 32; s > 0; s >>= 1) top[k] = fmaxf(top[k], __shfl_xor(top[k], s));
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][k] = top[k];
+    }
+    __syncthreads();
+    if (threadIdx.x < 3) part[threadIdx.x * kParts + blockIdx.x] = fmaxf(fmaxf(lds[0][threadIdx.x], lds[1][threadIdx.x]), fmaxf(lds[2][threadIdx.x], lds[3][threadIdx.x]));
+}
+
+// The largest of one of the three, for the whole block of 256.
+__device__ __forceinline__ float joined_top(const float* part, float* lds)
+{
+    float top = fmaxf(part[threadIdx.x], part[threadIdx.x + 256]);
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+    __syncthreads();
+    return top;
+}
+
+// ---- operands ----
+
+// Rows of `pitch` elements; what a pair's second numbers are kept in is `low` elements on, 0: there is none.
+template <class H>
+struct Plane {
+    H* at;
+    int64_t pitch, low;
+};
+
+template <class H>
+__device__ __forceinline__ Rows rows_of(const Plane<H>& p, int64_t row, int64_t rows, int64_t col, bool low)
+{
+    return {p.at + (low ? p.low : 0) + row * p.pitch + col, nullptr, (uint32_t)rows, (uint32_t)(p.pitch * sizeof(H))};
+}
+
+// A matrix to be laid out: by its rows, and transposed.  Either plane may have no address.
+template <class T, class H>
+struct Layout {
+    Source<T> from;
+    Plane<H> rows, turned;
+    uint32_t tiles_r, tiles_c;  // of 64 x 64, padding included
+};
+
+template <class H, bool Pairs>
+__device__ __forceinline__ void put8(const Plane<H>& o, int64_t r, int64_t c, const float (&v)[8])
+{
+    typedef H h8 __attribute__((ext_vector_type(8)));
+    h8 h, l;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        h[i] = (H)v[i];
+        l[i] = (H)(v[i] - (float)h[i]);
+    }
+    H* p = o.at + r * o.pitch + c;
+    *(h8*)p = h;
+    if (Pairs) *(h8*)(p + o.low) = l;
+}
+
+// 64 x 64 elements a block, of x and then of w.  Transposed, rows of padding are zeros whatever they hold: they are multiplied
+// with the zeros that P has for them.  With Scaled the partial results of k_top are joined, and block 0 writes them down.
+template <class M>
+__global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M::H> x, Layout<typename M::T, typename M::H> w, const float* part,
+                                                Scales* scales)
+{
+    typedef typename M::H H;
+    __shared__ float tile[64][65];
+    __shared__ float lds[4];
+    const uint32_t first = x.tiles_r * x.tiles_c;
+    const bool second = blockIdx.x >= first;
+    const Layout<typename M::T, H>& p = second ? w : x;
+    const uint32_t t = second ? blockIdx.x - first : blockIdx.x;
+    float scale = 1.0f;
+    if (M::kScaled && (M::kPairs || blockIdx.x == 0)) {
+        if (M::kPairs) scale = scale_of(joined_top(part + (second ? kParts : 0), lds));
+        if (blockIdx.x == 0) {
+            const float sx = M::kPairs ? scale_of(joined_top(part, lds)) : 1.0f, sw = M::kPairs ? scale_of(joined_top(part + kParts, lds)) : 1.0f;
+            const float sp = scale_of(joined_top(part + 2 * kParts, lds));
+            if (threadIdx.x == 0) *scales = {sx, sw, sp};
+        }
+    }
+    if (first + w.tiles_r * w.tiles_c <= blockIdx.x) return;
+    const int64_t r0 = (int64_t)(t / p.tiles_c) * 64, c0 = (int64_t)(t % p.tiles_c) * 64;
+    const int row = threadIdx.x >> 3, col = (threadIdx.x & 7) * 8;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int64_t r = r0 + k * 32 + row, c = c0 + col;
+        float v[8] = {};
+        if (r < p.from.rows && c < p.from.cols) {
+            Eight<typename M::T> e;
+            e.load(p.from.at + r * p.from.ld + c, p.from.cols - c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = M::kPairs ? e.get(i) * scale : e.get(i);
+        }
+        if (p.rows.at && r < p.from.rows && c < p.rows.pitch) put8<H, M::kPairs>(p.rows, r, c, v);
+        if (p.turned.at) {
+            const bool none = p.from.words.at && r < p.from.rows && p.from.words.none(r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) tile[k * 32 + row][col + i] = none ? 0.0f : v[i];
+        }
+    }
+    if (!p.turned.at) return;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c = k * 32 + row;
+        if (c0 + c >= p.from.cols || r0 + col >= p.turned.pitch) continue;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = tile[col + i][c];
+        put8<H, M::kPairs>(p.turned, c0 + c, r0 + col, v);
+    }
+}
+
+// ---- the products ----
+
+// Terms of a product of pairs and single numbers, the small ones first.
+template <int Terms, class Tl, class H>
+__device__ __forceinline__ void take(Tl& t, int term, const Plane<H>& a, int64_t rows_a, const Plane<H>& b, int64_t rows_b, int64_t col, uint32_t m0,
+                                     uint32_t n0)
+{
+    t.take(rows_of(a, 0, rows_a, col, Terms > 1 && term == 0), rows_of(b, 0, rows_b, col, Terms == 3 && term == 1), m0, n0);
+}
+
+template <class Tl, class H>
+constexpr int lds_of()
+{
+    return Tl::kLds + Tl::kWaves * Tl::template out_bytes<H>();
+}
+
+struct Places {
+    uint32_t tm, tn, total;  // total: of all splits
+    __device__ __forceinline__ void at(uint32_t tile, uint32_t& i, uint32_t& j, uint32_t& split) const
+    {
+        const uint32_t w = xcd_run(tile, total);
+        split = w / (tm * tn);
+        tile_of(w - split * (tm * tn), tm, tn, i, j);
+    }
+};
+
+// Logits of a tile as its rows' largest, in powers of two, and sums of 2^(logit - largest): pairs `width` a row, one for each
+// wave's columns.  The logit of a row's word is written down by the wave that has it.
+template <class H>
+struct Forward {
+    Plane<H> x, w;
+    int64_t n, vocab;
+    WordList words;  // of these rows
+    float2* part;
+    uint32_t width;
+    float* mine;
+    const Scales* scales;
+};
+
+template <class M, class Tl>
+__global__ __launch_bounds__(Tl::kThreads) void k_logits(Forward<typename M::H> p, Span span, Places places)
+{
+    __shared__ __align__(1024) char lds[Tl::kLds];
+    Tl t;
+    t.template run<M::kPairs ? 3 : 1>(
+        places.total, span, lds,
+        [&](uint32_t tile, int term) {
+            uint32_t i, j, split;
+            places.at(tile, i, j, split);
+            take<M::kPairs ? 3 : 1>(t, term, p.x, p.n, p.w, p.vocab, 0, i * Tl::kM, j * Tl::kN);
+        },
+        [&](uint32_t tile) {
+            uint32_t ti, tj, split;
+            places.at(tile, ti, tj, split);
+            const uint32_t m0 = ti * Tl::kM, n0 = tj * Tl::kN;
+            const float k = M::kPairs ? kLog2e / (p.scales->x * p.scales->w) : kLog2e;
+            const bool edge = n0 + Tl::kN > p.vocab;
+            const uint32_t place = tj * (Tl::kN / (Tl::kNt * 16)) + t.wave % (Tl::kN / (Tl::kNt * 16));
+            t.strips([&](int, uint32_t row, uint32_t col, v4f(&acc)[Tl::kNt]) {
+                const uint32_t r = m0 + row;
+                const uint32_t word = r < p.n ? p.words[r] : p.words.vocab;
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < Tl::kNt; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (edge && n0 + col + j * 16 + e >= p.vocab) acc[j][e] = -INFINITY;
+                        acc[j][e] *= k;
+                        top = fmaxf(top, acc[j][e]);
+                    }
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                top = fminf(fmaxf(top, -kFar), kFar);
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < Tl::kNt; ++j) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (word == n0 + col + j * 16 + e && word < p.words.vocab) p.mine[r] = acc[j][e];
+                        sum += __builtin_amdgcn_exp2f(acc[j][e] - top);
+                    }
+                }
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+                if (t.lane < 16 && r < p.n) p.part[(int64_t)r * p.width + place] = make_float2(top, sum);
+            });
+        });
+}
+
+// A wave joins a row's pairs.  An infinite largest logit has made the sum infinite, a NaN among them a NaN.
+__global__ __launch_bounds__(256) void k_join_rows(const float2* part, uint32_t width, int64_t n, WordList words, const float* mine, float* loss,
+                                                   float* lse)
+{
+    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= n) return;
+    const int lane = threadIdx.x & 63;
+    float top = -kFar, sum = 0.0f;
+    for (uint32_t i = lane; i < width; i += 64) {
+        const float2 v = part[r * width + i];
+        const float next = fmaxf(top, v.x);
+        sum = sum * __builtin_amdgcn_exp2f(top - next) + v.y * __builtin_amdgcn_exp2f(v.x - next);
+        top = next;
+    }
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) {
+        const float other = __shfl_xor(top, s), more = __shfl_xor(sum, s), next = fmaxf(top, other);
+        // the larger index second, so that both lanes round alike
+        const float a = sum * __builtin_amdgcn_exp2f(top - next), b = more * __builtin_amdgcn_exp2f(other - next);
+        sum = a + b;
+        top = next;
+    }
+    if (lane == 0) {
+        const double all = (double)top + (double)log2f(sum);
+        const float l = (float)(all * kLn2);
+        if (lse) lse[r] = l;
+        if (loss) {
+            loss[r] = words.none(r) ? 0.0f : (float)((all - (double)mine[r]) * kLn2);
+        }
+    }
+}
+
+// P of a piece of the vocabulary, words from `first` on.
+template <class H>
+struct Probs {
+    Plane<H> x, w;  // w: the piece's rows
+    int64_t n, count;
+    uint32_t first;
+    WordList words;
+    const float *lse, *loss_grad;
+    Plane<H> out, turned;  // n rows of words, words of n rows; either may have no address
+    const Scales* scales;
+};
+
+template <class M, class Tl>
+__global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, Span span, Places places)
+{
+    typedef typename M::H H;
+    typedef H h8 __attribute__((ext_vector_type(8)));
+    __shared__ __align__(1024) char lds[lds_of<Tl, H>()];
+    Tl t;
+    t.template run<M::kPairs ? 3 : 1>(
+        places.total, span, lds,
+        [&](uint32_t tile, int term) {
+            uint32_t i, j, split;
+            places.at(tile, i, j, split);
+            take<M::kPairs ? 3 : 1>(t, term, p.x, p.n, p.w, p.count, 0, i * Tl::kM, j * Tl::kN);
+        },
+        [&](uint32_t tile) {
+            uint32_t ti, tj, split;
+            places.at(tile, ti, tj, split);
+            const uint32_t m0 = ti * Tl::kM, n0 = tj * Tl::kN;
+            const float k = M::kPairs ? kLog2e / (p.scales->x * p.scales->w) : kLog2e, sp = M::kScaled ? p.scales->p : 1.0f;
+            t.strips([&](int, uint32_t row, uint32_t col, v4f(&acc)[Tl::kNt]) {
+                const uint32_t r = m0 + row;
+                uint32_t word = p.words.vocab;
+                float lse = 0.0f, gain = 0.0f;
+                if (r < p.n) {
+                    word = p.words[r];
+                    lse = p.lse[r] * -kLog2e;
+                    gain = (p.loss_grad ? p.loss_grad[r] : 1.0f) * sp;
+                }
+                const uint32_t here = word - p.first - n0 - col;
+                const bool none = word == p.words.vocab;
+#pragma unroll
+                for (int j = 0; j < Tl::kNt; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float q = __builtin_amdgcn_exp2f(fmaf(acc[j][e], k, lse)) - (here == (uint32_t)(j * 16 + e) ? 1.0f : 0.0f);
+                        acc[j][e] = none ? 0.0f : q * gain;
+                    }
+                // P goes back where the sums were
+#pragma unroll
+                for (int j = 0; j < Tl::kNt; ++j) asm volatile("" : "+a"(acc[j]));
+            });
+            // eight neighbours of row r from column c on; columns behind the last are zeros up to the pitch
+            auto put = [](const Plane<H>& o, int64_t rows, int64_t cols, bool low) {
+                return [&o, rows, cols, low](uint32_t r, uint32_t c, h8 v) {
+                    if (r >= rows || c >= o.pitch) return;
+                    if (c + 8 > cols) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? v[i] : (H)0.0f;
+                    }
+                    *(h8*)(o.at + (low ? o.low : 0) + (int64_t)r * o.pitch + c) = v;
+                };
+            };
+            auto whole = [](uint32_t, uint32_t, const v4f& v) -> v4f { return v; };
+            auto rest = [](uint32_t, uint32_t, const v4f& v) -> v4f {
+                const v4f w = rounded(v);
+                v4f l;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) l[i] = w[i] - (float)(H)w[i];
+                return l;
+            };
+            char* by = lds + Tl::kLds;
+            if (p.out.at) {
+                const auto high = put(p.out, p.n, p.count, false), low = put(p.out, p.n, p.count, true);
+                t.template out<H, false>(by, whole, [&](uint32_t r, uint32_t c, const h8& v) { high(m0 + r, n0 + c, v); });
+                if (M::kPairs) t.template out<H, false>(by, rest, [&](uint32_t r, uint32_t c, const h8& v) { low(m0 + r, n0 + c, v); });
+            }
+            if (p.turned.at) {
+                const auto high = put(p.turned, p.count, p.n, false), low = put(p.turned, p.count, p.n, true);
+                t.template out<H, true>(by, whole, [&](uint32_t r, uint32_t c, const h8& v) { high(n0 + r, m0 + c, v); });
+                if (M::kPairs || p.turned.low) t.template out<H, true>(by, rest, [&](uint32_t r, uint32_t c, const h8& v) { low(n0 + r, m0 + c, v); });
+            }
+        });
+}
+
+// C = alpha A B^T over the columns that span.lines cover, of split number s from column s * lines on: rounded to T, on top of
+// `before` (fp32) and of C itself with `accumulate`.  Each split has a C of its own.
+template <class H>
+struct Product {
+    Plane<H> a, b;
+    int64_t m, n;
+    const Scales* scales;  // alpha is one over its p and that of w, or with of_x of x; NULL: one
+    bool of_x;
+    void* c;
+    int64_t ldc, split_stride;
+    bool accumulate;
+    const float* before;   // m x n; NULL: nothing
+};
+
+template <class T>
+__device__ __forceinline__ void finish4(T* c, const float* before, bool accumulate, int64_t left, v4f v)
+{
+    typedef T t4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+    if (left >= 4) {
+        if (before) v += *(const f4*)before;
+        if (accumulate) {
+            const t4 old = *(const t4*)c;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += (float)old[i];
+        }
+        t4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (T)v[i];
+        *(t4*)c = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) c[i] = (T)(v[i] + (before ? before[i] : 0.0f) + (accumulate ? (float)c[i] : 0.0f));
+    }
+}
+
+template <class T, class H, int Terms, class Tl>
+__global__ __launch_bounds__(Tl::kThreads) void k_product(Product<H> p, Span span, Places places)
+{
+    __shared__ __align__(1024) char lds[Tl::kLds];
+    Tl t;
+    t.template run<Terms>(
+        places.total, span, lds,
+        [&](uint32_t tile, int term) {
+            uint32_t i, j, split;
+            places.at(tile, i, j, split);
+            take<Terms>(t, term, p.a, p.m, p.b, p.n, (int64_t)split * span.lines * (kLine / (int)sizeof(H)), i * Tl::kM, j * Tl::kN);
+        },
+        [&](uint32_t tile) {
+            uint32_t ti, tj, split;
+            places.at(tile, ti, tj, split);
+            const float alpha = p.scales ? 1.0f / (p.scales->p * (p.of_x ? p.scales->x : p.scales->w)) : 1.0f;
+            t.each([&](uint32_t row, uint32_t col, const v4f& v) {
+                const int64_t r = (int64_t)ti * Tl::kM + row, c = (int64_t)tj * Tl::kN + col;
+                if (r >= p.m || c >= p.n) return;
+                finish4<T>((T*)p.c + split * p.split_stride + r * p.ldc + c, p.before ? p.before + r * p.n + c : nullptr, p.accumulate, p.n - c,
+                           v * alpha);
+            });
+        });
+}
+
+// The splits' sums joined, in their order.
+template <class T>
+__global__ __launch_bounds__(256) void k_join_sums(const float* sums, int splits, int64_t m, int64_t n, T* c, int64_t ldc)
+{
+    const int64_t per = (n + 3) / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= m * per) return;
+    const int64_t r = i / per, k = i % per * 4, left = n - k;
+    v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < splits; ++s) {
+        const float* from = sums + (s * m + r) * n + k;
+        typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+        if (left >= 4) {
+            v += *(const f4*)from;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += j < left ? from[j] : 0.0f;
+        }
+    }
+    finish4<T>(c + r * ldc + k, nullptr, false, left, v);
+}
+
+// ---- the calls ----
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+int64_t parts(int64_t n, int64_t of) { return (n + of - 1) / of; }
+
+template <class M>
+constexpr int kPer = kLine / (int)sizeof(typename M::H);  // elements of a line
+
+// Whether a matrix can be read where it is.
+template <class M>
+bool lies_in_lines(const Matrix& x, int64_t dim)
+{
+    if (sizeof(typename M::T) != sizeof(typename M::H)) return false;
+    return dim % kPer<M> == 0 && x.ld % kPer<M> == 0 && x.ld * (int64_t)sizeof(typename M::H) < (1 << 24) && (uintptr_t)x.at % 16 == 0;
+}
+
+// The workspace, handed out in order.
+struct Space {
+    char* at;
+    size_t used;
+    template <class T>
+    T* get(int64_t count)
+    {
+        T* p = (T*)(at + used);
+        used += (size_t)up(count * (int64_t)sizeof(T), 256);
+        return at ? p : nullptr;
+    }
+    template <class H>
+    Plane<H> plane(int64_t rows, int64_t pitch, bool pairs)
+    {
+        return {get<H>(rows * pitch * (pairs ? 2 : 1)), pitch, pairs ? rows * pitch : 0};
+    }
+};
+
+template <class Tl>
+struct Shape {
+    typedef Tl Is;
+};
+
+// f(a tile's type) for the tile of kTileCosts[pick]
+template <class M, class F>
+void by_tile(int pick, const F& f)
+{
+    typedef typename M::Core Core;
+    if (pick == 0)
+        f(Shape<Tile<Core, 256, 256, 2, 2, 2>>());
+    else if (pick == 1)
+        f(Shape<Tile<Core, 192, 192, 2, 2, 3>>());
+    else if (pick == 2)
+        f(Shape<Tile<Core, 128, 128, 2, 2, 2>>());
+    else
+        f(Shape<Tile<Core, 64, 64, 2, 2, 4>>());
+}
+
+template <class T>
+Source<T> source(const Matrix& m, int64_t rows, int64_t cols, const WordList& words = {}, int64_t first = 0)
+{
+    return {m.at ? (const T*)m.at + first * m.ld : nullptr, m.ld, rows, cols, words};
+}
+
+constexpr int64_t kRowsAtOnce = 16384;  // of the forward pass
+
+// The tile of the product of that many rows with the vocabulary.
+template <class M>
+int forward_tile(int64_t rows, int64_t vocab, int64_t lines)
+{
+    return best_tile([&](int64_t side) { return parts(rows, side) * parts(vocab, side); }, lines * (M::kPairs ? 3 : 1));
+}
+int64_t forward_width(int pick, int64_t vocab) { return 2 * parts(vocab, kTileCosts[pick].side); }
+
+template <class M>
+struct ForwardPlan {
+    typedef typename M::H H;
+    int64_t pitch;
+    bool lay_x, lay_w;
+    float* part;
+    Scales* scales;
+    Plane<H> x, w;
+    float2* pairs;
+    float* mine;
+    size_t bytes;
+    ForwardPlan(const Entropy& q, char* scratch)
+    {
+        Space s = {scratch, 0};
+        const int64_t n = q.words.n, v = q.words.vocab, at_once = std::min(n, kRowsAtOnce);
+        pitch = up(q.dim, kPer<M>);
+        lay_x = !lies_in_lines<M>(q.x, q.dim);
+        lay_w = !lies_in_lines<M>(q.w, q.dim);
+        scales = s.get<Scales>(1);
+        part = s.get<float>(M::kPairs ? 3 * kParts : 0);
+        x = lay_x ? s.plane<H>(n, pitch, M::kPairs) : Plane<H>{(H*)q.x.at, q.x.ld, 0};
+        w = lay_w ? s.plane<H>(v, pitch, M::kPairs) : Plane<H>{(H*)q.w.at, q.w.ld, 0};
+        auto pairs_of = [&](int64_t rows) { return rows * forward_width(forward_tile<M>(rows, v, pitch / kPer<M>), v); };
+        pairs = s.get<float2>(std::max(pairs_of(at_once), pairs_of((n - 1) % kRowsAtOnce + 1)));
+        mine = s.get<float>(at_once);
+        bytes = s.used;
+    }
+};
+
+WordList list(const Words& w) { return {w.at, w.wide, (uint32_t)w.vocab}; }
+
+template <class M>
+void tops(const Entropy& q, bool of_matrices, bool of_gains, float* part, hipStream_t s)
+{
+    typedef typename M::T T;
+    Source<T> none = {};
+    const WordList words = list(q.words);
+    const Source<float> g = {of_gains ? q.loss_grad : nullptr, 1, q.words.n, 1, words};
+    k_top<T><<<kParts, 256, 0, s>>>(of_matrices ? source<T>(q.x, q.words.n, q.dim, words) : none,
+                                    of_matrices ? source<T>(q.w, q.words.vocab, q.dim) : none, g, part);
+}
+
+template <class M>
+void forward(const Entropy& q, char* scratch, hipStream_t s)
+{
+    typedef typename M::T T;
+    typedef typename M::H H;
+    const ForwardPlan<M> f(q, scratch);
+    const int64_t n = q.words.n, v = q.words.vocab;
+    if (M::kPairs) tops<M>(q, true, false, f.part, s);
+    if (f.lay_x || f.lay_w) {
+        const uint32_t across = (uint32_t)parts(f.pitch, 64);
+        const Layout<T, H> lx = {source<T>(q.x, n, q.dim), f.lay_x ? f.x : Plane<H>{}, {}, f.lay_x ? (uint32_t)parts(n, 64) : 0, across};
+        const Layout<T, H> lw = {source<T>(q.w, v, q.dim), f.lay_w ? f.w : Plane<H>{}, {}, f.lay_w ? (uint32_t)parts(v, 64) : 0, across};
+        k_layout<M><<<(lx.tiles_r + lw.tiles_r) * across, 256, 0, s>>>(lx, lw, f.part, f.scales);
+    }
+    for (int64_t r = 0; r < n; r += kRowsAtOnce) {
+        const int64_t rows = std::min(n - r, kRowsAtOnce);
+        const WordList words = list(q.words).from(r);
+        const Span span = {(uint32_t)(f.x.pitch * sizeof(H)), (uint32_t)(f.w.pitch * sizeof(H)), (uint32_t)(f.pitch / kPer<M>)};
+        const int pick = forward_tile<M>(rows, v, span.lines);
+        const uint32_t width = (uint32_t)forward_width(pick, v);
+        by_tile<M>(pick, [&](auto shape) {
+            typedef typename decltype(shape)::Is Tl;
+            const Places places = {(uint32_t)parts(rows, Tl::kM), (uint32_t)parts(v, Tl::kN), (uint32_t)(parts(rows, Tl::kM) * parts(v, Tl::kN))};
+            const Plane<H> x = {f.x.at + r * f.x.pitch, f.x.pitch, f.x.low};
+            const Forward<H> p = {x, f.w, rows, v, words, f.pairs, width, f.mine, f.scales};
+            k_logits<M, Tl><<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places);
+        });
+        k_join_rows<<<(uint32_t)parts(rows, 4), 256, 0, s>>>(f.pairs, width, rows, words, f.mine, q.loss ? q.loss + r : nullptr,
+                                                            q.lse ? q.lse + r : nullptr);
+    }
+}
+
+// A piece of the vocabulary: as many words as keep P, both ways, at this size.
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;
+
+template <class M>
+struct GradPlan {
+    typedef typename M::H H;
+    int64_t pitch, pitch_n, pitch_v, piece, pieces;
+    int splits, pick_x;   // of the product for x's gradient
+    bool lay_x, lay_w, wide;  // wide: w's gradient in fp32, of 16-bit operands
+    float* part;
+    Scales* scales;
+    Plane<H> x, xt, w, wt, p, pt;
+    float* sums;
+    size_t bytes;
+    GradPlan(const Entropy& q, char* scratch)
+    {
+        Space s = {scratch, 0};
+        const int64_t n = q.words.n, v = q.words.vocab;
+        pitch = up(q.dim, kPer<M>);
+        pitch_n = up(n, kPer<M>);
+        lay_x = !lies_in_lines<M>(q.x, q.dim);
+        lay_w = !lies_in_lines<M>(q.w, q.dim);
+        wide = !M::kPairs && q.w_grad.at && q.w_grad.type == kGradF32;
+        const int64_t word = pitch_n * (int64_t)sizeof(H) * (q.x_grad.at ? 1 : 0) + pitch_n * (int64_t)sizeof(H) * (q.w_grad.at ? 1 : 0);
+        const int64_t most = std::min(std::max(kPieceBytes / (word * (M::kPairs ? 2 : 1)), (int64_t)1024), (int64_t)1 << 22);
+        pieces = parts(v, most);
+        piece = std::min(up(parts(v, pieces), 256), v);
+        pieces = parts(v, piece);
+        // The contraction over words is long and its tiles may be few.
+        splits = 1;
+        pick_x = 0;
+        int64_t lines = parts(piece, kPer<M>);
+        if (q.x_grad.at) {
+            double least = 0.0;
+            for (int k = 1; k <= 64 && k * 8 <= std::max(lines, (int64_t)8); k *= 2) {
+                double t = 0.0;
+                const int64_t each = parts(lines, k);
+                const int pick = best_tile([&](int64_t side) { return parts(n, side) * parts(q.dim, side) * k; }, each * (M::kPairs ? 3 : 1), &t);
+                if (k > 1) t += 4.0 + 2e-6 * (double)n * (double)q.dim * k;  // sums through memory, and their launch
+                if (k == 1 || t < least) least = t, splits = k, pick_x = pick;
+            }
+        }
+        lines = parts(lines, splits) * splits;
+        pitch_v = lines * kPer<M>;
+        scales = s.get<Scales>(1);
+        part = s.get<float>(M::kScaled ? 3 * kParts : 0);
+        x = lay_x ? s.plane<H>(n, pitch, M::kPairs) : Plane<H>{(H*)q.x.at, q.x.ld, 0};
+        w = lay_w ? s.plane<H>(piece, pitch, M::kPairs) : Plane<H>{};
+        xt = wt = p = pt = Plane<H>{};
+        if (q.w_grad.at) {
+            xt = s.plane<H>(q.dim, pitch_n, M::kPairs);
+            pt = s.plane<H>(piece, pitch_n, M::kPairs || wide);
+        }
+        if (q.x_grad.at) {
+            wt = s.plane<H>(q.dim, pitch_v, M::kPairs);
+            p = s.plane<H>(n, pitch_v, M::kPairs);
+        }
+        sums = q.x_grad.at && (splits > 1 || pieces > 1) ? s.get<float>(splits * n * q.dim) : nullptr;
+        bytes = s.used;
+    }
+};
+
+template <class T, class M, int Terms>
+void product(int pick, const Product<typename M::H>& p, int64_t lines, int splits, hipStream_t s)
+{
+    typedef typename M::H H;
+    by_tile<M>(pick, [&](auto shape) {
+        typedef typename decltype(shape)::Is Tl;
+        const uint32_t tm = (uint32_t)parts(p.m, Tl::kM), tn = (uint32_t)parts(p.n, Tl::kN);
+        const Places places = {tm, tn, tm * tn * splits};
+        const Span span = {(uint32_t)(p.a.pitch * sizeof(H)), (uint32_t)(p.b.pitch * sizeof(H)), (uint32_t)lines};
+        k_product<T, H, Terms, Tl><<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places);
+    });
+}
+
+template <class M>
+void gradient(const Entropy& q, char* scratch, hipStream_t s)
+{
+    typedef typename M::T T;
+    typedef typename M::H H;
+    constexpr int kTerms = M::kPairs ? 3 : 1;
+    const GradPlan<M> g(q, scratch);
+    const int64_t n = q.words.n, v = q.words.vocab;
+    const WordList words = list(q.words);
+    if (M::kScaled) tops<M>(q, M::kPairs, true, g.part, s);
+    for (int64_t k = 0; k < g.pieces; ++k) {
+        const int64_t first = k * g.piece, count = std::min(g.piece, v - first);
+        const Plane<H> w = g.lay_w ? g.w : Plane<H>{(H*)q.w.at + first * q.w.ld, q.w.ld, 0};
+        // x once, and this piece of w
+        Layout<T, H> lx = {source<T>(q.x, n, q.dim, words), g.lay_x ? g.x : Plane<H>{}, g.xt, 0, (uint32_t)parts(g.pitch, 64)};
+        Layout<T, H> lw = {source<T>(q.w, count, q.dim, {}, first), g.lay_w ? g.w : Plane<H>{}, g.wt, 0, lx.tiles_c};
+        if (k == 0 && (g.lay_x || g.xt.at)) lx.tiles_r = (uint32_t)parts(g.pitch_n, 64);
+        if (g.lay_w || g.wt.at) lw.tiles_r = (uint32_t)parts(g.wt.at ? g.pitch_v : count, 64);
+        const uint32_t blocks = (lx.tiles_r + lw.tiles_r) * lx.tiles_c;
+        if (blocks || (k == 0 && M::kScaled)) k_layout<M><<<blocks ? blocks : 1, 256, 0, s>>>(lx, lw, g.part, g.scales);
+
+        const Span span = {(uint32_t)(g.x.pitch * sizeof(H)), (uint32_t)(w.pitch * sizeof(H)), (uint32_t)(g.pitch / kPer<M>)};
+        const int64_t wide = g.p.at ? g.pitch_v : count;  // padding of P's rows is written with the last tiles
+        const int pick = best_tile([&](int64_t side) { return parts(n, side) * parts(wide, side); }, span.lines * kTerms);
+        by_tile<M>(pick, [&](auto shape) {
+            typedef typename decltype(shape)::Is Tl;
+            const uint32_t tm = (uint32_t)parts(n, Tl::kM), tn = (uint32_t)parts(wide, Tl::kN);
+            const Places places = {tm, tn, tm * tn};
+            const Probs<H> p = {g.x, w, n, count, (uint32_t)first, words, q.lse, q.loss_grad, g.p, g.pt, g.scales};
+            k_probs<M, Tl><<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places);
+        });
+        const Scales* scales = M::kScaled ? g.scales : nullptr;
+        if (q.x_grad.at) {
+            const int64_t lines = g.pitch_v / kPer<M> / g.splits;
+            if (g.splits > 1 || k + 1 < g.pieces) {
+                const Product<H> p = {g.p, g.wt, n, q.dim, scales, false, g.sums, q.dim, n * q.dim, k > 0, nullptr};
+                product<float, M, kTerms>(g.pick_x, p, lines, g.splits, s);
+            } else {
+                const Product<H> p = {g.p, g.wt, n, q.dim, scales, false, q.x_grad.at, q.x_grad.ld, 0, false, g.pieces > 1 ? g.sums : nullptr};
+                product<T, M, kTerms>(g.pick_x, p, lines, 1, s);
+            }
+        }
+        if (q.w_grad.at) {
+            char* c = (char*)q.w_grad.at + first * q.w_grad.ld * (q.w_grad.type == kGradF32 ? 4 : 2);
+            const Product<H> p = {g.pt, g.xt, count, q.dim, scales, true, c, q.w_grad.ld, 0, q.accumulate, nullptr};
+            const int64_t lines = g.pitch_n / kPer<M>;
+            const int terms = M::kPairs ? 3 : (g.wide ? 2 : 1);
+            const int pw = best_tile([&](int64_t side) { return parts(count, side) * parts(q.dim, side); }, lines * terms);
+            if constexpr (M::kPairs) {
+                product<float, M, 3>(pw, p, lines, 1, s);
+            } else {
+                if (g.wide)
+                    product<float, M, 2>(pw, p, lines, 1, s);
+                else
+                    product<T, M, 1>(pw, p, lines, 1, s);
+            }
+        }
+    }
+    if (q.x_grad.at && g.splits > 1)
+        k_join_sums<T><<<(uint32_t)parts(n * parts(q.dim, 4), 256), 256, 0, s>>>(g.sums, g.splits, n, q.dim, (T*)q.x_grad.at, q.x_grad.ld);
+}
+
+}  // namespace
+
+size_t entropy_scratch(const Entropy& q)
+{
+    size_t bytes = 0;
+    by_mode(q.x.type, [&](auto m) { bytes = ForwardPlan<decltype(m)>(q, nullptr).bytes; });
+    return bytes;
+}
+
+size_t entropy_grad_scratch(const Entropy& q)
+{
+    size_t bytes = 0;
+    by_mode(q.x.type, [&](auto m) { bytes = GradPlan<decltype(m)>(q, nullptr).bytes; });
+    return bytes;
+}
+
+void launch_entropy(const Entropy& q, char* scratch, hipStream_t s)
+{
+    by_mode(q.x.type, [&](auto m) { forward<decltype(m)>(q, scratch, s); });
+}
+
+void launch_entropy_grad(const Entropy& q, char* scratch, hipStream_t s)
+{
+    by_mode(q.x.type, [&](auto m) { gradient<decltype(m)>(q, scratch, s); });
+}
+
+}  // namespace sidco

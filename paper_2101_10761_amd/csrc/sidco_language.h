@@ -46,5 +46,21 @@ struct Dropout {
 };
 void launch_dropout(const Dropout& q, hipStream_t s);
 
+// Logits are x w^T: words.n rows of x, words.vocab rows of w, both of one type and of `dim` columns.
+struct Entropy {
+    Words words;
+    int64_t dim;
+    Matrix x, w;
+    float *loss, *lse;         // written by the forward pass, either may be NULL; lse is read by the gradient
+    const float* loss_grad;    // NULL: ones
+    Matrix x_grad, w_grad;     // one of the two may be NULL
+    bool accumulate;           // onto w_grad
+};
+constexpr int64_t kEntropyMaxRows = 1 << 22, kEntropyMaxDim = 1 << 21;
+size_t entropy_scratch(const Entropy& q);       // of x, w only whether they lie in whole lines
+size_t entropy_grad_scratch(const Entropy& q);  // and of the gradients which there are and w_grad's type
+void launch_entropy(const Entropy& q, char* scratch, hipStream_t s);
+void launch_entropy_grad(const Entropy& q, char* scratch, hipStream_t s);
+
 }  // namespace sidco
 #endif

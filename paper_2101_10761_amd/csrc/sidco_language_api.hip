@@ -32,6 +32,32 @@ int check_words(const void* words, int type, int64_t n, int64_t vocab)
 
 Matrix matrix(const void* p, int dtype, int64_t ld) { return {(void*)p, type_of(dtype), ld}; }
 
+bool entropy_sizes(int64_t n, int64_t dim, int64_t vocab)
+{
+    if (n < 1 || n > kEntropyMaxRows || dim < 1 || dim > kEntropyMaxDim || !extent(vocab)) return false;
+    // a tile's number has 31 bits
+    return ((n + 63) / 64) * ((vocab + 63) / 64) <= (int64_t)INT32_MAX && ((vocab + 63) / 64) * ((dim + 63) / 64) <= (int64_t)INT32_MAX;
+}
+
+int check_entropy(const void* x, const void* w, int dtype, int64_t n, int64_t dim, int64_t vocab, int64_t ldx, int64_t ldw, const void* words,
+                  int word_type)
+{
+    if (int rc = check_words(words, word_type, n, vocab)) return rc;
+    if (int rc = check_matrix(x, dtype, dim, ldx)) return rc;
+    if (int rc = check_matrix(w, dtype, dim, ldw)) return rc;
+    return entropy_sizes(n, dim, vocab) ? SIDCO_OK : SIDCO_ERR_SIZE;
+}
+
+// Of any call with these sizes: x and w as if they had to be laid out.
+Entropy any_entropy(int64_t n, int64_t dim, int64_t vocab, int dtype)
+{
+    Entropy q = {};
+    q.words = {nullptr, true, n, vocab};
+    q.dim = dim;
+    q.x = q.w = {(void*)1, type_of(dtype), dim};
+    return q;
+}
+
 }  // namespace
 
 extern "C" {
@@ -89,6 +115,77 @@ int sidco_dropout(void* stream, const void* x, int x_dtype, int64_t rows, int64_
     const Dropout q = {rows, cols, matrix(x, x_dtype, ldx), matrix(residual, y_dtype, ldr), matrix(y, y_dtype, ldy),
                        (uint32_t)floor(65536.0 * p + 0.5), seed, offset, device_offset};
     launch_dropout(q, (hipStream_t)stream);
+    return launched();
+}
+
+size_t sidco_workspace_bytes_cross_entropy(int64_t n, int64_t dim, int64_t vocab, int dtype)
+{
+    if (!entropy_sizes(n, dim, vocab) || !element_type(dtype)) return 0;
+    return workspace_with_scratch(entropy_scratch(any_entropy(n, dim, vocab, dtype)));
+}
+
+int sidco_cross_entropy(void* stream, const void* x, const void* w, int dtype, int64_t n, int64_t dim, int64_t vocab, int64_t ldx, int64_t ldw,
+                        const void* targets, int word_type, float* loss, float* lse)
+{
+    if (!loss && !lse) return SIDCO_ERR_NULL;
+    if (int rc = check_entropy(x, w, dtype, n, dim, vocab, ldx, ldw, targets, word_type)) return rc;
+    if (!aligned(loss, 4) || !aligned(lse, 4)) return SIDCO_ERR_ALIGN;
+    if (loss == lse) return SIDCO_ERR_ARG;
+    Entropy q = {};
+    q.words = {targets, word_type == SIDCO_WORD_I64, n, vocab};
+    q.dim = dim;
+    q.x = matrix(x, dtype, ldx);
+    q.w = matrix(w, dtype, ldw);
+    q.loss = loss;
+    q.lse = lse;
+    StreamScratch ws(stream, entropy_scratch(q));
+    if (ws.rc != SIDCO_OK) return ws.rc;
+    launch_entropy(q, ws.data, (hipStream_t)stream);
+    return launched();
+}
+
+size_t sidco_workspace_bytes_cross_entropy_grad(int64_t n, int64_t dim, int64_t vocab, int dtype, int w_grad_dtype)
+{
+    if (!entropy_sizes(n, dim, vocab) || !element_type(dtype) || (w_grad_dtype != dtype && w_grad_dtype != SIDCO_GRAD_F32)) return 0;
+    size_t most = 0;
+    for (int which = 1; which <= 3; ++which) {  // a call for one gradient alone takes larger pieces
+        Entropy q = any_entropy(n, dim, vocab, dtype);
+        if (which & 1) q.x_grad = q.x;
+        if (which & 2) q.w_grad = {(void*)1, type_of(w_grad_dtype), dim};
+        const size_t bytes = entropy_grad_scratch(q);
+        most = bytes > most ? bytes : most;
+    }
+    return workspace_with_scratch(most);
+}
+
+int sidco_cross_entropy_grad(void* stream, const void* x, const void* w, int dtype, int64_t n, int64_t dim, int64_t vocab, int64_t ldx,
+                             int64_t ldw, const void* targets, int word_type, const float* lse, const float* loss_grad, void* x_grad,
+                             int64_t ldgx, void* w_grad, int w_grad_dtype, int64_t ldgw, int accumulate)
+{
+    if (!lse || (!x_grad && !w_grad)) return SIDCO_ERR_NULL;
+    if (int rc = check_entropy(x, w, dtype, n, dim, vocab, ldx, ldw, targets, word_type)) return rc;
+    if (!aligned(lse, 4) || !aligned(loss_grad, 4)) return SIDCO_ERR_ALIGN;
+    if (x_grad)
+        if (int rc = check_matrix(x_grad, dtype, dim, ldgx)) return rc;
+    if (w_grad) {
+        if (int rc = check_matrix(w_grad, w_grad_dtype, dim, ldgw)) return rc;
+        if (w_grad_dtype != dtype && w_grad_dtype != SIDCO_GRAD_F32) return SIDCO_ERR_ARG;
+    }
+    if (!flag(accumulate) || (x_grad && (x_grad == x || x_grad == w || x_grad == w_grad)) || (w_grad && (w_grad == x || w_grad == w)))
+        return SIDCO_ERR_ARG;
+    Entropy q = {};
+    q.words = {targets, word_type == SIDCO_WORD_I64, n, vocab};
+    q.dim = dim;
+    q.x = matrix(x, dtype, ldx);
+    q.w = matrix(w, dtype, ldw);
+    q.lse = (float*)lse;
+    q.loss_grad = loss_grad;
+    if (x_grad) q.x_grad = matrix(x_grad, dtype, ldgx);
+    if (w_grad) q.w_grad = matrix(w_grad, w_grad_dtype, ldgw);
+    q.accumulate = accumulate != 0;
+    StreamScratch ws(stream, entropy_grad_scratch(q));
+    if (ws.rc != SIDCO_OK) return ws.rc;
+    launch_entropy_grad(q, ws.data, (hipStream_t)stream);
     return launched();
 }
 

@@ -33,6 +33,12 @@ struct Rows {
     uint32_t pitch;
 };
 
+// The rows' bytes from one row to the next of either operand, and the lines that are multiplied of each: all of them, or fewer,
+// of a row that goes on.
+struct Span {
+    uint32_t pitch_a, pitch_b, lines;
+};
+
 typedef __attribute__((address_space(3))) char lds_char;
 
 // A block's part of an operand as the loads take it: base address, bytes, raw 32-bit words.
@@ -144,6 +150,14 @@ struct HalfCore {
     }
 };
 
+struct Bf16Core {
+    static constexpr bool kScaled = false;
+    static __device__ __forceinline__ void mul(const v4i& a, const v4i& b, v4f& c, int, int)
+    {
+        asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+    }
+};
+
 struct Mx4Core {
     static constexpr bool kScaled = true;
     static __device__ __forceinline__ void mul(const v4i& a, const v4i& b, v4f& c, int sa, int sb)  // 4: e2m1
@@ -222,26 +236,33 @@ struct Tile {
     }
 
     // The lanes' places in a stage, the same for every tile.
-    __device__ __forceinline__ void aim(uint32_t pitch)
+    __device__ __forceinline__ void aim(const Span& span)
     {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        stages = pitch / kLine;
+        stages = span.lines;
         const int r = lane / 8, c = place(r, lane % 8);  // a load's first row is a multiple of 8
 #pragma unroll
         for (int k = 0; k < kLoadsA + kLoadsB; ++k)
-            src[k] = (uint32_t)(((k < kLoadsA ? k : k - kLoadsA) * kWaves + wave) * kRowsLoad + r) * pitch + c * 16;
+            src[k] = (uint32_t)(((k < kLoadsA ? k : k - kLoadsA) * kWaves + wave) * kRowsLoad + r) * (k < kLoadsA ? span.pitch_a : span.pitch_b) + c * 16;
 #pragma unroll
         for (int k = 0; k < kLoadsS; ++k) {
             const uint32_t at = (uint32_t)(k * kWaves + wave) * kRowsExps;  // row of the tile, B's after A's
-            ssrc[k] = ((at < BM ? at : at - BM) + lane / 2) * (pitch / 16) + lane % 2 * 4;
+            ssrc[k] = ((at < BM ? at : at - BM) + lane / 2) * ((at < BM ? span.pitch_a : span.pitch_b) / 16) + lane % 2 * 4;
         }
+    }
+
+    // A tile may lie behind the last row altogether: none.
+    static __device__ __forceinline__ uint32_t rows_left(uint32_t rows, uint32_t from, uint32_t most)
+    {
+        const uint32_t left = rows > from ? rows - from : 0;
+        return left < most ? left : most;
     }
 
     // The tile whose stages are fetched from now on.  Rows past the operand's end are out of range: zeros come for them.
     __device__ __forceinline__ void take(const Rows& a, const Rows& b, uint32_t m0, uint32_t n0)
     {
-        const uint32_t ra = a.rows - m0 < BM ? a.rows - m0 : BM, rb = b.rows - n0 < BN ? b.rows - n0 : BN;
+        const uint32_t ra = rows_left(a.rows, m0, BM), rb = rows_left(b.rows, n0, BN);
         from_a = resource((const char*)a.data + (size_t)m0 * a.pitch, ra * a.pitch);
         from_b = resource((const char*)b.data + (size_t)n0 * b.pitch, rb * b.pitch);
 #pragma unroll
@@ -347,7 +368,12 @@ struct Tile {
     template <int Terms, class Operands, class Finish>
     __device__ __forceinline__ void run(uint32_t tiles, uint32_t pitch, char* lds, const Operands& operands, const Finish& finish)
     {
-        aim(pitch);
+        run<Terms>(tiles, Span{pitch, pitch, pitch / kLine}, lds, operands, finish);
+    }
+    template <int Terms, class Operands, class Finish>
+    __device__ __forceinline__ void run(uint32_t tiles, const Span& span, char* lds, const Operands& operands, const Finish& finish)
+    {
+        aim(span);
         Sequence coming = {blockIdx.x, 0, 0};  // what is fetched next
         operands(coming.tile, coming.term);
         auto advance = [&] {
@@ -421,6 +447,19 @@ struct Tile {
             asm volatile("" : "+v"(row), "+v"(col));  // addresses of later rows are not kept from here on
 #pragma unroll
             for (int j = 0; j < kNt; ++j) acc[i][j] = f(row + i * 16, col + j * 16, acc[i][j]);
+        }
+    }
+
+    // f(strip, row, column, sums): the strip's number, C's row and the first of the columns of its kNt sums, which are 16
+    // apart; relative to the tile.  f may change the sums.
+    template <class F>
+    __device__ __forceinline__ void strips(const F& f)
+    {
+        uint32_t row = wave / WN * (BM / WM) + (lane & 15), col = wave % WN * (BN / WN) + 4 * (lane >> 4);
+#pragma unroll
+        for (int i = 0; i < kMt; ++i) {
+            asm volatile("" : "+v"(row), "+v"(col));  // addresses of later rows are not kept from here on
+            f(i, row + i * 16, col, acc[i]);
         }
     }
 

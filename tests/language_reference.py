@@ -54,3 +54,70 @@ def embedding_grad(grad, words, vocab, scale):
     np.add.at(total, words[ok], grad[ok])
     np.add.at(size, words[ok], np.abs(grad[ok]))
     return scale * total, abs(scale) * size, np.bincount(words[ok], minlength=vocab)
+
+
+class CrossEntropy:
+    """Losses and gradients of x (n x k), w (v x k) in 64 bits, torch tensors wherever they lie, and how far from them results may
+    be whose operands and sums are those that the calls document.
+
+    u = 2^-24 is a rounding to 32 bits.  A logit is a sum of k products in 32 bits, off by at most (k + 16) u times the sum of
+    their magnitudes; fp32 operands as pairs of halves miss 2^-22 of each factor and the product of what the first halves
+    leave, 2^-22 again, and below the halves' range 2^-40 of the largest magnitude.  exp and log are those of powers of two, of
+    an argument rounded to 32 bits twice.  P is rounded once to what it is stored in."""
+
+    def __init__(self, x, w, words, g=None):
+        import torch
+        f32 = x.dtype is torch.float32
+        self.type, self.words, self.u = x.dtype, words.long(), 2.0**-24
+        self.x, self.w = x.double(), w.double()
+        self.ok = (self.words >= 0) & (self.words < len(w))
+        self.x[~self.ok] = torch.where(torch.isfinite(self.x[~self.ok]), self.x[~self.ok], 0.0)
+        k = x.shape[1]
+        self.l = self.x @ self.w.t()
+        size = self.x.abs() @ self.w.abs().t()
+        self.l_off = ((k + 16) * self.u + (3 * 2.0**-22 if f32 else 0.0)) * size
+        if f32:
+            tops = self.x[self.ok].abs().max() if self.ok.any() else 0.0, self.w.abs().max()
+            self.l_off += 2.0**-40 * (tops[0] * self.w.abs().sum(1)[None] + tops[1] * self.x.abs().sum(1)[:, None])
+        self.lse = torch.logsumexp(self.l, 1)
+        exponent = self.l_off + 4 * self.u * (self.l.abs() + self.lse.abs()[:, None])
+        p = torch.exp(self.l - self.lse[:, None])
+        # the exponentials' errors weighted by what they add, a sum in several steps, the result rounded
+        self.lse_off = (p * torch.expm1(exponent)).sum(1) + 64 * self.u + 2 * self.u * self.lse.abs()
+        at = torch.where(self.ok, self.words, 0)
+        mine, mine_off = self.l.gather(1, at[:, None])[:, 0], exponent.gather(1, at[:, None])[:, 0]
+        self.loss = torch.where(self.ok, self.lse - mine, 0.0)
+        self.loss_off = torch.where(self.ok, self.lse_off + mine_off + 2 * self.u * self.loss.abs(), 0.0)
+        g = torch.where(self.ok, torch.ones_like(self.lse) if g is None else g.double(), 0.0)
+        self.p_off = g.abs()[:, None] * (p * torch.expm1(exponent + self.lse_off[:, None]) + 4 * self.u)
+        p[torch.arange(len(x), device=x.device), at] -= 1
+        self.p, self.g = p * g[:, None], g
+
+    def _gradient(self, p, p_off, other, pairs, out):
+        """p @ other, both in 64 bits, and the bound; pairs: P is a pair of the operands' halves."""
+        import torch
+        f32, bf16 = self.type is torch.float32, self.type is torch.bfloat16
+        step = 2.0**-8 if bf16 else 2.0**-11
+        step = step * step if pairs or f32 else step
+        least = 0.0 if bf16 else 2.0**-39 * float(self.g.abs().max())
+        off = (p_off + p.abs() * step + least) @ other.abs()
+        off = off + ((p.shape[1] + 16) * self.u + (3 * 2.0**-22 if f32 else 0.0)) * (p.abs() @ other.abs())
+        if f32 and other.numel():
+            off = off + 2.0**-40 * other.abs().max() * p.abs().sum(1)[:, None]
+        info = torch.finfo(out)
+        want = p @ other
+        return want, off, info.eps / 2, info.tiny * info.eps / 2
+
+    def x_grad(self):
+        """(value, bound)"""
+        want, off, rel, least = self._gradient(self.p, self.p_off, self.w, False, self.type)
+        return want, off + (want.abs() + off) * rel + least
+
+    def w_grad(self, out, before=None):
+        import torch
+        x = torch.where(self.ok[:, None], self.x, 0.0)
+        want, off, rel, least = self._gradient(self.p.t(), self.p_off.t(), x, out is torch.float32, out)
+        if before is not None:
+            off = off + self.u * (before.double().abs() + want.abs())
+            want = want + before.double()
+        return want, off + (want.abs() + off) * rel + least

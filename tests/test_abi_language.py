@@ -90,6 +90,41 @@ def test_dropout_refusals(lib):
               dict(res=OTHER, ldr=24)])])
 
 
+def test_cross_entropy_refusals(lib):
+    good = dict(stream=None, x=OK, w=OTHER, t=0, n=5, dim=20, vocab=10, ldx=20, ldw=20, words=OK, wt=0, loss=OK, lse=OTHER)
+    both = [(-1, [dict(x=None), dict(w=None), dict(words=None)]),
+            (-2, [dict(n=0), dict(n=2**22 + 1), dict(dim=0), dict(dim=2**21 + 1, ldx=2**22, ldw=2**22), dict(vocab=0), dict(vocab=2**31), dict(ldx=19),
+                  dict(ldw=19), dict(n=2**22, vocab=2**31 - 1), dict(vocab=2**31 - 1, dim=2**13, ldx=2**13, ldw=2**13)]),
+            (-8, [dict(x=C.c_void_p(4098)), dict(t=1, w=C.c_void_p(4097)), dict(words=C.c_void_p(4098)), dict(wt=1, words=C.c_void_p(4100)),
+                  dict(lse=C.c_void_p(4098))]),
+            (-9, [dict(t=3), dict(t=-1), dict(wt=2)])]
+    _refuses(lib.sidco_cross_entropy, good, both + [(-1, [dict(loss=None, lse=None)]), (-8, [dict(loss=C.c_void_p(4098))]), (-9, [dict(lse=OK)])])
+    good = dict(stream=None, x=OK, w=OTHER, t=0, n=5, dim=20, vocab=10, ldx=20, ldw=20, words=OK, wt=0, lse=OK, g=None, dx=C.c_void_p(1 << 14), ldgx=20,
+                dw=C.c_void_p(1 << 15), dt=0, ldgw=20, acc=0)
+    _refuses(lib.sidco_cross_entropy_grad, good, both + [
+        (-1, [dict(lse=None), dict(dx=None, dw=None)]),
+        (-2, [dict(ldgx=19), dict(ldgw=19), dict(ldgw=2**31)]),
+        (-8, [dict(g=C.c_void_p(4098)), dict(dx=C.c_void_p(4098)), dict(dw=C.c_void_p(4098))]),
+        (-9, [dict(dt=2), dict(dt=1), dict(t=1, dt=2), dict(acc=2), dict(dx=OK), dict(dx=OTHER), dict(dw=OK), dict(dw=OTHER), dict(dw=C.c_void_p(1 << 14))])])
+    assert sidco.sidco_workspace_bytes_cross_entropy(0, 5, 5, 0) == 0 and sidco.sidco_workspace_bytes_cross_entropy(5, 5, 5, 3) == 0
+    assert sidco.sidco_workspace_bytes_cross_entropy_grad(5, 5, 5, 1, 2) == 0
+    half = sidco.sidco_workspace_bytes_cross_entropy_grad(700, 1500, 10_000, 1, 1)
+    assert 0 < half < sidco.sidco_workspace_bytes_cross_entropy_grad(700, 1500, 10_000, 1, 0) < sidco.sidco_workspace_bytes_cross_entropy_grad(
+        700, 1500, 10_000, 0, 0)
+
+
+def test_reference_loss_by_hand():
+    torch = pytest.importorskip("torch")
+    x, w = torch.tensor([[0.0, 1.0], [2.0, 0.0], [1.0, 1.0]]), torch.tensor([[math.log(2.0), 0.0], [0.0, math.log(3.0)]])
+    r = ref.CrossEntropy(x, w, torch.tensor([1, 0, -1]), torch.tensor([1.0, 0.5, 1.0]))
+    # logits (0, log 3), (log 4, 0): probabilities 1/4, 3/4 and 4/5, 1/5
+    assert torch.allclose(r.loss, torch.tensor([math.log(4 / 3), math.log(5 / 4), 0.0], dtype=torch.float64), atol=1e-6)
+    p = torch.tensor([[0.25, -0.25], [-0.1, 0.1], [0.0, 0.0]], dtype=torch.float64)
+    assert torch.allclose(r.p, p, atol=1e-6)
+    assert torch.allclose(r.x_grad()[0], p @ w.double(), atol=1e-6) and torch.allclose(r.w_grad(torch.float32)[0], p.t() @ x.double(), atol=1e-6)
+    assert float(r.x_grad()[1].max()) < 1e-5
+
+
 def test_binding_refuses_what_is_no_tensor_of_the_card(lib):
     torch = pytest.importorskip("torch")
     x = torch.zeros(4, 8)
