@@ -3,6 +3,8 @@
 // The gradient adds up the rows of each word.  Places are first sorted by their words, places of the same word in order, so
 // that a word's sum is formed in one order whatever runs when, without atomics: a wave walks along sorted places with the sum
 // of its columns in registers and writes a row when the word changes.
+#include <utility>
+
 #include "sidco_elements.h"
 
 namespace sidco {
@@ -22,22 +24,28 @@ struct Look {
     int lanes;
 };
 
-template <class I, class T, class R>
+// Each: rows that a thread has under way at once.
+template <class I, class T, class R, int Each>
 __global__ __launch_bounds__(kRowBlock) void k_embedding(Look<I, T, R> p)
 {
     const int lane = threadIdx.x & (p.lanes - 1);
-    const int64_t per = kRowBlock / p.lanes, row0 = threadIdx.x / p.lanes;
-    for (int64_t i = (int64_t)blockIdx.x * per + row0; i < p.n; i += (int64_t)gridDim.x * per) {
-        const uint32_t word = word_at<I>(p.words, i, p.vocab);
-        const T* from = p.table + (int64_t)word * p.ldt;
-        R* to = p.rows + i * p.ldr;
-        for (int64_t c = ((int64_t)blockIdx.y * p.lanes + lane) * 8; c < p.cols; c += (int64_t)gridDim.y * p.lanes * 8) {
-            Eight<T> t;
-            Eight<R> r;
-            if (word < p.vocab) t.load(from + c, p.cols - c);
+    const int64_t per = kRowBlock / p.lanes, step = (int64_t)gridDim.x * per;
+    for (int64_t i = (int64_t)blockIdx.x * per + threadIdx.x / p.lanes; i < p.n; i += step * Each) {
+        uint32_t word[Each];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) r.set(k, word < p.vocab ? t.get(k) * p.scale : 0.0f);
-            r.store(to + c, p.cols - c);
+        for (int e = 0; e < Each; ++e) word[e] = i + e * step < p.n ? word_at<I>(p.words, i + e * step, p.vocab) : p.vocab;
+        for (int64_t c = ((int64_t)blockIdx.y * p.lanes + lane) * 8; c < p.cols; c += (int64_t)gridDim.y * p.lanes * 8) {
+            Eight<T> t[Each];
+#pragma unroll
+            for (int e = 0; e < Each; ++e)
+                if (word[e] < p.vocab) t[e].load(p.table + (int64_t)word[e] * p.ldt + c, p.cols - c);
+#pragma unroll
+            for (int e = 0; e < Each; ++e) {
+                Eight<R> r;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) r.set(k, word[e] < p.vocab ? t[e].get(k) * p.scale : 0.0f);
+                if (i + e * step < p.n) r.store(p.rows + (i + e * step) * p.ldr + c, p.cols - c);
+            }
         }
     }
 }
@@ -65,7 +73,14 @@ __global__ __launch_bounds__(256) void k_sort_run(const void* words, int64_t n, 
     const int64_t first = (int64_t)blockIdx.x * kPlaces, run = first / kRun * kRun;
     const int64_t len = n - run < kRun ? n - run : kRun;
     __shared__ __align__(16) uint32_t keys[kRun];
-    for (int64_t j = threadIdx.x; j < kRun; j += 256) keys[j] = j < len ? word_at<I>(words, run + j, vocab) : ~0u;
+    uint32_t own[kRun / 256];
+#pragma unroll
+    for (int k = 0; k < kRun / 256; ++k) {
+        const int j = k * 256 + threadIdx.x;
+        own[k] = j < len ? word_at<I>(words, run + j, vocab) : ~0u;
+    }
+#pragma unroll
+    for (int k = 0; k < kRun / 256; ++k) keys[k * 256 + threadIdx.x] = own[k];
     __syncthreads();
     const int lane = threadIdx.x % kSortLanes, group = threadIdx.x / kSortLanes;
     uint32_t mine[Each], rank[Each];
@@ -76,17 +91,30 @@ __global__ __launch_bounds__(256) void k_sort_run(const void* words, int64_t n, 
         mine[e] = keys[at[e]];
         rank[e] = 0;
     }
+    // chunks of 64: before the block's own the same word counts, behind it not
     const int chunk = (int)(first - run) / 64, chunks = (int)((len + 63) / 64);
     typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-    for (int k = 0; k < chunks; ++k) {
-        const u4 v = *(const u4*)(keys + k * 64 + lane * 4);
+    const u4* list = (const u4*)keys + lane;
+#pragma unroll 4
+    for (int k = 0; k < chunk; ++k) {
+        const u4 v = list[k * 16];
 #pragma unroll
         for (int e = 0; e < Each; ++e)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool before = k < chunk || (k == chunk && k * 64 + lane * 4 + i < at[e]);
-                rank[e] += v[i] < mine[e] || (before && v[i] == mine[e]);
-            }
+            for (int i = 0; i < 4; ++i) rank[e] += v[i] <= mine[e];
+    }
+    const u4 v = list[chunk * 16];
+#pragma unroll
+    for (int e = 0; e < Each; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rank[e] += v[i] < mine[e] || (v[i] == mine[e] && chunk * 64 + lane * 4 + i < at[e]);
+#pragma unroll 4
+    for (int k = chunk + 1; k < chunks; ++k) {
+        const u4 v = list[k * 16];
+#pragma unroll
+        for (int e = 0; e < Each; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) rank[e] += v[i] < mine[e];
     }
 #pragma unroll
     for (int e = 0; e < Each; ++e) {
@@ -99,35 +127,48 @@ __global__ __launch_bounds__(256) void k_sort_run(const void* words, int64_t n, 
     }
 }
 
-// Runs of `len` places, kWays of them to one.  kWays lanes share a place, each searches one run.
-__global__ __launch_bounds__(256) void k_merge(Sorted in, Sorted out, int64_t n, int64_t len)
+// Runs of `len` places, kWays of them to one.  A wave searches four runs at a time for 64 neighbours of one run, whose places
+// there lie close together; eight waves share the runs.
+constexpr int kMergeWaves = 8, kMergeEach = kWays / kMergeWaves;
+__global__ __launch_bounds__(64 * kMergeWaves) void k_merge(Sorted in, Sorted out, int64_t n, int64_t len)
 {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kWays;
-    if (i >= n) return;
-    const int way = threadIdx.x % kWays;
-    const int64_t all = i / (len * kWays) * (len * kWays), own = i / len * len, start = all + way * len;
+    __shared__ uint32_t counts[kMergeWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t first = (int64_t)blockIdx.x * 64, all = first / (len * kWays) * (len * kWays), own = first / len * len;
+    const int64_t i = first + lane < n ? first + lane : n - 1;
     const uint32_t word = in.word[i];
-    uint32_t before = 0;
-    if (start == own) {
-        before = (uint32_t)(i - own);
-    } else if (start < n) {
-        // places of that run which come first: smaller words, and of runs before this one's the same word too
-        const uint32_t up = start < own ? 1 : 0;
-        int64_t lo = 0, hi = n - start < len ? n - start : len;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) / 2;
-            if (in.word[start + mid] < word + up)
-                lo = mid + 1;
-            else
-                hi = mid;
-        }
-        before = (uint32_t)lo;
-    }
+    // places of each run which come first: smaller words, and of runs before this one's the same word too
+    const uint32_t* run[kMergeEach];
+    uint32_t count[kMergeEach], below[kMergeEach], before[kMergeEach];
 #pragma unroll
-    for (int s = kWays / 2; s > 0; s >>= 1) before += __shfl_xor(before, s);
-    if (way == 0) {
-        out.word[all + before] = word;
-        out.place[all + before] = in.place[i];
+    for (int k = 0; k < kMergeEach; ++k) {
+        const int64_t start = all + (wave * kMergeEach + k) * len, left = n - start;
+        run[k] = in.word + start;
+        count[k] = start == own || left <= 0 ? 0 : (uint32_t)(left < len ? left : len);
+        below[k] = word + (start < own ? 1 : 0);
+        before[k] = 0;
+    }
+    for (uint32_t step = (uint32_t)len; step > 0; step >>= 1) {  // len is a power of two
+        uint32_t seen[kMergeEach];
+#pragma unroll
+        for (int k = 0; k < kMergeEach; ++k) {
+            const uint32_t to = before[k] + step;
+            seen[k] = to <= count[k] ? run[k][to - 1] : ~0u;
+        }
+#pragma unroll
+        for (int k = 0; k < kMergeEach; ++k) before[k] += seen[k] < below[k] ? step : 0;
+    }
+    uint32_t sum = 0;
+#pragma unroll
+    for (int k = 0; k < kMergeEach; ++k) sum += before[k];
+    counts[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && first + lane < n) {
+        uint32_t to = (uint32_t)(i - own);
+#pragma unroll
+        for (int k = 0; k < kMergeWaves; ++k) to += counts[k][lane];
+        out.word[all + to] = word;
+        out.place[all + to] = in.place[i];
     }
 }
 
@@ -135,6 +176,7 @@ __global__ __launch_bounds__(256) void k_merge(Sorted in, Sorted out, int64_t n,
 
 constexpr int kStrip = 512;  // columns of a wave
 constexpr int kFillRows = 16;
+constexpr int kSumBlock = 512;  // threads of a block that adds up or fills rows
 
 template <class G, class T>
 struct Sum {
@@ -167,7 +209,8 @@ template <class G, class T>
 __device__ __forceinline__ void fill_rows(const Sum<G, T>& p, int64_t v0)
 {
     // 16 lanes search for the first sorted place of a word, 16 probes at a time
-    constexpr int kLanes = 256 / kFillRows;
+    constexpr int kLanes = kSumBlock / kFillRows;
+    static_assert(kLanes <= 32 && 64 % kLanes == 0, "a row's lanes are a wave's");
     __shared__ int present[kFillRows];
     const int row = threadIdx.x / kLanes, lane = threadIdx.x % kLanes, shift = threadIdx.x % 64 / kLanes * kLanes;
     const uint32_t word = (uint32_t)(v0 + row);
@@ -175,7 +218,7 @@ __device__ __forceinline__ void fill_rows(const Sum<G, T>& p, int64_t v0)
     while (__any(hi > lo)) {
         const int64_t step = (hi - lo + kLanes - 1) / kLanes, at = lo + lane * step;
         const bool less = at < hi && p.sorted.word[at] < word;
-        const int count = __popc((uint32_t)(__ballot(less) >> shift) & ((1u << kLanes) - 1));  // the first probes
+        const int count = __popc((uint32_t)(__ballot(less) >> shift) & (uint32_t)((1ull << kLanes) - 1));  // the first probes
         if (count == 0) {
             hi = lo;
         } else {
@@ -186,91 +229,181 @@ __device__ __forceinline__ void fill_rows(const Sum<G, T>& p, int64_t v0)
     }
     if (lane == 0) present[row] = lo < p.n && p.sorted.word[lo] == word;
     __syncthreads();
-    for (int r = 0; r < kFillRows && v0 + r < p.vocab; ++r) {
+    typedef typename Eight<T>::part part;
+    constexpr int kPer = Eight<T>::kPer;
+    for (int r = threadIdx.x >> 6; r < kFillRows && v0 + r < p.vocab; r += kSumBlock / 64) {
         if (present[r]) continue;
         T* to = p.table + (v0 + r) * p.ldt;
-        for (int64_t c = threadIdx.x * 8; c < p.cols; c += 256 * 8) {
-            Eight<T> z;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) z.set(k, 0.0f);
-            z.store(to + c, p.cols - c);
-        }
+        const int64_t whole = p.cols / kPer * kPer;
+        const part zeros = {};
+        for (int64_t c = (threadIdx.x & 63) * kPer; c < whole; c += 64 * kPer) *(part*)(to + c) = zeros;
+        if (whole + (threadIdx.x & 63) < p.cols) to[whole + (threadIdx.x & 63)] = (T)0.0f;
     }
 }
 
-// A wave adds up the rows of `chunk` sorted places in one strip of columns.  A word whose places all lie in the chunk is
-// done; the sums of one that began before it or goes on after it are kept for k_join.
+// The sum of `count` rows from sorted place `at` on, in their order; eight of them are read at a time.
 template <class G, class T>
-__global__ __launch_bounds__(256) void k_sum(Sum<G, T> p)
+__device__ __forceinline__ void sum_rows(const Sum<G, T>& p, int64_t at, int64_t count, int64_t c, int64_t left, float (&sum)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+    if (left <= 0) return;
+    for (int64_t i = 0; i < count; i += 8) {
+        Eight<G> g[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i + u < count) g[u].load(p.rows + (int64_t)p.sorted.place[at + i + u] * p.ldr + c, left);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i + u < count) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum[k] += g[u].get(k);
+            }
+    }
+}
+
+// How many sorted places from `at` on, `stride` apart and before `end`, have that word.
+__device__ __forceinline__ int64_t length_of(const uint32_t* word, int64_t at, int64_t stride, int64_t end, uint32_t of)
+{
+    int64_t count = 0;
+    for (;;) {
+        const int64_t i = at + (count + (threadIdx.x & 63)) * stride;
+        const int same = __popcll(__ballot(i < end && word[i] == of));  // sorted: the first of them
+        count += same;
+        if (same < 64) return count;
+    }
+}
+
+// The waves' sums added up in order; the whole is wave 0's.
+__device__ __forceinline__ void join_waves(float (&sum)[8], float (*lds)[64][9])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) lds[wave][lane][k] = sum[k];
+    __syncthreads();
+    if (wave == 0) {
+        for (int w = 1; w < kSumBlock / 64; ++w)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] += lds[w][lane][k];
+    }
+}
+
+// Few places: a wave takes a word whole, from the place at which it begins, and a word of many places is taken by the block's
+// waves together.
+constexpr int kFewPlaces = 16, kAlone = 32;  // of a block, of a wave
+template <class G, class T>
+__global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p)
 {
     if (blockIdx.x >= p.sum_blocks) return fill_rows(p, (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows);
-    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ float lds[kSumBlock / 64][64][9];
+    __shared__ int many[kFewPlaces];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t first = blockIdx.x / p.strips * kFewPlaces, c = blockIdx.x % p.strips * kStrip + (threadIdx.x & 63) * 8, left = p.cols - c;
+    float sum[8];
+    for (int k = wave; k < kFewPlaces; k += kSumBlock / 64) {
+        const int64_t at = first + k;
+        int64_t count = 0;
+        if (at < p.n) {
+            const uint32_t word = p.sorted.word[at];
+            if (word < p.vocab && (at == 0 || p.sorted.word[at - 1] != word)) count = length_of(p.sorted.word, at, 1, p.n, word);
+            if (count > 0 && count <= kAlone) {
+                sum_rows(p, at, count, c, left, sum);
+                if (left > 0) put_row(p.table + (int64_t)word * p.ldt + c, sum, p.scale, p.accumulate, left);
+            }
+        }
+        if ((threadIdx.x & 63) == 0) many[k] = count > kAlone ? (int)count : 0;
+    }
+    __syncthreads();
+    for (int k = 0; k < kFewPlaces; ++k) {
+        if (!many[k]) continue;
+        const int64_t each = (many[k] + kSumBlock / 64 - 1) / (kSumBlock / 64), from = wave * each, rest = many[k] - from;
+        sum_rows(p, first + k + from, rest < each ? rest : each, c, left, sum);
+        join_waves(sum, lds);
+        if (wave == 0 && left > 0) put_row(p.table + (int64_t)p.sorted.word[first + k] * p.ldt + c, sum, p.scale, p.accumulate, left);
+    }
+}
+
+// Many places: a wave adds up the rows of `chunk` sorted ones in one strip of columns.  A word whose places all lie in the chunk
+// is done; the sums of one that began before it or goes on after it are kept for k_join.
+template <class G, class T>
+__global__ __launch_bounds__(kSumBlock) void k_sum(Sum<G, T> p)
+{
+    if (blockIdx.x >= p.sum_blocks) return fill_rows(p, (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows);
+    const int64_t item = (int64_t)blockIdx.x * (kSumBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t chunk = item / p.strips, strip = item % p.strips;
     if (chunk >= p.chunks) return;
     const int64_t from = chunk * p.chunk, to = from + p.chunk < p.n ? from + p.chunk : p.n;
     const int64_t c = strip * kStrip + (threadIdx.x & 63) * 8, left = p.cols - c;
-    const uint32_t before = from > 0 ? p.sorted.word[from - 1] : ~0u, after = to < p.n ? p.sorted.word[to] : ~0u;
+    if (left <= 0) return;
+    const uint32_t before = from > 0 ? p.sorted.word[from - 1] : ~0u;
     float sum[8] = {};
-    uint32_t word = p.sorted.word[from];
-    bool head = word == before;  // the sum began in an earlier chunk
-    for (int64_t at = from; at < to; ++at) {
-        if (word >= p.vocab) break;  // padding comes last
-        const G* row = p.rows + (int64_t)p.sorted.place[at] * p.ldr + c;
-        if (left > 0) {
-            Eight<G> g;
-            g.load(row, left);
+    bool head = p.sorted.word[from] == before;  // the sum began in an earlier chunk
+    for (int64_t base = from; base < to; base += 8) {
+        Eight<G> g[8];
+        uint32_t word[9];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += g.get(k);
-        }
-        const uint32_t next = at + 1 < to ? p.sorted.word[at + 1] : after;
-        if (at + 1 < to && next == word) continue;
-        const bool tail = at + 1 == to && next == word;
-        if (left > 0) {
-            if (head || tail) {
+        for (int u = 0; u < 9; ++u) word[u] = base + u < p.n ? p.sorted.word[base + u] : ~0u;
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (base + u < to && word[u] < p.vocab) g[u].load(p.rows + (int64_t)p.sorted.place[base + u] * p.ldr + c, left);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (base + u >= to || word[u] >= p.vocab) return;  // padding comes last
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] += g[u].get(k);
+            const bool same = word[u + 1] == word[u], last = base + u + 1 == to;
+            if (same && !last) continue;
+            if (head || same) {
                 Eight<float> f;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) f.set(k, sum[k]);
                 f.store(p.partial + (chunk * 2 + (head ? 0 : 1)) * p.cols + c, left);
             } else {
-                put_row(p.table + (int64_t)word * p.ldt + c, sum, p.scale, p.accumulate, left);
+                put_row(p.table + (int64_t)word[u] * p.ldt + c, sum, p.scale, p.accumulate, left);
             }
-        }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
-        word = next;
-        head = false;
+            for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+            head = false;
+        }
     }
 }
 
-// The sums of words whose places lie in several chunks: a wave for each chunk in which one begins and strip.
+// The sums of words whose places lie in several chunks: a block for each strip and chunk in which one begins.
 template <class G, class T>
-__global__ __launch_bounds__(256) void k_join(Sum<G, T> p)
+__global__ __launch_bounds__(kSumBlock) void k_join(Sum<G, T> p)
 {
-    const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t chunk = item / p.strips, strip = item % p.strips;
-    if (chunk + 1 >= p.chunks) return;  // the last one's do not go on
-    const int64_t from = chunk * p.chunk, to = from + p.chunk;
+    const int64_t chunk = blockIdx.x / p.strips, from = chunk * p.chunk, to = from + p.chunk;
     const uint32_t word = p.sorted.word[to - 1];
-    if (word >= p.vocab || p.sorted.word[to] != word) return;              // none goes on
+    if (word >= p.vocab || p.sorted.word[to] != word) return;                                // none goes on
     if (p.sorted.word[from] == word && from > 0 && p.sorted.word[from - 1] == word) return;  // it began before
-    const int64_t c = strip * kStrip + (threadIdx.x & 63) * 8, left = p.cols - c;
-    if (left <= 0) return;
-    float sum[8];
-    Eight<float> f;
-    f.load(p.partial + (chunk * 2 + 1) * p.cols + c, left);
+    __shared__ float lds[kSumBlock / 64][64][9];
+    const int64_t c = blockIdx.x % p.strips * kStrip + (threadIdx.x & 63) * 8, left = p.cols - c;
+    const int64_t count = 1 + length_of(p.sorted.word, to, p.chunk, p.n, word);  // partial sums, of this chunk the second
+    const int64_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), each = (count + kSumBlock / 64 - 1) / (kSumBlock / 64);
+    const int64_t first = wave * each, end = first + each < count ? first + each : count;
+    float sum[8] = {};
+    if (left > 0) {
+        for (int64_t i = first; i < end; i += 4) {
+            Eight<float> f[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum[k] = f.get(k);
-    for (int64_t i = chunk + 1; i < p.chunks && p.sorted.word[i * p.chunk] == word; ++i) {
-        f.load(p.partial + i * 2 * p.cols + c, left);
+            for (int u = 0; u < 4; ++u)
+                if (i + u < end) f[u].load(p.partial + ((chunk + i + u) * 2 + (i + u == 0 ? 1 : 0)) * p.cols + c, left);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum[k] += f.get(k);
+            for (int u = 0; u < 4; ++u)
+                if (i + u < end) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sum[k] += f[u].get(k);
+                }
+        }
     }
-    put_row(p.table + (int64_t)word * p.ldt + c, sum, p.scale, p.accumulate, left);
+    join_waves(sum, lds);
+    if (wave == 0 && left > 0) put_row(p.table + (int64_t)word * p.ldt + c, sum, p.scale, p.accumulate, left);
 }
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-int chunk_of(int64_t n, int64_t cols) { return n * ((cols + kStrip - 1) / kStrip) < 16384 ? 8 : 32; }
+int chunk_of(int64_t n, int64_t cols) { return n * ((cols + kStrip - 1) / kStrip) < 65536 ? 8 : 32; }
 
 // Words and places, twice where they are merged, and the partial sums.
 struct SumLayout {
@@ -279,7 +412,7 @@ struct SumLayout {
     {
         each = up(n * 4, 256);
         const int64_t chunks = (n + chunk_of(n, cols) - 1) / chunk_of(n, cols);
-        partial = up(chunks * 2 * cols * 4, 256);
+        partial = n > kRun ? up(chunks * 2 * cols * 4, 256) : 0;
         total = each * (n > kRun ? 4 : 2) + partial;
     }
 };
@@ -289,7 +422,8 @@ struct SumLayout {
 void launch_embedding(const Lookup& q, hipStream_t s)
 {
     const RowGrid g(q.cols);
-    const int64_t blocks = (q.words.n + g.per - 1) / g.per, across = (q.cols + g.lanes * 8 - 1) / (g.lanes * 8);
+    const bool many = q.words.n / g.per >= 8192;  // blocks enough for four rows each
+    const int64_t blocks = (q.words.n + g.per * (many ? 4 : 1) - 1) / (g.per * (many ? 4 : 1)), across = (q.cols + g.lanes * 8 - 1) / (g.lanes * 8);
     const dim3 grid((uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20), (uint32_t)(across < 65535 ? across : 65535));
     by_word(q.words, [&](auto i) {
         by_element(q.table.type, [&](auto t) {
@@ -299,7 +433,10 @@ void launch_embedding(const Lookup& q, hipStream_t s)
                 typedef typename decltype(r)::T R;
                 const Look<I, T, R> p = {q.words.at, q.words.n, (uint32_t)q.words.vocab, (const T*)q.table.at, (R*)q.rows.at,
                                          q.table.ld, q.rows.ld, q.cols, q.scale, g.lanes};
-                k_embedding<I, T, R><<<grid, kRowBlock, 0, s>>>(p);
+                if (many)
+                    k_embedding<I, T, R, 4><<<grid, kRowBlock, 0, s>>>(p);
+                else
+                    k_embedding<I, T, R, 1><<<grid, kRowBlock, 0, s>>>(p);
             });
         });
     });
@@ -316,25 +453,32 @@ void launch_embedding_grad(const Lookup& q, char* scratch, hipStream_t s)
     float* partial = (float*)(scratch + l.total - l.partial);
     by_word(q.words, [&](auto i) {
         typedef decltype(i) I;
-        k_sort_run<I, 4><<<(uint32_t)((n + 63) / 64), 256, 0, s>>>(q.words.at, n, (uint32_t)q.words.vocab, now);
+        if (n <= 8192)  // few blocks: less for each
+            k_sort_run<I, 1><<<(uint32_t)((n + 15) / 16), 256, 0, s>>>(q.words.at, n, (uint32_t)q.words.vocab, now);
+        else
+            k_sort_run<I, 4><<<(uint32_t)((n + 63) / 64), 256, 0, s>>>(q.words.at, n, (uint32_t)q.words.vocab, now);
     });
     for (int64_t len = kRun; len < n; len *= kWays) {
-        k_merge<<<(uint32_t)((n + 256 / kWays - 1) / (256 / kWays)), 256, 0, s>>>(now, other, n, len);
-        const Sorted t = now;
-        now = other;
-        other = t;
+        k_merge<<<(uint32_t)((n + 63) / 64), 64 * kMergeWaves, 0, s>>>(now, other, n, len);
+        std::swap(now, other);
     }
     by_element(q.rows.type, [&](auto g) {
         by_element(q.table.type, [&](auto t) {
             typedef typename decltype(g)::T G;
             typedef typename decltype(t)::T T;
-            const int chunk = chunk_of(n, q.cols);
-            const int64_t chunks = (n + chunk - 1) / chunk, strips = (q.cols + kStrip - 1) / kStrip, blocks = (chunks * strips + 3) / 4;
+            const bool few = n <= kRun;
+            const int chunk = few ? kFewPlaces : chunk_of(n, q.cols);
+            const int64_t chunks = (n + chunk - 1) / chunk, strips = (q.cols + kStrip - 1) / kStrip, waves = kSumBlock / 64;
+            const int64_t blocks = few ? chunks * strips : (chunks * strips + waves - 1) / waves;
             const int64_t fill = q.accumulate ? 0 : (q.words.vocab + kFillRows - 1) / kFillRows;
             const Sum<G, T> p = {now, n, (uint32_t)q.words.vocab, (const G*)q.rows.at, (T*)q.table.at, q.rows.ld, q.table.ld, q.cols, strips,
                                  q.scale, q.accumulate, chunk, chunks, partial, blocks};
-            k_sum<G, T><<<(uint32_t)(blocks + fill), 256, 0, s>>>(p);
-            if (chunks > 1) k_join<G, T><<<(uint32_t)blocks, 256, 0, s>>>(p);
+            if (few) {
+                k_sum_few<G, T><<<(uint32_t)(blocks + fill), kSumBlock, 0, s>>>(p);
+                return;
+            }
+            k_sum<G, T><<<(uint32_t)(blocks + fill), kSumBlock, 0, s>>>(p);
+            k_join<G, T><<<(uint32_t)((chunks - 1) * strips), kSumBlock, 0, s>>>(p);
         });
     });
 }

@@ -17,6 +17,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "sidco_elements.h"
 #include "sidco_product.h"
@@ -228,6 +229,14 @@ __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M
 
 // ---- the products ----
 
+// The largest of three; a NaN among them is left out.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "v"(c));
+    return d;
+}
+
 // Terms of a product of pairs and single numbers, the small ones first.
 template <int Terms, class Tl, class H>
 __device__ __forceinline__ void take(Tl& t, int term, const Plane<H>& a, int64_t rows_a, const Plane<H>& b, int64_t rows_b, int64_t col, uint32_t m0,
@@ -257,7 +266,7 @@ struct Places {
 template <class H>
 struct Forward {
     Plane<H> x, w;
-    int64_t n, vocab;
+    uint32_t n;      // rows; w has the vocabulary's
     WordList words;  // of these rows
     float2* part;
     uint32_t width;
@@ -270,80 +279,230 @@ __global__ __launch_bounds__(Tl::kThreads) void k_logits(Forward<typename M::H> 
 {
     __shared__ __align__(1024) char lds[Tl::kLds];
     Tl t;
-    t.template run<M::kPairs ? 3 : 1>(
+    t.template run<M::kPairs ? 3 : 1, true>(
         places.total, span, lds,
         [&](uint32_t tile, int term) {
             uint32_t i, j, split;
             places.at(tile, i, j, split);
-            take<M::kPairs ? 3 : 1>(t, term, p.x, p.n, p.w, p.vocab, 0, i * Tl::kM, j * Tl::kN);
+            take<M::kPairs ? 3 : 1>(t, term, p.x, p.n, p.w, p.words.vocab, 0, i * Tl::kM, j * Tl::kN);
         },
         [&](uint32_t tile) {
             uint32_t ti, tj, split;
             places.at(tile, ti, tj, split);
             const uint32_t m0 = ti * Tl::kM, n0 = tj * Tl::kN;
             const float k = M::kPairs ? kLog2e / (p.scales->x * p.scales->w) : kLog2e;
-            const bool edge = n0 + Tl::kN > p.vocab;
+            const bool edge = n0 + Tl::kN > p.words.vocab;
             const uint32_t place = tj * (Tl::kN / (Tl::kNt * 16)) + t.wave % (Tl::kN / (Tl::kNt * 16));
             t.strips([&](int, uint32_t row, uint32_t col, v4f(&acc)[Tl::kNt]) {
-                const uint32_t r = m0 + row;
-                const uint32_t word = r < p.n ? p.words[r] : p.words.vocab;
+                const uint32_t r = m0 + row, left = p.words.vocab - n0 - col;  // a word's columns, wrapped around if there are none
+                const uint32_t here = (r < p.n ? p.words[r] : p.words.vocab) - n0 - col;
+                if (edge) {
+#pragma unroll
+                    for (int j = 0; j < Tl::kNt; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[j][e] = (int)left > j * 16 + e ? acc[j][e] : -INFINITY;
+                }
                 float top = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < Tl::kNt; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (edge && n0 + col + j * 16 + e >= p.vocab) acc[j][e] = -INFINITY;
-                        acc[j][e] *= k;
-                        top = fmaxf(top, acc[j][e]);
-                    }
+                for (int j = 0; j < Tl::kNt; ++j) top = max3(max3(top, acc[j][0], acc[j][1]), acc[j][2], acc[j][3]);
+                top *= k;  // k > 0
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 top = fminf(fmaxf(top, -kFar), kFar);
                 float sum = 0.0f;
 #pragma unroll
-                for (int j = 0; j < Tl::kNt; ++j) {
+                for (int j = 0; j < Tl::kNt; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (word == n0 + col + j * 16 + e && word < p.words.vocab) p.mine[r] = acc[j][e];
-                        sum += __builtin_amdgcn_exp2f(acc[j][e] - top);
-                    }
-                }
+                    for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[j][e], k, -top));
                 sum += __shfl_xor(sum, 16);
                 sum += __shfl_xor(sum, 32);
                 if (t.lane < 16 && r < p.n) p.part[(int64_t)r * p.width + place] = make_float2(top, sum);
+                // of 128 columns one lane has the row's word, or none
+                if (here < Tl::kNt * 16 && here % 16 < 4 && here < left) {
+                    float mine = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < Tl::kNt; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) mine = here == (uint32_t)(j * 16 + e) ? acc[j][e] : mine;
+                    p.mine[r] = mine * k;
+                }
             });
         });
 }
 
-// A wave joins a row's pairs.  An infinite largest logit has made the sum infinite, a NaN among them a NaN.
+// ---- few rows ----
+//
+// Up to 32 rows read each word's weight once and do little with it: bound by memory.  Blocks of eight waves take 16 words after
+// 16 words; the waves share the contraction, each keeps its part of x in registers, and the next words' loads go out as soon
+// as the ones before are multiplied.  Operands are multiplied as they are, fp32 ones by fp32 instructions.
+constexpr int kFewWaves = 8, kFewRows = 32;
+
+template <class T>
+struct FewCore;
+template <>
+struct FewCore<float> {
+    typedef float piece __attribute__((ext_vector_type(4), aligned(4)));
+    static constexpr int kStep = 16;  // elements of a step of a wave: four lanes' pieces
+    static __device__ __forceinline__ v4f mul(const piece& a, const piece& b, v4f c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+};
+template <>
+struct FewCore<_Float16> {
+    typedef _Float16 piece __attribute__((ext_vector_type(8), aligned(2)));
+    static constexpr int kStep = 32;
+    static __device__ __forceinline__ v4f mul(const piece& a, const piece& b, const v4f& c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16((v8h)a, (v8h)b, c, 0, 0, 0);
+    }
+};
+template <>
+struct FewCore<__bf16> {
+    typedef __bf16 piece __attribute__((ext_vector_type(8), aligned(2)));
+    typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+    static constexpr int kStep = 32;
+    static __device__ __forceinline__ v4f mul(const piece& a, const piece& b, const v4f& c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16((v8b)a, (v8b)b, c, 0, 0, 0);
+    }
+};
+
+template <class T>
+struct Few {
+    const T *x, *w;
+    int64_t ldx, ldw;
+    uint32_t n, dim, groups;
+    WordList words;
+    float2* part;  // a pair for each row and block
+    float* mine;
+};
+
+// Steps: of the contraction, 8 kStep elements each; Tiles: of 16 rows.
+template <class T, int Steps, int Tiles>
+__global__ __launch_bounds__(64 * kFewWaves) void k_few(Few<T> p)
+{
+    typedef FewCore<T> Core;
+    typedef typename Core::piece piece;
+    constexpr uint32_t kPiece = Core::kStep / 4, kAll = kFewWaves * Core::kStep;
+    __shared__ v4f sums[2][kFewWaves][Tiles][64];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
+    const uint32_t at = wave * Core::kStep + q * kPiece;
+    auto load = [&](const T* row, int s) -> piece {
+        const uint32_t k = s * kAll + at;
+        if ((s + 1) * kAll <= p.dim) return *(const piece*)(row + k);
+        piece v;
+        if (k + kPiece <= p.dim) {
+            v = *(const piece*)(row + k);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < kPiece; ++i) v[i] = k + i < p.dim ? row[k + i] : (T)0.0f;
+        }
+        return v;
+    };
+    auto row_of = [&](uint32_t group) -> const T* {
+        const uint32_t v = group * 16 + r;
+        return p.w + (int64_t)(v < p.words.vocab ? v : p.words.vocab - 1) * p.ldw;
+    };
+    piece x[Tiles][Steps], w[Steps];
+    const T* row = row_of(blockIdx.x);
+#pragma unroll
+    for (int s = 0; s < Steps; ++s) w[s] = load(row, s);
+#pragma unroll
+    for (int t = 0; t < Tiles; ++t) {
+        const T* from = p.x + (int64_t)(t * 16 + r < p.n ? t * 16 + r : 0) * p.ldx;
+#pragma unroll
+        for (int s = 0; s < Steps; ++s) x[t][s] = load(from, s);
+    }
+    const uint32_t mine = wave * 16 + r;  // the row whose sums this lane joins, if its wave is one of the first
+    const uint32_t word = wave < Tiles && mine < p.n ? p.words[mine] : p.words.vocab;
+    float top = -kFar, sum = 0.0f;
+    uint32_t turn = 0;
+    for (uint32_t group = blockIdx.x; group < p.groups; group += gridDim.x, turn ^= 1) {
+        row = row_of(group + gridDim.x < p.groups ? group + gridDim.x : group);
+        v4f acc[Tiles];
+#pragma unroll
+        for (int t = 0; t < Tiles; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int s = 0; s < Steps; ++s) {
+#pragma unroll
+            for (int t = 0; t < Tiles; ++t) acc[t] = Core::mul(w[s], x[t][s], acc[t]);
+            w[s] = load(row, s);
+        }
+#pragma unroll
+        for (int t = 0; t < Tiles; ++t) sums[turn][wave][t][lane] = acc[t];
+        __syncthreads();
+        if (wave < Tiles) {
+            v4f l = sums[turn][0][wave][lane];
+#pragma unroll
+            for (int k = 1; k < kFewWaves; ++k) l += sums[turn][k][wave][lane];
+            l *= kLog2e;
+            const uint32_t v = group * 16 + 4 * q;
+            float most = top;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                l[e] = v + e < p.words.vocab ? l[e] : -INFINITY;
+                most = fmaxf(most, l[e]);
+                if (word == v + e && word < p.words.vocab) p.mine[mine] = l[e];
+            }
+            most = fminf(most, kFar);
+            sum *= __builtin_amdgcn_exp2f(top - most);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(l[e] - most);
+            top = most;
+        }
+    }
+    if (wave >= Tiles) return;
+#pragma unroll
+    for (int s = 16; s <= 32; s *= 2) {
+        const float other = __shfl_xor(top, s), more = __shfl_xor(sum, s), next = fmaxf(top, other);
+        sum = sum * __builtin_amdgcn_exp2f(top - next) + more * __builtin_amdgcn_exp2f(other - next);
+        top = next;
+    }
+    if (q == 0 && mine < p.n) p.part[(int64_t)mine * gridDim.x + blockIdx.x] = make_float2(top, sum);
+}
+
+// A row's pairs joined by Lanes threads.  An infinite largest logit has made the sum infinite, a NaN among them a NaN.
+template <int Lanes>
 __global__ __launch_bounds__(256) void k_join_rows(const float2* part, uint32_t width, int64_t n, WordList words, const float* mine, float* loss,
                                                    float* lse)
 {
-    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (r >= n) return;
-    const int lane = threadIdx.x & 63;
+    const int64_t r = (int64_t)blockIdx.x * (256 / Lanes) + threadIdx.x / Lanes;
+    const uint32_t lane = threadIdx.x % Lanes;
     float top = -kFar, sum = 0.0f;
-    for (uint32_t i = lane; i < width; i += 64) {
-        const float2 v = part[r * width + i];
-        const float next = fmaxf(top, v.x);
-        sum = sum * __builtin_amdgcn_exp2f(top - next) + v.y * __builtin_amdgcn_exp2f(v.x - next);
-        top = next;
+    if (r < n) {
+#pragma unroll 4
+        for (uint32_t i = lane; i < width; i += Lanes) {
+            const float2 v = part[r * width + i];
+            const float next = fmaxf(top, v.x);
+            sum = sum * __builtin_amdgcn_exp2f(top - next) + v.y * __builtin_amdgcn_exp2f(v.x - next);
+            top = next;
+        }
     }
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) {
         const float other = __shfl_xor(top, s), more = __shfl_xor(sum, s), next = fmaxf(top, other);
-        // the larger index second, so that both lanes round alike
-        const float a = sum * __builtin_amdgcn_exp2f(top - next), b = more * __builtin_amdgcn_exp2f(other - next);
-        sum = a + b;
+        sum = sum * __builtin_amdgcn_exp2f(top - next) + more * __builtin_amdgcn_exp2f(other - next);
         top = next;
     }
-    if (lane == 0) {
-        const double all = (double)top + (double)log2f(sum);
-        const float l = (float)(all * kLn2);
-        if (lse) lse[r] = l;
-        if (loss) {
-            loss[r] = words.none(r) ? 0.0f : (float)((all - (double)mine[r]) * kLn2);
+    if constexpr (Lanes == 256) {
+        __shared__ float2 lds[4];
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(top, sum);
+        __syncthreads();
+        top = -kFar, sum = 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            const float2 v = lds[i];
+            const float next = fmaxf(top, v.x);
+            sum = sum * __builtin_amdgcn_exp2f(top - next) + v.y * __builtin_amdgcn_exp2f(v.x - next);
+            top = next;
         }
+    }
+    if (lane == 0 && r < n) {
+        const double all = (double)top + (double)log2f(sum);
+        if (lse) lse[r] = (float)(all * kLn2);
+        if (loss) loss[r] = words.none(r) ? 0.0f : (float)((all - (double)mine[r]) * kLn2);
     }
 }
 
@@ -351,22 +510,20 @@ __global__ __launch_bounds__(256) void k_join_rows(const float2* part, uint32_t 
 template <class H>
 struct Probs {
     Plane<H> x, w;  // w: the piece's rows
-    int64_t n, count;
-    uint32_t first;
+    uint32_t n, count, first;
     WordList words;
     const float *lse, *loss_grad;
     Plane<H> out, turned;  // n rows of words, words of n rows; either may have no address
     const Scales* scales;
 };
 
-template <class M, class Tl>
+template <class M, bool Low, class Tl>
 __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, Span span, Places places)
 {
     typedef typename M::H H;
-    typedef H h8 __attribute__((ext_vector_type(8)));
     __shared__ __align__(1024) char lds[lds_of<Tl, H>()];
     Tl t;
-    t.template run<M::kPairs ? 3 : 1>(
+    t.template run<M::kPairs ? 3 : 1, true>(
         places.total, span, lds,
         [&](uint32_t tile, int term) {
             uint32_t i, j, split;
@@ -378,7 +535,9 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
             places.at(tile, ti, tj, split);
             const uint32_t m0 = ti * Tl::kM, n0 = tj * Tl::kN;
             const float k = M::kPairs ? kLog2e / (p.scales->x * p.scales->w) : kLog2e, sp = M::kScaled ? p.scales->p : 1.0f;
-            t.strips([&](int, uint32_t row, uint32_t col, v4f(&acc)[Tl::kNt]) {
+            const bool edge = n0 + Tl::kN > p.count;
+            Four16 high[Tl::kMt][Tl::kNt], low[Low ? Tl::kMt : 1][Tl::kNt];  // in 16 bits P takes half the room of the sums
+            t.strips([&](int i, uint32_t row, uint32_t col, v4f(&acc)[Tl::kNt]) {
                 const uint32_t r = m0 + row;
                 uint32_t word = p.words.vocab;
                 float lse = 0.0f, gain = 0.0f;
@@ -392,43 +551,55 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
 #pragma unroll
                 for (int j = 0; j < Tl::kNt; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float q = __builtin_amdgcn_exp2f(fmaf(acc[j][e], k, lse)) - (here == (uint32_t)(j * 16 + e) ? 1.0f : 0.0f);
-                        acc[j][e] = none ? 0.0f : q * gain;
-                    }
-                // P goes back where the sums were
+                    for (int e = 0; e < 4; ++e) acc[j][e] = __builtin_amdgcn_exp2f(fmaf(acc[j][e], k, lse));
+                if (here < Tl::kNt * 16) {  // one lane in 128 columns, if any
 #pragma unroll
-                for (int j = 0; j < Tl::kNt; ++j) asm volatile("" : "+a"(acc[j]));
-            });
-            // eight neighbours of row r from column c on; columns behind the last are zeros up to the pitch
-            auto put = [](const Plane<H>& o, int64_t rows, int64_t cols, bool low) {
-                return [&o, rows, cols, low](uint32_t r, uint32_t c, h8 v) {
-                    if (r >= rows || c >= o.pitch) return;
-                    if (c + 8 > cols) {
+                    for (int j = 0; j < Tl::kNt; ++j)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? v[i] : (H)0.0f;
-                    }
-                    *(h8*)(o.at + (low ? o.low : 0) + (int64_t)r * o.pitch + c) = v;
+                        for (int e = 0; e < 4; ++e) acc[j][e] -= here == (uint32_t)(j * 16 + e) ? 1.0f : 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < Tl::kNt; ++j) acc[j] *= gain;
+                if (edge) {  // zeros behind the piece's last word
+                    const int left = (int)(p.count - n0 - col);
+#pragma unroll
+                    for (int j = 0; j < Tl::kNt; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[j][e] = left > j * 16 + e ? acc[j][e] : 0.0f;
+                }
+                auto packed = [&](const v4f& v) -> Four16 {
+                    typedef H h2 __attribute__((ext_vector_type(2)));
+                    const uint32_t a = __builtin_bit_cast(uint32_t, h2{(H)v[0], (H)v[1]}), b = __builtin_bit_cast(uint32_t, h2{(H)v[2], (H)v[3]});
+                    return {none ? 0 : a, none ? 0 : b};
                 };
-            };
-            auto whole = [](uint32_t, uint32_t, const v4f& v) -> v4f { return v; };
-            auto rest = [](uint32_t, uint32_t, const v4f& v) -> v4f {
-                const v4f w = rounded(v);
-                v4f l;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) l[i] = w[i] - (float)(H)w[i];
-                return l;
+                for (int j = 0; j < Tl::kNt; ++j) {
+                    const v4f v = rounded(acc[j]);
+                    high[i][j] = packed(v);
+                    if constexpr (Low) {
+                        v4f l;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) l[e] = v[e] - (float)(H)v[e];
+                        low[i][j] = packed(l);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            // Eight neighbours of row r from column c on; columns behind the last are zeros up to the pitch.
+            auto put = [](const Plane<H>& o, uint32_t rows, uint32_t m, uint32_t n, bool low) {
+                H* at = o.at + (low ? o.low : 0);
+                return [at, pitch = o.pitch, rows, m, n](uint32_t r, uint32_t c, const v4i& v) {
+                    if (m + r < rows && n + c < (uint32_t)pitch) *(v4i*)(at + (int64_t)(m + r) * pitch + (n + c)) = v;
+                };
             };
             char* by = lds + Tl::kLds;
             if (p.out.at) {
-                const auto high = put(p.out, p.n, p.count, false), low = put(p.out, p.n, p.count, true);
-                t.template out<H, false>(by, whole, [&](uint32_t r, uint32_t c, const h8& v) { high(m0 + r, n0 + c, v); });
-                if (M::kPairs) t.template out<H, false>(by, rest, [&](uint32_t r, uint32_t c, const h8& v) { low(m0 + r, n0 + c, v); });
+                t.template out16<false>(by, high, put(p.out, p.n, m0, n0, false));
+                if constexpr (M::kPairs) t.template out16<false>(by, low, put(p.out, p.n, m0, n0, true));
             }
             if (p.turned.at) {
-                const auto high = put(p.turned, p.count, p.n, false), low = put(p.turned, p.count, p.n, true);
-                t.template out<H, true>(by, whole, [&](uint32_t r, uint32_t c, const h8& v) { high(n0 + r, m0 + c, v); });
-                if (M::kPairs || p.turned.low) t.template out<H, true>(by, rest, [&](uint32_t r, uint32_t c, const h8& v) { low(n0 + r, m0 + c, v); });
+                t.template out16<true>(by, high, put(p.turned, p.count, n0, m0, false));
+                if constexpr (Low) t.template out16<true>(by, low, put(p.turned, p.count, n0, m0, true));
             }
         });
 }
@@ -586,11 +757,32 @@ int forward_tile(int64_t rows, int64_t vocab, int64_t lines)
 }
 int64_t forward_width(int pick, int64_t vocab) { return 2 * parts(vocab, kTileCosts[pick].side); }
 
+// Whether few rows have a kernel of their own, the steps that it takes, and its blocks.
+constexpr int64_t kFewBlocks = 512;
+template <class M>
+int64_t few_steps(int64_t rows, int64_t dim)
+{
+    return rows <= kFewRows ? parts(dim, kFewWaves * FewCore<typename M::T>::kStep) : 1 << 30;
+}
+template <class M>
+bool takes_few(int64_t rows, int64_t dim)
+{
+    return few_steps<M>(rows, dim) <= 16;
+}
+
+void join_rows(const float2* pairs, uint32_t width, int64_t rows, const WordList& words, const float* mine, float* loss, float* lse, hipStream_t s)
+{
+    if (width >= 512 && rows <= 4096)
+        k_join_rows<256><<<(uint32_t)rows, 256, 0, s>>>(pairs, width, rows, words, mine, loss, lse);
+    else
+        k_join_rows<64><<<(uint32_t)parts(rows, 4), 256, 0, s>>>(pairs, width, rows, words, mine, loss, lse);
+}
+
 template <class M>
 struct ForwardPlan {
     typedef typename M::H H;
     int64_t pitch;
-    bool lay_x, lay_w;
+    bool few, lay_x, lay_w;
     float* part;
     Scales* scales;
     Plane<H> x, w;
@@ -602,14 +794,15 @@ struct ForwardPlan {
         Space s = {scratch, 0};
         const int64_t n = q.words.n, v = q.words.vocab, at_once = std::min(n, kRowsAtOnce);
         pitch = up(q.dim, kPer<M>);
-        lay_x = !lies_in_lines<M>(q.x, q.dim);
-        lay_w = !lies_in_lines<M>(q.w, q.dim);
+        few = takes_few<M>(n, q.dim);
+        lay_x = !few && !lies_in_lines<M>(q.x, q.dim);
+        lay_w = !few && !lies_in_lines<M>(q.w, q.dim);
         scales = s.get<Scales>(1);
         part = s.get<float>(M::kPairs ? 3 * kParts : 0);
         x = lay_x ? s.plane<H>(n, pitch, M::kPairs) : Plane<H>{(H*)q.x.at, q.x.ld, 0};
         w = lay_w ? s.plane<H>(v, pitch, M::kPairs) : Plane<H>{(H*)q.w.at, q.w.ld, 0};
         auto pairs_of = [&](int64_t rows) { return rows * forward_width(forward_tile<M>(rows, v, pitch / kPer<M>), v); };
-        pairs = s.get<float2>(std::max(pairs_of(at_once), pairs_of((n - 1) % kRowsAtOnce + 1)));
+        pairs = s.get<float2>(few ? n * kFewBlocks : std::max(pairs_of(at_once), pairs_of((n - 1) % kRowsAtOnce + 1)));
         mine = s.get<float>(at_once);
         bytes = s.used;
     }
@@ -635,6 +828,30 @@ void forward(const Entropy& q, char* scratch, hipStream_t s)
     typedef typename M::H H;
     const ForwardPlan<M> f(q, scratch);
     const int64_t n = q.words.n, v = q.words.vocab;
+    if (f.few) {
+        const int64_t groups = parts(v, 16), blocks = std::min(groups, kFewBlocks), steps = few_steps<M>(n, q.dim);
+        const Few<T> p = {(const T*)q.x.at, (const T*)q.w.at, q.x.ld, q.w.ld, (uint32_t)n, (uint32_t)q.dim, (uint32_t)groups, list(q.words), f.pairs, f.mine};
+        auto go = [&](auto kernel) { kernel<<<(uint32_t)blocks, 64 * kFewWaves, 0, s>>>(p); };
+        auto by_steps = [&](auto tiles) {
+            constexpr int kTiles = decltype(tiles)::value;
+            if (steps <= 2)
+                go(k_few<T, 2, kTiles>);
+            else if (steps <= 4)
+                go(k_few<T, 4, kTiles>);
+            else if (steps <= 8)
+                go(k_few<T, 8, kTiles>);
+            else if (steps <= 12)
+                go(k_few<T, 12, kTiles>);
+            else
+                go(k_few<T, 16, kTiles>);
+        };
+        if (n <= 16)
+            by_steps(std::integral_constant<int, 1>());
+        else
+            by_steps(std::integral_constant<int, 2>());
+        join_rows(f.pairs, (uint32_t)blocks, n, list(q.words), f.mine, q.loss, q.lse, s);
+        return;
+    }
     if (M::kPairs) tops<M>(q, true, false, f.part, s);
     if (f.lay_x || f.lay_w) {
         const uint32_t across = (uint32_t)parts(f.pitch, 64);
@@ -652,11 +869,10 @@ void forward(const Entropy& q, char* scratch, hipStream_t s)
             typedef typename decltype(shape)::Is Tl;
             const Places places = {(uint32_t)parts(rows, Tl::kM), (uint32_t)parts(v, Tl::kN), (uint32_t)(parts(rows, Tl::kM) * parts(v, Tl::kN))};
             const Plane<H> x = {f.x.at + r * f.x.pitch, f.x.pitch, f.x.low};
-            const Forward<H> p = {x, f.w, rows, v, words, f.pairs, width, f.mine, f.scales};
+            const Forward<H> p = {x, f.w, (uint32_t)rows, words, f.pairs, width, f.mine, f.scales};
             k_logits<M, Tl><<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places);
         });
-        k_join_rows<<<(uint32_t)parts(rows, 4), 256, 0, s>>>(f.pairs, width, rows, words, f.mine, q.loss ? q.loss + r : nullptr,
-                                                            q.lse ? q.lse + r : nullptr);
+        join_rows(f.pairs, width, rows, words, f.mine, q.loss ? q.loss + r : nullptr, q.lse ? q.lse + r : nullptr, s);
     }
 }
 
@@ -763,8 +979,14 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
             typedef typename decltype(shape)::Is Tl;
             const uint32_t tm = (uint32_t)parts(n, Tl::kM), tn = (uint32_t)parts(wide, Tl::kN);
             const Places places = {tm, tn, tm * tn};
-            const Probs<H> p = {g.x, w, n, count, (uint32_t)first, words, q.lse, q.loss_grad, g.p, g.pt, g.scales};
-            k_probs<M, Tl><<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places);
+            const Probs<H> p = {g.x, w, (uint32_t)n, (uint32_t)count, (uint32_t)first, words, q.lse, q.loss_grad, g.p, g.pt, g.scales};
+            auto go = [&](auto kernel) { kernel<<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places); };
+            if constexpr (M::kPairs)
+                go(k_probs<M, true, Tl>);
+            else if (g.wide)
+                go(k_probs<M, true, Tl>);
+            else
+                go(k_probs<M, false, Tl>);
         });
         const Scales* scales = M::kScaled ? g.scales : nullptr;
         if (q.x_grad.at) {

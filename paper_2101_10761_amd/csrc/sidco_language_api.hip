@@ -85,6 +85,7 @@ int sidco_embedding_grad(void* stream, const void* grad, int grad_dtype, int64_t
     if (int rc = check_words(words, word_type, n, vocab)) return rc;
     if (int rc = check_matrix(grad, grad_dtype, dim, ldg)) return rc;
     if (int rc = check_matrix(table_grad, table_dtype, dim, ldt)) return rc;
+    if ((n + 31) / 32 * ((dim + 511) / 512) > (int64_t)INT32_MAX / 2) return SIDCO_ERR_SIZE;  // a block's number has 31 bits
     if (!isfinite(scale) || !flag(accumulate) || grad == table_grad) return SIDCO_ERR_ARG;
     StreamScratch ws(stream, embedding_grad_scratch(n, dim));
     if (ws.rc != SIDCO_OK) return ws.rc;

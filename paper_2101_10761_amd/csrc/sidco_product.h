@@ -122,6 +122,21 @@ __device__ __forceinline__ v4f turned(v4f v)
     return v;
 }
 
+// The same with 16-bit numbers, two to a register.
+struct Four16 {
+    uint32_t a, b;
+};
+__device__ __forceinline__ Four16 turned(Four16 v)
+{
+    auto swap1 = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, true); };
+    auto swap2 = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, true); };
+    const bool upper = threadIdx.x & 2;
+    const uint32_t got = swap2(upper ? v.a : v.b);
+    const uint32_t a = upper ? got : v.a, b = upper ? v.b : got;  // two columns of this row, and of the row two on
+    const uint32_t pick = threadIdx.x & 1 ? 0x03020706 : 0x05040100;
+    return {__builtin_amdgcn_perm(swap1(a), a, pick), __builtin_amdgcn_perm(swap1(b), b, pick)};
+}
+
 // The values as rounded to fp32.  A product rounded to fp32 and then to half is otherwise rounded once, by an instruction that
 // does both, in one place and not in another: the half and what it leaves of the value would belong to different halves.
 __device__ __forceinline__ v4f rounded(v4f v)
@@ -364,13 +379,14 @@ struct Tile {
     //   finish(tile)         is called with the sums
     // While four pieces are multiplied the next four are read from LDS into other registers.  Once every wave has read the last
     // of a stage its place is free, and the stage after it has to be there: one barrier a stage.  The stages of all tiles are
-    // one sequence: the next tile's are under way while this one's sums go out.
+    // one sequence: the next tile's are under way while this one's sums go out.  Long says that a
+    // finish is long beside the loop's code and that its registers are not to be had from the loop's.
     template <int Terms, class Operands, class Finish>
     __device__ __forceinline__ void run(uint32_t tiles, uint32_t pitch, char* lds, const Operands& operands, const Finish& finish)
     {
         run<Terms>(tiles, Span{pitch, pitch, pitch / kLine}, lds, operands, finish);
     }
-    template <int Terms, class Operands, class Finish>
+    template <int Terms, bool Long = false, class Operands, class Finish>
     __device__ __forceinline__ void run(uint32_t tiles, const Span& span, char* lds, const Operands& operands, const Finish& finish)
     {
         aim(span);
@@ -416,7 +432,7 @@ struct Tile {
                 turn(p1, p0, fresh);
                 fresh = 0;
                 asm volatile("" : "+s"(fresh));  // a copy of the loop for its first turn would move the sums
-            } while (++f < Terms * stages);
+            } while (Long ? __builtin_expect_with_probability(++f < Terms * stages, 1, 0.999) : ++f < Terms * stages);
             rest();
             hold();
             finish(tile);
@@ -455,6 +471,8 @@ struct Tile {
     template <class F>
     __device__ __forceinline__ void strips(const F& f)
     {
+        int lane = this->lane;
+        asm volatile("" : "+v"(lane));  // places are not kept from tile to tile
         uint32_t row = wave / WN * (BM / WM) + (lane & 15), col = wave % WN * (BN / WN) + 4 * (lane >> 4);
 #pragma unroll
         for (int i = 0; i < kMt; ++i) {
@@ -473,6 +491,37 @@ struct Tile {
     static constexpr int out_bytes()  // of LDS for each wave, besides the stages
     {
         return 16 * pad((kNt > kMt ? kNt : kMt) * 16 * (int)sizeof(S));
+    }
+
+    // The tile from 16-bit numbers in registers, v[i][j] in the place of acc[i][j]; store(row, column, 16 bytes) as below.
+    template <bool Turn, class Store>
+    __device__ __forceinline__ void out16(char* lds, const Four16 (&v)[kMt][kNt], const Store& store) const
+    {
+        constexpr int kStrips = Turn ? kNt : kMt, kTiles = Turn ? kMt : kNt, kPitch = pad(kTiles * 32), kLanes = kTiles * 2;
+        static_assert(16 * kLanes % 64 == 0, "whole waves");
+        int lane = this->lane;
+        asm volatile("" : "+v"(lane));  // nor are places kept from tile to tile
+        char* mine = lds + wave * out_bytes<_Float16>();
+        const int r = lane & 15, q = lane >> 4;
+        uint32_t row0 = wave / WN * (BM / WM), col0 = wave % WN * (BN / WN);
+#pragma unroll
+        for (int x = 0; x < kStrips; ++x) {
+            asm volatile("" : "+v"(row0), "+v"(col0));  // addresses of later strips are not kept from here on
+#pragma unroll
+            for (int y = 0; y < kTiles; ++y) {
+                if (Turn)
+                    *(Four16*)(mine + (4 * q + (r & 3)) * kPitch + (y * 16 + (r & ~3)) * 2) = turned(v[y][x]);
+                else
+                    *(Four16*)(mine + r * kPitch + (y * 16 + 4 * q) * 2) = v[x][y];
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int k = 0; k < 16 * kLanes / 64; ++k) {
+                const int at = k * 64 + lane, row = at / kLanes, col = at % kLanes * 8;
+                store((uint32_t)((Turn ? col0 : row0) + x * 16 + row), (uint32_t)((Turn ? row0 : col0) + col), *(const v4i*)(mine + row * kPitch + col * 2));
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
     }
 
     // value(row, column, sums) gives the four values of C's row from a column on; store(row, column, 16 bytes of S) takes

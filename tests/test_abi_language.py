@@ -76,6 +76,7 @@ def test_embedding_refusals(lib):
     good = dict(stream=None, grad=OK, t=0, n=5, dim=20, ldo=20, words=OK, wt=0, vocab=10, scale=1.0, acc=0, table=OTHER, ot=0, ldt=20)
     _refuses(lib.sidco_embedding_grad, good, words + [
         (-1, [dict(table=None), dict(grad=None)]),
+        (-2, [dict(n=2**31 - 1, dim=2**20, ldo=2**20, ldt=2**20)]),
         (-8, [dict(grad=C.c_void_p(4098)), dict(ot=1, table=C.c_void_p(4097))]),
         (-9, [dict(acc=2), dict(acc=-1), dict(table=OK)])])
 
