@@ -204,11 +204,26 @@ __device__ __forceinline__ void put_row(T* to, const float (&sum)[8], float scal
     t.store(to, left);
 }
 
-// Zeros for the rows of kFillRows words from v0 on that do not occur.
+// Zeros for those of the kFillRows rows from v0 on that are not present.
 template <class G, class T>
-__device__ __forceinline__ void fill_rows(const Sum<G, T>& p, int64_t v0)
+__device__ __forceinline__ void fill_rows(const Sum<G, T>& p, int64_t v0, const int* present)
 {
-    // 16 lanes search for the first sorted place of a word, 16 probes at a time
+    typedef typename Eight<T>::part part;
+    constexpr int kPer = Eight<T>::kPer;
+    for (int r = threadIdx.x >> 6; r < kFillRows && v0 + r < p.vocab; r += kSumBlock / 64) {
+        if (present[r]) continue;
+        T* to = p.table + (v0 + r) * p.ldt;
+        const int64_t whole = p.cols / kPer * kPer;
+        const part zeros = {};
+        for (int64_t c = (threadIdx.x & 63) * kPer; c < whole; c += 64 * kPer) *(part*)(to + c) = zeros;
+        if (whole + (threadIdx.x & 63) < p.cols) to[whole + (threadIdx.x & 63)] = (T)0.0f;
+    }
+}
+
+// The same, from the sorted places: 32 lanes search for the first place of a word, 32 probes at a time.
+template <class G, class T>
+__device__ __forceinline__ void fill_missing(const Sum<G, T>& p, int64_t v0)
+{
     constexpr int kLanes = kSumBlock / kFillRows;
     static_assert(kLanes <= 32 && 64 % kLanes == 0, "a row's lanes are a wave's");
     __shared__ int present[kFillRows];
@@ -229,30 +244,21 @@ __device__ __forceinline__ void fill_rows(const Sum<G, T>& p, int64_t v0)
     }
     if (lane == 0) present[row] = lo < p.n && p.sorted.word[lo] == word;
     __syncthreads();
-    typedef typename Eight<T>::part part;
-    constexpr int kPer = Eight<T>::kPer;
-    for (int r = threadIdx.x >> 6; r < kFillRows && v0 + r < p.vocab; r += kSumBlock / 64) {
-        if (present[r]) continue;
-        T* to = p.table + (v0 + r) * p.ldt;
-        const int64_t whole = p.cols / kPer * kPer;
-        const part zeros = {};
-        for (int64_t c = (threadIdx.x & 63) * kPer; c < whole; c += 64 * kPer) *(part*)(to + c) = zeros;
-        if (whole + (threadIdx.x & 63) < p.cols) to[whole + (threadIdx.x & 63)] = (T)0.0f;
-    }
+    fill_rows(p, v0, present);
 }
 
-// The sum of `count` rows from sorted place `at` on, in their order; eight of them are read at a time.
+// The sum of the rows at `count` places, in their order; eight of them are read at a time.
 template <class G, class T>
-__device__ __forceinline__ void sum_rows(const Sum<G, T>& p, int64_t at, int64_t count, int64_t c, int64_t left, float (&sum)[8])
+__device__ __forceinline__ void sum_rows(const Sum<G, T>& p, const uint16_t* places, int count, int64_t c, int64_t left, float (&sum)[8])
 {
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
     if (left <= 0) return;
-    for (int64_t i = 0; i < count; i += 8) {
+    for (int i = 0; i < count; i += 8) {
         Eight<G> g[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-            if (i + u < count) g[u].load(p.rows + (int64_t)p.sorted.place[at + i + u] * p.ldr + c, left);
+            if (i + u < count) g[u].load(p.rows + (int64_t)places[i + u] * p.ldr + c, left);
 #pragma unroll
         for (int u = 0; u < 8; ++u)
             if (i + u < count) {
@@ -275,6 +281,7 @@ __device__ __forceinline__ int64_t length_of(const uint32_t* word, int64_t at, i
 }
 
 // The waves' sums added up in order; the whole is wave 0's.
+template <int Waves = kSumBlock / 64>
 __device__ __forceinline__ void join_waves(float (&sum)[8], float (*lds)[64][9])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -283,44 +290,89 @@ __device__ __forceinline__ void join_waves(float (&sum)[8], float (*lds)[64][9])
     for (int k = 0; k < 8; ++k) lds[wave][lane][k] = sum[k];
     __syncthreads();
     if (wave == 0) {
-        for (int w = 1; w < kSumBlock / 64; ++w)
+        for (int w = 1; w < Waves; ++w)
 #pragma unroll
             for (int k = 0; k < 8; ++k) sum[k] += lds[w][lane][k];
     }
 }
 
-// Few places: a wave takes a word whole, from the place at which it begins, and a word of many places is taken by the block's
+// Few places, in one launch and without a workspace: every block has all words in LDS.  A wave looks at a place, and if its word
+// occurs at no place before it, lists the word's places and adds up their rows; a word of many places is taken by the block's
 // waves together.
 constexpr int kFewPlaces = 16, kAlone = 32;  // of a block, of a wave
-template <class G, class T>
-__global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p)
+
+// Places of `word` among n: their number and, in order, the first `room` of them.  -1 where one lies before `at`.
+__device__ __forceinline__ int list_places(const uint32_t* keys, int n, uint32_t word, int at, uint16_t* list, int room)
 {
-    if (blockIdx.x >= p.sum_blocks) return fill_rows(p, (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows);
+    const int lane = threadIdx.x & 63;
+    int count = 0;
+    bool first = true;
+    for (int j = 0; j < n; j += 64) {
+        const uint64_t same = __ballot(j + lane < n && keys[j + lane] == word);
+        first = first && (same == 0 || j + __builtin_ctzll(same) >= at || count > 0);
+        const int to = count + __popcll(same & ((1ull << lane) - 1));
+        if (same >> lane & 1 && to < room) list[to] = (uint16_t)(j + lane);
+        count += __popcll(same);
+    }
+    return first ? count : -1;
+}
+
+template <class I, class G, class T>
+__global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p, const void* words)
+{
+    __shared__ uint32_t keys[kRun];
     __shared__ float lds[kSumBlock / 64][64][9];
+    __shared__ uint16_t list[kSumBlock / 64][kAlone], all[kRun];
     __shared__ int many[kFewPlaces];
+    const int n = (int)p.n;
+    uint32_t own[kRun / kSumBlock];
+#pragma unroll
+    for (int k = 0; k < kRun / kSumBlock; ++k) {
+        const int j = k * kSumBlock + threadIdx.x;
+        own[k] = j < n ? word_at<I>(words, j, p.vocab) : p.vocab;
+    }
+    if (blockIdx.x >= p.sum_blocks) {
+        const int64_t v0 = (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows;
+        if (threadIdx.x < kFillRows) many[threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kRun / kSumBlock; ++k)
+            if (own[k] < p.vocab && own[k] - (uint32_t)v0 < kFillRows) many[own[k] - (uint32_t)v0] = 1;
+        __syncthreads();
+        return fill_rows(p, v0, many);
+    }
+#pragma unroll
+    for (int k = 0; k < kRun / kSumBlock; ++k) keys[k * kSumBlock + threadIdx.x] = own[k];
+    __syncthreads();
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t first = blockIdx.x / p.strips * kFewPlaces, c = blockIdx.x % p.strips * kStrip + (threadIdx.x & 63) * 8, left = p.cols - c;
+    const int first = (int)(blockIdx.x / p.strips) * kFewPlaces;
+    const int64_t c = blockIdx.x % p.strips * kStrip + (threadIdx.x & 63) * 8, left = p.cols - c;
     float sum[8];
     for (int k = wave; k < kFewPlaces; k += kSumBlock / 64) {
-        const int64_t at = first + k;
-        int64_t count = 0;
-        if (at < p.n) {
-            const uint32_t word = p.sorted.word[at];
-            if (word < p.vocab && (at == 0 || p.sorted.word[at - 1] != word)) count = length_of(p.sorted.word, at, 1, p.n, word);
+        const int at = first + k;
+        int count = 0;
+        if (at < n && keys[at] < p.vocab) {
+            const uint32_t word = keys[at];
+            count = list_places(keys, n, word, at, list[wave], kAlone);
+            __builtin_amdgcn_wave_barrier();
             if (count > 0 && count <= kAlone) {
-                sum_rows(p, at, count, c, left, sum);
+                sum_rows(p, list[wave], count, c, left, sum);
                 if (left > 0) put_row(p.table + (int64_t)word * p.ldt + c, sum, p.scale, p.accumulate, left);
             }
         }
-        if ((threadIdx.x & 63) == 0) many[k] = count > kAlone ? (int)count : 0;
+        if ((threadIdx.x & 63) == 0) many[k] = count > kAlone ? count : 0;
     }
     __syncthreads();
     for (int k = 0; k < kFewPlaces; ++k) {
-        if (!many[k]) continue;
-        const int64_t each = (many[k] + kSumBlock / 64 - 1) / (kSumBlock / 64), from = wave * each, rest = many[k] - from;
-        sum_rows(p, first + k + from, rest < each ? rest : each, c, left, sum);
+        const int count = many[k];
+        if (count == 0) continue;
+        const uint32_t word = keys[first + k];
+        if (wave == 0) list_places(keys, n, word, first + k, all, kRun);
+        __syncthreads();
+        const int each = (count + kSumBlock / 64 - 1) / (kSumBlock / 64), from = wave * each, rest = count - from;
+        sum_rows(p, all + from, rest < each ? rest : each, c, left, sum);
         join_waves(sum, lds);
-        if (wave == 0 && left > 0) put_row(p.table + (int64_t)p.sorted.word[first + k] * p.ldt + c, sum, p.scale, p.accumulate, left);
+        if (wave == 0 && left > 0) put_row(p.table + (int64_t)word * p.ldt + c, sum, p.scale, p.accumulate, left);
     }
 }
 
@@ -329,7 +381,7 @@ __global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p)
 template <class G, class T>
 __global__ __launch_bounds__(kSumBlock) void k_sum(Sum<G, T> p)
 {
-    if (blockIdx.x >= p.sum_blocks) return fill_rows(p, (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows);
+    if (blockIdx.x >= p.sum_blocks) return fill_missing(p, (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows);
     const int64_t item = (int64_t)blockIdx.x * (kSumBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t chunk = item / p.strips, strip = item % p.strips;
     if (chunk >= p.chunks) return;
@@ -370,17 +422,18 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sum<G, T> p)
 }
 
 // The sums of words whose places lie in several chunks: a block for each strip and chunk in which one begins.
+constexpr int kJoinWaves = 4;
 template <class G, class T>
-__global__ __launch_bounds__(kSumBlock) void k_join(Sum<G, T> p)
+__global__ __launch_bounds__(64 * kJoinWaves) void k_join(Sum<G, T> p)
 {
     const int64_t chunk = blockIdx.x / p.strips, from = chunk * p.chunk, to = from + p.chunk;
     const uint32_t word = p.sorted.word[to - 1];
     if (word >= p.vocab || p.sorted.word[to] != word) return;                                // none goes on
     if (p.sorted.word[from] == word && from > 0 && p.sorted.word[from - 1] == word) return;  // it began before
-    __shared__ float lds[kSumBlock / 64][64][9];
+    __shared__ float lds[kJoinWaves][64][9];
     const int64_t c = blockIdx.x % p.strips * kStrip + (threadIdx.x & 63) * 8, left = p.cols - c;
     const int64_t count = 1 + length_of(p.sorted.word, to, p.chunk, p.n, word);  // partial sums, of this chunk the second
-    const int64_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), each = (count + kSumBlock / 64 - 1) / (kSumBlock / 64);
+    const int64_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), each = (count + kJoinWaves - 1) / kJoinWaves;
     const int64_t first = wave * each, end = first + each < count ? first + each : count;
     float sum[8] = {};
     if (left > 0) {
@@ -397,7 +450,7 @@ __global__ __launch_bounds__(kSumBlock) void k_join(Sum<G, T> p)
                 }
         }
     }
-    join_waves(sum, lds);
+    join_waves<kJoinWaves>(sum, lds);
     if (wave == 0 && left > 0) put_row(p.table + (int64_t)word * p.ldt + c, sum, p.scale, p.accumulate, left);
 }
 
@@ -412,8 +465,8 @@ struct SumLayout {
     {
         each = up(n * 4, 256);
         const int64_t chunks = (n + chunk_of(n, cols) - 1) / chunk_of(n, cols);
-        partial = n > kRun ? up(chunks * 2 * cols * 4, 256) : 0;
-        total = each * (n > kRun ? 4 : 2) + partial;
+        partial = up(chunks * 2 * cols * 4, 256);
+        total = n > kRun ? each * 4 + partial : 0;
     }
 };
 
@@ -446,39 +499,38 @@ size_t embedding_grad_scratch(int64_t n, int64_t cols) { return (size_t)SumLayou
 
 void launch_embedding_grad(const Lookup& q, char* scratch, hipStream_t s)
 {
-    const int64_t n = q.words.n;
+    const int64_t n = q.words.n, strips = (q.cols + kStrip - 1) / kStrip, waves = kSumBlock / 64;
+    const int64_t fill = q.accumulate ? 0 : (q.words.vocab + kFillRows - 1) / kFillRows;
+    const bool few = n <= kRun;
     const SumLayout l(n, q.cols);
     Sorted now = {(uint32_t*)scratch, (uint32_t*)(scratch + l.each)};
     Sorted other = {(uint32_t*)(scratch + 2 * l.each), (uint32_t*)(scratch + 3 * l.each)};
-    float* partial = (float*)(scratch + l.total - l.partial);
+    float* partial = (float*)(scratch + 4 * l.each);
     by_word(q.words, [&](auto i) {
         typedef decltype(i) I;
-        if (n <= 8192)  // few blocks: less for each
+        if (!few && n <= 8192)  // few blocks: less for each
             k_sort_run<I, 1><<<(uint32_t)((n + 15) / 16), 256, 0, s>>>(q.words.at, n, (uint32_t)q.words.vocab, now);
-        else
+        else if (!few)
             k_sort_run<I, 4><<<(uint32_t)((n + 63) / 64), 256, 0, s>>>(q.words.at, n, (uint32_t)q.words.vocab, now);
-    });
-    for (int64_t len = kRun; len < n; len *= kWays) {
-        k_merge<<<(uint32_t)((n + 63) / 64), 64 * kMergeWaves, 0, s>>>(now, other, n, len);
-        std::swap(now, other);
-    }
-    by_element(q.rows.type, [&](auto g) {
-        by_element(q.table.type, [&](auto t) {
-            typedef typename decltype(g)::T G;
-            typedef typename decltype(t)::T T;
-            const bool few = n <= kRun;
-            const int chunk = few ? kFewPlaces : chunk_of(n, q.cols);
-            const int64_t chunks = (n + chunk - 1) / chunk, strips = (q.cols + kStrip - 1) / kStrip, waves = kSumBlock / 64;
-            const int64_t blocks = few ? chunks * strips : (chunks * strips + waves - 1) / waves;
-            const int64_t fill = q.accumulate ? 0 : (q.words.vocab + kFillRows - 1) / kFillRows;
-            const Sum<G, T> p = {now, n, (uint32_t)q.words.vocab, (const G*)q.rows.at, (T*)q.table.at, q.rows.ld, q.table.ld, q.cols, strips,
-                                 q.scale, q.accumulate, chunk, chunks, partial, blocks};
-            if (few) {
-                k_sum_few<G, T><<<(uint32_t)(blocks + fill), kSumBlock, 0, s>>>(p);
-                return;
-            }
-            k_sum<G, T><<<(uint32_t)(blocks + fill), kSumBlock, 0, s>>>(p);
-            k_join<G, T><<<(uint32_t)((chunks - 1) * strips), kSumBlock, 0, s>>>(p);
+        for (int64_t len = kRun; len < n; len *= kWays) {
+            k_merge<<<(uint32_t)((n + 63) / 64), 64 * kMergeWaves, 0, s>>>(now, other, n, len);
+            std::swap(now, other);
+        }
+        by_element(q.rows.type, [&](auto g) {
+            by_element(q.table.type, [&](auto t) {
+                typedef typename decltype(g)::T G;
+                typedef typename decltype(t)::T T;
+                const int chunk = few ? kFewPlaces : chunk_of(n, q.cols);
+                const int64_t chunks = (n + chunk - 1) / chunk, blocks = few ? chunks * strips : (chunks * strips + waves - 1) / waves;
+                const Sum<G, T> p = {now, n, (uint32_t)q.words.vocab, (const G*)q.rows.at, (T*)q.table.at, q.rows.ld, q.table.ld, q.cols, strips,
+                                     q.scale, q.accumulate, chunk, chunks, partial, blocks};
+                if (few) {
+                    k_sum_few<I, G, T><<<(uint32_t)(blocks + fill), kSumBlock, 0, s>>>(p, q.words.at);
+                    return;
+                }
+                k_sum<G, T><<<(uint32_t)(blocks + fill), kSumBlock, 0, s>>>(p);
+                k_join<G, T><<<(uint32_t)((chunks - 1) * strips), 64 * kJoinWaves, 0, s>>>(p);
+            });
         });
     });
 }

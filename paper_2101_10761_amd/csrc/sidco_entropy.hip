@@ -514,6 +514,7 @@ struct Probs {
     WordList words;
     const float *lse, *loss_grad;
     Plane<H> out, turned;  // n rows of words, words of n rows; either may have no address
+    uint32_t turned_cols;  // with the zeros behind the last row
     const Scales* scales;
 };
 
@@ -586,20 +587,20 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                 __builtin_amdgcn_sched_barrier(0);
             });
             // Eight neighbours of row r from column c on; columns behind the last are zeros up to the pitch.
-            auto put = [](const Plane<H>& o, uint32_t rows, uint32_t m, uint32_t n, bool low) {
+            auto put = [](const Plane<H>& o, uint32_t rows, uint32_t cols, uint32_t m, uint32_t n, bool low) {
                 H* at = o.at + (low ? o.low : 0);
-                return [at, pitch = o.pitch, rows, m, n](uint32_t r, uint32_t c, const v4i& v) {
-                    if (m + r < rows && n + c < (uint32_t)pitch) *(v4i*)(at + (int64_t)(m + r) * pitch + (n + c)) = v;
+                return [at, pitch = o.pitch, rows, cols, m, n](uint32_t r, uint32_t c, const v4i& v) {
+                    if (m + r < rows && n + c < cols) *(v4i*)(at + (int64_t)(m + r) * pitch + (n + c)) = v;
                 };
             };
             char* by = lds + Tl::kLds;
             if (p.out.at) {
-                t.template out16<false>(by, high, put(p.out, p.n, m0, n0, false));
-                if constexpr (M::kPairs) t.template out16<false>(by, low, put(p.out, p.n, m0, n0, true));
+                t.template out16<false>(by, high, put(p.out, p.n, (uint32_t)p.out.pitch, m0, n0, false));
+                if constexpr (M::kPairs) t.template out16<false>(by, low, put(p.out, p.n, (uint32_t)p.out.pitch, m0, n0, true));
             }
             if (p.turned.at) {
-                t.template out16<true>(by, high, put(p.turned, p.count, n0, m0, false));
-                if constexpr (Low) t.template out16<true>(by, low, put(p.turned, p.count, n0, m0, true));
+                t.template out16<true>(by, high, put(p.turned, p.count, p.turned_cols, n0, m0, false));
+                if constexpr (Low) t.template out16<true>(by, low, put(p.turned, p.count, p.turned_cols, n0, m0, true));
             }
         });
 }
@@ -747,13 +748,36 @@ Source<T> source(const Matrix& m, int64_t rows, int64_t cols, const WordList& wo
     return {m.at ? (const T*)m.at + first * m.ld : nullptr, m.ld, rows, cols, words};
 }
 
+// Rows in one launch or two: as many large tiles as fill whole rounds or whole tiles, and the rest in tiles of its own.
+struct RowPlan {
+    int pick, rest_pick;
+    int64_t rows;  // of the first launch
+};
+RowPlan plan_rows(int64_t m, int64_t n, int64_t lines)
+{
+    auto tiles = [&](int64_t rows, int64_t side) { return parts(rows, side) * parts(n, side); };
+    double least = 0.0;
+    RowPlan plan = {best_tile([&](int64_t side) { return tiles(m, side); }, lines, &least), 0, m};
+    for (int i = 0; i < 3; ++i) {
+        const int64_t side = kTileCosts[i].side, strip = parts(n, side), slots = (int64_t)kCus * kTileCosts[i].per_cu;
+        for (const int64_t rows : {m / side * side, tiles(m, side) / slots * slots / strip * side}) {
+            if (rows <= 0 || rows >= m) continue;
+            double rest = 0.0;
+            const int rest_pick = best_tile([&](int64_t s) { return tiles(m - rows, s); }, lines, &rest);
+            const double t = tile_time(i, tiles(rows, side), lines) + rest;
+            if (t < least) least = t, plan = {i, rest_pick, rows};
+        }
+    }
+    return plan;
+}
+
 constexpr int64_t kRowsAtOnce = 16384;  // of the forward pass
 
-// The tile of the product of that many rows with the vocabulary.
+// The products of that many rows with the vocabulary.
 template <class M>
-int forward_tile(int64_t rows, int64_t vocab, int64_t lines)
+RowPlan forward_plan(int64_t rows, int64_t vocab, int64_t lines)
 {
-    return best_tile([&](int64_t side) { return parts(rows, side) * parts(vocab, side); }, lines * (M::kPairs ? 3 : 1));
+    return plan_rows(rows, vocab, lines * (M::kPairs ? 3 : 1));
 }
 int64_t forward_width(int pick, int64_t vocab) { return 2 * parts(vocab, kTileCosts[pick].side); }
 
@@ -801,7 +825,10 @@ struct ForwardPlan {
         part = s.get<float>(M::kPairs ? 3 * kParts : 0);
         x = lay_x ? s.plane<H>(n, pitch, M::kPairs) : Plane<H>{(H*)q.x.at, q.x.ld, 0};
         w = lay_w ? s.plane<H>(v, pitch, M::kPairs) : Plane<H>{(H*)q.w.at, q.w.ld, 0};
-        auto pairs_of = [&](int64_t rows) { return rows * forward_width(forward_tile<M>(rows, v, pitch / kPer<M>), v); };
+        auto pairs_of = [&](int64_t rows) {
+            const RowPlan plan = forward_plan<M>(rows, v, pitch / kPer<M>);
+            return std::max(plan.rows * forward_width(plan.pick, v), (rows - plan.rows) * forward_width(plan.rest_pick, v));
+        };
         pairs = s.get<float2>(few ? n * kFewBlocks : std::max(pairs_of(at_once), pairs_of((n - 1) % kRowsAtOnce + 1)));
         mine = s.get<float>(at_once);
         bytes = s.used;
@@ -829,7 +856,9 @@ void forward(const Entropy& q, char* scratch, hipStream_t s)
     const ForwardPlan<M> f(q, scratch);
     const int64_t n = q.words.n, v = q.words.vocab;
     if (f.few) {
-        const int64_t groups = parts(v, 16), blocks = std::min(groups, kFewBlocks), steps = few_steps<M>(n, q.dim);
+        const int64_t groups = parts(v, 16), steps = few_steps<M>(n, q.dim);
+        // a CU's registers hold two blocks where a wave's operands take few of them
+        const int64_t blocks = std::min(groups, steps <= (n <= 16 ? 8 : 4) ? kFewBlocks : kFewBlocks / 2);
         const Few<T> p = {(const T*)q.x.at, (const T*)q.w.at, q.x.ld, q.w.ld, (uint32_t)n, (uint32_t)q.dim, (uint32_t)groups, list(q.words), f.pairs, f.mine};
         auto go = [&](auto kernel) { kernel<<<(uint32_t)blocks, 64 * kFewWaves, 0, s>>>(p); };
         auto by_steps = [&](auto tiles) {
@@ -861,18 +890,22 @@ void forward(const Entropy& q, char* scratch, hipStream_t s)
     }
     for (int64_t r = 0; r < n; r += kRowsAtOnce) {
         const int64_t rows = std::min(n - r, kRowsAtOnce);
-        const WordList words = list(q.words).from(r);
         const Span span = {(uint32_t)(f.x.pitch * sizeof(H)), (uint32_t)(f.w.pitch * sizeof(H)), (uint32_t)(f.pitch / kPer<M>)};
-        const int pick = forward_tile<M>(rows, v, span.lines);
-        const uint32_t width = (uint32_t)forward_width(pick, v);
-        by_tile<M>(pick, [&](auto shape) {
-            typedef typename decltype(shape)::Is Tl;
-            const Places places = {(uint32_t)parts(rows, Tl::kM), (uint32_t)parts(v, Tl::kN), (uint32_t)(parts(rows, Tl::kM) * parts(v, Tl::kN))};
-            const Plane<H> x = {f.x.at + r * f.x.pitch, f.x.pitch, f.x.low};
-            const Forward<H> p = {x, f.w, (uint32_t)rows, words, f.pairs, width, f.mine, f.scales};
-            k_logits<M, Tl><<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places);
-        });
-        join_rows(f.pairs, width, rows, words, f.mine, q.loss ? q.loss + r : nullptr, q.lse ? q.lse + r : nullptr, s);
+        auto logits = [&](int pick, int64_t row, int64_t rows) {
+            const uint32_t width = (uint32_t)forward_width(pick, v);
+            const WordList words = list(q.words).from(r + row);
+            by_tile<M>(pick, [&](auto shape) {
+                typedef typename decltype(shape)::Is Tl;
+                const Places places = {(uint32_t)parts(rows, Tl::kM), (uint32_t)parts(v, Tl::kN), (uint32_t)(parts(rows, Tl::kM) * parts(v, Tl::kN))};
+                const Plane<H> x = {f.x.at + (r + row) * f.x.pitch, f.x.pitch, f.x.low};
+                const Forward<H> p = {x, f.w, (uint32_t)rows, words, f.pairs, width, f.mine, f.scales};
+                k_logits<M, Tl><<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places);
+            });
+            join_rows(f.pairs, width, rows, words, f.mine, q.loss ? q.loss + r + row : nullptr, q.lse ? q.lse + r + row : nullptr, s);
+        };
+        const RowPlan plan = forward_plan<M>(rows, v, span.lines);
+        logits(plan.pick, 0, plan.rows);
+        if (plan.rows < rows) logits(plan.rest_pick, plan.rows, rows - plan.rows);
     }
 }
 
@@ -910,7 +943,7 @@ struct GradPlan {
         int64_t lines = parts(piece, kPer<M>);
         if (q.x_grad.at) {
             double least = 0.0;
-            for (int k = 1; k <= 64 && k * 8 <= std::max(lines, (int64_t)8); k *= 2) {
+            for (int k = 1; k <= 64 && k * 8 <= std::max(lines, (int64_t)8); ++k) {
                 double t = 0.0;
                 const int64_t each = parts(lines, k);
                 const int pick = best_tile([&](int64_t side) { return parts(n, side) * parts(q.dim, side) * k; }, each * (M::kPairs ? 3 : 1), &t);
@@ -939,7 +972,7 @@ struct GradPlan {
 };
 
 template <class T, class M, int Terms>
-void product(int pick, const Product<typename M::H>& p, int64_t lines, int splits, hipStream_t s)
+void product_part(int pick, const Product<typename M::H>& p, int64_t lines, int splits, hipStream_t s)
 {
     typedef typename M::H H;
     by_tile<M>(pick, [&](auto shape) {
@@ -949,6 +982,23 @@ void product(int pick, const Product<typename M::H>& p, int64_t lines, int split
         const Span span = {(uint32_t)(p.a.pitch * sizeof(H)), (uint32_t)(p.b.pitch * sizeof(H)), (uint32_t)lines};
         k_product<T, H, Terms, Tl><<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places);
     });
+}
+
+// The same without splits, in the launches of a plan.
+template <class T, class M, int Terms>
+void product(const Product<typename M::H>& p, int64_t lines, hipStream_t s)
+{
+    const RowPlan plan = plan_rows(p.m, p.n, lines * Terms);
+    auto part = [&](int pick, int64_t first, int64_t rows) {
+        Product<typename M::H> r = p;
+        r.a.at += first * p.a.pitch;
+        r.m = rows;
+        r.c = (T*)p.c + first * p.ldc;
+        if (p.before) r.before = p.before + first * p.n;
+        product_part<T, M, Terms>(pick, r, lines, 1, s);
+    };
+    part(plan.pick, 0, plan.rows);
+    if (plan.rows < p.m) part(plan.rest_pick, plan.rows, p.m - plan.rows);
 }
 
 template <class M>
@@ -974,44 +1024,51 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
 
         const Span span = {(uint32_t)(g.x.pitch * sizeof(H)), (uint32_t)(w.pitch * sizeof(H)), (uint32_t)(g.pitch / kPer<M>)};
         const int64_t wide = g.p.at ? g.pitch_v : count;  // padding of P's rows is written with the last tiles
-        const int pick = best_tile([&](int64_t side) { return parts(n, side) * parts(wide, side); }, span.lines * kTerms);
-        by_tile<M>(pick, [&](auto shape) {
-            typedef typename decltype(shape)::Is Tl;
-            const uint32_t tm = (uint32_t)parts(n, Tl::kM), tn = (uint32_t)parts(wide, Tl::kN);
-            const Places places = {tm, tn, tm * tn};
-            const Probs<H> p = {g.x, w, (uint32_t)n, (uint32_t)count, (uint32_t)first, words, q.lse, q.loss_grad, g.p, g.pt, g.scales};
-            auto go = [&](auto kernel) { kernel<<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places); };
-            if constexpr (M::kPairs)
-                go(k_probs<M, true, Tl>);
-            else if (g.wide)
-                go(k_probs<M, true, Tl>);
-            else
-                go(k_probs<M, false, Tl>);
-        });
+        auto probs = [&](int pick, int64_t row, int64_t rows) {
+            by_tile<M>(pick, [&](auto shape) {
+                typedef typename decltype(shape)::Is Tl;
+                const uint32_t tm = (uint32_t)parts(rows, Tl::kM), tn = (uint32_t)parts(wide, Tl::kN);
+                const Places places = {tm, tn, tm * tn};
+                const Plane<H> x = {g.x.at + row * g.x.pitch, g.x.pitch, g.x.low}, out = {g.p.at ? g.p.at + row * g.p.pitch : nullptr, g.p.pitch, g.p.low};
+                // columns of the transpose up to the pitch are this launch's if the last rows are
+                const Plane<H> turned = {g.pt.at ? g.pt.at + row : nullptr, g.pt.pitch, g.pt.low};
+                const Probs<H> p = {x, w, (uint32_t)rows, (uint32_t)count, (uint32_t)first, words.from(row), q.lse + row,
+                                    q.loss_grad ? q.loss_grad + row : nullptr, out, turned,
+                                    (uint32_t)(row + rows < n ? rows : g.pitch_n - row), g.scales};
+                auto go = [&](auto kernel) { kernel<<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places); };
+                if constexpr (M::kPairs)
+                    go(k_probs<M, true, Tl>);
+                else if (g.wide)
+                    go(k_probs<M, true, Tl>);
+                else
+                    go(k_probs<M, false, Tl>);
+            });
+        };
+        const RowPlan plan = plan_rows(n, wide, span.lines * kTerms);
+        probs(plan.pick, 0, plan.rows);
+        if (plan.rows < n) probs(plan.rest_pick, plan.rows, n - plan.rows);
         const Scales* scales = M::kScaled ? g.scales : nullptr;
         if (q.x_grad.at) {
             const int64_t lines = g.pitch_v / kPer<M> / g.splits;
             if (g.splits > 1 || k + 1 < g.pieces) {
                 const Product<H> p = {g.p, g.wt, n, q.dim, scales, false, g.sums, q.dim, n * q.dim, k > 0, nullptr};
-                product<float, M, kTerms>(g.pick_x, p, lines, g.splits, s);
+                product_part<float, M, kTerms>(g.pick_x, p, lines, g.splits, s);
             } else {
                 const Product<H> p = {g.p, g.wt, n, q.dim, scales, false, q.x_grad.at, q.x_grad.ld, 0, false, g.pieces > 1 ? g.sums : nullptr};
-                product<T, M, kTerms>(g.pick_x, p, lines, 1, s);
+                product_part<T, M, kTerms>(g.pick_x, p, lines, 1, s);
             }
         }
         if (q.w_grad.at) {
             char* c = (char*)q.w_grad.at + first * q.w_grad.ld * (q.w_grad.type == kGradF32 ? 4 : 2);
             const Product<H> p = {g.pt, g.xt, count, q.dim, scales, true, c, q.w_grad.ld, 0, q.accumulate, nullptr};
             const int64_t lines = g.pitch_n / kPer<M>;
-            const int terms = M::kPairs ? 3 : (g.wide ? 2 : 1);
-            const int pw = best_tile([&](int64_t side) { return parts(count, side) * parts(q.dim, side); }, lines * terms);
             if constexpr (M::kPairs) {
-                product<float, M, 3>(pw, p, lines, 1, s);
+                product<float, M, 3>(p, lines, s);
             } else {
                 if (g.wide)
-                    product<float, M, 2>(pw, p, lines, 1, s);
+                    product<float, M, 2>(p, lines, s);
                 else
-                    product<T, M, 1>(pw, p, lines, 1, s);
+                    product<T, M, 1>(p, lines, s);
             }
         }
     }

@@ -87,10 +87,15 @@ int sidco_embedding_grad(void* stream, const void* grad, int grad_dtype, int64_t
     if (int rc = check_matrix(table_grad, table_dtype, dim, ldt)) return rc;
     if ((n + 31) / 32 * ((dim + 511) / 512) > (int64_t)INT32_MAX / 2) return SIDCO_ERR_SIZE;  // a block's number has 31 bits
     if (!isfinite(scale) || !flag(accumulate) || grad == table_grad) return SIDCO_ERR_ARG;
-    StreamScratch ws(stream, embedding_grad_scratch(n, dim));
-    if (ws.rc != SIDCO_OK) return ws.rc;
     const Lookup q = {{words, word_type == SIDCO_WORD_I64, n, vocab}, matrix(table_grad, table_dtype, ldt), matrix(grad, grad_dtype, ldg), dim,
                       scale, accumulate != 0};
+    const size_t bytes = embedding_grad_scratch(n, dim);
+    if (bytes == 0) {
+        launch_embedding_grad(q, nullptr, (hipStream_t)stream);
+        return launched();
+    }
+    StreamScratch ws(stream, bytes);
+    if (ws.rc != SIDCO_OK) return ws.rc;
     launch_embedding_grad(q, ws.data, (hipStream_t)stream);
     return launched();
 }
