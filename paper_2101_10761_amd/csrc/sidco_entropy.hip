@@ -711,9 +711,9 @@ struct Space {
     template <class T>
     T* get(int64_t count)
     {
-        T* p = (T*)(at + used);
+        T* p = at ? (T*)(at + used) : nullptr;
         used += (size_t)up(count * (int64_t)sizeof(T), 256);
-        return at ? p : nullptr;
+        return p;
     }
     template <class H>
     Plane<H> plane(int64_t rows, int64_t pitch, bool pairs)
