@@ -914,8 +914,11 @@ constexpr int64_t kPieceBytes = (int64_t)512 << 20;
 
 template <class M>
 struct GradPlan {
+    // Rows that are a large power of two apart would meet in a few of the memory's channels: a line more between them.
+    static int64_t spread(int64_t cols) { return cols * (int64_t)sizeof(typename M::H) % 4096 == 0 ? cols + kPer<M> : cols; }
+
     typedef typename M::H H;
-    int64_t pitch, pitch_n, pitch_v, piece, pieces;
+    int64_t pitch, cols_n, cols_v, piece, pieces;  // columns of rows over n and over a piece's words
     int splits, pick_x;   // of the product for x's gradient
     bool lay_x, lay_w, wide;  // wide: w's gradient in fp32, of 16-bit operands
     float* part;
@@ -928,11 +931,11 @@ struct GradPlan {
         Space s = {scratch, 0};
         const int64_t n = q.words.n, v = q.words.vocab;
         pitch = up(q.dim, kPer<M>);
-        pitch_n = up(n, kPer<M>);
+        cols_n = up(n, kPer<M>);
         lay_x = !lies_in_lines<M>(q.x, q.dim);
         lay_w = !lies_in_lines<M>(q.w, q.dim);
         wide = !M::kPairs && q.w_grad.at && q.w_grad.type == kGradF32;
-        const int64_t word = pitch_n * (int64_t)sizeof(H) * (q.x_grad.at ? 1 : 0) + pitch_n * (int64_t)sizeof(H) * (q.w_grad.at ? 1 : 0);
+        const int64_t word = cols_n * (int64_t)sizeof(H) * ((q.x_grad.at ? 1 : 0) + (q.w_grad.at ? 1 : 0));
         const int64_t most = std::min(std::max(kPieceBytes / (word * (M::kPairs ? 2 : 1)), (int64_t)1024), (int64_t)1 << 22);
         pieces = parts(v, most);
         piece = std::min(up(parts(v, pieces), 256), v);
@@ -952,7 +955,8 @@ struct GradPlan {
             }
         }
         lines = parts(lines, splits) * splits;
-        pitch_v = lines * kPer<M>;
+        cols_v = lines * kPer<M>;
+        const int64_t pitch_n = spread(cols_n), pitch_v = spread(cols_v);
         scales = s.get<Scales>(1);
         part = s.get<float>(M::kScaled ? 3 * kParts : 0);
         x = lay_x ? s.plane<H>(n, pitch, M::kPairs) : Plane<H>{(H*)q.x.at, q.x.ld, 0};
@@ -1017,13 +1021,13 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
         // x once, and this piece of w
         Layout<T, H> lx = {source<T>(q.x, n, q.dim, words), g.lay_x ? g.x : Plane<H>{}, g.xt, 0, (uint32_t)parts(g.pitch, 64)};
         Layout<T, H> lw = {source<T>(q.w, count, q.dim, {}, first), g.lay_w ? g.w : Plane<H>{}, g.wt, 0, lx.tiles_c};
-        if (k == 0 && (g.lay_x || g.xt.at)) lx.tiles_r = (uint32_t)parts(g.pitch_n, 64);
-        if (g.lay_w || g.wt.at) lw.tiles_r = (uint32_t)parts(g.wt.at ? g.pitch_v : count, 64);
+        if (k == 0 && (g.lay_x || g.xt.at)) lx.tiles_r = (uint32_t)parts(g.cols_n, 64);
+        if (g.lay_w || g.wt.at) lw.tiles_r = (uint32_t)parts(g.wt.at ? g.cols_v : count, 64);
         const uint32_t blocks = (lx.tiles_r + lw.tiles_r) * lx.tiles_c;
         if (blocks || (k == 0 && M::kScaled)) k_layout<M><<<blocks ? blocks : 1, 256, 0, s>>>(lx, lw, g.part, g.scales);
 
         const Span span = {(uint32_t)(g.x.pitch * sizeof(H)), (uint32_t)(w.pitch * sizeof(H)), (uint32_t)(g.pitch / kPer<M>)};
-        const int64_t wide = g.p.at ? g.pitch_v : count;  // padding of P's rows is written with the last tiles
+        const int64_t wide = g.p.at ? g.cols_v : count;  // padding of P's rows is written with the last tiles
         auto probs = [&](int pick, int64_t row, int64_t rows) {
             by_tile<M>(pick, [&](auto shape) {
                 typedef typename decltype(shape)::Is Tl;
@@ -1034,7 +1038,7 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
                 const Plane<H> turned = {g.pt.at ? g.pt.at + row : nullptr, g.pt.pitch, g.pt.low};
                 const Probs<H> p = {x, w, (uint32_t)rows, (uint32_t)count, (uint32_t)first, words.from(row), q.lse + row,
                                     q.loss_grad ? q.loss_grad + row : nullptr, out, turned,
-                                    (uint32_t)(row + rows < n ? rows : g.pitch_n - row), g.scales};
+                                    (uint32_t)(row + rows < n ? rows : g.cols_n - row), g.scales};
                 auto go = [&](auto kernel) { kernel<<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places); };
                 if constexpr (M::kPairs)
                     go(k_probs<M, true, Tl>);
@@ -1049,7 +1053,7 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
         if (plan.rows < n) probs(plan.rest_pick, plan.rows, n - plan.rows);
         const Scales* scales = M::kScaled ? g.scales : nullptr;
         if (q.x_grad.at) {
-            const int64_t lines = g.pitch_v / kPer<M> / g.splits;
+            const int64_t lines = g.cols_v / kPer<M> / g.splits;
             if (g.splits > 1 || k + 1 < g.pieces) {
                 const Product<H> p = {g.p, g.wt, n, q.dim, scales, false, g.sums, q.dim, n * q.dim, k > 0, nullptr};
                 product_part<float, M, kTerms>(g.pick_x, p, lines, g.splits, s);
@@ -1061,7 +1065,7 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
         if (q.w_grad.at) {
             char* c = (char*)q.w_grad.at + first * q.w_grad.ld * (q.w_grad.type == kGradF32 ? 4 : 2);
             const Product<H> p = {g.pt, g.xt, count, q.dim, scales, true, c, q.w_grad.ld, 0, q.accumulate, nullptr};
-            const int64_t lines = g.pitch_n / kPer<M>;
+            const int64_t lines = g.cols_n / kPer<M>;
             if constexpr (M::kPairs) {
                 product<float, M, 3>(p, lines, s);
             } else {
