@@ -710,9 +710,10 @@ size_t sidco_workspace_bytes_cross_entropy(int64_t n, int64_t dim, int64_t vocab
  *                                                       (dtype or SIDCO_GRAD_F32, row stride ldgw)
  * Either may be NULL, not both.  loss_grad (device, n floats) is 1 / n for the gradient of the
  * mean, times the loss scale if there is one; NULL stands for ones.  P is formed for one piece of
- * the vocabulary at a time; it has 22 bits where the gradient it makes is fp32 and the operands are
- * halves or fp32, 16 where they are bf16, and for a 16-bit gradient the operands' own, halves
- * under a power of two.  Rows of x whose target is padding do not enter w_grad whatever they
+ * the vocabulary at a time, in halves under a power of two of the largest loss_grad: 11 bits for a bf16
+ * gradient, else 22, down to 2^-29 of the largest and 2^-39 of that below; bf16 operands of its
+ * products are exact down to 2^-29 of their matrix's largest magnitude in the same way, and there
+ * an infinity counts as a NaN.  Rows of x whose target is padding do not enter w_grad whatever they
  * hold.  The gradients must not overlap x, w or each other.  Uses the stream's workspace, of
  * sidco_workspace_bytes_cross_entropy_grad(n, dim, vocab, dtype, w_grad_dtype) at most.
  */

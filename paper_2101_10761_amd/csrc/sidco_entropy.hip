@@ -4,16 +4,22 @@
 //   P_iv = g_i (exp(l_iv - lse_i) - [v = t_i]),  dx = P w,  dw = P^T x.
 //
 // The forward pass is one product whose tiles go out as the largest logit of each row and the sum of exponentials below it, in
-// powers of two; a second kernel joins the tiles' pairs.  The gradient forms the logits again, a piece of the vocabulary at a
+// powers of two and without the row's word, whose logit goes out by itself; a second kernel joins the tiles' pairs to z = sum over
+// v != t of exp(l_v - l_t), loss = log(1 + z), lse = l_t + loss: a small loss is not the difference of two large numbers.  The gradient forms the logits again, a piece of the vocabulary at a
 // time, and P leaves the product's registers both by rows of x and by words, for the two products that contract over words
 // and over rows: four products for the three that an arithmetic minimum takes, and no N x V array.
 //
 // Products are those of sidco_product.h and want both operands by rows along the contraction, in whole lines of 128 bytes.
 // 16-bit operands that lie like that are read where they are; others, and the transposes that the gradient needs, are laid out
 // in the workspace first.  fp32 operands become pairs of halves, 22 bits, under a power of two that brings the largest
-// magnitude of the matrix to 2^14 to 2^15, and a product is three: low high + high low + high high.  P is held in the
-// operands' 16 bits (its rounding, 2^-9 or 2^-12 of each element, is that of the gradient's own type, and dx and dw add many
-// of them up), times a power of two for halves, whose smallest numbers it would reach; for a gradient in fp32 it is a pair.
+// magnitude of the matrix to 2^14 to 2^15, and a product is three: low high + high low + high high.
+//
+// P is in halves, times a power of two, for its smallest elements would reach theirs: 11 bits, or as a pair 22.  Its rounding adds
+// up like a rounding of the gradient itself, so that it takes more bits than the gradient has: one half for bf16 gradients (an
+// error of 1.7e-3 in the 2-norm, the gradient's own rounding; with P in bf16 it was up to 2.4e-3), a pair for those of halves and
+// of fp32 (2.1e-4 for halves; with one half up to 3.1e-4).  bf16 operands of the products with P are halves too, exactly but for
+// those under 2^-29 of the largest, under a power of two as for fp32; they multiply at nearly the rate of bf16 (a training pass
+// of 8192 x 4096 x 131072 takes 3 % longer).
 #include <math.h>
 
 #include <algorithm>
@@ -29,23 +35,25 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr double kLn2 = 0.69314718055994530942;
 constexpr float kFar = 3.0e38f;  // stands for an infinite largest logit
 
-// How element types are multiplied: what operands are held in, and whether as pairs.
+// How element types are multiplied: what the operands of the logits are held in, whether operands are pairs, whether those of the
+// gradient's products, always halves, are scaled, and whether P is a pair in all of them.
 struct ModeF32 {
     typedef float T;
     typedef _Float16 H;
     typedef HalfCore Core;
-    static constexpr bool kPairs = true, kScaled = true;
+    static constexpr bool kPairs = true, kScaled = true, kPairP = true;
 };
 struct ModeF16 {
     typedef _Float16 T, H;
     typedef HalfCore Core;
-    static constexpr bool kPairs = false, kScaled = true;
+    static constexpr bool kPairs = false, kScaled = false, kPairP = true;
 };
 struct ModeBf16 {
     typedef __bf16 T, H;
     typedef Bf16Core Core;
-    static constexpr bool kPairs = false, kScaled = false;  // has fp32's range
+    static constexpr bool kPairs = false, kScaled = true, kPairP = false;
 };
+typedef _Float16 G;  // of the gradient's products
 
 template <class F>
 void by_mode(int type, const F& f)
@@ -60,7 +68,7 @@ void by_mode(int type, const F& f)
 
 // ---- scales ----
 
-// Powers of two: of x and w as they are laid out, and of P.
+// Powers of two: of x and w as the gradient's products (fp32: all) take them, and of P.
 struct Scales {
     float x, w, p;
 };
@@ -153,7 +161,8 @@ __device__ __forceinline__ Rows rows_of(const Plane<H>& p, int64_t row, int64_t 
 template <class T, class H>
 struct Layout {
     Source<T> from;
-    Plane<H> rows, turned;
+    Plane<H> rows;
+    Plane<G> turned;
     uint32_t tiles_r, tiles_c;  // of 64 x 64, padding included
 };
 
@@ -173,8 +182,9 @@ __device__ __forceinline__ void put8(const Plane<H>& o, int64_t r, int64_t c, co
 }
 
 // 64 x 64 elements a block, of x and then of w.  Transposed, rows of padding are zeros whatever they hold: they are multiplied
-// with the zeros that P has for them.  With Scaled the partial results of k_top are joined, and block 0 writes them down.
-template <class M>
+// with the zeros that P has for them.  With Scaled (not in the forward pass of 16-bit operands, whose transposes nobody takes)
+// the partial results of k_top are joined; block 0 writes them down for the products.
+template <class M, bool Scaled>
 __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M::H> x, Layout<typename M::T, typename M::H> w, const float* part,
                                                 Scales* scales)
 {
@@ -186,10 +196,10 @@ __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M
     const Layout<typename M::T, H>& p = second ? w : x;
     const uint32_t t = second ? blockIdx.x - first : blockIdx.x;
     float scale = 1.0f;
-    if (M::kScaled && (M::kPairs || blockIdx.x == 0)) {
-        if (M::kPairs) scale = scale_of(joined_top(part + (second ? kParts : 0), lds));
+    if (Scaled) {
+        if (M::kScaled) scale = scale_of(joined_top(part + (second ? kParts : 0), lds));
         if (blockIdx.x == 0) {
-            const float sx = M::kPairs ? scale_of(joined_top(part, lds)) : 1.0f, sw = M::kPairs ? scale_of(joined_top(part + kParts, lds)) : 1.0f;
+            const float sx = M::kScaled ? scale_of(joined_top(part, lds)) : 1.0f, sw = M::kScaled ? scale_of(joined_top(part + kParts, lds)) : 1.0f;
             const float sp = scale_of(joined_top(part + 2 * kParts, lds));
             if (threadIdx.x == 0) *scales = {sx, sw, sp};
         }
@@ -211,7 +221,7 @@ __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M
         if (p.turned.at) {
             const bool none = p.from.words.at && r < p.from.rows && p.from.words.none(r);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) tile[k * 32 + row][col + i] = none ? 0.0f : v[i];
+            for (int i = 0; i < 8; ++i) tile[k * 32 + row][col + i] = none ? 0.0f : (M::kPairs ? v[i] : v[i] * scale);
         }
     }
     if (!p.turned.at) return;
@@ -223,7 +233,7 @@ __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = tile[col + i][c];
-        put8<H, M::kPairs>(p.turned, c0 + c, r0 + col, v);
+        put8<G, M::kPairs>(p.turned, c0 + c, r0 + col, v);
     }
 }
 
@@ -302,6 +312,19 @@ __global__ __launch_bounds__(Tl::kThreads) void k_logits(Forward<typename M::H> 
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[j][e] = (int)left > j * 16 + e ? acc[j][e] : -INFINITY;
                 }
+                // of 128 columns one lane has the row's word, or none
+                if (here < Tl::kNt * 16 && here % 16 < 4 && here < left) {
+                    float mine = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < Tl::kNt; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool it = here == (uint32_t)(j * 16 + e);
+                            mine = it ? acc[j][e] : mine;
+                            acc[j][e] = it ? -INFINITY : acc[j][e];
+                        }
+                    p.mine[r] = mine * k;
+                }
                 float top = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < Tl::kNt; ++j) top = max3(max3(top, acc[j][0], acc[j][1]), acc[j][2], acc[j][3]);
@@ -317,15 +340,6 @@ __global__ __launch_bounds__(Tl::kThreads) void k_logits(Forward<typename M::H> 
                 sum += __shfl_xor(sum, 16);
                 sum += __shfl_xor(sum, 32);
                 if (t.lane < 16 && r < p.n) p.part[(int64_t)r * p.width + place] = make_float2(top, sum);
-                // of 128 columns one lane has the row's word, or none
-                if (here < Tl::kNt * 16 && here % 16 < 4 && here < left) {
-                    float mine = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < Tl::kNt; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) mine = here == (uint32_t)(j * 16 + e) ? acc[j][e] : mine;
-                    p.mine[r] = mine * k;
-                }
             });
         });
 }
@@ -380,7 +394,7 @@ struct Few {
     float* mine;
 };
 
-// Steps: of the contraction, 8 kStep elements each; Tiles: of 16 rows.
+// Steps: of the contraction, 8 kStep elements each, as many as there are or one more; Tiles: of 16 rows.
 template <class T, int Steps, int Tiles>
 __global__ __launch_bounds__(64 * kFewWaves) void k_few(Few<T> p)
 {
@@ -390,17 +404,28 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(Few<T> p)
     __shared__ v4f sums[2][kFewWaves][Tiles][64];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
     const uint32_t at = wave * Core::kStep + q * kPiece;
+    // A piece that would reach past the row's end is the row's last one instead, of which `keep` leaves what no other piece holds;
+    // of one behind the end nothing.  Only the last two steps have such.  (A branch between them and whole steps would have the
+    // compiler wait for all loads at each step.)
+    const uint32_t last = p.dim - kPiece;
+    v4i keep[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int skip = (int)((Steps - 2 + i) * kAll + at - last);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            if constexpr (sizeof(T) == 4)
+                keep[i][d] = d >= skip ? -1 : 0;
+            else
+                keep[i][d] = (2 * d >= skip ? 0xffff : 0) | (2 * d + 1 >= skip ? (int)0xffff0000 : 0);
+        }
+    }
     auto load = [&](const T* row, int s) -> piece {
         const uint32_t k = s * kAll + at;
-        if ((s + 1) * kAll <= p.dim) return *(const piece*)(row + k);
-        piece v;
-        if (k + kPiece <= p.dim) {
-            v = *(const piece*)(row + k);
-        } else {
-#pragma unroll
-            for (uint32_t i = 0; i < kPiece; ++i) v[i] = k + i < p.dim ? row[k + i] : (T)0.0f;
-        }
-        return v;
+        return *(const piece*)(row + (s + 2 < Steps || k < last ? k : last));
+    };
+    auto kept = [&](const piece& v, int s) -> piece {
+        return s + 2 < Steps ? v : __builtin_bit_cast(piece, __builtin_bit_cast(v4i, v) & keep[s + 2 - Steps]);
     };
     auto row_of = [&](uint32_t group) -> const T* {
         const uint32_t v = group * 16 + r;
@@ -414,7 +439,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(Few<T> p)
     for (int t = 0; t < Tiles; ++t) {
         const T* from = p.x + (int64_t)(t * 16 + r < p.n ? t * 16 + r : 0) * p.ldx;
 #pragma unroll
-        for (int s = 0; s < Steps; ++s) x[t][s] = load(from, s);
+        for (int s = 0; s < Steps; ++s) x[t][s] = kept(load(from, s), s);
     }
     const uint32_t mine = wave * 16 + r;  // the row whose sums this lane joins, if its wave is one of the first
     const uint32_t word = wave < Tiles && mine < p.n ? p.words[mine] : p.words.vocab;
@@ -427,9 +452,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(Few<T> p)
         for (int t = 0; t < Tiles; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int s = 0; s < Steps; ++s) {
+            const piece a = kept(w[s], s);
 #pragma unroll
-            for (int t = 0; t < Tiles; ++t) acc[t] = Core::mul(w[s], x[t][s], acc[t]);
-            w[s] = load(row, s);
+            for (int t = 0; t < Tiles; ++t) acc[t] = Core::mul(a, x[t][s], acc[t]);
+            w[s] = load(row, s);  // where the operand was
+            __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int t = 0; t < Tiles; ++t) sums[turn][wave][t][lane] = acc[t];
@@ -443,9 +470,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(Few<T> p)
             float most = top;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                l[e] = v + e < p.words.vocab ? l[e] : -INFINITY;
+                const bool it = word == v + e && word < p.words.vocab;
+                if (it) p.mine[mine] = l[e];
+                l[e] = v + e < p.words.vocab && !it ? l[e] : -INFINITY;
                 most = fmaxf(most, l[e]);
-                if (word == v + e && word < p.words.vocab) p.mine[mine] = l[e];
             }
             most = fminf(most, kFar);
             sum *= __builtin_amdgcn_exp2f(top - most);
@@ -500,9 +528,19 @@ __global__ __launch_bounds__(256) void k_join_rows(const float2* part, uint32_t 
         }
     }
     if (lane == 0 && r < n) {
-        const double all = (double)top + (double)log2f(sum);
-        if (lse) lse[r] = (float)(all * kLn2);
-        if (loss) loss[r] = words.none(r) ? 0.0f : (float)((all - (double)mine[r]) * kLn2);
+        const bool none = words.none(r);
+        const double own = none ? -INFINITY : (double)mine[r], over = (double)top - own;
+        double all, more;  // lse, and the loss
+        if (over < 64.0) {
+            more = log1p((double)sum * exp2(over));
+            all = own * kLn2 + more;
+            if (own == INFINITY) more = NAN;  // the difference of two infinities
+        } else {  // or there is no word, or its logit is a NaN
+            all = none || own == -INFINITY ? ((double)top + log2((double)sum)) * kLn2 : ((double)top + log2((double)sum + exp2(-over))) * kLn2;
+            more = all - own * kLn2;
+        }
+        if (lse) lse[r] = (float)all;
+        if (loss) loss[r] = none ? 0.0f : (float)more;
     }
 }
 
@@ -513,7 +551,7 @@ struct Probs {
     uint32_t n, count, first;
     WordList words;
     const float *lse, *loss_grad;
-    Plane<H> out, turned;  // n rows of words, words of n rows; either may have no address
+    Plane<G> out, turned;  // n rows of words, words of n rows; either may have no address
     uint32_t turned_cols;  // with the zeros behind the last row
     const Scales* scales;
 };
@@ -521,8 +559,8 @@ struct Probs {
 template <class M, bool Low, class Tl>
 __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, Span span, Places places)
 {
-    typedef typename M::H H;
-    __shared__ __align__(1024) char lds[lds_of<Tl, H>()];
+    constexpr bool kLow = Low || M::kPairP;
+    __shared__ __align__(1024) char lds[lds_of<Tl, G>()];
     Tl t;
     t.template run<M::kPairs ? 3 : 1, true>(
         places.total, span, lds,
@@ -535,9 +573,9 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
             uint32_t ti, tj, split;
             places.at(tile, ti, tj, split);
             const uint32_t m0 = ti * Tl::kM, n0 = tj * Tl::kN;
-            const float k = M::kPairs ? kLog2e / (p.scales->x * p.scales->w) : kLog2e, sp = M::kScaled ? p.scales->p : 1.0f;
+            const float k = M::kPairs ? kLog2e / (p.scales->x * p.scales->w) : kLog2e, sp = p.scales->p;
             const bool edge = n0 + Tl::kN > p.count;
-            Four16 high[Tl::kMt][Tl::kNt], low[Low ? Tl::kMt : 1][Tl::kNt];  // in 16 bits P takes half the room of the sums
+            Four16 high[Tl::kMt][Tl::kNt], low[kLow ? Tl::kMt : 1][Tl::kNt];  // in 16 bits P takes half the room of the sums
             t.strips([&](int i, uint32_t row, uint32_t col, v4f(&acc)[Tl::kNt]) {
                 const uint32_t r = m0 + row;
                 uint32_t word = p.words.vocab;
@@ -569,26 +607,26 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                         for (int e = 0; e < 4; ++e) acc[j][e] = left > j * 16 + e ? acc[j][e] : 0.0f;
                 }
                 auto packed = [&](const v4f& v) -> Four16 {
-                    typedef H h2 __attribute__((ext_vector_type(2)));
-                    const uint32_t a = __builtin_bit_cast(uint32_t, h2{(H)v[0], (H)v[1]}), b = __builtin_bit_cast(uint32_t, h2{(H)v[2], (H)v[3]});
+                    typedef G h2 __attribute__((ext_vector_type(2)));
+                    const uint32_t a = __builtin_bit_cast(uint32_t, h2{(G)v[0], (G)v[1]}), b = __builtin_bit_cast(uint32_t, h2{(G)v[2], (G)v[3]});
                     return {none ? 0 : a, none ? 0 : b};
                 };
 #pragma unroll
                 for (int j = 0; j < Tl::kNt; ++j) {
                     const v4f v = rounded(acc[j]);
                     high[i][j] = packed(v);
-                    if constexpr (Low) {
+                    if constexpr (kLow) {
                         v4f l;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) l[e] = v[e] - (float)(H)v[e];
+                        for (int e = 0; e < 4; ++e) l[e] = v[e] - (float)(G)v[e];
                         low[i][j] = packed(l);
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
             // Eight neighbours of row r from column c on; columns behind the last are zeros up to the pitch.
-            auto put = [](const Plane<H>& o, uint32_t rows, uint32_t cols, uint32_t m, uint32_t n, bool low) {
-                H* at = o.at + (low ? o.low : 0);
+            auto put = [](const Plane<G>& o, uint32_t rows, uint32_t cols, uint32_t m, uint32_t n, bool low) {
+                G* at = o.at + (low ? o.low : 0);
                 return [at, pitch = o.pitch, rows, cols, m, n](uint32_t r, uint32_t c, const v4i& v) {
                     if (m + r < rows && n + c < cols) *(v4i*)(at + (int64_t)(m + r) * pitch + (n + c)) = v;
                 };
@@ -596,22 +634,21 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
             char* by = lds + Tl::kLds;
             if (p.out.at) {
                 t.template out16<false>(by, high, put(p.out, p.n, (uint32_t)p.out.pitch, m0, n0, false));
-                if constexpr (M::kPairs) t.template out16<false>(by, low, put(p.out, p.n, (uint32_t)p.out.pitch, m0, n0, true));
+                if constexpr (M::kPairP) t.template out16<false>(by, low, put(p.out, p.n, (uint32_t)p.out.pitch, m0, n0, true));
             }
             if (p.turned.at) {
                 t.template out16<true>(by, high, put(p.turned, p.count, p.turned_cols, n0, m0, false));
-                if constexpr (Low) t.template out16<true>(by, low, put(p.turned, p.count, p.turned_cols, n0, m0, true));
+                if constexpr (kLow) t.template out16<true>(by, low, put(p.turned, p.count, p.turned_cols, n0, m0, true));
             }
         });
 }
 
 // C = alpha A B^T over the columns that span.lines cover, of split number s from column s * lines on: rounded to T, on top of
 // `before` (fp32) and of C itself with `accumulate`.  Each split has a C of its own.
-template <class H>
 struct Product {
-    Plane<H> a, b;
+    Plane<G> a, b;
     int64_t m, n;
-    const Scales* scales;  // alpha is one over its p and that of w, or with of_x of x; NULL: one
+    const Scales* scales;  // alpha is one over its p and that of w, or with of_x of x
     bool of_x;
     void* c;
     int64_t ldc, split_stride;
@@ -642,8 +679,8 @@ __device__ __forceinline__ void finish4(T* c, const float* before, bool accumula
     }
 }
 
-template <class T, class H, int Terms, class Tl>
-__global__ __launch_bounds__(Tl::kThreads) void k_product(Product<H> p, Span span, Places places)
+template <class T, int Terms, class Tl>
+__global__ __launch_bounds__(Tl::kThreads) void k_product(Product p, Span span, Places places)
 {
     __shared__ __align__(1024) char lds[Tl::kLds];
     Tl t;
@@ -652,12 +689,12 @@ __global__ __launch_bounds__(Tl::kThreads) void k_product(Product<H> p, Span spa
         [&](uint32_t tile, int term) {
             uint32_t i, j, split;
             places.at(tile, i, j, split);
-            take<Terms>(t, term, p.a, p.m, p.b, p.n, (int64_t)split * span.lines * (kLine / (int)sizeof(H)), i * Tl::kM, j * Tl::kN);
+            take<Terms>(t, term, p.a, p.m, p.b, p.n, (int64_t)split * span.lines * (kLine / (int)sizeof(G)), i * Tl::kM, j * Tl::kN);
         },
         [&](uint32_t tile) {
             uint32_t ti, tj, split;
             places.at(tile, ti, tj, split);
-            const float alpha = p.scales ? 1.0f / (p.scales->p * (p.of_x ? p.scales->x : p.scales->w)) : 1.0f;
+            const float alpha = 1.0f / (p.scales->p * (p.of_x ? p.scales->x : p.scales->w));
             t.each([&](uint32_t row, uint32_t col, const v4f& v) {
                 const int64_t r = (int64_t)ti * Tl::kM + row, c = (int64_t)tj * Tl::kN + col;
                 if (r >= p.m || c >= p.n) return;
@@ -693,15 +730,14 @@ __global__ __launch_bounds__(256) void k_join_sums(const float* sums, int splits
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 int64_t parts(int64_t n, int64_t of) { return (n + of - 1) / of; }
 
-template <class M>
-constexpr int kPer = kLine / (int)sizeof(typename M::H);  // elements of a line
+constexpr int kPer = kLine / 2;  // elements of a line
 
 // Whether a matrix can be read where it is.
 template <class M>
 bool lies_in_lines(const Matrix& x, int64_t dim)
 {
     if (sizeof(typename M::T) != sizeof(typename M::H)) return false;
-    return dim % kPer<M> == 0 && x.ld % kPer<M> == 0 && x.ld * (int64_t)sizeof(typename M::H) < (1 << 24) && (uintptr_t)x.at % 16 == 0;
+    return dim % kPer == 0 && x.ld % kPer == 0 && x.ld * (int64_t)sizeof(typename M::H) < (1 << 24) && (uintptr_t)x.at % 16 == 0;
 }
 
 // The workspace, handed out in order.
@@ -728,10 +764,9 @@ struct Shape {
 };
 
 // f(a tile's type) for the tile of kTileCosts[pick]
-template <class M, class F>
+template <class Core, class F>
 void by_tile(int pick, const F& f)
 {
-    typedef typename M::Core Core;
     if (pick == 0)
         f(Shape<Tile<Core, 256, 256, 2, 2, 2>>());
     else if (pick == 1)
@@ -786,7 +821,7 @@ constexpr int64_t kFewBlocks = 512;
 template <class M>
 int64_t few_steps(int64_t rows, int64_t dim)
 {
-    return rows <= kFewRows ? parts(dim, kFewWaves * FewCore<typename M::T>::kStep) : 1 << 30;
+    return rows <= kFewRows && dim >= 8 ? parts(dim, kFewWaves * FewCore<typename M::T>::kStep) : 1 << 30;
 }
 template <class M>
 bool takes_few(int64_t rows, int64_t dim)
@@ -817,7 +852,7 @@ struct ForwardPlan {
     {
         Space s = {scratch, 0};
         const int64_t n = q.words.n, v = q.words.vocab, at_once = std::min(n, kRowsAtOnce);
-        pitch = up(q.dim, kPer<M>);
+        pitch = up(q.dim, kPer);
         few = takes_few<M>(n, q.dim);
         lay_x = !few && !lies_in_lines<M>(q.x, q.dim);
         lay_w = !few && !lies_in_lines<M>(q.w, q.dim);
@@ -826,7 +861,7 @@ struct ForwardPlan {
         x = lay_x ? s.plane<H>(n, pitch, M::kPairs) : Plane<H>{(H*)q.x.at, q.x.ld, 0};
         w = lay_w ? s.plane<H>(v, pitch, M::kPairs) : Plane<H>{(H*)q.w.at, q.w.ld, 0};
         auto pairs_of = [&](int64_t rows) {
-            const RowPlan plan = forward_plan<M>(rows, v, pitch / kPer<M>);
+            const RowPlan plan = forward_plan<M>(rows, v, pitch / kPer);
             return std::max(plan.rows * forward_width(plan.pick, v), (rows - plan.rows) * forward_width(plan.rest_pick, v));
         };
         pairs = s.get<float2>(few ? n * kFewBlocks : std::max(pairs_of(at_once), pairs_of((n - 1) % kRowsAtOnce + 1)));
@@ -858,19 +893,28 @@ void forward(const Entropy& q, char* scratch, hipStream_t s)
     if (f.few) {
         const int64_t groups = parts(v, 16), steps = few_steps<M>(n, q.dim);
         // a CU's registers hold two blocks where a wave's operands take few of them
-        const int64_t blocks = std::min(groups, steps <= (n <= 16 ? 8 : 4) ? kFewBlocks : kFewBlocks / 2);
+        const int64_t blocks = std::min(groups, steps <= (n <= 16 ? 10 : 6) ? kFewBlocks : kFewBlocks / 2);
         const Few<T> p = {(const T*)q.x.at, (const T*)q.w.at, q.x.ld, q.w.ld, (uint32_t)n, (uint32_t)q.dim, (uint32_t)groups, list(q.words), f.pairs, f.mine};
         auto go = [&](auto kernel) { kernel<<<(uint32_t)blocks, 64 * kFewWaves, 0, s>>>(p); };
         auto by_steps = [&](auto tiles) {
             constexpr int kTiles = decltype(tiles)::value;
-            if (steps <= 2)
+            // the kernel's steps are the call's or one more
+            if (steps <= 1)
+                go(k_few<T, 1, kTiles>);
+            else if (steps <= 2)
                 go(k_few<T, 2, kTiles>);
             else if (steps <= 4)
                 go(k_few<T, 4, kTiles>);
+            else if (steps <= 6)
+                go(k_few<T, 6, kTiles>);
             else if (steps <= 8)
                 go(k_few<T, 8, kTiles>);
+            else if (steps <= 10)
+                go(k_few<T, 10, kTiles>);
             else if (steps <= 12)
                 go(k_few<T, 12, kTiles>);
+            else if (steps <= 14)
+                go(k_few<T, 14, kTiles>);
             else
                 go(k_few<T, 16, kTiles>);
         };
@@ -886,15 +930,15 @@ void forward(const Entropy& q, char* scratch, hipStream_t s)
         const uint32_t across = (uint32_t)parts(f.pitch, 64);
         const Layout<T, H> lx = {source<T>(q.x, n, q.dim), f.lay_x ? f.x : Plane<H>{}, {}, f.lay_x ? (uint32_t)parts(n, 64) : 0, across};
         const Layout<T, H> lw = {source<T>(q.w, v, q.dim), f.lay_w ? f.w : Plane<H>{}, {}, f.lay_w ? (uint32_t)parts(v, 64) : 0, across};
-        k_layout<M><<<(lx.tiles_r + lw.tiles_r) * across, 256, 0, s>>>(lx, lw, f.part, f.scales);
+        k_layout<M, M::kPairs><<<(lx.tiles_r + lw.tiles_r) * across, 256, 0, s>>>(lx, lw, f.part, f.scales);
     }
     for (int64_t r = 0; r < n; r += kRowsAtOnce) {
         const int64_t rows = std::min(n - r, kRowsAtOnce);
-        const Span span = {(uint32_t)(f.x.pitch * sizeof(H)), (uint32_t)(f.w.pitch * sizeof(H)), (uint32_t)(f.pitch / kPer<M>)};
+        const Span span = {(uint32_t)(f.x.pitch * sizeof(H)), (uint32_t)(f.w.pitch * sizeof(H)), (uint32_t)(f.pitch / kPer)};
         auto logits = [&](int pick, int64_t row, int64_t rows) {
             const uint32_t width = (uint32_t)forward_width(pick, v);
             const WordList words = list(q.words).from(r + row);
-            by_tile<M>(pick, [&](auto shape) {
+            by_tile<typename M::Core>(pick, [&](auto shape) {
                 typedef typename decltype(shape)::Is Tl;
                 const Places places = {(uint32_t)parts(rows, Tl::kM), (uint32_t)parts(v, Tl::kN), (uint32_t)(parts(rows, Tl::kM) * parts(v, Tl::kN))};
                 const Plane<H> x = {f.x.at + (r + row) * f.x.pitch, f.x.pitch, f.x.low};
@@ -910,96 +954,97 @@ void forward(const Entropy& q, char* scratch, hipStream_t s)
 }
 
 // A piece of the vocabulary: as many words as keep P, both ways, at this size.
-constexpr int64_t kPieceBytes = (int64_t)512 << 20;
+constexpr int64_t kPieceBytes = (int64_t)1 << 30;
 
 template <class M>
 struct GradPlan {
     // Rows that are a large power of two apart would meet in a few of the memory's channels: a line more between them.
-    static int64_t spread(int64_t cols) { return cols * (int64_t)sizeof(typename M::H) % 4096 == 0 ? cols + kPer<M> : cols; }
+    static int64_t spread(int64_t cols) { return cols * (int64_t)sizeof(G) % 4096 == 0 ? cols + kPer : cols; }
 
     typedef typename M::H H;
     int64_t pitch, cols_n, cols_v, piece, pieces;  // columns of rows over n and over a piece's words
     int splits, pick_x;   // of the product for x's gradient
-    bool lay_x, lay_w, wide;  // wide: w's gradient in fp32, of 16-bit operands
+    bool lay_x, lay_w, wide;  // wide: w's gradient has more bits than the operands
     float* part;
     Scales* scales;
-    Plane<H> x, xt, w, wt, p, pt;
+    Plane<H> x, w;
+    Plane<G> xt, wt, p, pt;
     float* sums;
     size_t bytes;
+    static constexpr int kTerms = M::kPairs ? 3 : (M::kPairP ? 2 : 1);  // of the product for x's gradient
     GradPlan(const Entropy& q, char* scratch)
     {
         Space s = {scratch, 0};
         const int64_t n = q.words.n, v = q.words.vocab;
-        pitch = up(q.dim, kPer<M>);
-        cols_n = up(n, kPer<M>);
+        pitch = up(q.dim, kPer);
+        cols_n = up(n, kPer);
         lay_x = !lies_in_lines<M>(q.x, q.dim);
         lay_w = !lies_in_lines<M>(q.w, q.dim);
         wide = !M::kPairs && q.w_grad.at && q.w_grad.type == kGradF32;
-        const int64_t word = cols_n * (int64_t)sizeof(H) * ((q.x_grad.at ? 1 : 0) + (q.w_grad.at ? 1 : 0));
-        const int64_t most = std::min(std::max(kPieceBytes / (word * (M::kPairs ? 2 : 1)), (int64_t)1024), (int64_t)1 << 22);
+        const int64_t word = cols_n * (int64_t)sizeof(G) * ((q.x_grad.at ? 1 : 0) + (q.w_grad.at ? 1 : 0));
+        const int64_t most = std::min(std::max(kPieceBytes / (word * (M::kPairP ? 2 : 1)), (int64_t)1024), (int64_t)1 << 22);
         pieces = parts(v, most);
         piece = std::min(up(parts(v, pieces), 256), v);
         pieces = parts(v, piece);
         // The contraction over words is long and its tiles may be few.
         splits = 1;
         pick_x = 0;
-        int64_t lines = parts(piece, kPer<M>);
+        int64_t lines = parts(piece, kPer);
         if (q.x_grad.at) {
             double least = 0.0;
             for (int k = 1; k <= 64 && k * 8 <= std::max(lines, (int64_t)8); ++k) {
                 double t = 0.0;
                 const int64_t each = parts(lines, k);
-                const int pick = best_tile([&](int64_t side) { return parts(n, side) * parts(q.dim, side) * k; }, each * (M::kPairs ? 3 : 1), &t);
+                const int pick = best_tile([&](int64_t side) { return parts(n, side) * parts(q.dim, side) * k; }, each * kTerms, &t);
                 if (k > 1) t += 4.0 + 2e-6 * (double)n * (double)q.dim * k;  // sums through memory, and their launch
                 if (k == 1 || t < least) least = t, splits = k, pick_x = pick;
             }
         }
         lines = parts(lines, splits) * splits;
-        cols_v = lines * kPer<M>;
+        cols_v = lines * kPer;
         const int64_t pitch_n = spread(cols_n), pitch_v = spread(cols_v);
         scales = s.get<Scales>(1);
-        part = s.get<float>(M::kScaled ? 3 * kParts : 0);
+        part = s.get<float>(3 * kParts);
         x = lay_x ? s.plane<H>(n, pitch, M::kPairs) : Plane<H>{(H*)q.x.at, q.x.ld, 0};
         w = lay_w ? s.plane<H>(piece, pitch, M::kPairs) : Plane<H>{};
-        xt = wt = p = pt = Plane<H>{};
+        xt = wt = p = pt = Plane<G>{};
         if (q.w_grad.at) {
-            xt = s.plane<H>(q.dim, pitch_n, M::kPairs);
-            pt = s.plane<H>(piece, pitch_n, M::kPairs || wide);
+            xt = s.plane<G>(q.dim, pitch_n, M::kPairs);
+            pt = s.plane<G>(piece, pitch_n, M::kPairP || wide);
         }
         if (q.x_grad.at) {
-            wt = s.plane<H>(q.dim, pitch_v, M::kPairs);
-            p = s.plane<H>(n, pitch_v, M::kPairs);
+            wt = s.plane<G>(q.dim, pitch_v, M::kPairs);
+            p = s.plane<G>(n, pitch_v, M::kPairP);
         }
         sums = q.x_grad.at && (splits > 1 || pieces > 1) ? s.get<float>(splits * n * q.dim) : nullptr;
         bytes = s.used;
     }
 };
 
-template <class T, class M, int Terms>
-void product_part(int pick, const Product<typename M::H>& p, int64_t lines, int splits, hipStream_t s)
+template <class T, int Terms>
+void product_part(int pick, const Product& p, int64_t lines, int splits, hipStream_t s)
 {
-    typedef typename M::H H;
-    by_tile<M>(pick, [&](auto shape) {
+    by_tile<HalfCore>(pick, [&](auto shape) {
         typedef typename decltype(shape)::Is Tl;
         const uint32_t tm = (uint32_t)parts(p.m, Tl::kM), tn = (uint32_t)parts(p.n, Tl::kN);
         const Places places = {tm, tn, tm * tn * splits};
-        const Span span = {(uint32_t)(p.a.pitch * sizeof(H)), (uint32_t)(p.b.pitch * sizeof(H)), (uint32_t)lines};
-        k_product<T, H, Terms, Tl><<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places);
+        const Span span = {(uint32_t)(p.a.pitch * sizeof(G)), (uint32_t)(p.b.pitch * sizeof(G)), (uint32_t)lines};
+        k_product<T, Terms, Tl><<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places);
     });
 }
 
 // The same without splits, in the launches of a plan.
-template <class T, class M, int Terms>
-void product(const Product<typename M::H>& p, int64_t lines, hipStream_t s)
+template <class T, int Terms>
+void product(const Product& p, int64_t lines, hipStream_t s)
 {
     const RowPlan plan = plan_rows(p.m, p.n, lines * Terms);
     auto part = [&](int pick, int64_t first, int64_t rows) {
-        Product<typename M::H> r = p;
+        Product r = p;
         r.a.at += first * p.a.pitch;
         r.m = rows;
         r.c = (T*)p.c + first * p.ldc;
         if (p.before) r.before = p.before + first * p.n;
-        product_part<T, M, Terms>(pick, r, lines, 1, s);
+        product_part<T, Terms>(pick, r, lines, 1, s);
     };
     part(plan.pick, 0, plan.rows);
     if (plan.rows < p.m) part(plan.rest_pick, plan.rows, p.m - plan.rows);
@@ -1010,11 +1055,11 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
 {
     typedef typename M::T T;
     typedef typename M::H H;
-    constexpr int kTerms = M::kPairs ? 3 : 1;
+    constexpr int kTerms = GradPlan<M>::kTerms;
     const GradPlan<M> g(q, scratch);
     const int64_t n = q.words.n, v = q.words.vocab;
     const WordList words = list(q.words);
-    if (M::kScaled) tops<M>(q, M::kPairs, true, g.part, s);
+    tops<M>(q, M::kScaled, true, g.part, s);
     for (int64_t k = 0; k < g.pieces; ++k) {
         const int64_t first = k * g.piece, count = std::min(g.piece, v - first);
         const Plane<H> w = g.lay_w ? g.w : Plane<H>{(H*)q.w.at + first * q.w.ld, q.w.ld, 0};
@@ -1024,23 +1069,24 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
         if (k == 0 && (g.lay_x || g.xt.at)) lx.tiles_r = (uint32_t)parts(g.cols_n, 64);
         if (g.lay_w || g.wt.at) lw.tiles_r = (uint32_t)parts(g.wt.at ? g.cols_v : count, 64);
         const uint32_t blocks = (lx.tiles_r + lw.tiles_r) * lx.tiles_c;
-        if (blocks || (k == 0 && M::kScaled)) k_layout<M><<<blocks ? blocks : 1, 256, 0, s>>>(lx, lw, g.part, g.scales);
+        k_layout<M, true><<<blocks, 256, 0, s>>>(lx, lw, g.part, g.scales);  // one gradient at least has a transpose
 
-        const Span span = {(uint32_t)(g.x.pitch * sizeof(H)), (uint32_t)(w.pitch * sizeof(H)), (uint32_t)(g.pitch / kPer<M>)};
+        const Span span = {(uint32_t)(g.x.pitch * sizeof(H)), (uint32_t)(w.pitch * sizeof(H)), (uint32_t)(g.pitch / kPer)};
         const int64_t wide = g.p.at ? g.cols_v : count;  // padding of P's rows is written with the last tiles
         auto probs = [&](int pick, int64_t row, int64_t rows) {
-            by_tile<M>(pick, [&](auto shape) {
+            by_tile<typename M::Core>(pick, [&](auto shape) {
                 typedef typename decltype(shape)::Is Tl;
                 const uint32_t tm = (uint32_t)parts(rows, Tl::kM), tn = (uint32_t)parts(wide, Tl::kN);
                 const Places places = {tm, tn, tm * tn};
-                const Plane<H> x = {g.x.at + row * g.x.pitch, g.x.pitch, g.x.low}, out = {g.p.at ? g.p.at + row * g.p.pitch : nullptr, g.p.pitch, g.p.low};
+                const Plane<H> x = {g.x.at + row * g.x.pitch, g.x.pitch, g.x.low};
+                const Plane<G> out = {g.p.at ? g.p.at + row * g.p.pitch : nullptr, g.p.pitch, g.p.low};
                 // columns of the transpose up to the pitch are this launch's if the last rows are
-                const Plane<H> turned = {g.pt.at ? g.pt.at + row : nullptr, g.pt.pitch, g.pt.low};
+                const Plane<G> turned = {g.pt.at ? g.pt.at + row : nullptr, g.pt.pitch, g.pt.low};
                 const Probs<H> p = {x, w, (uint32_t)rows, (uint32_t)count, (uint32_t)first, words.from(row), q.lse + row,
                                     q.loss_grad ? q.loss_grad + row : nullptr, out, turned,
                                     (uint32_t)(row + rows < n ? rows : g.cols_n - row), g.scales};
                 auto go = [&](auto kernel) { kernel<<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places); };
-                if constexpr (M::kPairs)
+                if constexpr (M::kPairP)
                     go(k_probs<M, true, Tl>);
                 else if (g.wide)
                     go(k_probs<M, true, Tl>);
@@ -1048,31 +1094,30 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
                     go(k_probs<M, false, Tl>);
             });
         };
-        const RowPlan plan = plan_rows(n, wide, span.lines * kTerms);
+        const RowPlan plan = plan_rows(n, wide, span.lines * (M::kPairs ? 3 : 1));
         probs(plan.pick, 0, plan.rows);
         if (plan.rows < n) probs(plan.rest_pick, plan.rows, n - plan.rows);
-        const Scales* scales = M::kScaled ? g.scales : nullptr;
         if (q.x_grad.at) {
-            const int64_t lines = g.cols_v / kPer<M> / g.splits;
+            const int64_t lines = g.cols_v / kPer / g.splits;
             if (g.splits > 1 || k + 1 < g.pieces) {
-                const Product<H> p = {g.p, g.wt, n, q.dim, scales, false, g.sums, q.dim, n * q.dim, k > 0, nullptr};
-                product_part<float, M, kTerms>(g.pick_x, p, lines, g.splits, s);
+                const Product p = {g.p, g.wt, n, q.dim, g.scales, false, g.sums, q.dim, n * q.dim, k > 0, nullptr};
+                product_part<float, kTerms>(g.pick_x, p, lines, g.splits, s);
             } else {
-                const Product<H> p = {g.p, g.wt, n, q.dim, scales, false, q.x_grad.at, q.x_grad.ld, 0, false, g.pieces > 1 ? g.sums : nullptr};
-                product_part<T, M, kTerms>(g.pick_x, p, lines, 1, s);
+                const Product p = {g.p, g.wt, n, q.dim, g.scales, false, q.x_grad.at, q.x_grad.ld, 0, false, g.pieces > 1 ? g.sums : nullptr};
+                product_part<T, kTerms>(g.pick_x, p, lines, 1, s);
             }
         }
         if (q.w_grad.at) {
             char* c = (char*)q.w_grad.at + first * q.w_grad.ld * (q.w_grad.type == kGradF32 ? 4 : 2);
-            const Product<H> p = {g.pt, g.xt, count, q.dim, scales, true, c, q.w_grad.ld, 0, q.accumulate, nullptr};
-            const int64_t lines = g.cols_n / kPer<M>;
+            const Product p = {g.pt, g.xt, count, q.dim, g.scales, true, c, q.w_grad.ld, 0, q.accumulate, nullptr};
+            const int64_t lines = g.cols_n / kPer;
             if constexpr (M::kPairs) {
-                product<float, M, 3>(p, lines, s);
+                product<float, 3>(p, lines, s);
             } else {
                 if (g.wide)
-                    product<float, M, 2>(p, lines, s);
+                    product<float, 2>(p, lines, s);
                 else
-                    product<T, M, 1>(p, lines, s);
+                    product<T, kTerms>(p, lines, s);
             }
         }
     }

@@ -63,7 +63,9 @@ class CrossEntropy:
     u = 2^-24 is a rounding to 32 bits.  A logit is a sum of k products in 32 bits, off by at most (k + 16) u times the sum of
     their magnitudes; fp32 operands as pairs of halves miss 2^-22 of each factor and the product of what the first halves
     leave, 2^-22 again, and below the halves' range 2^-40 of the largest magnitude.  exp and log are those of powers of two, of
-    an argument rounded to 32 bits twice.  P is rounded once to what it is stored in."""
+    an argument rounded to 32 bits twice.  P is rounded once to what it is stored in: a half for bf16 gradients, else a pair of
+    halves, under a power of two of which its largest element may have 2^15; bf16 operands of its products are halves like
+    fp32 ones, exactly but for that range."""
 
     def __init__(self, x, w, words, g=None):
         import torch
@@ -93,16 +95,15 @@ class CrossEntropy:
         p[torch.arange(len(x), device=x.device), at] -= 1
         self.p, self.g = p * g[:, None], g
 
-    def _gradient(self, p, p_off, other, pairs, out):
-        """p @ other, both in 64 bits, and the bound; pairs: P is a pair of the operands' halves."""
+    def _gradient(self, p, p_off, other, out):
+        """p @ other, both in 64 bits, and the bound."""
         import torch
-        f32, bf16 = self.type is torch.float32, self.type is torch.bfloat16
-        step = 2.0**-8 if bf16 else 2.0**-11
-        step = step * step if pairs or f32 else step
-        least = 0.0 if bf16 else 2.0**-39 * float(self.g.abs().max())
+        f32 = self.type is torch.float32
+        step = 2.0**-11 if out is torch.bfloat16 else 2.0**-22
+        least = 2.0**-39 * float(self.g.abs().max())
         off = (p_off + p.abs() * step + least) @ other.abs()
         off = off + ((p.shape[1] + 16) * self.u + (3 * 2.0**-22 if f32 else 0.0)) * (p.abs() @ other.abs())
-        if f32 and other.numel():
+        if self.type is not torch.float16:
             off = off + 2.0**-40 * other.abs().max() * p.abs().sum(1)[:, None]
         info = torch.finfo(out)
         want = p @ other
@@ -110,13 +111,13 @@ class CrossEntropy:
 
     def x_grad(self):
         """(value, bound)"""
-        want, off, rel, least = self._gradient(self.p, self.p_off, self.w, False, self.type)
+        want, off, rel, least = self._gradient(self.p, self.p_off, self.w, self.type)
         return want, off + (want.abs() + off) * rel + least
 
     def w_grad(self, out, before=None):
         import torch
         x = torch.where(self.ok[:, None], self.x, 0.0)
-        want, off, rel, least = self._gradient(self.p.t(), self.p_off.t(), x, out is torch.float32, out)
+        want, off, rel, least = self._gradient(self.p.t(), self.p_off.t(), x, out)
         if before is not None:
             off = off + self.u * (before.double().abs() + want.abs())
             want = want + before.double()
