@@ -72,7 +72,7 @@ void by_mode(int type, const F& f)
 struct Scales {
     float x, w, p;
 };
-constexpr int kParts = 512;  // blocks of k_top, and partial results of each of the three
+constexpr int kParts = 1024;  // blocks of k_top, and partial results of each of the three
 
 // What brings a largest magnitude to 2^14 to 2^15; 1 for zeros.
 __device__ __forceinline__ float scale_of(float top)
@@ -94,17 +94,29 @@ struct Source {
 template <class T>
 __device__ __forceinline__ float top_of(const Source<T>& p)
 {
+    constexpr int kEach = 4;  // rows under way
     float top = 0.0f;
-    for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
-        if (p.words.at && p.words.none(r)) continue;
-        for (int64_t c = threadIdx.x * 8; c < p.cols; c += 256 * 8) {
-            Eight<T> v;
-            v.load(p.at + r * p.ld + c, p.cols - c);
+    for (int64_t r = blockIdx.x; r < p.rows; r += (int64_t)gridDim.x * kEach) {
+        bool in[kEach];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float m = fabsf(v.get(i));
-                top = m < INFINITY && m > top ? m : top;
-            }
+        for (int e = 0; e < kEach; ++e) {
+            const int64_t row = r + (int64_t)e * gridDim.x;
+            in[e] = row < p.rows && !(p.words.at && p.words.none(row));
+        }
+        for (int64_t c = threadIdx.x * 8; c < p.cols; c += 256 * 8) {
+            Eight<T> v[kEach];
+#pragma unroll
+            for (int e = 0; e < kEach; ++e)
+                if (in[e]) v[e].load(p.at + (r + (int64_t)e * gridDim.x) * p.ld + c, p.cols - c);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e)
+                if (in[e]) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float m = fabsf(v[e].get(i));
+                        top = m < INFINITY && m > top ? m : top;
+                    }
+                }
         }
     }
     return top;
@@ -132,7 +144,9 @@ __global__ __launch_bounds__(256) void k_top(Source<T> x, Source<T> w, Source<fl
 // The largest of one of the three, for the whole block of 256.
 __device__ __forceinline__ float joined_top(const float* part, float* lds)
 {
-    float top = fmaxf(part[threadIdx.x], part[threadIdx.x + 256]);
+    float top = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kParts / 256; ++k) top = fmaxf(top, part[k * 256 + threadIdx.x]);
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
@@ -599,6 +613,10 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                 }
 #pragma unroll
                 for (int j = 0; j < Tl::kNt; ++j) acc[j] *= gain;
+                if (none) {  // zeros whatever the row holds
+#pragma unroll
+                    for (int j = 0; j < Tl::kNt; ++j) acc[j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                }
                 if (edge) {  // zeros behind the piece's last word
                     const int left = (int)(p.count - n0 - col);
 #pragma unroll
@@ -606,10 +624,10 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[j][e] = left > j * 16 + e ? acc[j][e] : 0.0f;
                 }
-                auto packed = [&](const v4f& v) -> Four16 {
+                auto packed = [](const v4f& v) -> Four16 {
                     typedef G h2 __attribute__((ext_vector_type(2)));
                     const uint32_t a = __builtin_bit_cast(uint32_t, h2{(G)v[0], (G)v[1]}), b = __builtin_bit_cast(uint32_t, h2{(G)v[2], (G)v[3]});
-                    return {none ? 0 : a, none ? 0 : b};
+                    return {a, b};
                 };
 #pragma unroll
                 for (int j = 0; j < Tl::kNt; ++j) {
@@ -624,11 +642,12 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
-            // Eight neighbours of row r from column c on; columns behind the last are zeros up to the pitch.
+            // Eight neighbours of row r from column c on, of the tile at (m, n); columns behind the last are zeros up to the pitch.  A
+            // tile's places are within 32 bits of its first.
             auto put = [](const Plane<G>& o, uint32_t rows, uint32_t cols, uint32_t m, uint32_t n, bool low) {
-                G* at = o.at + (low ? o.low : 0);
-                return [at, pitch = o.pitch, rows, cols, m, n](uint32_t r, uint32_t c, const v4i& v) {
-                    if (m + r < rows && n + c < cols) *(v4i*)(at + (int64_t)(m + r) * pitch + (n + c)) = v;
+                char* at = (char*)(o.at + (low ? o.low : 0) + (int64_t)m * o.pitch + n);
+                return [at, pitch = (uint32_t)o.pitch * 2, rows = rows - m, cols = cols - n](uint32_t r, uint32_t c, const v4i& v) {
+                    if ((int)r < (int)rows && (int)c < (int)cols) *(v4i*)(at + (r * pitch + c * 2)) = v;
                 };
             };
             char* by = lds + Tl::kLds;
