@@ -940,29 +940,74 @@ WORD_I32, WORD_I64 = 0, 1
 _word_types = None  # torch's integer types as the C ABI numbers them
 
 
-def _words(words, name):
-    """Address, type and number of a contiguous CUDA tensor of words, of any shape."""
+# Small calls take the GPU about as long as the host, so these do in fewer steps what _matrix and _stream_handle do, and leave to them
+# whatever is out of the ordinary.  A call's tensors are all on the current device: what another one's memory looks like from here
+# is not known.
+
+
+def _words(words, name, device):
+    """Address, type and number of a contiguous tensor of words on that device, of any shape."""
     global _word_types
     if _word_types is None:
         torch = _torch or _import_torch()
         _word_types = {torch.int32: WORD_I32, torch.int64: WORD_I64}
-    torch = _torch or _import_torch()
-    code = _word_types.get(words.dtype) if isinstance(words, torch.Tensor) else None
+    code = _word_types.get(words.dtype) if isinstance(words, _torch.Tensor) else None
     if code is None or not words.is_cuda or not words.is_contiguous():
         raise TypeError(f"{name} must be a contiguous CUDA tensor of dtype int32 or int64")
+    if words.get_device() != device:
+        raise ValueError(f"{name} must be on the other tensors' device")
     return words.data_ptr(), code, words.numel()
+
+
+def _rows(x, name, device=None):
+    """Address, element code, rows, columns, row stride and device of a CUDA matrix whose rows are contiguous."""
+    ordinary = False
+    if _types is not None and isinstance(x, _torch.Tensor) and x.dim() == 2:
+        code, own = _types.get(x.dtype), x.get_device()
+        rows, cols = x.shape
+        ld, step = x.stride()
+        ordinary = code is not None and own >= 0 and step == 1 and ld >= cols and rows > 1
+    if not ordinary:
+        code, ld = _matrix(x, name)
+        rows, cols = x.shape
+        own = x.get_device()
+    if device is not None and own != device:
+        raise ValueError(f"{name} must be on the other tensors' device")
+    return x.data_ptr(), code, rows, cols, ld, own
+
+
+def _vector(t, name, n, device):
+    """Address of a contiguous float32 tensor of at least n elements on that device."""
+    torch = _torch or _import_torch()
+    _check_tensor(t, torch.float32, name, n)
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the other tensors' device")
+    return t.data_ptr()
+
+
+_raw_stream = _current_device = None
+
+
+def _stream_on(stream, device):
+    """The handle of a stream, or of the current one, of the tensors' device, which has to be the current one."""
+    global _raw_stream, _current_device
+    if _current_device is None:
+        raw, current = getattr(_torch._C, "_cuda_getCurrentRawStream", None), getattr(_torch._C, "_cuda_getDevice", None)
+        _current_device = current or _torch.cuda.current_device
+        _raw_stream = raw or (lambda device: _torch.cuda.current_stream(device).cuda_stream)
+    if device != _current_device():
+        raise ValueError("the tensors must be on the current device")
+    return _raw_stream(device) if stream is None else stream.cuda_stream
 
 
 def sidco_embedding(table, words, out, scale: float = 1.0, stream=None) -> None:
     """out[i] = scale * table[words[i]], zeros where words[i] is no row of the table; out has a row for each word."""
-    code, ldt = _matrix(table, "table")
-    out_code, ldo = _matrix(out, "out")
-    w, word_type, n = _words(words, "words")
-    vocab, dim = table.shape
-    if out.shape[0] != n or out.shape[1] != dim:
+    t, code, vocab, dim, ldt, device = _rows(table, "table")
+    o, out_code, rows, cols, ldo, _ = _rows(out, "out", device)
+    w, word_type, n = _words(words, "words", device)
+    if rows != n or cols != dim:
         raise ValueError("out must have a row of the table's length for each word")
-    rc = load().sidco_embedding(_stream_handle(stream), table.data_ptr(), code, vocab, dim, ldt, w, word_type, n, scale, out.data_ptr(),
-                                out_code, ldo)
+    rc = load().sidco_embedding(_stream_on(stream, device), t, code, vocab, dim, ldt, w, word_type, n, scale, o, out_code, ldo)
     if rc:
         raise SidcoError(rc, "sidco_embedding")
 
@@ -973,14 +1018,13 @@ def sidco_workspace_bytes_embedding_grad(n: int, dim: int) -> int:
 
 def sidco_embedding_grad(grad, words, table_grad, scale: float = 1.0, accumulate: bool = False, stream=None) -> None:
     """table_grad[v] (+)= scale * the sum of grad's rows whose word is v."""
-    code, ldg = _matrix(grad, "grad")
-    table_code, ldt = _matrix(table_grad, "table_grad")
-    w, word_type, n = _words(words, "words")
-    vocab, dim = table_grad.shape
-    if grad.shape[0] != n or grad.shape[1] != dim:
+    g, code, rows, cols, ldg, device = _rows(grad, "grad")
+    t, table_code, vocab, dim, ldt, _ = _rows(table_grad, "table_grad", device)
+    w, word_type, n = _words(words, "words", device)
+    if rows != n or cols != dim:
         raise ValueError("grad must have a row of the table's length for each word")
-    rc = load().sidco_embedding_grad(_stream_handle(stream), grad.data_ptr(), code, n, dim, ldg, w, word_type, vocab, scale,
-                                     1 if accumulate else 0, table_grad.data_ptr(), table_code, ldt)
+    rc = load().sidco_embedding_grad(_stream_on(stream, device), g, code, n, dim, ldg, w, word_type, vocab, scale, 1 if accumulate else 0, t,
+                                     table_code, ldt)
     if rc:
         raise SidcoError(rc, "sidco_embedding_grad")
 
@@ -996,38 +1040,37 @@ def sidco_dropout(x, out, p: float, seed: int, offset: int = 0, residual=None, d
     """out = x with elements dropped with probability p and the others scaled, plus residual (of out's type) if given.  seed and
     offset (in blocks of the sequence) are taken modulo 2^64; device_offset, a CUDA tensor of one int64, is added to the
     offset when the call runs."""
-    code, ldx = _matrix(x, "x")
-    out_code, ldo = _matrix(out, "out")
-    rows, cols = x.shape
-    if out.shape[0] != rows or out.shape[1] != cols:
+    a, code, rows, cols, ldx, device = _rows(x, "x")
+    o, out_code, out_rows, out_cols, ldo, _ = _rows(out, "out", device)
+    if out_rows != rows or out_cols != cols:
         raise ValueError("out must have x's shape")
-    ldr, torch = 0, _torch
+    r, ldr = None, 0
     if residual is not None:
-        res_code, ldr = _matrix(residual, "residual")
+        r, res_code, res_rows, res_cols, ldr, _ = _rows(residual, "residual", device)
         if res_code != out_code:
             raise TypeError("residual must have out's dtype")
-        if residual.shape != out.shape:
+        if res_rows != rows or res_cols != cols:
             raise ValueError("residual must have x's shape")
     if device_offset is not None:
-        _check_tensor(device_offset, torch.int64, "device_offset", 1)
-    rc = load().sidco_dropout(_stream_handle(stream), x.data_ptr(), code, rows, cols, ldx, p, seed & 0xFFFFFFFFFFFFFFFF,
-                              offset & 0xFFFFFFFFFFFFFFFF, _ptr(device_offset), _ptr(residual), ldr, out.data_ptr(), out_code, ldo)
+        _check_tensor(device_offset, _torch.int64, "device_offset", 1)
+        if device_offset.get_device() != device:
+            raise ValueError("device_offset must be on the other tensors' device")
+    rc = load().sidco_dropout(_stream_on(stream, device), a, code, rows, cols, ldx, p, seed & 0xFFFFFFFFFFFFFFFF, offset & 0xFFFFFFFFFFFFFFFF,
+                              _ptr(device_offset), r, ldr, o, out_code, ldo)
     if rc:
         raise SidcoError(rc, "sidco_dropout")
 
 
 def _logits(x, weight, targets):
     """Arguments that both cross entropy calls begin with, and their sizes."""
-    code, ldx = _matrix(x, "x")
-    w_code, ldw = _matrix(weight, "weight")
+    a, code, rows, dim, ldx, device = _rows(x, "x")
+    b, w_code, vocab, cols, ldw, _ = _rows(weight, "weight", device)
     if w_code != code:
         raise TypeError("weight must have x's dtype")
-    w, word_type, n = _words(targets, "targets")
-    dim = x.shape[1]
-    if weight.shape[1] != dim or x.shape[0] != n:
+    w, word_type, n = _words(targets, "targets", device)
+    if cols != dim or rows != n:
         raise ValueError("weight must have x's columns, and targets a word for each of its rows")
-    vocab = weight.shape[0]
-    return (x.data_ptr(), weight.data_ptr(), code, n, dim, vocab, ldx, ldw, w, word_type), n, dim, vocab, code
+    return (a, b, code, n, dim, vocab, ldx, ldw, w, word_type), n, code, device
 
 
 def sidco_workspace_bytes_cross_entropy(n: int, dim: int, vocab: int, dtype: int) -> int:
@@ -1036,12 +1079,10 @@ def sidco_workspace_bytes_cross_entropy(n: int, dim: int, vocab: int, dtype: int
 
 def sidco_cross_entropy(x, weight, targets, loss, lse, stream=None) -> None:
     """loss[i] = lse[i] - (x weight^T)[i, targets[i]], lse[i] the logarithm of the row's sum of exponentials; either may be None."""
-    torch = _torch or _import_torch()
-    args, n, *_ = _logits(x, weight, targets)
-    for t, name in ((loss, "loss"), (lse, "lse")):
-        if t is not None:
-            _check_tensor(t, torch.float32, name, n)
-    rc = load().sidco_cross_entropy(_stream_handle(stream), *args, _ptr(loss), _ptr(lse))
+    args, n, _, device = _logits(x, weight, targets)
+    a = None if loss is None else _vector(loss, "loss", n, device)
+    b = None if lse is None else _vector(lse, "lse", n, device)
+    rc = load().sidco_cross_entropy(_stream_on(stream, device), *args, a, b)
     if rc:
         raise SidcoError(rc, "sidco_cross_entropy")
 
@@ -1055,24 +1096,22 @@ def sidco_cross_entropy_grad(x, weight, targets, lse, loss_grad, x_grad=None, we
     """The gradients of the sum of loss_grad[i] * loss[i] (None: of the losses' sum) with respect to x, in its dtype, and weight, in its
     dtype or float32, or with `accumulate` added to what weight_grad holds; either may be None.  lse is what sidco_cross_entropy
     wrote."""
-    torch = _torch or _import_torch()
-    args, n, dim, vocab, code = _logits(x, weight, targets)
-    _check_tensor(lse, torch.float32, "lse", n)
-    if loss_grad is not None:
-        _check_tensor(loss_grad, torch.float32, "loss_grad", n)
+    args, n, code, device = _logits(x, weight, targets)
+    sums = _vector(lse, "lse", n, device)
+    g = None if loss_grad is None else _vector(loss_grad, "loss_grad", n, device)
+    gx = gw = None
     ldgx = ldgw = w_code = 0
     if x_grad is not None:
-        x_code, ldgx = _matrix(x_grad, "x_grad")
+        gx, x_code, rows, cols, ldgx, _ = _rows(x_grad, "x_grad", device)
         if x_code != code:
             raise TypeError("x_grad must have x's dtype")
         if x_grad.shape != x.shape:
             raise ValueError("x_grad must have x's shape")
     if weight_grad is not None:
-        w_code, ldgw = _matrix(weight_grad, "weight_grad")
+        gw, w_code, rows, cols, ldgw, _ = _rows(weight_grad, "weight_grad", device)
         if weight_grad.shape != weight.shape:
             raise ValueError("weight_grad must have weight's shape")
-    rc = load().sidco_cross_entropy_grad(_stream_handle(stream), *args, lse.data_ptr(), _ptr(loss_grad), _ptr(x_grad), ldgx, _ptr(weight_grad),
-                                         w_code, ldgw, 1 if accumulate else 0)
+    rc = load().sidco_cross_entropy_grad(_stream_on(stream, device), *args, sums, g, gx, ldgx, gw, w_code, ldgw, 1 if accumulate else 0)
     if rc:
         raise SidcoError(rc, "sidco_cross_entropy_grad")
 

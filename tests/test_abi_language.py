@@ -109,9 +109,8 @@ def test_cross_entropy_refusals(lib):
         (-9, [dict(dt=2), dict(dt=1), dict(t=1, dt=2), dict(acc=2), dict(dx=OK), dict(dx=OTHER), dict(dw=OK), dict(dw=OTHER), dict(dw=C.c_void_p(1 << 14))])])
     assert sidco.sidco_workspace_bytes_cross_entropy(0, 5, 5, 0) == 0 and sidco.sidco_workspace_bytes_cross_entropy(5, 5, 5, 3) == 0
     assert sidco.sidco_workspace_bytes_cross_entropy_grad(5, 5, 5, 1, 2) == 0
-    half = sidco.sidco_workspace_bytes_cross_entropy_grad(700, 1500, 10_000, 1, 1)
-    assert 0 < half < sidco.sidco_workspace_bytes_cross_entropy_grad(700, 1500, 10_000, 1, 0) < sidco.sidco_workspace_bytes_cross_entropy_grad(
-        700, 1500, 10_000, 0, 0)
+    bytes_of = lambda t, o: sidco.sidco_workspace_bytes_cross_entropy_grad(700, 1500, 10_000, t, o)  # noqa: E731
+    assert 0 < bytes_of(2, 2) < bytes_of(2, 0) < bytes_of(1, 0) == bytes_of(1, 1) < bytes_of(0, 0)
 
 
 def test_reference_loss_by_hand():
@@ -132,6 +131,7 @@ def test_binding_refuses_what_is_no_tensor_of_the_card(lib):
     words = torch.zeros(4, dtype=torch.int64)
     for call in (lambda: sidco.sidco_embedding(x, words, x), lambda: sidco.sidco_embedding(None, words, x),
                  lambda: sidco.sidco_embedding_grad(x, words, x), lambda: sidco.sidco_dropout(x, x, 0.5, 1),
-                 lambda: sidco.sidco_dropout([1.0], x, 0.5, 1)):
+                 lambda: sidco.sidco_dropout([1.0], x, 0.5, 1), lambda: sidco.sidco_cross_entropy(x, x, words, x, x),
+                 lambda: sidco.sidco_cross_entropy_grad(x, x, words, x, None, x)):
         with pytest.raises(TypeError):
             call()

@@ -198,3 +198,27 @@ def test_far_rows():
     assert torch.equal(out, torch.arange(40, device="cuda").view(5, 8).float())
     sidco.sidco_embedding_grad(out, words, table, accumulate=True)
     assert torch.equal(table[words].float(), 2 * out)
+
+
+def test_binding_refuses_other_shapes_and_types():
+    torch, sidco = _torch(), _sidco()
+    x, words = torch.zeros(6, 8, device="cuda"), torch.zeros(6, dtype=torch.int64, device="cuda")
+    table, loss = torch.zeros(10, 8, device="cuda"), torch.zeros(6, device="cuda")
+    for wrong in (lambda: sidco.sidco_embedding(table, words, x[:5]), lambda: sidco.sidco_embedding(table, words, x[:, :7]),
+                  lambda: sidco.sidco_embedding_grad(x[:5], words, table), lambda: sidco.sidco_dropout(x, table, 0.5, 1),
+                  lambda: sidco.sidco_dropout(x, x, 0.5, 1, residual=table), lambda: sidco.sidco_cross_entropy(x, table, words[:5], loss, None),
+                  lambda: sidco.sidco_cross_entropy(x, table[:, :7], words, loss, None), lambda: sidco.sidco_cross_entropy(x, table, words, loss[:5], None),
+                  lambda: sidco.sidco_cross_entropy_grad(x, table, words, loss, None, x_grad=table),
+                  lambda: sidco.sidco_cross_entropy_grad(x, table, words, loss, None, weight_grad=x)):
+        with pytest.raises(ValueError):
+            wrong()
+    for wrong in (lambda: sidco.sidco_embedding(table, words.float(), x), lambda: sidco.sidco_embedding(table, words[::2], x[:3]),
+                  lambda: sidco.sidco_embedding(table.t(), words, x), lambda: sidco.sidco_embedding(table.double(), words, x),
+                  lambda: sidco.sidco_embedding(table.cpu(), words, x), lambda: sidco.sidco_embedding(table, words.cpu(), x),
+                  lambda: sidco.sidco_dropout(x, x, 0.5, 1, residual=x.half()), lambda: sidco.sidco_cross_entropy(x, table.half(), words, loss, None),
+                  lambda: sidco.sidco_cross_entropy(x, table, words, loss.double(), None),
+                  lambda: sidco.sidco_cross_entropy_grad(x, table, words, loss, None, x_grad=x.half())):
+        with pytest.raises(TypeError):
+            wrong()
+    with pytest.raises(sidco.SidcoError):
+        sidco.sidco_cross_entropy_grad(x, table, words, loss, None, weight_grad=table.half())
