@@ -802,24 +802,64 @@ Source<T> source(const Matrix& m, int64_t rows, int64_t cols, const WordList& wo
     return {m.at ? (const T*)m.at + first * m.ld : nullptr, m.ld, rows, cols, words};
 }
 
+// Which tile: as for the products of codes, the time of a product is that of its rounds, with what these products' ends cost.  A
+// round ends with all tiles' stores at once; two blocks to a CU have one's end beside the other's products.  Measured, us a
+// kernel, tiles of 256, 192, 128, 64 (n x dim x vocab, pairs of P but for bf16):
+//   logits   700 x 1500 x 10000 fp32 98 71 68 103; 2049 x 1024 x 49999 fp16 235 256 265 421; 4000 x 512 x 20000 102 115 102 171;
+//            300 x 700 x 5000 bf16 23.6 17.4 12.4 8.2; 512 x 1024 x 32768 bf16 42 59 42 64
+//   P        116 84 76 110; 367 387 431 590; 218 210 189 259; 30 20 13.4 8.8; 51 72 46 64
+//   w_grad   72 69 73 103; 460 494 498 796; 204 250 257 331; 22.9 15 9.4 8.8; 64 76 51 73
+enum Kind { kLogits, kProbs, kProbPairs, kProduct };
+struct HalfCost {
+    float alone, line, thrice;  // us a line of 128 bytes, one tile to a CU or kTileCosts' per_cu; of pairs, whose lines come three times
+    float launch, end[4];
+};
+constexpr HalfCost kHalfCosts[] = {{1.27f, 1.27f, 1.20f, 8.0f, {9.0f, 23.0f, 34.0f, 16.0f}},
+                                   {1.06f, 1.06f, 0.95f, 7.0f, {4.0f, 10.0f, 15.0f, 6.0f}},
+                                   {0.80f, 1.27f, 0.95f, 5.5f, {1.0f, 2.0f, 10.0f, 2.5f}},
+                                   {0.25f, 0.48f, 0.35f, 4.5f, {0.5f, 1.0f, 1.5f, 1.0f}}};
+
+double half_time(Kind kind, int terms, int pick, int64_t tiles, int64_t lines)
+{
+    const HalfCost& c = kHalfCosts[pick];
+    const int64_t slots = (int64_t)kCus * kTileCosts[pick].per_cu, left = tiles % slots;
+    const float line = terms == 3 ? c.thrice : c.line, alone = line < c.alone ? line : c.alone;
+    double t = c.launch + (double)(tiles / slots) * (lines * terms * line + c.end[kind]);
+    if (left) t += lines * terms * (left <= kCus ? alone : line) + c.end[kind];
+    return t;
+}
+
+// count(side): tiles of the whole launch.
+template <class Count>
+int best_half(Kind kind, int terms, const Count& count, int64_t lines, double* time)
+{
+    int best = 0;
+    for (int i = 0; i < 4; ++i) {
+        const double t = half_time(kind, terms, i, count(kTileCosts[i].side), lines);
+        if (i == 0 || t < *time) *time = t, best = i;
+    }
+    return best;
+}
+
 // Rows in one launch or two: as many large tiles as fill whole rounds or whole tiles, and the rest in tiles of its own.
 struct RowPlan {
     int pick, rest_pick;
     int64_t rows;  // of the first launch
 };
-RowPlan plan_rows(int64_t m, int64_t n, int64_t lines)
+RowPlan plan_rows(Kind kind, int terms, int64_t m, int64_t n, int64_t lines)
 {
     auto tiles = [&](int64_t rows, int64_t side) { return parts(rows, side) * parts(n, side); };
-    double least = 0.0;
-    RowPlan plan = {best_tile([&](int64_t side) { return tiles(m, side); }, lines, &least), 0, m};
+    double least = 0.0, best = 0.0;
+    RowPlan plan = {best_half(kind, terms, [&](int64_t side) { return tiles(m, side); }, lines, &least), 0, m};
+    best = least;
     for (int i = 0; i < 3; ++i) {
         const int64_t side = kTileCosts[i].side, strip = parts(n, side), slots = (int64_t)kCus * kTileCosts[i].per_cu;
         for (const int64_t rows : {m / side * side, tiles(m, side) / slots * slots / strip * side}) {
             if (rows <= 0 || rows >= m) continue;
             double rest = 0.0;
-            const int rest_pick = best_tile([&](int64_t s) { return tiles(m - rows, s); }, lines, &rest);
-            const double t = tile_time(i, tiles(rows, side), lines) + rest;
-            if (t < least) least = t, plan = {i, rest_pick, rows};
+            const int rest_pick = best_half(kind, terms, [&](int64_t s) { return tiles(m - rows, s); }, lines, &rest);
+            const double t = half_time(kind, terms, i, tiles(rows, side), lines) + rest + 5.0 + 0.05 * least;  // two are worth it if clearly better
+            if (t < best) best = t, plan = {i, rest_pick, rows};
         }
     }
     return plan;
@@ -831,7 +871,7 @@ constexpr int64_t kRowsAtOnce = 16384;  // of the forward pass
 template <class M>
 RowPlan forward_plan(int64_t rows, int64_t vocab, int64_t lines)
 {
-    return plan_rows(rows, vocab, lines * (M::kPairs ? 3 : 1));
+    return plan_rows(kLogits, M::kPairs ? 3 : 1, rows, vocab, lines);
 }
 int64_t forward_width(int pick, int64_t vocab) { return 2 * parts(vocab, kTileCosts[pick].side); }
 
@@ -1014,7 +1054,7 @@ struct GradPlan {
             for (int k = 1; k <= 64 && k * 8 <= std::max(lines, (int64_t)8); ++k) {
                 double t = 0.0;
                 const int64_t each = parts(lines, k);
-                const int pick = best_tile([&](int64_t side) { return parts(n, side) * parts(q.dim, side) * k; }, each * kTerms, &t);
+                const int pick = best_half(kProduct, kTerms, [&](int64_t side) { return parts(n, side) * parts(q.dim, side) * k; }, each, &t);
                 if (k > 1) t += 4.0 + 2e-6 * (double)n * (double)q.dim * k;  // sums through memory, and their launch
                 if (k == 1 || t < least) least = t, splits = k, pick_x = pick;
             }
@@ -1056,7 +1096,7 @@ void product_part(int pick, const Product& p, int64_t lines, int splits, hipStre
 template <class T, int Terms>
 void product(const Product& p, int64_t lines, hipStream_t s)
 {
-    const RowPlan plan = plan_rows(p.m, p.n, lines * Terms);
+    const RowPlan plan = plan_rows(kProduct, Terms, p.m, p.n, lines);
     auto part = [&](int pick, int64_t first, int64_t rows) {
         Product r = p;
         r.a.at += first * p.a.pitch;
@@ -1113,7 +1153,7 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
                     go(k_probs<M, false, Tl>);
             });
         };
-        const RowPlan plan = plan_rows(n, wide, span.lines * (M::kPairs ? 3 : 1));
+        const RowPlan plan = plan_rows(M::kPairP || g.wide ? kProbPairs : kProbs, M::kPairs ? 3 : 1, n, wide, span.lines);
         probs(plan.pick, 0, plan.rows);
         if (plan.rows < n) probs(plan.rest_pick, plan.rows, n - plan.rows);
         if (q.x_grad.at) {
