@@ -693,10 +693,11 @@ int64_t sidco_dropout_blocks(int64_t rows, int64_t cols);
  * floats each; one of them may be NULL) must not overlap anything.  n <= 2^22, dim <= 2^21, and
  * vocab / 64 times n / 64 or dim / 64, each rounded up, at most 2^31-1 (SIDCO_ERR_SIZE).
  *
- * Sums are fp32.  16-bit operands are multiplied exactly; fp32 ones as pairs of halves under a
- * power of two for each matrix, 22 bits of its elements down to 2^-28 of its largest magnitude
- * and 2^-39 of that below, and there an infinity counts as a NaN.  From one row on.  Uses the
- * stream's workspace, of sidco_workspace_bytes_cross_entropy(n, dim, vocab, dtype) at most.
+ * Sums are fp32.  16-bit operands are multiplied exactly; fp32 ones as they are where rows are few, by
+ * n, dim and alignment, else as pairs of halves under a power of two for each matrix, 22 bits of its
+ * elements down to 2^-28 of its largest magnitude and 2^-39 of that below, and there an infinity counts
+ * as a NaN.  From one row on.  Uses the stream's workspace, of
+ * sidco_workspace_bytes_cross_entropy(n, dim, vocab, dtype) at most.
  */
 int sidco_cross_entropy(void *stream, const void *x, const void *w, int dtype, int64_t n, int64_t dim, int64_t vocab, int64_t ldx, int64_t ldw,
                         const void *targets, int word_type, float *loss, float *lse);

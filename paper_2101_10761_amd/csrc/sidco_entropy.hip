@@ -875,17 +875,22 @@ RowPlan forward_plan(int64_t rows, int64_t vocab, int64_t lines)
 }
 int64_t forward_width(int pick, int64_t vocab) { return 2 * parts(vocab, kTileCosts[pick].side); }
 
-// Whether few rows have a kernel of their own, the steps that it takes, and its blocks.
+// The blocks of k_few, the steps that it takes, and whether it is what a call takes.  It reads the weight once for every 32 rows; the
+// way by tiles reads it once, and where it has to be laid out first a second time, for fp32 a third, beside writing it.  us, here /
+// there: against 10000 x 1500 fp32 64 rows 44 / 63, 96 rows 64 / 74; 100000 x 2048 fp32 292 / 740, 436 / 791; 10000 x 1502 bf16 33 rows
+// 24 / 28; 100000 x 3002 bf16 20 rows 113 / 403.  Rows of 16 bits that start between two words are read at half the rate: 10000 x 1501 bf16
+// 20 rows 31 / 28, 33 rows 54 / 28; 100000 x 3001 207 / 404, 420 / 404.
 constexpr int64_t kFewBlocks = 512;
 template <class M>
-int64_t few_steps(int64_t rows, int64_t dim)
+int64_t few_steps(int64_t dim)
 {
-    return rows <= kFewRows && dim >= 8 ? parts(dim, kFewWaves * FewCore<typename M::T>::kStep) : 1 << 30;
+    return parts(dim, kFewWaves * FewCore<typename M::T>::kStep);
 }
 template <class M>
-bool takes_few(int64_t rows, int64_t dim)
+bool takes_few(int64_t rows, int64_t dim, const Matrix& w, bool lay_w)
 {
-    return few_steps<M>(rows, dim) <= 16;
+    const bool between = sizeof(typename M::T) == 2 && (w.ld % 2 != 0 || (uintptr_t)w.at % 4 != 0);
+    return parts(rows, kFewRows) <= (lay_w && !between ? 3 : 1) && dim >= 8 && few_steps<M>(dim) <= 16;
 }
 
 void join_rows(const float2* pairs, uint32_t width, int64_t rows, const WordList& words, const float* mine, float* loss, float* lse, hipStream_t s)
@@ -912,9 +917,10 @@ struct ForwardPlan {
         Space s = {scratch, 0};
         const int64_t n = q.words.n, v = q.words.vocab, at_once = std::min(n, kRowsAtOnce);
         pitch = up(q.dim, kPer);
-        few = takes_few<M>(n, q.dim);
-        lay_x = !few && !lies_in_lines<M>(q.x, q.dim);
-        lay_w = !few && !lies_in_lines<M>(q.w, q.dim);
+        lay_x = !lies_in_lines<M>(q.x, q.dim);
+        lay_w = !lies_in_lines<M>(q.w, q.dim);
+        few = takes_few<M>(n, q.dim, q.w, lay_w);
+        if (few) lay_x = lay_w = false;
         scales = s.get<Scales>(1);
         part = s.get<float>(M::kPairs ? 3 * kParts : 0);
         x = lay_x ? s.plane<H>(n, pitch, M::kPairs) : Plane<H>{(H*)q.x.at, q.x.ld, 0};
@@ -950,11 +956,15 @@ void forward(const Entropy& q, char* scratch, hipStream_t s)
     const ForwardPlan<M> f(q, scratch);
     const int64_t n = q.words.n, v = q.words.vocab;
     if (f.few) {
-        const int64_t groups = parts(v, 16), steps = few_steps<M>(n, q.dim);
+        const int64_t groups = parts(v, 16), steps = few_steps<M>(q.dim);
         // a CU's registers hold two blocks where a wave's operands take few of them
         const int64_t blocks = std::min(groups, steps <= (n <= 16 ? 10 : 6) ? kFewBlocks : kFewBlocks / 2);
-        const Few<T> p = {(const T*)q.x.at, (const T*)q.w.at, q.x.ld, q.w.ld, (uint32_t)n, (uint32_t)q.dim, (uint32_t)groups, list(q.words), f.pairs, f.mine};
-        auto go = [&](auto kernel) { kernel<<<(uint32_t)blocks, 64 * kFewWaves, 0, s>>>(p); };
+        int64_t r = 0, rows = 0;
+        auto go = [&](auto kernel) {
+            const Few<T> p = {(const T*)q.x.at + r * q.x.ld, (const T*)q.w.at, q.x.ld, q.w.ld, (uint32_t)rows, (uint32_t)q.dim, (uint32_t)groups,
+                              list(q.words).from(r), f.pairs + r * blocks, f.mine + r};
+            kernel<<<(uint32_t)blocks, 64 * kFewWaves, 0, s>>>(p);
+        };
         auto by_steps = [&](auto tiles) {
             constexpr int kTiles = decltype(tiles)::value;
             // the kernel's steps are the call's or one more
@@ -977,10 +987,13 @@ void forward(const Entropy& q, char* scratch, hipStream_t s)
             else
                 go(k_few<T, 16, kTiles>);
         };
-        if (n <= 16)
-            by_steps(std::integral_constant<int, 1>());
-        else
-            by_steps(std::integral_constant<int, 2>());
+        for (; r < n; r += rows) {
+            rows = std::min(n - r, (int64_t)kFewRows);
+            if (rows <= 16)
+                by_steps(std::integral_constant<int, 1>());
+            else
+                by_steps(std::integral_constant<int, 2>());
+        }
         join_rows(f.pairs, (uint32_t)blocks, n, list(q.words), f.mine, q.loss, q.lse, s);
         return;
     }

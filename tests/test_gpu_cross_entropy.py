@@ -84,11 +84,42 @@ def test_losses_and_gradients(n, dim, vocab, t, o, accumulate):
     _near(dw, *r.w_grad(_dtype(o), before), "w_grad")
 
 
+@pytest.mark.parametrize("n,dim,vocab", [(16, 8, 16), (17, 9, 40), (32, 1024, 33), (33, 100, 700), (40, 1001, 333), (64, 2050, 130), (96, 10, 2000), (97, 64, 300),
+                                         (3, 4097, 100), (32, 7, 64), (1, 129, 5000), (31, 4096, 17)])
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("gap", [0, 1, 2])
+def test_losses_of_few_rows(n, dim, vocab, t, gap):
+    """On both sides of what the kernel for few rows takes, rows that start at any element, steps that are not whole."""
+    torch, sidco = _torch(), _sidco()
+    x, w, words = _case(n, dim, vocab, t, seed=3, gap=gap)
+    loss, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    sidco.sidco_cross_entropy(x, w, words, loss, lse)
+    torch.cuda.synchronize()
+    r = ref.CrossEntropy(x, w, words)
+    _near(lse, r.lse, r.lse_off, "lse")
+    _near(loss, r.loss, r.loss_off, "loss")
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+def test_infinite_weights_of_few_rows(t):
+    """In the last elements of rows that end within a step, where a piece is read twice."""
+    torch, sidco = _torch(), _sidco()
+    for dim in (9, 37, 203):
+        x, w = torch.ones(2, dim, dtype=_dtype(t), device="cuda"), torch.zeros(40, dim, dtype=_dtype(t), device="cuda")
+        w[3, dim - 1], w[5, dim - 5], w[7, dim - 1] = float("inf"), float("-inf"), float("-inf")
+        loss, lse = torch.empty(2, device="cuda"), torch.empty(2, device="cuda")
+        sidco.sidco_cross_entropy(x, w, torch.tensor([1, 5], device="cuda"), loss, lse)
+        assert lse.tolist() == [math.inf, math.inf] and loss.tolist() == [math.inf, math.inf]
+        sidco.sidco_cross_entropy(x, w[4:], torch.tensor([0, 1], device="cuda"), loss, lse)
+        # 36 words, two of them impossible
+        assert abs(float(lse[0]) - math.log(34)) < 1e-6 * math.log(34) and loss[1] == math.inf
+
+
 @pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
 def test_many_pieces_and_rows(t):
     """The gradient's pieces of the vocabulary, and the forward pass's of the rows."""
     torch = _torch()
-    n, dim, vocab = 17_000, 24, 9000 if t == "f32" else 18_000
+    n, dim, vocab = 17_000, 24, 18_000 if t == "bf16" else 9000
     x, w, words = _case(n, dim, vocab, t, padding=0.3)
     g = torch.rand(n, device="cuda")
     loss, lse, dx, dw = _run(x, w, words, g)
