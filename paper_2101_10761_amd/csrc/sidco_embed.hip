@@ -215,7 +215,7 @@ __device__ __forceinline__ void fill_rows(const Sum<G, T>& p, int64_t v0, const 
         T* to = p.table + (v0 + r) * p.ldt;
         const int64_t whole = p.cols / kPer * kPer;
         const part zeros = {};
-        for (int64_t c = (threadIdx.x & 63) * kPer; c < whole; c += 64 * kPer) *(part*)(to + c) = zeros;
+        for (int64_t c = (threadIdx.x & 63) * kPer; c < whole; c += 64 * kPer) __builtin_nontemporal_store(zeros, (part*)(to + c));
         if (whole + (threadIdx.x & 63) < p.cols) to[whole + (threadIdx.x & 63)] = (T)0.0f;
     }
 }
@@ -299,22 +299,32 @@ __device__ __forceinline__ void join_waves(float (&sum)[8], float (*lds)[64][9])
 // Few places, in one launch and without a workspace: every block has all words in LDS.  A wave looks at a place, and if its word
 // occurs at no place before it, lists the word's places and adds up their rows; a word of many places is taken by the block's
 // waves together.
-constexpr int kFewPlaces = 16, kAlone = 32;  // of a block, of a wave
+constexpr int kFewPlaces = kSumBlock / 64;     // of a block
+constexpr int kAlone = 16, kListed = 64;       // of a wave, and those that it lists
 
-// Places of `word` among n: their number and, in order, the first `room` of them.  -1 where one lies before `at`.
+// Places of `word`: their number and, in order, the first `room` of them; -1 where one lies before `at`.  Keys behind the last are
+// no word.
 __device__ __forceinline__ int list_places(const uint32_t* keys, int n, uint32_t word, int at, uint16_t* list, int room)
 {
     const int lane = threadIdx.x & 63;
     int count = 0;
-    bool first = true;
-    for (int j = 0; j < n; j += 64) {
-        const uint64_t same = __ballot(j + lane < n && keys[j + lane] == word);
-        first = first && (same == 0 || j + __builtin_ctzll(same) >= at || count > 0);
-        const int to = count + __popcll(same & ((1ull << lane) - 1));
-        if (same >> lane & 1 && to < room) list[to] = (uint16_t)(j + lane);
-        count += __popcll(same);
+    for (int j = 0; j < n; j += 256) {
+        uint64_t same[4];
+        uint32_t key[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) key[k] = keys[j + k * 64 + lane];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) same[k] = __ballot(key[k] == word);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (same[k] == 0) continue;
+            if (count == 0 && j + k * 64 + __builtin_ctzll(same[k]) < at) return -1;
+            const int to = count + __popcll(same[k] & ((1ull << lane) - 1));
+            if (same[k] >> lane & 1 && to < room) list[to] = (uint16_t)(j + k * 64 + lane);
+            count += __popcll(same[k]);
+        }
     }
-    return first ? count : -1;
+    return count;
 }
 
 template <class I, class G, class T>
@@ -322,8 +332,8 @@ __global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p, const void* 
 {
     __shared__ uint32_t keys[kRun];
     __shared__ float lds[kSumBlock / 64][64][9];
-    __shared__ uint16_t list[kSumBlock / 64][kAlone], all[kRun];
-    __shared__ int many[kFewPlaces];
+    __shared__ uint16_t list[kFewPlaces][kListed], all[kRun];
+    __shared__ int many[kFillRows];
     const int n = (int)p.n;
     uint32_t own[kRun / kSumBlock];
 #pragma unroll
@@ -345,32 +355,31 @@ __global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p, const void* 
     for (int k = 0; k < kRun / kSumBlock; ++k) keys[k * kSumBlock + threadIdx.x] = own[k];
     __syncthreads();
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int first = (int)(blockIdx.x / p.strips) * kFewPlaces;
+    const int first = (int)(blockIdx.x / p.strips) * kFewPlaces, at = first + wave;
     const int64_t c = blockIdx.x % p.strips * kStrip + (threadIdx.x & 63) * 8, left = p.cols - c;
     float sum[8];
-    for (int k = wave; k < kFewPlaces; k += kSumBlock / 64) {
-        const int at = first + k;
-        int count = 0;
-        if (at < n && keys[at] < p.vocab) {
-            const uint32_t word = keys[at];
-            count = list_places(keys, n, word, at, list[wave], kAlone);
-            __builtin_amdgcn_wave_barrier();
-            if (count > 0 && count <= kAlone) {
-                sum_rows(p, list[wave], count, c, left, sum);
-                if (left > 0) put_row(p.table + (int64_t)word * p.ldt + c, sum, p.scale, p.accumulate, left);
-            }
+    int count = 0;
+    if (at < n && keys[at] < p.vocab) {
+        const uint32_t word = keys[at];
+        count = list_places(keys, n, word, at, list[wave], kListed);
+        __builtin_amdgcn_wave_barrier();
+        if (count > 0 && count <= kAlone) {
+            sum_rows(p, list[wave], count, c, left, sum);
+            if (left > 0) put_row(p.table + (int64_t)word * p.ldt + c, sum, p.scale, p.accumulate, left);
         }
-        if ((threadIdx.x & 63) == 0) many[k] = count > kAlone ? count : 0;
     }
+    if ((threadIdx.x & 63) == 0) many[wave] = count > kAlone ? count : 0;
     __syncthreads();
     for (int k = 0; k < kFewPlaces; ++k) {
         const int count = many[k];
         if (count == 0) continue;
         const uint32_t word = keys[first + k];
-        if (wave == 0) list_places(keys, n, word, first + k, all, kRun);
-        __syncthreads();
+        if (count > kListed) {
+            if (wave == 0) list_places(keys, n, word, first + k, all, kRun);
+            __syncthreads();
+        }
         const int each = (count + kSumBlock / 64 - 1) / (kSumBlock / 64), from = wave * each, rest = count - from;
-        sum_rows(p, all + from, rest < each ? rest : each, c, left, sum);
+        sum_rows(p, (count > kListed ? all : list[k]) + from, rest < each ? rest : each, c, left, sum);
         join_waves(sum, lds);
         if (wave == 0 && left > 0) put_row(p.table + (int64_t)word * p.ldt + c, sum, p.scale, p.accumulate, left);
     }
