@@ -24,7 +24,9 @@ struct Look {
     int lanes;
 };
 
-// Each: rows that a thread has under way at once.
+// Bound by memory: 65536 rows of 4096 in bf16, of 131072, 166 us for 0.79 GB of distinct rows and results, 4.8 TB/s (a copy reaches
+// 4.8 to 5.0); 700 of 1500 in fp32 4.0 us, a launch and two trips to memory.  Each: rows that a thread has under way at once, four
+// where there are blocks enough for it (197 to 160 us for the first of these), else one.
 template <class I, class T, class R, int Each>
 __global__ __launch_bounds__(kRowBlock) void k_embedding(Look<I, T, R> p)
 {
@@ -55,7 +57,7 @@ __global__ __launch_bounds__(kRowBlock) void k_embedding(Look<I, T, R> p)
 // Runs of kRun places are sorted by counting: a place's rank in its run is the number of places with a smaller word, and of
 // the same word before it.  All comparisons are independent of each other, kRun a place, so that one launch of many small
 // blocks does them.  Then up to kWays neighbouring runs are merged at a time: a place moves up by the number of places of
-// each other run that come before it, which a search in that run finds.
+// each other run that come before it, which a search in that run finds.  65536 places 15.4 + 15.4 us, 4099 5.3 + 6.8.
 constexpr int kRun = 2048, kWays = 32;
 constexpr int kSortLanes = 16;  // lanes that share the comparisons of a place
 
@@ -128,7 +130,7 @@ __global__ __launch_bounds__(256) void k_sort_run(const void* words, int64_t n, 
 }
 
 // Runs of `len` places, kWays of them to one.  A wave searches four runs at a time for 64 neighbours of one run, whose places
-// there lie close together; eight waves share the runs.
+// there lie close together; eight waves share the runs.  (With a lane for each run, whose probes meet no line together, 39.7 us.)
 constexpr int kMergeWaves = 8, kMergeEach = kWays / kMergeWaves;
 __global__ __launch_bounds__(64 * kMergeWaves) void k_merge(Sorted in, Sorted out, int64_t n, int64_t len)
 {
@@ -204,7 +206,9 @@ __device__ __forceinline__ void put_row(T* to, const float (&sum)[8], float scal
     t.store(to, left);
 }
 
-// Zeros for those of the kFillRows rows from v0 on that are not present.
+// Zeros for those of the kFillRows rows from v0 on that are not present.  Past the caches: they are more than these hold, and with
+// ordinary stores the rows that other blocks of the launch wait for came later (700 words into 10000 x 1500 fp32, whole call, 21.0
+// us; so 15.1).
 template <class G, class T>
 __device__ __forceinline__ void fill_rows(const Sum<G, T>& p, int64_t v0, const int* present)
 {
@@ -298,7 +302,8 @@ __device__ __forceinline__ void join_waves(float (&sum)[8], float (*lds)[64][9])
 
 // Few places, in one launch and without a workspace: every block has all words in LDS.  A wave looks at a place, and if its word
 // occurs at no place before it, lists the word's places and adds up their rows; a word of many places is taken by the block's
-// waves together.
+// waves together.  Bound by the table's writes and by the chain of words, list, rows: whole calls for 10000 x 1500 fp32, 1, 700 and 2048
+// words 13.6, 15.1 and 26.0 us, where torch's zeros alone take 10.6; 2049 words, sorted, 31.8.
 constexpr int kFewPlaces = kSumBlock / 64;     // of a block
 constexpr int kAlone = 16, kListed = 64;       // of a wave, and those that it lists
 
@@ -386,7 +391,8 @@ __global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p, const void* 
 }
 
 // Many places: a wave adds up the rows of `chunk` sorted ones in one strip of columns.  A word whose places all lie in the chunk
-// is done; the sums of one that began before it or goes on after it are kept for k_join.
+// is done; the sums of one that began before it or goes on after it are kept for k_join.  Bound by memory: 65536 rows of 4096 in
+// bf16 into 131072 in fp32, 484 to 515 us for 2.7 GB, 5.2 to 5.5 TB/s.
 template <class G, class T>
 __global__ __launch_bounds__(kSumBlock) void k_sum(Sum<G, T> p)
 {
@@ -430,7 +436,8 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sum<G, T> p)
     }
 }
 
-// The sums of words whose places lie in several chunks: a block for each strip and chunk in which one begins.
+// The sums of words whose places lie in several chunks: a block for each strip and chunk in which one begins.  Bound by the launch of
+// its blocks, most of which have nothing to do: 22.7 us for the case above (35 with blocks of eight waves).
 constexpr int kJoinWaves = 4;
 template <class G, class T>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_join(Sum<G, T> p)
@@ -465,6 +472,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_join(Sum<G, T> p)
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
+// Sorted places of a wave: fewer where there would not be waves enough, for four times the partial sums at most.
 int chunk_of(int64_t n, int64_t cols) { return n * ((cols + kStrip - 1) / kStrip) < 65536 ? 8 : 32; }
 
 // Words and places, twice where they are merged, and the partial sums.
