@@ -694,9 +694,9 @@ int64_t sidco_dropout_blocks(int64_t rows, int64_t cols);
  * vocab / 64 times n / 64 or dim / 64, each rounded up, at most 2^31-1 (SIDCO_ERR_SIZE).
  *
  * Sums are fp32.  16-bit operands are multiplied exactly; fp32 ones as they are where rows are few, by
- * n, dim and alignment, else as pairs of halves under a power of two for each matrix, 22 bits of its
- * elements down to 2^-28 of its largest magnitude and 2^-39 of that below, and there an infinity counts
- * as a NaN.  From one row on.  Uses the stream's workspace, of
+ * n, dim and alignment, else as pairs of halves under a power of two for each matrix, off by 2^-22 of
+ * an element or 2^-32 of the largest magnitude, whichever is more, and there an infinity counts as a
+ * NaN.  From one row on.  Uses the stream's workspace, of
  * sidco_workspace_bytes_cross_entropy(n, dim, vocab, dtype) at most.
  */
 int sidco_cross_entropy(void *stream, const void *x, const void *w, int dtype, int64_t n, int64_t dim, int64_t vocab, int64_t ldx, int64_t ldw,
@@ -713,8 +713,8 @@ size_t sidco_workspace_bytes_cross_entropy(int64_t n, int64_t dim, int64_t vocab
  * mean, times the loss scale if there is one; NULL stands for ones.  P is formed for one piece of
  * the vocabulary at a time, in halves under a power of two of the largest loss_grad: 11 bits for a bf16
  * gradient, else 22, down to 2^-29 of the largest and 2^-39 of that below; bf16 operands of its
- * products are exact down to 2^-29 of their matrix's largest magnitude in the same way, and there
- * an infinity counts as a NaN.  Rows of x whose target is padding do not enter w_grad whatever they
+ * products are halves too, exact down to 2^-24 of their matrix's largest magnitude and off by 2^-32
+ * of that below.  Rows of x whose target is padding do not enter w_grad whatever they
  * hold.  The gradients must not overlap x, w or each other.  Uses the stream's workspace, of
  * sidco_workspace_bytes_cross_entropy_grad(n, dim, vocab, dtype, w_grad_dtype) at most.
  */

@@ -12,14 +12,14 @@
 //
 // Products are those of sidco_product.h and want both operands by rows along the contraction, in whole lines of 128 bytes.
 // 16-bit operands that lie like that are read where they are; others, and the transposes that the gradient needs, are laid out
-// in the workspace first.  fp32 operands become pairs of halves, 22 bits, under a power of two that brings the largest
-// magnitude of the matrix to 2^14 to 2^15, and a product is three: low high + high low + high high.
+// in the workspace first.  fp32 operands become pairs of halves, 22 bits, under a power of two for each matrix, and a product is
+// three: low high + high low + high high.
 //
 // P is in halves, times a power of two, for its smallest elements would reach theirs: 11 bits, or as a pair 22.  Its rounding adds
 // up like a rounding of the gradient itself, so that it takes more bits than the gradient has: one half for bf16 gradients (an
 // error of 1.7e-3 in the 2-norm, the gradient's own rounding; with P in bf16 it was up to 2.4e-3), a pair for those of halves and
 // of fp32 (2.1e-4 for halves; with one half up to 3.1e-4).  bf16 operands of the products with P are halves too, exactly but for
-// those under 2^-29 of the largest, under a power of two as for fp32; they multiply at nearly the rate of bf16 (a training pass
+// those under 2^-24 of the largest, under a power of two as for fp32; they multiply at nearly the rate of bf16 (a training pass
 // of 8192 x 4096 x 131072 takes 3 % longer).
 #include <math.h>
 
@@ -73,7 +73,11 @@ void by_mode(int type, const F& f)
 struct Scales {
     float x, w, p;
 };
-constexpr int kParts = 1024;  // blocks of k_top, and partial results of each of the three
+constexpr int kParts = 2048;  // blocks of k_layout, and partial results of each of the three
+
+// What x and w are laid out with at first.  Weights whose largest magnitude is 2^-7 to 2^1.5 and rows of 2^-3 to 2^5.5 stay so; k_settle
+// lays out others once more.
+constexpr float kGuessX = 1024.0f, kGuessW = 16384.0f;
 
 // What brings a largest magnitude to 2^14 to 2^15; 1 for zeros.
 __device__ __forceinline__ float scale_of(float top)
@@ -85,6 +89,13 @@ __device__ __forceinline__ float scale_of(float top)
     return ldexpf(1.0f, e > 120 ? 120 : e);
 }
 
+// The same, or the guess where it does: the largest is a half with room for rounding, and what halves cannot tell from zero is 2^-32 of it.
+__device__ __forceinline__ float settled(float top, float guess)
+{
+    const float t = top * guess;
+    return top == 0.0f || (t >= 128.0f && t < 46340.0f) ? guess : scale_of(top);
+}
+
 template <class T>
 struct Source {
     const T* at;
@@ -92,71 +103,31 @@ struct Source {
     WordList words;  // rows of padding are left out; without an address none is
 };
 
-template <class T>
-__device__ __forceinline__ float top_of(const Source<T>& p)
+__device__ __forceinline__ float more(float top, float v)
 {
-    constexpr int kEach = 4;  // rows under way
-    float top = 0.0f;
-    for (int64_t r = blockIdx.x; r < p.rows; r += (int64_t)gridDim.x * kEach) {
-        bool in[kEach];
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int64_t row = r + (int64_t)e * gridDim.x;
-            in[e] = row < p.rows && !(p.words.at && p.words.none(row));
-        }
-        for (int64_t c = threadIdx.x * 8; c < p.cols; c += 256 * 8) {
-            Eight<T> v[kEach];
-#pragma unroll
-            for (int e = 0; e < kEach; ++e)
-                if (in[e]) v[e].load(p.at + (r + (int64_t)e * gridDim.x) * p.ld + c, p.cols - c);
-#pragma unroll
-            for (int e = 0; e < kEach; ++e)
-                if (in[e]) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float m = fabsf(v[e].get(i));
-                        top = m < INFINITY && m > top ? m : top;
-                    }
-                }
-        }
-    }
-    return top;
+    const float m = fabsf(v);
+    return m < INFINITY && m > top ? m : top;
 }
 
-// Largest finite magnitudes of x, w and the rows' gradient, a partial result from each block.  Bound by memory: w of 131072 x 4096
-// in bf16 and x of 8192 rows 205 us for 1.14 GB, 5.6 TB/s; 10000 and 700 x 1500 in fp32 17.7 us for 64 MB.
-template <class T>
-__global__ __launch_bounds__(256) void k_top(Source<T> x, Source<T> w, Source<float> g, float* part)
+// The largest of the block's 256 threads, in thread 0.
+__device__ __forceinline__ float block_top(float top, float* lds)
 {
-    __shared__ float lds[4][3];
-    float top[3] = {0.0f, 0.0f, 0.0f};
-    if (x.at) top[0] = top_of(x);
-    if (w.at) top[1] = top_of(w);
-    if (g.at) top[2] = top_of(g);
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-#pragma unroll
-        for (int s = 32; s > 0; s >>= 1) top[k] = fmaxf(top[k], __shfl_xor(top[k], s));
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][k] = top[k];
-    }
-    __syncthreads();
-    const int k = threadIdx.x;
-    if (k < 3) part[k * kParts + blockIdx.x] = fmaxf(fmaxf(lds[0][k], lds[1][k]), fmaxf(lds[2][k], lds[3][k]));
-}
-
-// The largest of one of the three, for the whole block of 256.
-__device__ __forceinline__ float joined_top(const float* part, float* lds)
-{
-    float top = 0.0f;
-#pragma unroll
-    for (int k = 0; k < kParts / 256; ++k) top = fmaxf(top, part[k * 256 + threadIdx.x]);
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+    __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
     __syncthreads();
-    top = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
-    __syncthreads();
-    return top;
+    return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+}
+
+// The largest of one of the three over the blocks of k_layout, for the whole block of 256.
+__device__ __forceinline__ float joined_top(const float* part, uint32_t blocks, float* lds)
+{
+    float top = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kParts / 256; ++k)
+        if (k * 256 + threadIdx.x < blocks) top = fmaxf(top, part[k * 256 + threadIdx.x]);
+    return block_top(top, lds);
 }
 
 // ---- operands ----
@@ -198,51 +169,43 @@ __device__ __forceinline__ void put8(const Plane<H>& o, int64_t r, int64_t c, co
     if (Pairs) *(h8*)(p + o.low) = l;
 }
 
-// 64 x 64 elements a block, of x and then of w.  Transposed, rows of padding are zeros whatever they hold: they are multiplied
-// with the zeros that P has for them.  With Scaled (not in the forward pass of 16-bit operands, whose transposes nobody takes)
-// the partial results of k_top are joined; block 0 writes them down for the products.  Bound by memory: 32768 x 4096 in bf16 97 us for
-// 537 MB, 5.5 TB/s; 10000 and 700 x 1500 in fp32, both ways in pairs, 35.7 us for 196 MB.
-template <class M, bool Scaled>
-__global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M::H> x, Layout<typename M::T, typename M::H> w, const float* part,
-                                                Scales* scales)
+// 64 x 64 elements.  Transposed, rows of padding are zeros whatever they hold: they are multiplied with the zeros that P has for them.
+// Returns the largest finite magnitude, or top if that is larger.
+template <class M>
+__device__ __forceinline__ float lay(const Layout<typename M::T, typename M::H>& p, uint32_t t, float scale, float (*tile)[65], float top)
 {
     typedef typename M::H H;
-    __shared__ float tile[64][65];
-    __shared__ float lds[4];
-    const uint32_t first = x.tiles_r * x.tiles_c;
-    const bool second = blockIdx.x >= first;
-    const Layout<typename M::T, H>& p = second ? w : x;
-    const uint32_t t = second ? blockIdx.x - first : blockIdx.x;
-    float scale = 1.0f;
-    if (Scaled) {
-        if (M::kScaled) scale = scale_of(joined_top(part + (second ? kParts : 0), lds));
-        if (blockIdx.x == 0) {
-            const float sx = M::kScaled ? scale_of(joined_top(part, lds)) : 1.0f, sw = M::kScaled ? scale_of(joined_top(part + kParts, lds)) : 1.0f;
-            const float sp = scale_of(joined_top(part + 2 * kParts, lds));
-            if (threadIdx.x == 0) *scales = {sx, sw, sp};
-        }
-    }
-    if (first + w.tiles_r * w.tiles_c <= blockIdx.x) return;
     const int64_t r0 = (int64_t)(t / p.tiles_c) * 64, c0 = (int64_t)(t % p.tiles_c) * 64;
     const int row = threadIdx.x >> 3, col = (threadIdx.x & 7) * 8;
+    Eight<typename M::T> e[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int64_t r = r0 + k * 32 + row, c = c0 + col;
-        float v[8] = {};
         if (r < p.from.rows && c < p.from.cols) {
-            Eight<typename M::T> e;
-            e.load(p.from.at + r * p.from.ld + c, p.from.cols - c);
+            e[k].load(p.from.at + r * p.from.ld + c, p.from.cols - c);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = M::kPairs ? e.get(i) * scale : e.get(i);
+            for (int i = 0; i < 8; ++i) e[k].set(i, 0.0f);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int64_t r = r0 + k * 32 + row, c = c0 + col;
+        const bool none = p.from.words.at && r < p.from.rows && p.from.words.none(r);
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = e[k].get(i);
+            if (M::kScaled && !none) top = more(top, v[i]);
+            if (M::kPairs) v[i] *= scale;
         }
         if (p.rows.at && r < p.from.rows && c < p.rows.pitch) put8<H, M::kPairs>(p.rows, r, c, v);
         if (p.turned.at) {
-            const bool none = p.from.words.at && r < p.from.rows && p.from.words.none(r);
 #pragma unroll
             for (int i = 0; i < 8; ++i) tile[k * 32 + row][col + i] = none ? 0.0f : (M::kPairs ? v[i] : v[i] * scale);
         }
     }
-    if (!p.turned.at) return;
+    if (!p.turned.at) return top;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -252,6 +215,70 @@ __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = tile[col + i][c];
         put8<G, M::kPairs>(p.turned, c0 + c, r0 + col, v);
+    }
+    __syncthreads();
+    return top;
+}
+
+// x and w laid out with the guessed scales, and the largest finite magnitudes of x, w and the rows' gradient, a partial result from
+// each block (not in the forward pass of 16-bit operands, which nothing is scaled in).  The magnitudes are only known behind a pass over
+// everything: to find them first and lay out then is one read more.  Bound by memory: 700 and 10000 rows of 1500 fp32, 64 MB read and
+// 128 MB written (two halves of each by rows and transposed), 28 to 34 us; with the pass before it the training step took 391, not 380.
+template <class M, bool Scaled>
+__global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M::H> x, Layout<typename M::T, typename M::H> w, Source<float> g, float* part)
+{
+    __shared__ float tile[64][65];
+    __shared__ float lds[4];
+    const uint32_t first = x.tiles_r * x.tiles_c, all = first + w.tiles_r * w.tiles_c;
+    float top[3] = {0.0f, 0.0f, 0.0f};
+    for (uint32_t t = blockIdx.x; t < all; t += gridDim.x) {
+        if (t < first)
+            top[0] = lay<M>(x, t, M::kScaled ? kGuessX : 1.0f, tile, top[0]);
+        else
+            top[1] = lay<M>(w, t - first, M::kScaled ? kGuessW : 1.0f, tile, top[1]);
+    }
+    if (!Scaled) return;
+    if (g.at) {
+        for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < g.rows; r += (int64_t)gridDim.x * 256)
+            if (!g.words.none(r)) top[2] = more(top[2], g.at[r]);
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        const float most = block_top(top[k], lds);
+        if (threadIdx.x == 0) part[k * kParts + blockIdx.x] = most;
+    }
+}
+
+// The scales that the largest magnitudes ask for, and what was laid out with another one once more.  A piece of w after the first
+// leaves those of x and P as they are.  8.4 us where the guess does, three lists of 2048 partial results for each block and a
+// launch; 35 where all is laid out again.
+constexpr uint32_t kSettleBlocks = 512;
+template <class M>
+__global__ __launch_bounds__(256) void k_settle(Layout<typename M::T, typename M::H> x, Layout<typename M::T, typename M::H> w, uint32_t blocks, bool later,
+                                                const float* part, Scales* scales)
+{
+    __shared__ float tile[64][65];
+    __shared__ float lds[4];
+    const uint32_t first = x.tiles_r * x.tiles_c, all = first + w.tiles_r * w.tiles_c;
+    float sx = 1.0f, sw = 1.0f;
+    if (M::kScaled) {
+        if (!later) sx = settled(joined_top(part, blocks, lds), kGuessX);
+        sw = settled(joined_top(part + kParts, blocks, lds), kGuessW);
+    }
+    if (blockIdx.x == 0) {
+        const float sp = later ? 1.0f : scale_of(joined_top(part + 2 * kParts, blocks, lds));
+        if (threadIdx.x == 0) {
+            scales->w = sw;
+            if (!later) scales->x = sx, scales->p = sp;
+        }
+    }
+    if (!M::kScaled) return;
+    const uint32_t from = sx == kGuessX ? first : 0, to = sw == kGuessW ? first : all;
+    for (uint32_t t = from + blockIdx.x; t < to; t += gridDim.x) {
+        if (t < first)
+            (void)lay<M>(x, t, sx, tile, 0.0f);
+        else
+            (void)lay<M>(w, t - first, sw, tile, 0.0f);
     }
 }
 
@@ -949,15 +976,16 @@ struct ForwardPlan {
 
 WordList list(const Words& w) { return {w.at, w.wide, (uint32_t)w.vocab}; }
 
-template <class M>
-void tops(const Entropy& q, bool of_matrices, bool of_gains, float* part, hipStream_t s)
+// x and w laid out and their scales settled; g is the rows' gradient, or has no address.
+template <class M, bool Scaled>
+void lay_out(const Layout<typename M::T, typename M::H>& x, const Layout<typename M::T, typename M::H>& w, const Source<float>& g, bool later,
+             float* part, Scales* scales, hipStream_t s)
 {
-    typedef typename M::T T;
-    Source<T> none = {};
-    const WordList words = list(q.words);
-    const Source<float> g = {of_gains ? q.loss_grad : nullptr, 1, q.words.n, 1, words};
-    k_top<T><<<kParts, 256, 0, s>>>(of_matrices ? source<T>(q.x, q.words.n, q.dim, words) : none,
-                                    of_matrices ? source<T>(q.w, q.words.vocab, q.dim) : none, g, part);
+    const int64_t tiles = (int64_t)x.tiles_r * x.tiles_c + (int64_t)w.tiles_r * w.tiles_c;
+    if (tiles == 0) return;  // a later piece of a w that is read where it is
+    const uint32_t blocks = (uint32_t)std::min(tiles, (int64_t)kParts);
+    k_layout<M, Scaled><<<blocks, 256, 0, s>>>(x, w, g, part);
+    if (Scaled) k_settle<M><<<M::kScaled ? std::min(blocks, kSettleBlocks) : 1, 256, 0, s>>>(x, w, blocks, later, part, scales);
 }
 
 template <class M>
@@ -1009,12 +1037,11 @@ void forward(const Entropy& q, char* scratch, hipStream_t s)
         join_rows(f.pairs, (uint32_t)blocks, n, list(q.words), f.mine, q.loss, q.lse, s);
         return;
     }
-    if (M::kPairs) tops<M>(q, true, false, f.part, s);
     if (f.lay_x || f.lay_w) {
         const uint32_t across = (uint32_t)parts(f.pitch, 64);
-        const Layout<T, H> lx = {source<T>(q.x, n, q.dim), f.lay_x ? f.x : Plane<H>{}, {}, f.lay_x ? (uint32_t)parts(n, 64) : 0, across};
+        const Layout<T, H> lx = {source<T>(q.x, n, q.dim, list(q.words)), f.lay_x ? f.x : Plane<H>{}, {}, f.lay_x ? (uint32_t)parts(n, 64) : 0, across};
         const Layout<T, H> lw = {source<T>(q.w, v, q.dim), f.lay_w ? f.w : Plane<H>{}, {}, f.lay_w ? (uint32_t)parts(v, 64) : 0, across};
-        k_layout<M, M::kPairs><<<(lx.tiles_r + lw.tiles_r) * across, 256, 0, s>>>(lx, lw, f.part, f.scales);
+        lay_out<M, M::kPairs>(lx, lw, {}, false, f.part, f.scales, s);
     }
     for (int64_t r = 0; r < n; r += kRowsAtOnce) {
         const int64_t rows = std::min(n - r, kRowsAtOnce);
@@ -1143,7 +1170,7 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
     const GradPlan<M> g(q, scratch);
     const int64_t n = q.words.n, v = q.words.vocab;
     const WordList words = list(q.words);
-    tops<M>(q, M::kScaled, true, g.part, s);
+    const Source<float> gains = {q.loss_grad, 1, n, 1, words};
     for (int64_t k = 0; k < g.pieces; ++k) {
         const int64_t first = k * g.piece, count = std::min(g.piece, v - first);
         const Plane<H> w = g.lay_w ? g.w : Plane<H>{(H*)q.w.at + first * q.w.ld, q.w.ld, 0};
@@ -1152,8 +1179,7 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
         Layout<T, H> lw = {source<T>(q.w, count, q.dim, {}, first), g.lay_w ? g.w : Plane<H>{}, g.wt, 0, lx.tiles_c};
         if (k == 0 && (g.lay_x || g.xt.at)) lx.tiles_r = (uint32_t)parts(g.cols_n, 64);
         if (g.lay_w || g.wt.at) lw.tiles_r = (uint32_t)parts(g.wt.at ? g.cols_v : count, 64);
-        const uint32_t blocks = (lx.tiles_r + lw.tiles_r) * lx.tiles_c;
-        k_layout<M, true><<<blocks, 256, 0, s>>>(lx, lw, g.part, g.scales);  // one gradient at least has a transpose
+        lay_out<M, true>(lx, lw, k == 0 ? gains : Source<float>{}, k > 0, g.part, g.scales, s);
 
         const Span span = {(uint32_t)(g.x.pitch * sizeof(H)), (uint32_t)(w.pitch * sizeof(H)), (uint32_t)(g.pitch / kPer)};
         const int64_t wide = g.p.at ? g.cols_v : count;  // padding of P's rows is written with the last tiles

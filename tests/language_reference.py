@@ -62,8 +62,8 @@ class CrossEntropy:
 
     u = 2^-24 is a rounding to 32 bits.  A logit is a sum of k products in 32 bits, off by at most (k + 16) u times the sum of
     their magnitudes; fp32 operands as pairs of halves miss 2^-22 of each factor and the product of what the first halves
-    leave, 2^-22 again, and below the halves' range 2^-40 of the largest magnitude.  exp and log are those of powers of two, of
-    an argument rounded to 32 bits twice.  P is rounded once to what it is stored in: a half for bf16 gradients, else a pair of
+    leave, 2^-22 again, and below the halves' range 2^-32 of the largest magnitude, which is 2^7 or more where a half is off
+    by 2^-25 at least.  exp and log are those of powers of two, of an argument rounded to 32 bits twice.  P is rounded once to what it is stored in: a half for bf16 gradients, else a pair of
     halves, under a power of two of which its largest element may have 2^15; bf16 operands of its products are halves like
     fp32 ones, exactly but for that range."""
 
@@ -80,7 +80,7 @@ class CrossEntropy:
         self.l_off = ((k + 16) * self.u + (3 * 2.0**-22 if f32 else 0.0)) * size
         if f32:
             tops = self.x[self.ok].abs().max() if self.ok.any() else 0.0, self.w.abs().max()
-            self.l_off += 2.0**-40 * (tops[0] * self.w.abs().sum(1)[None] + tops[1] * self.x.abs().sum(1)[:, None])
+            self.l_off += 2.0**-32 * (tops[0] * self.w.abs().sum(1)[None] + tops[1] * self.x.abs().sum(1)[:, None])
         self.lse = torch.logsumexp(self.l, 1)
         exponent = self.l_off + 4 * self.u * (self.l.abs() + self.lse.abs()[:, None])
         p = torch.exp(self.l - self.lse[:, None])
@@ -104,7 +104,7 @@ class CrossEntropy:
         off = (p_off + p.abs() * step + least) @ other.abs()
         off = off + ((p.shape[1] + 16) * self.u + (3 * 2.0**-22 if f32 else 0.0)) * (p.abs() @ other.abs())
         if self.type is not torch.float16:
-            off = off + 2.0**-40 * other.abs().max() * p.abs().sum(1)[:, None]
+            off = off + 2.0**-32 * other.abs().max() * p.abs().sum(1)[:, None]
         info = torch.finfo(out)
         want = p @ other
         return want, off, info.eps / 2, info.tiny * info.eps / 2

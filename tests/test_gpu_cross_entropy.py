@@ -192,6 +192,45 @@ def test_fp32_of_other_magnitudes(size):
     _near(dw, *r.w_grad(torch.float32), "w_grad")
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("low,high", [(2.0**-20, 2.0**9), (2.0**9, 2.0**-20), (2.0**-14, 1.0), (1.0, 2.0**-14)])
+def test_pieces_of_different_magnitudes(t, low, high):
+    """The vocabulary's pieces are scaled for themselves, x once."""
+    torch = _torch()
+    n, dim, vocab = 17_000, 24, 18_000 if t == "bf16" else 9000
+    x, w, words = _case(n, dim, vocab, t, padding=0.3)
+    w = w.clone()
+    w[:vocab // 2] *= low
+    w[vocab // 2:] *= high
+    x = x / max(low, high)
+    g = torch.rand(n, device="cuda")
+    loss, lse, dx, dw = _run(x, w, words, g)
+    r = ref.CrossEntropy(x, w, words, g)
+    _near(lse, r.lse, r.lse_off, "lse")
+    _near(loss, r.loss, r.loss_off, "loss")
+    _near(dx, *r.x_grad(), "x_grad")
+    _near(dw, *r.w_grad(w.dtype), "w_grad")
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("x_size,w_size", [(2.0**-8, 2.0**8), (2.0**7, 2.0**-10), (2.0**-8, 1.0), (1.0, 2.0**-9)])
+def test_one_gradient_alone_at_other_magnitudes(t, x_size, w_size):
+    torch, sidco = _torch(), _sidco()
+    for n, dim, vocab in ((70, 64, 520), (130, 72, 1024)):
+        x, w, words = _case(n, dim, vocab, t)
+        x, w = x * x_size, w * w_size
+        loss, lse, dx, dw = _run(x, w, words)
+        r = ref.CrossEntropy(x, w, words, None)
+        _near(lse, r.lse, r.lse_off, "lse")
+        _near(dx, *r.x_grad(), "x_grad")
+        _near(dw, *r.w_grad(w.dtype), "w_grad")
+        a, b = torch.empty_like(dx), torch.empty_like(dw)
+        sidco.sidco_cross_entropy_grad(x, w, words, lse, None, x_grad=a)
+        sidco.sidco_cross_entropy_grad(x, w, words, lse, None, weight_grad=b)
+        torch.cuda.synchronize()
+        assert torch.equal(a, dx) and torch.equal(b, dw)
+
+
 def test_one_gradient_alone_and_losses_alone():
     torch, sidco = _torch(), _sidco()
     for t in ("f32", "bf16"):
