@@ -120,13 +120,16 @@ __device__ __forceinline__ float block_top(float top, float* lds)
     return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
 }
 
-// The largest of one of the three over the blocks of k_layout, for the whole block of 256.
+// The largest of one of the three over the blocks of k_layout, for the whole block of 256.  Without branches all loads are under way
+// at once: k_settle takes 4.8 us, and 8.4 with them.
 __device__ __forceinline__ float joined_top(const float* part, uint32_t blocks, float* lds)
 {
+    float v[kParts / 256];
+#pragma unroll
+    for (uint32_t k = 0; k < kParts / 256; ++k) v[k] = part[min(k * 256 + threadIdx.x, blocks - 1)];
     float top = 0.0f;
 #pragma unroll
-    for (int k = 0; k < kParts / 256; ++k)
-        if (k * 256 + threadIdx.x < blocks) top = fmaxf(top, part[k * 256 + threadIdx.x]);
+    for (int k = 0; k < kParts / 256; ++k) top = fmaxf(top, v[k]);
     return block_top(top, lds);
 }
 
@@ -223,7 +226,7 @@ __device__ __forceinline__ float lay(const Layout<typename M::T, typename M::H>&
 // x and w laid out with the guessed scales, and the largest finite magnitudes of x, w and the rows' gradient, a partial result from
 // each block (not in the forward pass of 16-bit operands, which nothing is scaled in).  The magnitudes are only known behind a pass over
 // everything: to find them first and lay out then is one read more.  Bound by memory: 700 and 10000 rows of 1500 fp32, 64 MB read and
-// 128 MB written (two halves of each by rows and transposed), 28 to 34 us; with the pass before it the training step took 391, not 380.
+// 128 MB written (two halves of each by rows and transposed), 28 to 34 us; with the pass before it the training step took 391, not 378.
 template <class M, bool Scaled>
 __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M::H> x, Layout<typename M::T, typename M::H> w, Source<float> g, float* part)
 {
@@ -250,8 +253,8 @@ __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M
 }
 
 // The scales that the largest magnitudes ask for, and what was laid out with another one once more.  A piece of w after the first
-// leaves those of x and P as they are.  8.4 us where the guess does, three lists of 2048 partial results for each block and a
-// launch; 35 where all is laid out again.
+// leaves those of x and P as they are.  4.8 us where the guess does, three lists of 2048 partial results for each block; about
+// 32 where all of that size is laid out again.
 constexpr uint32_t kSettleBlocks = 512;
 template <class M>
 __global__ __launch_bounds__(256) void k_settle(Layout<typename M::T, typename M::H> x, Layout<typename M::T, typename M::H> w, uint32_t blocks, bool later,
