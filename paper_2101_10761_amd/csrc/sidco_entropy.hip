@@ -89,6 +89,9 @@ __device__ __forceinline__ float scale_of(float top)
     return ldexpf(1.0f, e > 120 ? 120 : e);
 }
 
+// Of a power of two.  Two of them may have a product that no float holds.
+__device__ __forceinline__ int exponent_of(float scale) { return (int)(__builtin_bit_cast(uint32_t, scale) >> 23) - 127; }
+
 // The same, or the guess where it does: the largest is a half with room for rounding, and what halves cannot tell from zero is 2^-32 of it.
 __device__ __forceinline__ float settled(float top, float guess)
 {
@@ -702,14 +705,14 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
         });
 }
 
-// C = alpha A B^T over the columns that span.lines cover, of split number s from column s * lines on: rounded to T, on top of
+// C = 2^e A B^T over the columns that span.lines cover, of split number s from column s * lines on: rounded to T, on top of
 // `before` (fp32) and of C itself with `accumulate`.  Each split has a C of its own.  Bound by the matrix cores, at the rate of the
 // library's halves, 1.30 PFLOP/s: 8192 x 4096 over 32768 words 1.62 to 1.70 ms, 1.29 to 1.36; 32768 x 4096 over 8192 rows 1.63 to 1.73 ms; 49152
 // x 1024 over 2049 rows in two terms 449 us, 0.92 (33 lines a term); 700 x 1500 over 10000 words in pairs, 8 splits, 69 us, 0.91.
 struct Product {
     Plane<G> a, b;
     int64_t m, n;
-    const Scales* scales;  // alpha is one over its p and that of w, or with of_x of x
+    const Scales* scales;  // 2^e is one over its p and over that of w, or with of_x of x
     bool of_x;
     void* c;
     int64_t ldc, split_stride;
@@ -755,12 +758,14 @@ __global__ __launch_bounds__(Tl::kThreads) void k_product(Product p, Span span, 
         [&](uint32_t tile) {
             uint32_t ti, tj, split;
             places.at(tile, ti, tj, split);
-            const float alpha = 1.0f / (p.scales->p * (p.of_x ? p.scales->x : p.scales->w));
-            t.each([&](uint32_t row, uint32_t col, const v4f& v) {
+            const int shift = -exponent_of(p.scales->p) - exponent_of(p.of_x ? p.scales->x : p.scales->w);
+            t.each([&](uint32_t row, uint32_t col, v4f v) {
                 const int64_t r = (int64_t)ti * Tl::kM + row, c = (int64_t)tj * Tl::kN + col;
                 if (r >= p.m || c >= p.n) return;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], shift);
                 finish4<T>((T*)p.c + split * p.split_stride + r * p.ldc + c, p.before ? p.before + r * p.n + c : nullptr, p.accumulate, p.n - c,
-                           v * alpha);
+                           v);
             });
         });
 }

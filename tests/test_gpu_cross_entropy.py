@@ -212,6 +212,19 @@ def test_pieces_of_different_magnitudes(t, low, high):
     _near(dw, *r.w_grad(w.dtype), "w_grad")
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e-30, 1e30])
+def test_rows_gradients_of_other_magnitudes(t, size):
+    """Its power of two and those of x and w have a product that no float holds."""
+    torch = _torch()
+    x, w, words = _case(70, 64, 520, t)
+    g = torch.rand(70, device="cuda") * size
+    loss, lse, dx, dw = _run(x, w, words, g)
+    r = ref.CrossEntropy(x, w, words, g)
+    _near(dx, *r.x_grad(), "x_grad")
+    _near(dw, *r.w_grad(w.dtype), "w_grad")
+
+
 @pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("x_size,w_size", [(2.0**-8, 2.0**8), (2.0**7, 2.0**-10), (2.0**-8, 1.0), (1.0, 2.0**-9)])
 def test_one_gradient_alone_at_other_magnitudes(t, x_size, w_size):
