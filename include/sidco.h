@@ -657,7 +657,8 @@ int sidco_embedding(void *stream, const void *table, int table_dtype, int64_t vo
  * (accumulate = 0), or that added to table_grad and rounded once, where rows of words that
  * do not occur are not touched (accumulate = 1: several batches, or a table that is the
  * decoder's weight too).  Padding has no gradient, whatever its row of grad holds.  grad is
- * n x dim with row stride ldg, table_grad vocab x dim with row stride ldt.  Uses the
+ * n x dim with row stride ldg, table_grad vocab x dim with row stride ldt; n / 32, up to 2048
+ * words n / 8, times dim / 512, each rounded up, is at most 2^22 (SIDCO_ERR_SIZE).  Uses the
  * stream's workspace, of sidco_workspace_bytes_embedding_grad(n, dim).
  */
 int sidco_embedding_grad(void *stream, const void *grad, int grad_dtype, int64_t n, int64_t dim, int64_t ldg, const void *words,

@@ -3,6 +3,7 @@
 // The gradient adds up the rows of each word.  Places are first sorted by their words, places of the same word in order, so
 // that a word's sum is formed in one order whatever runs when, without atomics: a wave walks along sorted places with the sum
 // of its columns in registers and writes a row when the word changes.
+#include <algorithm>
 #include <utility>
 
 #include "sidco_elements.h"
@@ -249,6 +250,7 @@ __device__ __forceinline__ void fill_missing(const Sum<G, T>& p, int64_t v0)
     if (lane == 0) present[row] = lo < p.n && p.sorted.word[lo] == word;
     __syncthreads();
     fill_rows(p, v0, present);
+    __syncthreads();
 }
 
 // The sum of the rows at `count` places, in their order; eight of them are read at a time.
@@ -347,14 +349,17 @@ __global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p, const void* 
         own[k] = j < n ? word_at<I>(words, j, p.vocab) : p.vocab;
     }
     if (blockIdx.x >= p.sum_blocks) {
-        const int64_t v0 = (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows;
-        if (threadIdx.x < kFillRows) many[threadIdx.x] = 0;
-        __syncthreads();
+        for (int64_t v0 = (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows; v0 < p.vocab; v0 += (int64_t)(gridDim.x - p.sum_blocks) * kFillRows) {
+            if (threadIdx.x < kFillRows) many[threadIdx.x] = 0;
+            __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kRun / kSumBlock; ++k)
-            if (own[k] < p.vocab && own[k] - (uint32_t)v0 < kFillRows) many[own[k] - (uint32_t)v0] = 1;
-        __syncthreads();
-        return fill_rows(p, v0, many);
+            for (int k = 0; k < kRun / kSumBlock; ++k)
+                if (own[k] < p.vocab && own[k] - (uint32_t)v0 < kFillRows) many[own[k] - (uint32_t)v0] = 1;
+            __syncthreads();
+            fill_rows(p, v0, many);
+            __syncthreads();
+        }
+        return;
     }
 #pragma unroll
     for (int k = 0; k < kRun / kSumBlock; ++k) keys[k * kSumBlock + threadIdx.x] = own[k];
@@ -396,7 +401,11 @@ __global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p, const void* 
 template <class G, class T>
 __global__ __launch_bounds__(kSumBlock) void k_sum(Sum<G, T> p)
 {
-    if (blockIdx.x >= p.sum_blocks) return fill_missing(p, (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows);
+    if (blockIdx.x >= p.sum_blocks) {
+        for (int64_t v0 = (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows; v0 < p.vocab; v0 += (int64_t)(gridDim.x - p.sum_blocks) * kFillRows)
+            fill_missing(p, v0);
+        return;
+    }
     const int64_t item = (int64_t)blockIdx.x * (kSumBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t chunk = item / p.strips, strip = item % p.strips;
     if (chunk >= p.chunks) return;
@@ -512,12 +521,21 @@ void launch_embedding(const Lookup& q, hipStream_t s)
     });
 }
 
+// A launch has less than 2^32 threads.  Blocks that fill rows, kMostFill at most, take more than kFillRows of them in a table of
+// more than 33 million.
+constexpr int64_t kMostBlocks = 1 << 22, kMostFill = 1 << 21;
+bool embedding_grad_fits(int64_t n, int64_t cols)
+{
+    const int64_t chunk = n <= kRun ? kFewPlaces : chunk_of(n, cols);
+    return (n + chunk - 1) / chunk * ((cols + kStrip - 1) / kStrip) <= kMostBlocks;
+}
+
 size_t embedding_grad_scratch(int64_t n, int64_t cols) { return (size_t)SumLayout(n, cols).total; }
 
 void launch_embedding_grad(const Lookup& q, char* scratch, hipStream_t s)
 {
     const int64_t n = q.words.n, strips = (q.cols + kStrip - 1) / kStrip, waves = kSumBlock / 64;
-    const int64_t fill = q.accumulate ? 0 : (q.words.vocab + kFillRows - 1) / kFillRows;
+    const int64_t fill = q.accumulate ? 0 : std::min((q.words.vocab + kFillRows - 1) / kFillRows, kMostFill);
     const bool few = n <= kRun;
     const SumLayout l(n, q.cols);
     Sorted now = {(uint32_t*)scratch, (uint32_t*)(scratch + l.each)};

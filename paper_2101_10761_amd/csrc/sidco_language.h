@@ -34,6 +34,7 @@ struct Lookup {
     bool accumulate;
 };
 void launch_embedding(const Lookup& q, hipStream_t s);
+bool embedding_grad_fits(int64_t n, int64_t cols);  // one launch's blocks
 size_t embedding_grad_scratch(int64_t n, int64_t cols);
 void launch_embedding_grad(const Lookup& q, char* scratch, hipStream_t s);
 

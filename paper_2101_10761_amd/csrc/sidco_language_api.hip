@@ -68,7 +68,7 @@ int sidco_embedding(void* stream, const void* table, int table_dtype, int64_t vo
     if (int rc = check_words(words, word_type, n, vocab)) return rc;
     if (int rc = check_matrix(table, table_dtype, dim, ldt)) return rc;
     if (int rc = check_matrix(out, out_dtype, dim, ldo)) return rc;
-    if (!isfinite(scale)) return SIDCO_ERR_ARG;
+    if (!isfinite(scale) || table == out) return SIDCO_ERR_ARG;
     const Lookup q = {{words, word_type == SIDCO_WORD_I64, n, vocab}, matrix(table, table_dtype, ldt), matrix(out, out_dtype, ldo), dim, scale, false};
     launch_embedding(q, (hipStream_t)stream);
     return launched();
@@ -76,7 +76,7 @@ int sidco_embedding(void* stream, const void* table, int table_dtype, int64_t vo
 
 size_t sidco_workspace_bytes_embedding_grad(int64_t n, int64_t dim)
 {
-    return extent(n) && extent(dim) ? workspace_with_scratch(embedding_grad_scratch(n, dim)) : 0;
+    return extent(n) && extent(dim) && embedding_grad_fits(n, dim) ? workspace_with_scratch(embedding_grad_scratch(n, dim)) : 0;
 }
 
 int sidco_embedding_grad(void* stream, const void* grad, int grad_dtype, int64_t n, int64_t dim, int64_t ldg, const void* words,
@@ -85,7 +85,7 @@ int sidco_embedding_grad(void* stream, const void* grad, int grad_dtype, int64_t
     if (int rc = check_words(words, word_type, n, vocab)) return rc;
     if (int rc = check_matrix(grad, grad_dtype, dim, ldg)) return rc;
     if (int rc = check_matrix(table_grad, table_dtype, dim, ldt)) return rc;
-    if ((n + 31) / 32 * ((dim + 511) / 512) > (int64_t)INT32_MAX / 2) return SIDCO_ERR_SIZE;  // a block's number has 31 bits
+    if (!embedding_grad_fits(n, dim)) return SIDCO_ERR_SIZE;
     if (!isfinite(scale) || !flag(accumulate) || grad == table_grad) return SIDCO_ERR_ARG;
     const Lookup q = {{words, word_type == SIDCO_WORD_I64, n, vocab}, matrix(table_grad, table_dtype, ldt), matrix(grad, grad_dtype, ldg), dim,
                       scale, accumulate != 0};

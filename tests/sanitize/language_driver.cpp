@@ -34,9 +34,12 @@ int main()
     EXPECT(sidco_embedding(nullptr, x, 0, INT64_MAX, 4, 4, words, 1, 4, 1.0f, y, 0, 4) == SIDCO_ERR_SIZE);
     EXPECT(sidco_embedding(nullptr, x, 0, 4, 4, INT64_MIN, words, 1, 4, 1.0f, y, 0, 4) == SIDCO_ERR_SIZE);
     EXPECT(sidco_embedding_grad(nullptr, x, 0, most, most, most, words, 1, most, 1.0f, 0, y, 0, most) == SIDCO_ERR_SIZE);
-    EXPECT(sidco_embedding_grad(nullptr, x, 0, most, 4, 4, words, 1, 4, 1.0f, 0, y, 0, 4) == SIDCO_ERR_WORKSPACE);
+    EXPECT(sidco_embedding_grad(nullptr, x, 0, most, 4, 4, words, 1, 4, 1.0f, 0, y, 0, 4) == SIDCO_ERR_SIZE);
+    EXPECT(sidco_embedding_grad(nullptr, x, 0, (int64_t)1 << 27, 4, 4, words, 1, 4, 1.0f, 0, y, 0, 4) == SIDCO_ERR_WORKSPACE);
+    EXPECT(sidco_embedding_grad(nullptr, x, 0, 9, most, most, words, 1, 4, 1.0f, 0, y, 0, most) == SIDCO_ERR_SIZE);
     EXPECT(sidco_embedding_grad(nullptr, x, 0, 4, 4, 4, words, 1, 4, 1.0f, 0, x, 0, 4) == SIDCO_ERR_ARG);
-    EXPECT(sidco_workspace_bytes_embedding_grad(most, 1) > 0 && sidco_workspace_bytes_embedding_grad(most, most) > 0);
+    EXPECT(sidco_workspace_bytes_embedding_grad((int64_t)1 << 27, 512) > 0 && sidco_workspace_bytes_embedding_grad(8, most) > 0);
+    EXPECT(sidco_workspace_bytes_embedding_grad(((int64_t)1 << 27) + 1, 1) == 0 && sidco_workspace_bytes_embedding_grad(most, most) == 0);
     EXPECT(sidco_workspace_bytes_embedding_grad(big, 1) == 0 && sidco_workspace_bytes_embedding_grad(1, INT64_MIN) == 0);
 
     EXPECT(sidco_dropout_blocks(most, most) == most * ((int64_t)1 << 28));

@@ -62,6 +62,7 @@ def test_sizes(lib):
             sidco.sidco_dropout_blocks(rows, cols)
     assert 0 < sidco.sidco_workspace_bytes_embedding_grad(1, 1) < sidco.sidco_workspace_bytes_embedding_grad(10**6, 1500)
     assert sidco.sidco_workspace_bytes_embedding_grad(0, 1) == 0 and sidco.sidco_workspace_bytes_embedding_grad(1, 2**31) == 0
+    assert sidco.sidco_workspace_bytes_embedding_grad(2**27, 512) > 0 and sidco.sidco_workspace_bytes_embedding_grad(2**27 + 1, 1) == 0
 
 
 def test_embedding_refusals(lib):
@@ -72,11 +73,12 @@ def test_embedding_refusals(lib):
     good = dict(stream=None, table=OK, t=0, vocab=10, dim=20, ldt=20, words=OK, wt=0, n=5, scale=1.0, out=OTHER, ot=0, ldo=20)
     _refuses(lib.sidco_embedding, good, words + [
         (-1, [dict(table=None), dict(out=None)]),
-        (-8, [dict(table=C.c_void_p(4098)), dict(ot=1, out=C.c_void_p(4097))])])
+        (-8, [dict(table=C.c_void_p(4098)), dict(ot=1, out=C.c_void_p(4097))]),
+        (-9, [dict(out=OK)])])
     good = dict(stream=None, grad=OK, t=0, n=5, dim=20, ldo=20, words=OK, wt=0, vocab=10, scale=1.0, acc=0, table=OTHER, ot=0, ldt=20)
     _refuses(lib.sidco_embedding_grad, good, words + [
         (-1, [dict(table=None), dict(grad=None)]),
-        (-2, [dict(n=2**31 - 1, dim=2**20, ldo=2**20, ldt=2**20)]),
+        (-2, [dict(n=2**31 - 1, dim=2**20, ldo=2**20, ldt=2**20), dict(n=2**27 + 1), dict(n=9, dim=2**31 - 1, ldo=2**31 - 1, ldt=2**31 - 1)]),
         (-8, [dict(grad=C.c_void_p(4098)), dict(ot=1, table=C.c_void_p(4097))]),
         (-9, [dict(acc=2), dict(acc=-1), dict(table=OK)])])
 

@@ -200,6 +200,19 @@ def test_far_rows():
     assert torch.equal(table[words].float(), 2 * out)
 
 
+@pytest.mark.parametrize("n", [3, 2049])
+def test_gradient_of_a_table_of_more_rows_than_blocks_for_them(n):
+    torch, sidco = _torch(), _sidco()
+    vocab = 2**27 + 5
+    words = torch.randint(0, vocab, (n,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(n))
+    words[:3] = torch.tensor([0, vocab - 1, vocab - 1], device="cuda")
+    table = torch.full((vocab, 1), 3.0, dtype=torch.float16, device="cuda")
+    sidco.sidco_embedding_grad(torch.ones(n, 1, device="cuda"), words, table)
+    torch.cuda.synchronize()
+    distinct, counts = torch.unique(words, return_counts=True)
+    assert torch.equal(table[distinct, 0].long(), counts) and int((table != 0).sum()) == len(distinct)
+
+
 def test_binding_refuses_other_shapes_and_types():
     torch, sidco = _torch(), _sidco()
     x, words = torch.zeros(6, 8, device="cuda"), torch.zeros(6, dtype=torch.int64, device="cuda")
