@@ -236,7 +236,7 @@ __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M
     __shared__ float tile[64][65];
     __shared__ float lds[4];
     const uint32_t first = x.tiles_r * x.tiles_c, all = first + w.tiles_r * w.tiles_c;
-    float top[3] = {0.0f, 0.0f, 0.0f};
+    float top[3] = {0.0f, 0.0f, g.at ? 0.0f : 1.0f};  // a gradient without an address is ones
     for (uint32_t t = blockIdx.x; t < all; t += gridDim.x) {
         if (t < first)
             top[0] = lay<M>(x, t, M::kScaled ? kGuessX : 1.0f, tile, top[0]);
@@ -984,7 +984,7 @@ struct ForwardPlan {
 
 WordList list(const Words& w) { return {w.at, w.wide, (uint32_t)w.vocab}; }
 
-// x and w laid out and their scales settled; g is the rows' gradient, or has no address.
+// x and w laid out and their scales settled; g is the rows' gradient, or without an address ones.
 template <class M, bool Scaled>
 void lay_out(const Layout<typename M::T, typename M::H>& x, const Layout<typename M::T, typename M::H>& w, const Source<float>& g, bool later,
              float* part, Scales* scales, hipStream_t s)

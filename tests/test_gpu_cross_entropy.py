@@ -274,6 +274,38 @@ def test_results_lie_within_their_rows():
             assert bool((whole == 9.0).all())
 
 
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+def test_no_loss_gradient_is_ones(t):
+    """To the last bit, where probabilities are small too."""
+    torch = _torch()
+    for n, dim, vocab in ((3, 40, 30_000), (130, 64, 5000)):
+        x, w, words = _case(n, dim, vocab, t)
+        _, _, dx, dw = _run(x, w, words)
+        _, _, ox, ow = _run(x, w, words, torch.ones(n, device="cuda"))
+        assert torch.equal(dx, ox) and torch.equal(dw, ow)
+
+
+@pytest.mark.parametrize("n", [3, 40])
+def test_far_words(n):
+    """Offsets into weight and gradient that pass 32 bits in elements and in bytes."""
+    torch = _torch()
+    dim, vocab = 2048, 1_100_000
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    w = torch.empty(vocab, dim, dtype=torch.bfloat16, device="cuda").normal_(std=dim**-0.5, generator=gen)
+    words = torch.randint(vocab - 2000, vocab, (n,), device="cuda", generator=gen)
+    words[0] = 0
+    x = (torch.randn(n, dim, device="cuda", generator=gen) + 4 * w[words]).bfloat16()
+    loss, lse, dx, dw = _run(x, w, words)
+    r = ref.CrossEntropy(x, w, words)
+    _near(lse, r.lse, r.lse_off, "lse")
+    _near(loss, r.loss, r.loss_off, "loss")
+    _near(dx, *r.x_grad(), "x_grad")
+    for part in (slice(0, 1000), slice(vocab // 2, vocab // 2 + 1000), slice(vocab - 2000, vocab)):
+        r.p, r.p_off, keep = r.p[:, part], r.p_off[:, part], (r.p, r.p_off)
+        _near(dw[part], *r.w_grad(w.dtype), ("w_grad", part))
+        r.p, r.p_off = keep
+
+
 def test_gradient_against_differences():
     """Central differences of the loss, for steps of one coordinate of x or w."""
     torch, sidco = _torch(), _sidco()
