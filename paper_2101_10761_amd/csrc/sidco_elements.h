@@ -67,6 +67,13 @@ struct Eight {
         for (int i = 0; i < 8; ++i)
             if (i < n) p[i] = v[i / kPer][i % kPer];
     }
+    // the last n of them, less than eight
+    __device__ __forceinline__ void store_last(T* p, int64_t n) const
+    {
+#pragma unroll
+        for (int i = 1; i < 8; ++i)
+            if (i >= 8 - n) p[i] = v[i / kPer][i % kPer];
+    }
     __device__ __forceinline__ float get(int i) const { return (float)v[i / kPer][i % kPer]; }
     __device__ __forceinline__ void set(int i, float x) { v[i / kPer][i % kPer] = (T)x; }
 };

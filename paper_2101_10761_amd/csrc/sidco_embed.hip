@@ -4,6 +4,7 @@
 // that a word's sum is formed in one order whatever runs when, without atomics: a wave walks along sorted places with the sum
 // of its columns in registers and writes a row when the word changes.
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "sidco_elements.h"
@@ -58,8 +59,9 @@ __global__ __launch_bounds__(kRowBlock) void k_embedding(Look<I, T, R> p)
 // Runs of kRun places are sorted by counting: a place's rank in its run is the number of places with a smaller word, and of
 // the same word before it.  All comparisons are independent of each other, kRun a place, so that one launch of many small
 // blocks does them.  Then up to kWays neighbouring runs are merged at a time: a place moves up by the number of places of
-// each other run that come before it, which a search in that run finds.  65536 places 15.4 + 15.4 us, 4099 5.3 + 6.8.
-constexpr int kRun = 2048, kWays = 32;
+// each other run that come before it, which a search in that run finds.  65536 places 13.3 + 15.7 us.  Up to kLongRun places are one
+// run: 4099 6.7 us, with runs of kRun 5.3 + 6.8.
+constexpr int kRun = 2048, kLongRun = 8192, kWays = 32;
 constexpr int kSortLanes = 16;  // lanes that share the comparisons of a place
 
 struct Sorted {
@@ -67,23 +69,24 @@ struct Sorted {
     uint32_t* place;
 };
 
-// Each: places that a group of lanes ranks at once.
-template <class I, int Each>
+// Each: places that a group of lanes ranks at once; Run: places of a run.
+template <class I, int Each, int Run>
 __global__ __launch_bounds__(256) void k_sort_run(const void* words, int64_t n, uint32_t vocab, Sorted out)
 {
     constexpr int kPlaces = 256 / kSortLanes * Each;  // of a block, within one chunk of 64
     static_assert(64 % kPlaces == 0, "a block's places lie in one chunk");
-    const int64_t first = (int64_t)blockIdx.x * kPlaces, run = first / kRun * kRun;
-    const int64_t len = n - run < kRun ? n - run : kRun;
-    __shared__ __align__(16) uint32_t keys[kRun];
-    uint32_t own[kRun / 256];
+    const int64_t first = (int64_t)blockIdx.x * kPlaces, run = first / Run * Run;
+    const int64_t len = n - run < Run ? n - run : Run;
+    __shared__ __align__(16) uint32_t keys[Run];
+    uint32_t own[Run / 256];
 #pragma unroll
-    for (int k = 0; k < kRun / 256; ++k) {
+    for (int k = 0; k < Run / 256; ++k) {
         const int j = k * 256 + threadIdx.x;
-        own[k] = j < len ? word_at<I>(words, run + j, vocab) : ~0u;
+        own[k] = word_at<I>(words, run + (j < len ? j : len - 1), vocab);  // without a branch, which would wait for each
+        own[k] = j < len ? own[k] : ~0u;
     }
 #pragma unroll
-    for (int k = 0; k < kRun / 256; ++k) keys[k * 256 + threadIdx.x] = own[k];
+    for (int k = 0; k < Run / 256; ++k) keys[k * 256 + threadIdx.x] = own[k];
     __syncthreads();
     const int lane = threadIdx.x % kSortLanes, group = threadIdx.x / kSortLanes;
     uint32_t mine[Each], rank[Each];
@@ -304,8 +307,9 @@ __device__ __forceinline__ void join_waves(float (&sum)[8], float (*lds)[64][9])
 
 // Few places, in one launch and without a workspace: every block has all words in LDS.  A wave looks at a place, and if its word
 // occurs at no place before it, lists the word's places and adds up their rows; a word of many places is taken by the block's
-// waves together.  Bound by the table's writes and by the chain of words, list, rows: whole calls for 10000 x 1500 fp32, 1, 700 and 2048
-// words 13.6, 15.1 and 26.0 us, where torch's zeros alone take 10.6; 2049 words, sorted, 31.8.
+// waves together.  Bound by the table's writes and by the chain of words, list, rows: whole calls for 10000 x 1500 fp32, 1, 700, 1024 and
+// 2048 words 14.3, 14.3, 16.1 and 20.8 us, where torch's zeros alone take 10.6; 2049 words, sorted, 23.8.  Onto 50000 x 1024 bf16 700, 2048
+// and 2049 words 6.3, 12.4 and 14.7.
 constexpr int kFewPlaces = kSumBlock / 64;     // of a block
 constexpr int kAlone = 16, kListed = 64;       // of a wave, and those that it lists
 
@@ -346,7 +350,8 @@ __global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p, const void* 
 #pragma unroll
     for (int k = 0; k < kRun / kSumBlock; ++k) {
         const int j = k * kSumBlock + threadIdx.x;
-        own[k] = j < n ? word_at<I>(words, j, p.vocab) : p.vocab;
+        own[k] = word_at<I>(words, j < n ? j : n - 1, p.vocab);
+        own[k] = j < n ? own[k] : p.vocab;
     }
     if (blockIdx.x >= p.sum_blocks) {
         for (int64_t v0 = (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows; v0 < p.vocab; v0 += (int64_t)(gridDim.x - p.sum_blocks) * kFillRows) {
@@ -397,8 +402,13 @@ __global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p, const void* 
 
 // Many places: a wave adds up the rows of `chunk` sorted ones in one strip of columns.  A word whose places all lie in the chunk
 // is done; the sums of one that began before it or goes on after it are kept for k_join.  Bound by memory: 65536 rows of 4096 in
-// bf16 into 131072 in fp32, 484 to 515 us for 2.7 GB, 5.2 to 5.5 TB/s.
-template <class G, class T>
+// bf16 into 131072 in fp32, 486 to 502 us for 2.7 GB, 5.4 to 5.6 TB/s.
+//
+// Where waves are few it is the chain of loads that counts: the chunk's words and places come with one load of the wave, and the
+// rows of eight places, and of the table if it is added to, are under way together, with nothing between them that waits: 4099 rows of
+// 1111 onto a table, fp16, 9.8 us, where a wait for each word, place and row took 16.3.
+// So a lane at the row's end takes its last eight columns, some of which are its neighbour's and not stored again.
+template <class G, class T, bool Accumulate>
 __global__ __launch_bounds__(kSumBlock) void k_sum(Sum<G, T> p)
 {
     if (blockIdx.x >= p.sum_blocks) {
@@ -409,40 +419,74 @@ __global__ __launch_bounds__(kSumBlock) void k_sum(Sum<G, T> p)
     const int64_t item = (int64_t)blockIdx.x * (kSumBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t chunk = item / p.strips, strip = item % p.strips;
     if (chunk >= p.chunks) return;
-    const int64_t from = chunk * p.chunk, to = from + p.chunk < p.n ? from + p.chunk : p.n;
-    const int64_t c = strip * kStrip + (threadIdx.x & 63) * 8, left = p.cols - c;
-    if (left <= 0) return;
-    const uint32_t before = from > 0 ? p.sorted.word[from - 1] : ~0u;
-    float sum[8] = {};
-    bool head = p.sorted.word[from] == before;  // the sum began in an earlier chunk
-    for (int64_t base = from; base < to; base += 8) {
-        Eight<G> g[8];
-        uint32_t word[9];
+    const int64_t from = chunk * p.chunk;
+    const int lane = threadIdx.x & 63, count = (int)(from + p.chunk < p.n ? p.chunk : p.n - from);
+    // of places from - 1 to from + 62
+    const int64_t mine = from - 1 + lane, real = mine < 0 ? 0 : (mine < p.n ? mine : p.n - 1);
+    const uint32_t words = p.sorted.word[real], places = p.sorted.place[real];
+    const uint32_t kept = mine == real ? words : ~0u;
+    auto word_at = [&](int k) { return (uint32_t)__builtin_amdgcn_readlane((int)kept, k + 1); };
+    auto place_at = [&](int k) { return (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)places, k + 1); };
+    if (word_at(0) >= p.vocab) return;  // padding comes last
+    const int64_t c = strip * kStrip + lane * 8;
+    auto walk = [&](auto narrow) {
+        constexpr bool kNarrow = decltype(narrow)::value;  // less than eight columns
+        const int64_t at = kNarrow || c < p.cols - 8 ? c : p.cols - 8, left = c < p.cols ? p.cols - c : 0;
+        auto load = [&](auto& e, auto* row) {
+            if constexpr (kNarrow)
+                e.load(row, left);
+            else
+                e.load(row + at);
+        };
+        auto store = [&](const auto& e, auto* row) {
+            if constexpr (kNarrow)
+                e.store(row, left);
+            else if (left >= 8)
+                e.store(row + at);
+            else
+                e.store_last(row + at, left);
+        };
+        float sum[8] = {};
+        bool head = word_at(0) == word_at(-1);  // the sum began in an earlier chunk
+        for (int base = 0; base < count; base += 8) {
+            Eight<G> g[8];
+            Eight<T> old[8];
+            // behind the chunk's last place, or among padding, these are rows that are not used
 #pragma unroll
-        for (int u = 0; u < 9; ++u) word[u] = base + u < p.n ? p.sorted.word[base + u] : ~0u;
+            for (int u = 0; u < 8; ++u) load(g[u], p.rows + place_at(base + u) * p.ldr);
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (base + u < to && word[u] < p.vocab) g[u].load(p.rows + (int64_t)p.sorted.place[base + u] * p.ldr + c, left);
+            for (int u = 0; u < 8; ++u)
+                if (Accumulate && word_at(base + u) < p.vocab && word_at(base + u + 1) != word_at(base + u))
+                    load(old[u], (const T*)p.table + (int64_t)word_at(base + u) * p.ldt);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            if (base + u >= to || word[u] >= p.vocab) return;  // padding comes last
+            for (int u = 0; u < 8; ++u) {
+                const uint32_t word = word_at(base + u);
+                if (base + u >= count || word >= p.vocab) return;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += g[u].get(k);
-            const bool same = word[u + 1] == word[u], last = base + u + 1 == to;
-            if (same && !last) continue;
-            if (head || same) {
-                Eight<float> f;
+                for (int k = 0; k < 8; ++k) sum[k] += g[u].get(k);
+                const bool same = word_at(base + u + 1) == word, last = base + u + 1 == count;
+                if (same && !last) continue;
+                if (head || same) {
+                    Eight<float> f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) f.set(k, sum[k]);
-                f.store(p.partial + (chunk * 2 + (head ? 0 : 1)) * p.cols + c, left);
-            } else {
-                put_row(p.table + (int64_t)word[u] * p.ldt + c, sum, p.scale, p.accumulate, left);
+                    for (int k = 0; k < 8; ++k) f.set(k, sum[k]);
+                    store(f, p.partial + (chunk * 2 + (head ? 0 : 1)) * p.cols);
+                } else {
+                    Eight<T> t;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) t.set(k, Accumulate ? fmaf(p.scale, sum[k], old[u].get(k)) : p.scale * sum[k]);
+                    store(t, p.table + (int64_t)word * p.ldt);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+                head = false;
             }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
-            head = false;
         }
-    }
+    };
+    if (p.cols < 8)
+        walk(std::true_type());
+    else
+        walk(std::false_type());
 }
 
 // The sums of words whose places lie in several chunks: a block for each strip and chunk in which one begins.  Bound by the launch of
@@ -452,9 +496,10 @@ template <class G, class T>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_join(Sum<G, T> p)
 {
     const int64_t chunk = blockIdx.x / p.strips, from = chunk * p.chunk, to = from + p.chunk;
-    const uint32_t word = p.sorted.word[to - 1];
-    if (word >= p.vocab || p.sorted.word[to] != word) return;                                // none goes on
-    if (p.sorted.word[from] == word && from > 0 && p.sorted.word[from - 1] == word) return;  // it began before
+    const uint32_t word = p.sorted.word[to - 1], next = p.sorted.word[to], first_word = p.sorted.word[from];
+    const uint32_t before = p.sorted.word[from > 0 ? from - 1 : 0];
+    if (word >= p.vocab || next != word) return;                            // none goes on
+    if (first_word == word && from > 0 && before == word) return;           // it began before
     __shared__ float lds[kJoinWaves][64][9];
     const int64_t c = blockIdx.x % p.strips * kStrip + (threadIdx.x & 63) * 8, left = p.cols - c;
     const int64_t count = 1 + length_of(p.sorted.word, to, p.chunk, p.n, word);  // partial sums, of this chunk the second
@@ -543,11 +588,11 @@ void launch_embedding_grad(const Lookup& q, char* scratch, hipStream_t s)
     float* partial = (float*)(scratch + 4 * l.each);
     by_word(q.words, [&](auto i) {
         typedef decltype(i) I;
-        if (!few && n <= 8192)  // few blocks: less for each
-            k_sort_run<I, 1><<<(uint32_t)((n + 15) / 16), 256, 0, s>>>(q.words.at, n, (uint32_t)q.words.vocab, now);
+        if (!few && n <= kLongRun)
+            k_sort_run<I, 1, kLongRun><<<(uint32_t)((n + 15) / 16), 256, 0, s>>>(q.words.at, n, (uint32_t)q.words.vocab, now);
         else if (!few)
-            k_sort_run<I, 4><<<(uint32_t)((n + 63) / 64), 256, 0, s>>>(q.words.at, n, (uint32_t)q.words.vocab, now);
-        for (int64_t len = kRun; len < n; len *= kWays) {
+            k_sort_run<I, 4, kRun><<<(uint32_t)((n + 63) / 64), 256, 0, s>>>(q.words.at, n, (uint32_t)q.words.vocab, now);
+        for (int64_t len = n <= kLongRun ? kLongRun : kRun; len < n; len *= kWays) {
             k_merge<<<(uint32_t)((n + 63) / 64), 64 * kMergeWaves, 0, s>>>(now, other, n, len);
             std::swap(now, other);
         }
@@ -563,7 +608,10 @@ void launch_embedding_grad(const Lookup& q, char* scratch, hipStream_t s)
                     k_sum_few<I, G, T><<<(uint32_t)(blocks + fill), kSumBlock, 0, s>>>(p, q.words.at);
                     return;
                 }
-                k_sum<G, T><<<(uint32_t)(blocks + fill), kSumBlock, 0, s>>>(p);
+                if (q.accumulate)
+                    k_sum<G, T, true><<<(uint32_t)blocks, kSumBlock, 0, s>>>(p);
+                else
+                    k_sum<G, T, false><<<(uint32_t)(blocks + fill), kSumBlock, 0, s>>>(p);
                 k_join<G, T><<<(uint32_t)((chunks - 1) * strips), 64 * kJoinWaves, 0, s>>>(p);
             });
         });
