@@ -183,6 +183,9 @@ __global__ __launch_bounds__(64 * kMergeWaves) void k_merge(Sorted in, Sorted ou
 constexpr int kStrip = 512;  // columns of a wave
 constexpr int kFillRows = 16;
 constexpr int kSumBlock = 512;  // threads of a block that adds up or fills rows
+// Of one of k_sum's that only adds up: 4099 rows of 1111 fp16 19.7 us with 256 and 20.4 with 512, 8192 of 4096 bf16 onto fp32 48.9 and
+// 53.5; with rows to be filled in the same launch, 65536 of 4096, 568 and 549.
+constexpr int kAddBlock = 256;
 
 template <class G, class T>
 struct Sum {
@@ -406,17 +409,18 @@ __global__ __launch_bounds__(kSumBlock) void k_sum_few(Sum<G, T> p, const void* 
 //
 // Where waves are few it is the chain of loads that counts: the chunk's words and places come with one load of the wave, and the
 // rows of eight places, and of the table if it is added to, are under way together, with nothing between them that waits: 4099 rows of
-// 1111 onto a table, fp16, 9.8 us, where a wait for each word, place and row took 16.3.
+// 1111 onto a table, fp16, 8.2 us, where a wait for each word, place and row took 16.3.
 // So a lane at the row's end takes its last eight columns, some of which are its neighbour's and not stored again.
 template <class G, class T, bool Accumulate>
-__global__ __launch_bounds__(kSumBlock) void k_sum(Sum<G, T> p)
+__global__ __launch_bounds__(Accumulate ? kAddBlock : kSumBlock) void k_sum(Sum<G, T> p)
 {
-    if (blockIdx.x >= p.sum_blocks) {
+    constexpr int kWaves = (Accumulate ? kAddBlock : kSumBlock) / 64;
+    if (!Accumulate && blockIdx.x >= p.sum_blocks) {
         for (int64_t v0 = (int64_t)(blockIdx.x - p.sum_blocks) * kFillRows; v0 < p.vocab; v0 += (int64_t)(gridDim.x - p.sum_blocks) * kFillRows)
             fill_missing(p, v0);
         return;
     }
-    const int64_t item = (int64_t)blockIdx.x * (kSumBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t item = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t chunk = item / p.strips, strip = item % p.strips;
     if (chunk >= p.chunks) return;
     const int64_t from = chunk * p.chunk;
@@ -579,7 +583,7 @@ size_t embedding_grad_scratch(int64_t n, int64_t cols) { return (size_t)SumLayou
 
 void launch_embedding_grad(const Lookup& q, char* scratch, hipStream_t s)
 {
-    const int64_t n = q.words.n, strips = (q.cols + kStrip - 1) / kStrip, waves = kSumBlock / 64;
+    const int64_t n = q.words.n, strips = (q.cols + kStrip - 1) / kStrip, waves = (q.accumulate ? kAddBlock : kSumBlock) / 64;
     const int64_t fill = q.accumulate ? 0 : std::min((q.words.vocab + kFillRows - 1) / kFillRows, kMostFill);
     const bool few = n <= kRun;
     const SumLayout l(n, q.cols);
@@ -609,7 +613,7 @@ void launch_embedding_grad(const Lookup& q, char* scratch, hipStream_t s)
                     return;
                 }
                 if (q.accumulate)
-                    k_sum<G, T, true><<<(uint32_t)blocks, kSumBlock, 0, s>>>(p);
+                    k_sum<G, T, true><<<(uint32_t)blocks, kAddBlock, 0, s>>>(p);
                 else
                     k_sum<G, T, false><<<(uint32_t)(blocks + fill), kSumBlock, 0, s>>>(p);
                 k_join<G, T><<<(uint32_t)((chunks - 1) * strips), 64 * kJoinWaves, 0, s>>>(p);
