@@ -940,6 +940,13 @@ bool takes_few(int64_t rows, int64_t dim, const Matrix& w, bool lay_w)
     return parts(rows, kFewRows) <= (lay_w && !between ? 3 : 1) && dim >= 8 && few_steps<M>(dim) <= 16;
 }
 
+// A CU's registers hold two blocks where a wave's operands take few of them.
+template <class M>
+int64_t few_blocks(int64_t rows, int64_t dim, int64_t vocab)
+{
+    return std::min(parts(vocab, 16), few_steps<M>(dim) <= (rows <= 16 ? 10 : 6) ? kFewBlocks : kFewBlocks / 2);
+}
+
 void join_rows(const float2* pairs, uint32_t width, int64_t rows, const WordList& words, const float* mine, float* loss, float* lse, hipStream_t s)
 {
     if (width >= 512 && rows <= 4096)
@@ -976,7 +983,7 @@ struct ForwardPlan {
             const RowPlan plan = forward_plan<M>(rows, v, pitch / kPer);
             return std::max(plan.rows * forward_width(plan.pick, v), (rows - plan.rows) * forward_width(plan.rest_pick, v));
         };
-        pairs = s.get<float2>(few ? n * kFewBlocks : std::max(pairs_of(at_once), pairs_of((n - 1) % kRowsAtOnce + 1)));
+        pairs = s.get<float2>(few ? n * few_blocks<M>(n, q.dim, v) : std::max(pairs_of(at_once), pairs_of((n - 1) % kRowsAtOnce + 1)));
         mine = s.get<float>(at_once);
         bytes = s.used;
     }
@@ -1004,9 +1011,7 @@ void forward(const Entropy& q, char* scratch, hipStream_t s)
     const ForwardPlan<M> f(q, scratch);
     const int64_t n = q.words.n, v = q.words.vocab;
     if (f.few) {
-        const int64_t groups = parts(v, 16), steps = few_steps<M>(q.dim);
-        // a CU's registers hold two blocks where a wave's operands take few of them
-        const int64_t blocks = std::min(groups, steps <= (n <= 16 ? 10 : 6) ? kFewBlocks : kFewBlocks / 2);
+        const int64_t groups = parts(v, 16), steps = few_steps<M>(q.dim), blocks = few_blocks<M>(n, q.dim, v);
         int64_t r = 0, rows = 0;
         auto go = [&](auto kernel) {
             const Few<T> p = {(const T*)q.x.at + r * q.x.ld, (const T*)q.w.at, q.x.ld, q.w.ld, (uint32_t)rows, (uint32_t)q.dim, (uint32_t)groups,

@@ -58,7 +58,7 @@ struct Entropy {
     bool accumulate;           // onto w_grad
 };
 constexpr int64_t kEntropyMaxRows = 1 << 22, kEntropyMaxDim = 1 << 21;
-size_t entropy_scratch(const Entropy& q);       // of x, w only whether they lie in whole lines
+size_t entropy_scratch(const Entropy& q);       // of x, w only how their rows lie
 size_t entropy_grad_scratch(const Entropy& q);  // and of the gradients which there are and w_grad's type
 void launch_entropy(const Entropy& q, char* scratch, hipStream_t s);
 void launch_entropy_grad(const Entropy& q, char* scratch, hipStream_t s);

@@ -48,13 +48,14 @@ int check_entropy(const void* x, const void* w, int dtype, int64_t n, int64_t di
     return entropy_sizes(n, dim, vocab) ? SIDCO_OK : SIDCO_ERR_SIZE;
 }
 
-// Of any call with these sizes: x and w as if they had to be laid out.
-Entropy any_entropy(int64_t n, int64_t dim, int64_t vocab, int dtype)
+// Of calls with these sizes: x and w as if they had to be laid out, their rows starting at whole 32-bit words or between them,
+// which the rule for few rows tells apart.
+Entropy any_entropy(int64_t n, int64_t dim, int64_t vocab, int dtype, bool between = true)
 {
     Entropy q = {};
     q.words = {nullptr, true, n, vocab};
     q.dim = dim;
-    q.x = q.w = {(void*)1, type_of(dtype), dim};
+    q.x = q.w = {between ? (void*)2 : (void*)4, type_of(dtype), between ? dim : dim + dim % 2};
     return q;
 }
 
@@ -127,7 +128,8 @@ int sidco_dropout(void* stream, const void* x, int x_dtype, int64_t rows, int64_
 size_t sidco_workspace_bytes_cross_entropy(int64_t n, int64_t dim, int64_t vocab, int dtype)
 {
     if (!entropy_sizes(n, dim, vocab) || !element_type(dtype)) return 0;
-    return workspace_with_scratch(entropy_scratch(any_entropy(n, dim, vocab, dtype)));
+    const size_t most = entropy_scratch(any_entropy(n, dim, vocab, dtype)), other = entropy_scratch(any_entropy(n, dim, vocab, dtype, false));
+    return workspace_with_scratch(other > most ? other : most);
 }
 
 int sidco_cross_entropy(void* stream, const void* x, const void* w, int dtype, int64_t n, int64_t dim, int64_t vocab, int64_t ldx, int64_t ldw,
