@@ -644,9 +644,9 @@ int sidco_muon_step(void *stream, const void *grad, int grad_dtype, float *momen
 #define SIDCO_WORD_I64 1
 
 /*
- * The lookup: out_i = scale * table[words_i] for n words, rounded once; zeros for
- * padding.  table is vocab x dim with row stride ldt, out n x dim with row stride ldo.
- * They must not overlap.  Needs no workspace.
+ * The lookup: out_i = scale * table[words_i] for n words, the product rounded to fp32 and
+ * then to out's type; zeros for padding.  table is vocab x dim with row stride ldt, out n x
+ * dim with row stride ldo.  They must not overlap.  Needs no workspace.
  */
 int sidco_embedding(void *stream, const void *table, int table_dtype, int64_t vocab, int64_t dim, int64_t ldt, const void *words,
                     int word_type, int64_t n, float scale, void *out, int out_dtype, int64_t ldo);
@@ -654,10 +654,10 @@ int sidco_embedding(void *stream, const void *table, int table_dtype, int64_t vo
 /*
  * The table's gradient: table_grad_v = scale * the sum of grad_i over the places i with
  * words_i = v, in an order that the words alone decide, zeros for words that do not occur
- * (accumulate = 0), or that added to table_grad and rounded once, where rows of words that
- * do not occur are not touched (accumulate = 1: several batches, or a table that is the
- * decoder's weight too).  Padding has no gradient, whatever its row of grad holds.  grad is
- * n x dim with row stride ldg, table_grad vocab x dim with row stride ldt; n / 32, up to 2048
+ * (accumulate = 0), or that added to table_grad, where rows of words that do not occur are not
+ * touched (accumulate = 1: several batches, or a table that is the decoder's weight too).
+ * What is formed in fp32 is then rounded to table_grad's type.  Padding has no gradient,
+ * whatever its row of grad holds.  grad is n x dim with row stride ldg, table_grad vocab x dim with row stride ldt; n / 32, up to 2048
  * words n / 8, times dim / 512, each rounded up, is at most 2^22 (SIDCO_ERR_SIZE).  Uses the
  * stream's workspace, of sidco_workspace_bytes_embedding_grad(n, dim).
  */
@@ -667,8 +667,8 @@ size_t sidco_workspace_bytes_embedding_grad(int64_t n, int64_t dim);
 
 /*
  * Dropout whose mask is a function of seed and place and is not stored: y = kept ? x *
- * 65536 / (65536 - T) : 0, plus residual if there is one (not NULL; of y's type).  The
- * backward pass is the same call on the gradient of y.
+ * 65536 / (65536 - T) : 0, plus residual if there is one (not NULL; of y's type), formed in
+ * fp32 and then rounded to y's type.  The backward pass is the same call on the gradient of y.
  *
  * Element (r, c) has number c % 8 of block offset + *device_offset + r * ceil(cols / 8) +
  * c / 8 of the seed's sequence, and is kept where that number is at least T = floor(65536 p
