@@ -724,6 +724,18 @@ int sidco_cross_entropy_grad(void *stream, const void *x, const void *w, int dty
                              int64_t ldgx, void *w_grad, int w_grad_dtype, int64_t ldgw, int accumulate);
 size_t sidco_workspace_bytes_cross_entropy_grad(int64_t n, int64_t dim, int64_t vocab, int dtype, int w_grad_dtype);
 
+/*
+ * The same from the losses too (device, n floats, of the same call as lse; NULL: the call above).
+ * A row's target has P = loss_grad (exp(l - lse) - 1), which lse as rounded to fp32 leaves off by
+ * 2^-23 |lse| of loss_grad: nothing beside a P of one, all of it where a row knows its target to 2^-23
+ * |lse|.  The loss is kept to its own last bits there, and P = loss_grad (exp(-loss) - 1) with it:
+ * give it where gradients of such rows count.
+ */
+int sidco_cross_entropy_grad_of_loss(void *stream, const void *x, const void *w, int dtype, int64_t n, int64_t dim, int64_t vocab,
+                                     int64_t ldx, int64_t ldw, const void *targets, int word_type, const float *loss, const float *lse,
+                                     const float *loss_grad, void *x_grad, int64_t ldgx, void *w_grad, int w_grad_dtype, int64_t ldgw,
+                                     int accumulate);
+
 /* Text for an error code; the HIP error string of the last SIDCO_ERR_HIP.     */
 const char *sidco_strerror(int code);
 const char *sidco_last_hip_error(void);

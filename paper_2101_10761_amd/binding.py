@@ -33,6 +33,7 @@ EXPORTS = [
     "sidco_newton_schulz_default", "sidco_workspace_bytes_orthogonalize", "sidco_orthogonalize", "sidco_muon_step",
     "sidco_embedding", "sidco_embedding_grad", "sidco_workspace_bytes_embedding_grad", "sidco_dropout", "sidco_dropout_blocks",
     "sidco_cross_entropy", "sidco_workspace_bytes_cross_entropy", "sidco_cross_entropy_grad", "sidco_workspace_bytes_cross_entropy_grad",
+    "sidco_cross_entropy_grad_of_loss",
 ]
 
 
@@ -239,6 +240,9 @@ def load() -> C.CDLL:
     lib.sidco_cross_entropy_grad.argtypes = [vp, vp, vp, C.c_int, i64, i64, i64, i64, i64, vp, C.c_int, f32p, f32p, vp, i64, vp, C.c_int, i64,
                                              C.c_int]
     lib.sidco_cross_entropy_grad.restype = C.c_int
+    lib.sidco_cross_entropy_grad_of_loss.argtypes = [vp, vp, vp, C.c_int, i64, i64, i64, i64, i64, vp, C.c_int, f32p, f32p, f32p, vp, i64, vp,
+                                                     C.c_int, i64, C.c_int]
+    lib.sidco_cross_entropy_grad_of_loss.restype = C.c_int
     lib.sidco_workspace_bytes_cross_entropy_grad.argtypes = [i64, i64, i64, C.c_int, C.c_int]
     lib.sidco_workspace_bytes_cross_entropy_grad.restype = C.c_size_t
     lib.sidco_strerror.argtypes = [C.c_int]
@@ -1092,12 +1096,13 @@ def sidco_workspace_bytes_cross_entropy_grad(n: int, dim: int, vocab: int, dtype
 
 
 def sidco_cross_entropy_grad(x, weight, targets, lse, loss_grad, x_grad=None, weight_grad=None, accumulate: bool = False,
-                             stream=None) -> None:
+                             stream=None, loss=None) -> None:
     """The gradients of the sum of loss_grad[i] * loss[i] (None: of the losses' sum) with respect to x, in its dtype, and weight, in its
     dtype or float32, or with `accumulate` added to what weight_grad holds; either may be None.  lse is what sidco_cross_entropy
-    wrote."""
+    wrote, and so is loss; without it (None) gradients of rows whose loss is tiny, about 2^-23 of |lse|, are lost in lse's rounding."""
     args, n, code, device = _logits(x, weight, targets)
     sums = _vector(lse, "lse", n, device)
+    known = None if loss is None else _vector(loss, "loss", n, device)
     g = None if loss_grad is None else _vector(loss_grad, "loss_grad", n, device)
     gx = gw = None
     ldgx = ldgw = w_code = 0
@@ -1111,7 +1116,8 @@ def sidco_cross_entropy_grad(x, weight, targets, lse, loss_grad, x_grad=None, we
         gw, w_code, rows, cols, ldgw, _ = _rows(weight_grad, "weight_grad", device)
         if weight_grad.shape != weight.shape:
             raise ValueError("weight_grad must have weight's shape")
-    rc = load().sidco_cross_entropy_grad(_stream_on(stream, device), *args, sums, g, gx, ldgx, gw, w_code, ldgw, 1 if accumulate else 0)
+    rc = load().sidco_cross_entropy_grad_of_loss(_stream_on(stream, device), *args, known, sums, g, gx, ldgx, gw, w_code, ldgw,
+                                                 1 if accumulate else 0)
     if rc:
         raise SidcoError(rc, "sidco_cross_entropy_grad")
 

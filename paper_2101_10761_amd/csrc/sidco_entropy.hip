@@ -599,7 +599,8 @@ __global__ __launch_bounds__(256) void k_join_rows(const float2* part, uint32_t 
     }
 }
 
-// P of a piece of the vocabulary, words from `first` on.  Bound by the matrix cores, and a round's end by memory: with all CUs' tiles
+// P of a piece of the vocabulary, words from `first` on.  A row's word has exp(l - lse) - 1, which for a row that knows its word is
+// the difference of two numbers near one, off by what lse is rounded by; given the loss it is exp(-loss) - 1 without it.  Bound by the matrix cores, and a round's end by memory: with all CUs' tiles
 // done at once, 256 KB of each (512 KB with low halves) leave at what HBM takes, 11 us (20).  8192 x 4096 x 32768 in bf16 1.65 to 1.69 ms,
 // 1.30 to 1.33 PFLOP/s; 2049 x 1024 x 49999 in fp16, P in pairs, 371 us, 0.57; 700 x 1500 x 10000 in pairs 73 us, 0.86.
 template <class H>
@@ -607,7 +608,7 @@ struct Probs {
     Plane<H> x, w;  // w: the piece's rows
     uint32_t n, count, first;
     WordList words;
-    const float *lse, *loss_grad;
+    const float *lse, *loss, *loss_grad;  // loss, loss_grad: may be NULL
     Plane<G> out, turned;  // n rows of words, words of n rows; either may have no address
     uint32_t turned_cols;  // with the zeros behind the last row
     const Scales* scales;
@@ -649,10 +650,11 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[j][e] = __builtin_amdgcn_exp2f(fmaf(acc[j][e], k, lse));
                 if (here < Tl::kNt * 16) {  // one lane in 128 columns, if any
+                    const float own = p.loss && r < p.n ? expm1f(-p.loss[r]) : 0.0f;
 #pragma unroll
                     for (int j = 0; j < Tl::kNt; ++j)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[j][e] -= here == (uint32_t)(j * 16 + e) ? 1.0f : 0.0f;
+                        for (int e = 0; e < 4; ++e) acc[j][e] = here == (uint32_t)(j * 16 + e) ? (p.loss ? own : acc[j][e] - 1.0f) : acc[j][e];
                 }
 #pragma unroll
                 for (int j = 0; j < Tl::kNt; ++j) acc[j] *= gain;
@@ -1206,7 +1208,7 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
                 // columns of the transpose up to the pitch are this launch's if the last rows are
                 const Plane<G> turned = {g.pt.at ? g.pt.at + row : nullptr, g.pt.pitch, g.pt.low};
                 const Probs<H> p = {x, w, (uint32_t)rows, (uint32_t)count, (uint32_t)first, words.from(row), q.lse + row,
-                                    q.loss_grad ? q.loss_grad + row : nullptr, out, turned,
+                                    q.loss ? q.loss + row : nullptr, q.loss_grad ? q.loss_grad + row : nullptr, out, turned,
                                     (uint32_t)(row + rows < n ? rows : g.cols_n - row), g.scales};
                 auto go = [&](auto kernel) { kernel<<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places); };
                 if constexpr (M::kPairP)

@@ -52,7 +52,7 @@ struct Entropy {
     Words words;
     int64_t dim;
     Matrix x, w;
-    float *loss, *lse;         // written by the forward pass, either may be NULL; lse is read by the gradient
+    float *loss, *lse;         // written by the forward pass, either may be NULL; read by the gradient, loss may be NULL
     const float* loss_grad;    // NULL: ones
     Matrix x_grad, w_grad;     // one of the two may be NULL
     bool accumulate;           // onto w_grad

@@ -170,9 +170,18 @@ int sidco_cross_entropy_grad(void* stream, const void* x, const void* w, int dty
                              int64_t ldw, const void* targets, int word_type, const float* lse, const float* loss_grad, void* x_grad,
                              int64_t ldgx, void* w_grad, int w_grad_dtype, int64_t ldgw, int accumulate)
 {
+    return sidco_cross_entropy_grad_of_loss(stream, x, w, dtype, n, dim, vocab, ldx, ldw, targets, word_type, nullptr, lse, loss_grad, x_grad, ldgx,
+                                            w_grad, w_grad_dtype, ldgw, accumulate);
+}
+
+int sidco_cross_entropy_grad_of_loss(void* stream, const void* x, const void* w, int dtype, int64_t n, int64_t dim, int64_t vocab, int64_t ldx,
+                                     int64_t ldw, const void* targets, int word_type, const float* loss, const float* lse,
+                                     const float* loss_grad, void* x_grad, int64_t ldgx, void* w_grad, int w_grad_dtype, int64_t ldgw,
+                                     int accumulate)
+{
     if (!lse || (!x_grad && !w_grad)) return SIDCO_ERR_NULL;
     if (int rc = check_entropy(x, w, dtype, n, dim, vocab, ldx, ldw, targets, word_type)) return rc;
-    if (!aligned(lse, 4) || !aligned(loss_grad, 4)) return SIDCO_ERR_ALIGN;
+    if (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(loss_grad, 4)) return SIDCO_ERR_ALIGN;
     if (x_grad)
         if (int rc = check_matrix(x_grad, dtype, dim, ldgx)) return rc;
     if (w_grad) {
@@ -186,6 +195,7 @@ int sidco_cross_entropy_grad(void* stream, const void* x, const void* w, int dty
     q.dim = dim;
     q.x = matrix(x, dtype, ldx);
     q.w = matrix(w, dtype, ldw);
+    q.loss = (float*)loss;
     q.lse = (float*)lse;
     q.loss_grad = loss_grad;
     if (x_grad) q.x_grad = matrix(x_grad, dtype, ldgx);

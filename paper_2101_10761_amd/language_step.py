@@ -64,7 +64,7 @@ class Model:
         """The gradients of the mean over the targets that are no padding."""
         valid = (self.targets >= 0) & (self.targets < len(self.table))
         self.loss_grad.copy_(1.0 / valid.sum().clamp(min=1))
-        sidco.sidco_cross_entropy_grad(self.y, self.table, self.targets, self.lse, self.loss_grad, self.dy, table_grad)
+        sidco.sidco_cross_entropy_grad(self.y, self.table, self.targets, self.lse, self.loss_grad, self.dy, table_grad, loss=self.loss)
         sidco.sidco_dropout(self.dy, self.dh, self.p, self.seed, offset=self.second)
         self.dh.mul_(self.h > 0)
         self.dx.copy_(self.layer.backward(self.dh, weight_grad)).add_(self.dy)
