@@ -657,9 +657,10 @@ int sidco_embedding(void *stream, const void *table, int table_dtype, int64_t vo
  * (accumulate = 0), or that added to table_grad, where rows of words that do not occur are not
  * touched (accumulate = 1: several batches, or a table that is the decoder's weight too).
  * What is formed in fp32 is then rounded to table_grad's type.  Padding has no gradient,
- * whatever its row of grad holds.  grad is n x dim with row stride ldg, table_grad vocab x dim with row stride ldt; n / 32, up to 2048
- * words n / 8, times dim / 512, each rounded up, is at most 2^22 (SIDCO_ERR_SIZE).  Uses the
- * stream's workspace, of sidco_workspace_bytes_embedding_grad(n, dim).
+ * whatever its row of grad holds.  grad is n x dim with row stride ldg, table_grad vocab x dim
+ * with row stride ldt; n / 32, up to 2048 words n / 8, times dim / 512, each rounded up, is at
+ * most 2^22 (SIDCO_ERR_SIZE).  Uses the stream's workspace, of
+ * sidco_workspace_bytes_embedding_grad(n, dim).
  */
 int sidco_embedding_grad(void *stream, const void *grad, int grad_dtype, int64_t n, int64_t dim, int64_t ldg, const void *words,
                          int word_type, int64_t vocab, float scale, int accumulate, void *table_grad, int table_dtype, int64_t ldt);
@@ -711,13 +712,15 @@ size_t sidco_workspace_bytes_cross_entropy(int64_t n, int64_t dim, int64_t vocab
  *   w_grad = P^T x (accumulate = 0) or w_grad + P^T x   (accumulate = 1)
  *                                                       (dtype or SIDCO_GRAD_F32, row stride ldgw)
  * Either may be NULL, not both.  loss_grad (device, n floats) is 1 / n for the gradient of the
- * mean, times the loss scale if there is one; NULL stands for ones.  P is formed for one piece of
- * the vocabulary at a time, in halves under a power of two of the largest loss_grad: 11 bits for a bf16
- * gradient, else 22, down to 2^-29 of the largest and 2^-39 of that below; bf16 operands of its
- * products are halves too, exact down to 2^-24 of their matrix's largest magnitude and off by 2^-32
- * of that below.  Rows of x whose target is padding do not enter w_grad whatever they
- * hold.  The gradients must not overlap x, w or each other.  Uses the stream's workspace, of
- * sidco_workspace_bytes_cross_entropy_grad(n, dim, vocab, dtype, w_grad_dtype) at most.
+ * mean, times the loss scale if there is one; NULL stands for ones.  P is formed for one piece
+ * of the vocabulary at a time, in halves under a power of two of the largest loss_grad: 11 bits
+ * for a bf16 gradient, else 22, down to 2^-29 of that loss_grad, and off by 2^-38 of it below.  Rows
+ * whose loss_grad is 2^-8 of the largest or less have a power of two of their own for x_grad, with as
+ * many bits there as if they were alone.  bf16 operands of P's products are halves too, exact down to
+ * 2^-24 of their matrix's largest magnitude and off by 2^-32 of that below.  Rows of x whose target
+ * is padding do not enter w_grad whatever they hold.  The gradients must not overlap x, w or each
+ * other.  Uses the stream's workspace, of sidco_workspace_bytes_cross_entropy_grad(n, dim, vocab,
+ * dtype, w_grad_dtype) at most.
  */
 int sidco_cross_entropy_grad(void *stream, const void *x, const void *w, int dtype, int64_t n, int64_t dim, int64_t vocab, int64_t ldx,
                              int64_t ldw, const void *targets, int word_type, const float *lse, const float *loss_grad, void *x_grad,

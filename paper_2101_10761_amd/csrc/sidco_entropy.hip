@@ -20,7 +20,8 @@
 // error of 1.7e-3 in the 2-norm, the gradient's own rounding; with P in bf16 it was up to 2.4e-3), a pair for those of halves and
 // of fp32 (2.1e-4 for halves; with one half up to 3.1e-4).  bf16 operands of the products with P are halves too, exactly but for
 // those under 2^-24 of the largest, under a power of two as for fp32; they multiply at nearly the rate of bf16 (a training pass
-// of 8192 x 4096 x 131072 takes 3 % longer).
+// of 8192 x 4096 x 131072 takes 3 % longer).  A row whose gradient is far below the largest has a power of two of its own in P by
+// rows, and leaves it in P by words.
 #include <math.h>
 
 #include <algorithm>
@@ -69,11 +70,13 @@ void by_mode(int type, const F& f)
 
 // ---- scales ----
 
-// Powers of two: of x and w as the gradient's products (fp32: all) take them, and of P.
+// Powers of two: of x and w as the gradient's products (fp32: all) take them, and of P; and whether rows have others besides.
 struct Scales {
     float x, w, p;
+    int by_row;
 };
-constexpr int kParts = 2048;  // blocks of k_layout, and partial results of each of the three
+constexpr int kParts = 2048;             // blocks of k_layout, and partial results of each kind
+enum { kTopX, kTopW, kTopG, kLeastG, kPartKinds };  // largest magnitudes, and how far below 2^128 the least of the rows' gradients is
 
 // What x and w are laid out with at first.  Weights whose largest magnitude is 2^-7 to 2^1.5 and rows of 2^-3 to 2^5.5 stay so; k_settle
 // lays out others once more.
@@ -92,7 +95,19 @@ __device__ __forceinline__ float scale_of(float top)
 // Of a power of two.  Two of them may have a product that no float holds.
 __device__ __forceinline__ int exponent_of(float scale) { return (int)(__builtin_bit_cast(uint32_t, scale) >> 23) - 127; }
 
-// The same, or the guess where it does: the largest is a half with room for rounding, and what halves cannot tell from zero is 2^-32 of it.
+// P's power of two is that of the largest gradient of a row.  Rows far below it, whose P would end in it, have a power of two of
+// their own besides in the product for x's gradient, where each row is a sum for itself: what brings `gain`, the row's gradient under
+// the common one, to 2^14 to 2^15.  From 2^8 on: so close P has all its bits down to 2^-21 of the row's own gradient, and no tile
+// of a batch with gradients like each other takes the way there and back.
+constexpr int kRowPower = 8;
+__device__ __forceinline__ int row_power(float gain)
+{
+    const float m = fabsf(gain);
+    const int e = m > 0.0f && m < INFINITY ? 14 - exponent_of(m) : 0;
+    return e < kRowPower ? 0 : (e < 120 ? e : 120);
+}
+
+// What scale_of says, or the guess where it does: the largest is a half with room for rounding, and what halves cannot tell from zero is 2^-32 of it.
 __device__ __forceinline__ float settled(float top, float guess)
 {
     const float t = top * guess;
@@ -236,7 +251,7 @@ __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M
     __shared__ float tile[64][65];
     __shared__ float lds[4];
     const uint32_t first = x.tiles_r * x.tiles_c, all = first + w.tiles_r * w.tiles_c;
-    float top[3] = {0.0f, 0.0f, g.at ? 0.0f : 1.0f};  // a gradient without an address is ones
+    float top[kPartKinds] = {0.0f, 0.0f, g.at ? 0.0f : 1.0f, 0.0f};  // a gradient without an address is ones
     for (uint32_t t = blockIdx.x; t < all; t += gridDim.x) {
         if (t < first)
             top[0] = lay<M>(x, t, M::kScaled ? kGuessX : 1.0f, tile, top[0]);
@@ -246,10 +261,13 @@ __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M
     if (!Scaled) return;
     if (g.at) {
         for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < g.rows; r += (int64_t)gridDim.x * 256)
-            if (!g.words.none(r)) top[2] = more(top[2], g.at[r]);
+            if (!g.words.none(r)) {
+                top[kTopG] = more(top[kTopG], g.at[r]);
+                if (const float m = fabsf(g.at[r]); m > 0.0f && m < INFINITY) top[kLeastG] = fmaxf(top[kLeastG], (float)(128 - exponent_of(m)));
+            }
     }
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < kPartKinds; ++k) {
         const float most = block_top(top[k], lds);
         if (threadIdx.x == 0) part[k * kParts + blockIdx.x] = most;
     }
@@ -268,14 +286,16 @@ __global__ __launch_bounds__(256) void k_settle(Layout<typename M::T, typename M
     const uint32_t first = x.tiles_r * x.tiles_c, all = first + w.tiles_r * w.tiles_c;
     float sx = 1.0f, sw = 1.0f;
     if (M::kScaled) {
-        if (!later) sx = settled(joined_top(part, blocks, lds), kGuessX);
-        sw = settled(joined_top(part + kParts, blocks, lds), kGuessW);
+        if (!later) sx = settled(joined_top(part + kTopX * kParts, blocks, lds), kGuessX);
+        sw = settled(joined_top(part + kTopW * kParts, blocks, lds), kGuessW);
     }
     if (blockIdx.x == 0) {
-        const float sp = later ? 1.0f : scale_of(joined_top(part + 2 * kParts, blocks, lds));
+        const float sp = later ? 1.0f : scale_of(joined_top(part + kTopG * kParts, blocks, lds));
+        const float least = later ? 0.0f : joined_top(part + kLeastG * kParts, blocks, lds);
         if (threadIdx.x == 0) {
             scales->w = sw;
-            if (!later) scales->x = sx, scales->p = sp;
+            // as row_power has it of the least one
+            if (!later) scales->x = sx, scales->p = sp, scales->by_row = least > 0.0f && 14 - (128 - (int)least + exponent_of(sp)) >= kRowPower;
         }
     }
     if (!M::kScaled) return;
@@ -614,6 +634,38 @@ struct Probs {
     const Scales* scales;
 };
 
+typedef G h2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ Four16 packed(const v4f& v)
+{
+    return {__builtin_bit_cast(uint32_t, h2{(G)v[0], (G)v[1]}), __builtin_bit_cast(uint32_t, h2{(G)v[2], (G)v[3]})};
+}
+__device__ __forceinline__ v4f unpacked(Four16 v)
+{
+    asm volatile("" : "+v"(v.a), "+v"(v.b));  // the values that were packed are not kept until here
+    const h2 a = __builtin_bit_cast(h2, v.a), b = __builtin_bit_cast(h2, v.b);
+    return v4f{(float)a[0], (float)a[1], (float)b[0], (float)b[1]};
+}
+// What halves leave of the values.
+__device__ __forceinline__ v4f left_over(const v4f& v)
+{
+    v4f l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) l[e] = v[e] - (float)(G)v[e];
+    return l;
+}
+__device__ __forceinline__ v4f ldexp4(v4f v, int by)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], by);
+    return v;
+}
+__device__ __forceinline__ void shift_pairs(Four16& high, Four16& low, int by)
+{
+    const v4f v = rounded(ldexp4(unpacked(high) + unpacked(low), by));
+    high = packed(v);
+    low = packed(left_over(v));
+}
+
 template <class M, bool Low, class Tl>
 __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, Span span, Places places)
 {
@@ -632,7 +684,8 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
             places.at(tile, ti, tj, split);
             const uint32_t m0 = ti * Tl::kM, n0 = tj * Tl::kN;
             const float k = M::kPairs ? kLog2e / (p.scales->x * p.scales->w) : kLog2e, sp = p.scales->p;
-            const bool edge = n0 + Tl::kN > p.count;
+            const bool edge = n0 + Tl::kN > p.count, by_row = p.scales->by_row;
+            int power[Tl::kMt];  // of the strips' rows
             Four16 high[Tl::kMt][Tl::kNt], low[kLow ? Tl::kMt : 1][Tl::kNt];  // in 16 bits P takes half the room of the sums
             t.strips([&](int i, uint32_t row, uint32_t col, v4f(&acc)[Tl::kNt]) {
                 const uint32_t r = m0 + row;
@@ -642,6 +695,11 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                     word = p.words[r];
                     lse = p.lse[r] * -kLog2e;
                     gain = (p.loss_grad ? p.loss_grad[r] : 1.0f) * sp;
+                }
+                power[i] = 0;
+                if (by_row) {
+                    power[i] = row_power(gain);
+                    gain = ldexpf(gain, power[i]);
                 }
                 const uint32_t here = word - p.first - n0 - col;
                 const bool none = word == p.words.vocab;
@@ -669,20 +727,13 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[j][e] = left > j * 16 + e ? acc[j][e] : 0.0f;
                 }
-                auto packed = [](const v4f& v) -> Four16 {
-                    typedef G h2 __attribute__((ext_vector_type(2)));
-                    const uint32_t a = __builtin_bit_cast(uint32_t, h2{(G)v[0], (G)v[1]}), b = __builtin_bit_cast(uint32_t, h2{(G)v[2], (G)v[3]});
-                    return {a, b};
-                };
 #pragma unroll
                 for (int j = 0; j < Tl::kNt; ++j) {
                     const v4f v = rounded(acc[j]);
                     high[i][j] = packed(v);
                     if constexpr (kLow) {
-                        v4f l;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) l[e] = v[e] - (float)(G)v[e];
-                        low[i][j] = packed(l);
+                        low[i][j] = packed(left_over(v));
+                        if constexpr (!M::kPairP) asm volatile("" : "+v"(low[i][j].a), "+v"(low[i][j].b));  // not where they are used
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -701,6 +752,19 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                 if constexpr (M::kPairP) t.template out16<false>(by, low, put(p.out, p.n, (uint32_t)p.out.pitch, m0, n0, true));
             }
             if (p.turned.at) {
+                if (__builtin_expect(by_row, 0)) {  // words have sums over rows, which share a power of two
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < Tl::kMt; ++i)
+#pragma unroll
+                        for (int j = 0; j < Tl::kNt; ++j) {
+                            if constexpr (kLow)
+                                shift_pairs(high[i][j], low[i][j], -power[i]);
+                            else
+                                high[i][j] = packed(ldexp4(unpacked(high[i][j]), -power[i]));
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                }
                 t.template out16<true>(by, high, put(p.turned, p.count, p.turned_cols, n0, m0, false));
                 if constexpr (kLow) t.template out16<true>(by, low, put(p.turned, p.count, p.turned_cols, n0, m0, true));
             }
@@ -716,6 +780,7 @@ struct Product {
     int64_t m, n;
     const Scales* scales;  // 2^e is one over its p and over that of w, or with of_x of x
     bool of_x;
+    const float* loss_grad;  // rows of A that may have powers of two of their own; NULL: none has
     void* c;
     int64_t ldc, split_stride;
     bool accumulate;
@@ -761,11 +826,11 @@ __global__ __launch_bounds__(Tl::kThreads) void k_product(Product p, Span span, 
             uint32_t ti, tj, split;
             places.at(tile, ti, tj, split);
             const int shift = -exponent_of(p.scales->p) - exponent_of(p.of_x ? p.scales->x : p.scales->w);
+            const bool by_row = p.loss_grad && p.scales->by_row;
             t.each([&](uint32_t row, uint32_t col, v4f v) {
                 const int64_t r = (int64_t)ti * Tl::kM + row, c = (int64_t)tj * Tl::kN + col;
                 if (r >= p.m || c >= p.n) return;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], shift);
+                v = ldexp4(v, by_row ? shift - row_power(p.loss_grad[r] * p.scales->p) : shift);
                 finish4<T>((T*)p.c + split * p.split_stride + r * p.ldc + c, p.before ? p.before + r * p.n + c : nullptr, p.accumulate, p.n - c,
                            v);
             });
@@ -978,7 +1043,7 @@ struct ForwardPlan {
         few = takes_few<M>(n, q.dim, q.w, lay_w);
         if (few) lay_x = lay_w = false;
         scales = s.get<Scales>(1);
-        part = s.get<float>(M::kPairs ? 3 * kParts : 0);
+        part = s.get<float>(M::kPairs ? kPartKinds * kParts : 0);
         x = lay_x ? s.plane<H>(n, pitch, M::kPairs) : Plane<H>{(H*)q.x.at, q.x.ld, 0};
         w = lay_w ? s.plane<H>(v, pitch, M::kPairs) : Plane<H>{(H*)q.w.at, q.w.ld, 0};
         auto pairs_of = [&](int64_t rows) {
@@ -1130,7 +1195,7 @@ struct GradPlan {
         cols_v = lines * kPer;
         const int64_t pitch_n = spread(cols_n), pitch_v = spread(cols_v);
         scales = s.get<Scales>(1);
-        part = s.get<float>(3 * kParts);
+        part = s.get<float>(kPartKinds * kParts);
         x = lay_x ? s.plane<H>(n, pitch, M::kPairs) : Plane<H>{(H*)q.x.at, q.x.ld, 0};
         w = lay_w ? s.plane<H>(piece, pitch, M::kPairs) : Plane<H>{};
         xt = wt = p = pt = Plane<G>{};
@@ -1225,16 +1290,16 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
         if (q.x_grad.at) {
             const int64_t lines = g.cols_v / kPer / g.splits;
             if (g.splits > 1 || k + 1 < g.pieces) {
-                const Product p = {g.p, g.wt, n, q.dim, g.scales, false, g.sums, q.dim, n * q.dim, k > 0, nullptr};
+                const Product p = {g.p, g.wt, n, q.dim, g.scales, false, q.loss_grad, g.sums, q.dim, n * q.dim, k > 0, nullptr};
                 product_part<float, kTerms>(g.pick_x, p, lines, g.splits, s);
             } else {
-                const Product p = {g.p, g.wt, n, q.dim, g.scales, false, q.x_grad.at, q.x_grad.ld, 0, false, g.pieces > 1 ? g.sums : nullptr};
+                const Product p = {g.p, g.wt, n, q.dim, g.scales, false, q.loss_grad, q.x_grad.at, q.x_grad.ld, 0, false, g.pieces > 1 ? g.sums : nullptr};
                 product_part<T, kTerms>(g.pick_x, p, lines, 1, s);
             }
         }
         if (q.w_grad.at) {
             char* c = (char*)q.w_grad.at + first * q.w_grad.ld * (q.w_grad.type == kGradF32 ? 4 : 2);
-            const Product p = {g.pt, g.xt, count, q.dim, g.scales, true, c, q.w_grad.ld, 0, q.accumulate, nullptr};
+            const Product p = {g.pt, g.xt, count, q.dim, g.scales, true, nullptr, c, q.w_grad.ld, 0, q.accumulate, nullptr};
             const int64_t lines = g.cols_n / kPer;
             if constexpr (M::kPairs) {
                 product<float, 3>(p, lines, s);
