@@ -127,28 +127,40 @@ __device__ __forceinline__ float more(float top, float v)
     return m < INFINITY && m > top ? m : top;
 }
 
-// The largest of the block's 256 threads, in thread 0.
-__device__ __forceinline__ float block_top(float top, float* lds)
+// The largest of the block's 256 threads, of each kind, in all of them.
+template <int Kinds>
+__device__ __forceinline__ void block_tops(float (&top)[Kinds], float (*lds)[4])
 {
 #pragma unroll
-    for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+    for (int k = 0; k < Kinds; ++k) {
+#pragma unroll
+        for (int s = 32; s > 0; s >>= 1) top[k] = fmaxf(top[k], __shfl_xor(top[k], s));
+    }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
+#pragma unroll
+    for (int k = 0; k < Kinds; ++k)
+        if ((threadIdx.x & 63) == 0) lds[k][threadIdx.x >> 6] = top[k];
     __syncthreads();
-    return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+#pragma unroll
+    for (int k = 0; k < Kinds; ++k) top[k] = fmaxf(fmaxf(lds[k][0], lds[k][1]), fmaxf(lds[k][2], lds[k][3]));
 }
 
-// The largest of one of the three over the blocks of k_layout, for the whole block of 256.  Without branches all loads are under way
-// at once: k_settle takes 4.8 us, and 8.4 with them.
-__device__ __forceinline__ float joined_top(const float* part, uint32_t blocks, float* lds)
+// The largest of two kinds that lie one behind the other, over the blocks of k_layout, for the whole block of 256.  Without branches
+// all loads are under way at once: k_settle takes 4.8 us, and 8.4 with them.
+__device__ __forceinline__ void joined_tops(const float* part, uint32_t blocks, float (*lds)[4], float (&top)[2])
 {
-    float v[kParts / 256];
+    float v[2][kParts / 256];
 #pragma unroll
-    for (uint32_t k = 0; k < kParts / 256; ++k) v[k] = part[min(k * 256 + threadIdx.x, blocks - 1)];
-    float top = 0.0f;
+    for (int kind = 0; kind < 2; ++kind)
 #pragma unroll
-    for (int k = 0; k < kParts / 256; ++k) top = fmaxf(top, v[k]);
-    return block_top(top, lds);
+        for (uint32_t k = 0; k < kParts / 256; ++k) v[kind][k] = part[kind * kParts + min(k * 256 + threadIdx.x, blocks - 1)];
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+        top[kind] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kParts / 256; ++k) top[kind] = fmaxf(top[kind], v[kind][k]);
+    }
+    block_tops(top, lds);
 }
 
 // ---- operands ----
@@ -249,7 +261,7 @@ template <class M, bool Scaled>
 __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M::H> x, Layout<typename M::T, typename M::H> w, Source<float> g, float* part)
 {
     __shared__ float tile[64][65];
-    __shared__ float lds[4];
+    __shared__ float lds[kPartKinds][4];
     const uint32_t first = x.tiles_r * x.tiles_c, all = first + w.tiles_r * w.tiles_c;
     float top[kPartKinds] = {0.0f, 0.0f, g.at ? 0.0f : 1.0f, 0.0f};  // a gradient without an address is ones
     for (uint32_t t = blockIdx.x; t < all; t += gridDim.x) {
@@ -266,10 +278,10 @@ __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M
                 if (const float m = fabsf(g.at[r]); m > 0.0f && m < INFINITY) top[kLeastG] = fmaxf(top[kLeastG], (float)(128 - exponent_of(m)));
             }
     }
+    block_tops(top, lds);
+    if (threadIdx.x == 0) {
 #pragma unroll
-    for (int k = 0; k < kPartKinds; ++k) {
-        const float most = block_top(top[k], lds);
-        if (threadIdx.x == 0) part[k * kParts + blockIdx.x] = most;
+        for (int k = 0; k < kPartKinds; ++k) part[k * kParts + blockIdx.x] = top[k];
     }
 }
 
@@ -282,21 +294,22 @@ __global__ __launch_bounds__(256) void k_settle(Layout<typename M::T, typename M
                                                 const float* part, Scales* scales)
 {
     __shared__ float tile[64][65];
-    __shared__ float lds[4];
+    __shared__ float lds[2][4];
     const uint32_t first = x.tiles_r * x.tiles_c, all = first + w.tiles_r * w.tiles_c;
     float sx = 1.0f, sw = 1.0f;
     if (M::kScaled) {
-        if (!later) sx = settled(joined_top(part + kTopX * kParts, blocks, lds), kGuessX);
-        sw = settled(joined_top(part + kTopW * kParts, blocks, lds), kGuessW);
+        float top[2];
+        joined_tops(part + kTopX * kParts, blocks, lds, top);
+        if (!later) sx = settled(top[0], kGuessX);
+        sw = settled(top[1], kGuessW);
     }
-    if (blockIdx.x == 0) {
-        const float sp = later ? 1.0f : scale_of(joined_top(part + kTopG * kParts, blocks, lds));
-        const float least = later ? 0.0f : joined_top(part + kLeastG * kParts, blocks, lds);
-        if (threadIdx.x == 0) {
-            scales->w = sw;
-            // as row_power has it of the least one
-            if (!later) scales->x = sx, scales->p = sp, scales->by_row = least > 0.0f && 14 - (128 - (int)least + exponent_of(sp)) >= kRowPower;
-        }
+    if (blockIdx.x == 0 && later && threadIdx.x == 0) scales->w = sw;
+    if (blockIdx.x == 0 && !later) {
+        float top[2];
+        joined_tops(part + kTopG * kParts, blocks, lds, top);
+        const float sp = scale_of(top[0]);
+        // by_row as row_power has it of the least one
+        if (threadIdx.x == 0) *scales = {sx, sw, sp, top[1] > 0.0f && 14 - (128 - (int)top[1] + exponent_of(sp)) >= kRowPower};
     }
     if (!M::kScaled) return;
     const uint32_t from = sx == kGuessX ? first : 0, to = sw == kGuessW ? first : all;
@@ -685,7 +698,6 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
             const uint32_t m0 = ti * Tl::kM, n0 = tj * Tl::kN;
             const float k = M::kPairs ? kLog2e / (p.scales->x * p.scales->w) : kLog2e, sp = p.scales->p;
             const bool edge = n0 + Tl::kN > p.count, by_row = p.scales->by_row;
-            int power[Tl::kMt];  // of the strips' rows
             Four16 high[Tl::kMt][Tl::kNt], low[kLow ? Tl::kMt : 1][Tl::kNt];  // in 16 bits P takes half the room of the sums
             t.strips([&](int i, uint32_t row, uint32_t col, v4f(&acc)[Tl::kNt]) {
                 const uint32_t r = m0 + row;
@@ -696,11 +708,7 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                     lse = p.lse[r] * -kLog2e;
                     gain = (p.loss_grad ? p.loss_grad[r] : 1.0f) * sp;
                 }
-                power[i] = 0;
-                if (by_row) {
-                    power[i] = row_power(gain);
-                    gain = ldexpf(gain, power[i]);
-                }
+                if (by_row) gain = ldexpf(gain, row_power(gain));
                 const uint32_t here = word - p.first - n0 - col;
                 const bool none = word == p.words.vocab;
 #pragma unroll
@@ -733,7 +741,7 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                     high[i][j] = packed(v);
                     if constexpr (kLow) {
                         low[i][j] = packed(left_over(v));
-                        if constexpr (!M::kPairP) asm volatile("" : "+v"(low[i][j].a), "+v"(low[i][j].b));  // not where they are used
+                        if constexpr (!M::kPairP) asm volatile("" : "+v"(low[i][j].a), "+v"(low[i][j].b));  // here, not where they are used
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -754,16 +762,20 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
             if (p.turned.at) {
                 if (__builtin_expect(by_row, 0)) {  // words have sums over rows, which share a power of two
                     __builtin_amdgcn_sched_barrier(0);
+                    uint32_t r = m0 + t.first_row();
 #pragma unroll
-                    for (int i = 0; i < Tl::kMt; ++i)
+                    for (int i = 0; i < Tl::kMt; ++i, r += 16) {
+                        asm volatile("" : "+v"(r));
+                        const int power = p.loss_grad && r < p.n ? row_power(p.loss_grad[r] * sp) : 0;
 #pragma unroll
                         for (int j = 0; j < Tl::kNt; ++j) {
                             if constexpr (kLow)
-                                shift_pairs(high[i][j], low[i][j], -power[i]);
+                                shift_pairs(high[i][j], low[i][j], -power);
                             else
-                                high[i][j] = packed(ldexp4(unpacked(high[i][j]), -power[i]));
+                                high[i][j] = packed(ldexp4(unpacked(high[i][j]), -power));
                             __builtin_amdgcn_sched_barrier(0);
                         }
+                    }
                 }
                 t.template out16<true>(by, high, put(p.turned, p.count, p.turned_cols, n0, m0, false));
                 if constexpr (kLow) t.template out16<true>(by, low, put(p.turned, p.count, p.turned_cols, n0, m0, true));

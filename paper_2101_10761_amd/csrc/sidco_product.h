@@ -466,6 +466,9 @@ struct Tile {
         }
     }
 
+    // The lane's row of the first strip, as strips() has it.
+    __device__ __forceinline__ uint32_t first_row() const { return wave / WN * (BM / WM) + (threadIdx.x & 15); }
+
     // f(strip, row, column, sums): the strip's number, C's row and the first of the columns of its kNt sums, which are 16
     // apart; relative to the tile.  f may change the sums.
     template <class F>
