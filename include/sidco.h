@@ -713,10 +713,10 @@ size_t sidco_workspace_bytes_cross_entropy(int64_t n, int64_t dim, int64_t vocab
  *                                                       (dtype or SIDCO_GRAD_F32, row stride ldgw)
  * Either may be NULL, not both.  loss_grad (device, n floats) is 1 / n for the gradient of the
  * mean, times the loss scale if there is one; NULL stands for ones.  P is formed for one piece
- * of the vocabulary at a time, in halves under a power of two of the largest loss_grad: 11 bits
- * for a bf16 gradient, else 22, down to 2^-29 of that loss_grad, and off by 2^-38 of it below.  Rows
- * whose loss_grad is 2^-8 of the largest or less have a power of two of their own for x_grad, with as
- * many bits there as if they were alone.  bf16 operands of P's products are halves too, exact down to
+ * of the vocabulary at a time, in halves under a power of two of the largest loss_grad: in 11 bits
+ * for a bf16 gradient, else 22, or off by 2^-38 of that loss_grad, whichever is more.  Rows whose
+ * loss_grad is 2^-8 of the largest or less have a power of two of their own for x_grad, with as many
+ * bits there as if they were alone.  bf16 operands of P's products are halves too, exact down to
  * 2^-24 of their matrix's largest magnitude and off by 2^-32 of that below.  Rows of x whose target
  * is padding do not enter w_grad whatever they hold.  The gradients must not overlap x, w or each
  * other.  Uses the stream's workspace, of sidco_workspace_bytes_cross_entropy_grad(n, dim, vocab,
@@ -729,10 +729,10 @@ size_t sidco_workspace_bytes_cross_entropy_grad(int64_t n, int64_t dim, int64_t 
 
 /*
  * The same from the losses too (device, n floats, of the same call as lse; NULL: the call above).
- * A row's target has P = loss_grad (exp(l - lse) - 1), which lse as rounded to fp32 leaves off by
- * 2^-23 |lse| of loss_grad: nothing beside a P of one, all of it where a row knows its target to 2^-23
- * |lse|.  The loss is kept to its own last bits there, and P = loss_grad (exp(-loss) - 1) with it:
- * give it where gradients of such rows count.
+ * A row's target has P = loss_grad (exp(l - lse) - 1), off by what l and lse are: 2^-23 |lse| of
+ * loss_grad, more where they came from sums in other orders, as for few rows.  That is little beside
+ * a P of one and all of it where a row knows its target that well.  The loss is kept to its own last
+ * bits there, and with it P = loss_grad (exp(-loss) - 1): give it where gradients of such rows count.
  */
 int sidco_cross_entropy_grad_of_loss(void *stream, const void *x, const void *w, int dtype, int64_t n, int64_t dim, int64_t vocab,
                                      int64_t ldx, int64_t ldw, const void *targets, int word_type, const float *loss, const float *lse,

@@ -652,12 +652,6 @@ __device__ __forceinline__ Four16 packed(const v4f& v)
 {
     return {__builtin_bit_cast(uint32_t, h2{(G)v[0], (G)v[1]}), __builtin_bit_cast(uint32_t, h2{(G)v[2], (G)v[3]})};
 }
-__device__ __forceinline__ v4f unpacked(Four16 v)
-{
-    asm volatile("" : "+v"(v.a), "+v"(v.b));  // the values that were packed are not kept until here
-    const h2 a = __builtin_bit_cast(h2, v.a), b = __builtin_bit_cast(h2, v.b);
-    return v4f{(float)a[0], (float)a[1], (float)b[0], (float)b[1]};
-}
 // What halves leave of the values.
 __device__ __forceinline__ v4f left_over(const v4f& v)
 {
@@ -672,11 +666,13 @@ __device__ __forceinline__ v4f ldexp4(v4f v, int by)
     for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], by);
     return v;
 }
-__device__ __forceinline__ void shift_pairs(Four16& high, Four16& low, int by)
+// Times 2^-by, in two steps: halves go down to 2^-24.  What is left below 2^-14 is off by 2^-25.
+__device__ __forceinline__ void shift_down(Four16& v, int by)
 {
-    const v4f v = rounded(ldexp4(unpacked(high) + unpacked(low), by));
-    high = packed(v);
-    low = packed(left_over(v));
+    const int first = by < 48 ? by / 2 : 24, second = by < 48 ? by - first : 24;
+    const G a = (G)ldexpf(1.0f, -first), b = (G)ldexpf(1.0f, -second);
+    v.a = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, v.a) * h2{a, a} * h2{b, b});
+    v.b = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, v.b) * h2{a, a} * h2{b, b});
 }
 
 template <class M, bool Low, class Tl>
@@ -739,10 +735,9 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                 for (int j = 0; j < Tl::kNt; ++j) {
                     const v4f v = rounded(acc[j]);
                     high[i][j] = packed(v);
-                    if constexpr (kLow) {
-                        low[i][j] = packed(left_over(v));
-                        if constexpr (!M::kPairP) asm volatile("" : "+v"(low[i][j].a), "+v"(low[i][j].b));  // here, not where they are used
-                    }
+                    if constexpr (kLow) low[i][j] = packed(left_over(v));
+                    if constexpr (kLow && !M::kPairP)  // packed here, not where they are used, which takes what they come from there too
+                        asm volatile("" : "+v"(high[i][j].a), "+v"(high[i][j].b), "+v"(low[i][j].a), "+v"(low[i][j].b));
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
@@ -769,10 +764,8 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                         const int power = p.loss_grad && r < p.n ? row_power(p.loss_grad[r] * sp) : 0;
 #pragma unroll
                         for (int j = 0; j < Tl::kNt; ++j) {
-                            if constexpr (kLow)
-                                shift_pairs(high[i][j], low[i][j], -power);
-                            else
-                                high[i][j] = packed(ldexp4(unpacked(high[i][j]), -power));
+                            shift_down(high[i][j], power);
+                            if constexpr (kLow) shift_down(low[i][j], power);
                             __builtin_amdgcn_sched_barrier(0);
                         }
                     }
@@ -838,14 +831,19 @@ __global__ __launch_bounds__(Tl::kThreads) void k_product(Product p, Span span, 
             uint32_t ti, tj, split;
             places.at(tile, ti, tj, split);
             const int shift = -exponent_of(p.scales->p) - exponent_of(p.of_x ? p.scales->x : p.scales->w);
-            const bool by_row = p.loss_grad && p.scales->by_row;
-            t.each([&](uint32_t row, uint32_t col, v4f v) {
-                const int64_t r = (int64_t)ti * Tl::kM + row, c = (int64_t)tj * Tl::kN + col;
-                if (r >= p.m || c >= p.n) return;
-                v = ldexp4(v, by_row ? shift - row_power(p.loss_grad[r] * p.scales->p) : shift);
-                finish4<T>((T*)p.c + split * p.split_stride + r * p.ldc + c, p.before ? p.before + r * p.n + c : nullptr, p.accumulate, p.n - c,
-                           v);
-            });
+            auto write = [&](auto by_row) {
+                t.each([&](uint32_t row, uint32_t col, v4f v) {
+                    const int64_t r = (int64_t)ti * Tl::kM + row, c = (int64_t)tj * Tl::kN + col;
+                    if (r >= p.m || c >= p.n) return;
+                    v = ldexp4(v, decltype(by_row)::value ? shift - row_power(p.loss_grad[r] * p.scales->p) : shift);
+                    finish4<T>((T*)p.c + split * p.split_stride + r * p.ldc + c, p.before ? p.before + r * p.n + c : nullptr, p.accumulate, p.n - c,
+                               v);
+                });
+            };
+            if (__builtin_expect(p.loss_grad && p.scales->by_row, 0))
+                write(std::true_type());
+            else
+                write(std::false_type());
         });
 }
 
