@@ -729,10 +729,12 @@ size_t sidco_workspace_bytes_cross_entropy_grad(int64_t n, int64_t dim, int64_t 
 
 /*
  * The same from the losses too (device, n floats, of the same call as lse; NULL: the call above).
- * A row's target has P = loss_grad (exp(l - lse) - 1), off by what l and lse are: 2^-23 |lse| of
- * loss_grad, more where they came from sums in other orders, as for few rows.  That is little beside
- * a P of one and all of it where a row knows its target that well.  The loss is kept to its own last
- * bits there, and with it P = loss_grad (exp(-loss) - 1): give it where gradients of such rows count.
+ * A row's target has P = loss_grad (exp(l - lse) - 1), a difference that l and lse are not near
+ * enough for where the row knows its target: with the losses it is loss_grad (exp(-loss) - 1),
+ * which keeps its own last bits.  Without them it is minus the sum of the row's others where a row
+ * knows its target to more than a quarter and P of all words takes no more than 2^30 bytes (n rounded
+ * up to a multiple of 64, times vocab, times 2, twice that for both gradients, twice that again but for
+ * bf16), at some microseconds; else it is that difference, off by 2^-23 |lse| of loss_grad.
  */
 int sidco_cross_entropy_grad_of_loss(void *stream, const void *x, const void *w, int dtype, int64_t n, int64_t dim, int64_t vocab,
                                      int64_t ldx, int64_t ldw, const void *targets, int word_type, const float *loss, const float *lse,

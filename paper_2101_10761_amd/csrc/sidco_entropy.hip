@@ -632,10 +632,14 @@ __global__ __launch_bounds__(256) void k_join_rows(const float2* part, uint32_t 
     }
 }
 
-// P of a piece of the vocabulary, words from `first` on.  A row's word has exp(l - lse) - 1, which for a row that knows its word is
-// the difference of two numbers near one, off by what lse is rounded by; given the loss it is exp(-loss) - 1 without it.  Bound by the matrix cores, and a round's end by memory: with all CUs' tiles
+// P of a piece of the vocabulary, words from `first` on.  Bound by the matrix cores, and a round's end by memory: with all CUs' tiles
 // done at once, 256 KB of each (512 KB with low halves) leave at what HBM takes, 11 us (20).  8192 x 4096 x 32768 in bf16 1.65 to 1.69 ms,
-// 1.30 to 1.33 PFLOP/s; 2049 x 1024 x 49999 in fp16, P in pairs, 371 us, 0.57; 700 x 1500 x 10000 in pairs 73 us, 0.86.
+// 1.30 to 1.33 PFLOP/s; 2049 x 1024 x 49999 in fp16, P in pairs, 384 us, 0.55; 700 x 1500 x 10000 in pairs 76 us, 0.83.
+//
+// A row's word has exp(l - lse) - 1, which for a row that knows its word is the difference of two numbers near one, off by what lse
+// was rounded by and by l, if lse came from sums in another order as those of few rows do: 2e-6 of a gradient in the 2-norm, and all
+// of one such row's.  So it is exp(-loss) - 1 if the loss is given, and else, where all words are in one piece, left out here and
+// written by k_own_words from the sum of the row's others: 3e-7.  That takes 4 to 7 us of a launch and 1 % in here.
 template <class H>
 struct Probs {
     Plane<H> x, w;  // w: the piece's rows
@@ -645,6 +649,9 @@ struct Probs {
     Plane<G> out, turned;  // n rows of words, words of n rows; either may have no address
     uint32_t turned_cols;  // with the zeros behind the last row
     const Scales* scales;
+    float* row_sums;       // `width` lists of n, one for each wave's columns; NULL: no row's word is left out
+    uint32_t width;
+    float* left_out;       // exp(l - lse) of the rows' words
 };
 
 typedef G h2 __attribute__((ext_vector_type(2)));
@@ -711,12 +718,19 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                 for (int j = 0; j < Tl::kNt; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[j][e] = __builtin_amdgcn_exp2f(fmaf(acc[j][e], k, lse));
-                if (here < Tl::kNt * 16) {  // one lane in 128 columns, if any
+                if (__builtin_expect_with_probability(here < Tl::kNt * 16 && here % 16 < 4, 0, 0.999)) {  // one lane in 128 columns, if any
                     const float own = p.loss && r < p.n ? expm1f(-p.loss[r]) : 0.0f;
+                    float is = 0.0f;
 #pragma unroll
                     for (int j = 0; j < Tl::kNt; ++j)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[j][e] = here == (uint32_t)(j * 16 + e) ? (p.loss ? own : acc[j][e] - 1.0f) : acc[j][e];
+                        for (int e = 0; e < 4; ++e) is = here == (uint32_t)(j * 16 + e) ? acc[j][e] : is;
+                    if (p.row_sums && r < p.n) p.left_out[r] = is;
+                    is = p.loss || p.row_sums ? own : is - 1.0f;
+#pragma unroll
+                    for (int j = 0; j < Tl::kNt; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[j][e] = here == (uint32_t)(j * 16 + e) ? is : acc[j][e];
                 }
 #pragma unroll
                 for (int j = 0; j < Tl::kNt; ++j) acc[j] *= gain;
@@ -731,13 +745,22 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[j][e] = left > j * 16 + e ? acc[j][e] : 0.0f;
                 }
+                v4f part = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int j = 0; j < Tl::kNt; ++j) {
                     const v4f v = rounded(acc[j]);
+                    part += v;
                     high[i][j] = packed(v);
                     if constexpr (kLow) low[i][j] = packed(left_over(v));
                     if constexpr (kLow && !M::kPairP)  // packed here, not where they are used, which takes what they come from there too
                         asm volatile("" : "+v"(high[i][j].a), "+v"(high[i][j].b), "+v"(low[i][j].a), "+v"(low[i][j].b));
+                }
+                if (p.row_sums) {
+                    float sum = (part[0] + part[1]) + (part[2] + part[3]);
+                    sum += __shfl_xor(sum, 16);
+                    sum += __shfl_xor(sum, 32);
+                    const uint32_t place = tj * (Tl::kN / (Tl::kNt * 16)) + t.wave % (Tl::kN / (Tl::kNt * 16));
+                    if (t.lane < 16 && r < p.n) p.row_sums[(int64_t)place * p.n + r] = sum;
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
@@ -774,6 +797,40 @@ __global__ __launch_bounds__(Tl::kThreads) void k_probs(Probs<typename M::H> p, 
                 if constexpr (kLow) t.template out16<true>(by, low, put(p.turned, p.count, p.turned_cols, n0, m0, true));
             }
         });
+}
+
+// The rows' words, which without the loss are left out of P.  One that a row knows well is minus the sum of its others: as near as
+// they are, and a row of P adds up to zero.  Another is nearer by itself than by that sum's roundings.  A block has 16 rows, 16 lanes to
+// each of them.
+constexpr float kKnown = 0.25f;
+template <class M, bool Low>
+__global__ __launch_bounds__(256) void k_own_words(Probs<typename M::H> p)
+{
+    __shared__ float lds[16][17];
+    const uint32_t at = threadIdx.x & 15, part = threadIdx.x >> 4, r = blockIdx.x * 16 + at;
+    float sum = 0.0f;
+    if (r < p.n) {
+#pragma unroll 8
+        for (uint32_t i = part; i < p.width; i += 16) sum += p.row_sums[(int64_t)i * p.n + r];
+    }
+    lds[part][at] = sum;
+    __syncthreads();
+    if (part != 0 || r >= p.n) return;
+    const uint32_t word = p.words[r];
+    if (word == p.words.vocab) return;
+    sum = 0.0f;
+    for (int i = 0; i < 16; ++i) sum += lds[i][at];
+    auto put = [](const Plane<G>& o, int64_t at, float v, bool low) {
+        asm volatile("" : "+v"(v));  // see rounded()
+        const G high = (G)v;
+        o.at[at] = high;
+        if (low) o.at[at + o.low] = (G)(v - (float)high);
+    };
+    const float gain = (p.loss_grad ? p.loss_grad[r] : 1.0f) * p.scales->p, is = p.left_out[r];
+    const int power = p.scales->by_row ? row_power(gain) : 0;
+    const float v = is > kKnown && is < INFINITY ? -sum : (is - 1.0f) * ldexpf(gain, power);
+    if (p.out.at) put(p.out, (int64_t)r * p.out.pitch + word, v, M::kPairP);
+    if (p.turned.at) put(p.turned, (int64_t)word * p.turned.pitch + r, ldexpf(v, -power), Low || M::kPairP);
 }
 
 // C = 2^e A B^T over the columns that span.lines cover, of split number s from column s * lines on: rounded to T, on top of
@@ -1171,6 +1228,7 @@ struct GradPlan {
     Plane<H> x, w;
     Plane<G> xt, wt, p, pt;
     float* sums;
+    float *row_sums, *left_out;  // of P, for the rows' words; NULL where there are several pieces, whose first are multiplied before the last are known
     size_t bytes;
     static constexpr int kTerms = M::kPairs ? 3 : (M::kPairP ? 2 : 1);  // of the product for x's gradient
     GradPlan(const Entropy& q, char* scratch)
@@ -1218,8 +1276,21 @@ struct GradPlan {
             p = s.plane<G>(n, pitch_v, M::kPairP);
         }
         sums = q.x_grad.at && (splits > 1 || pieces > 1) ? s.get<float>(splits * n * q.dim) : nullptr;
+        row_sums = left_out = nullptr;
+        if (pieces == 1) {
+            const int64_t cols = q.x_grad.at ? cols_v : v;
+            const RowPlan plan = probs_plan(n, cols);
+            row_sums = s.get<float>(std::max(plan.rows * probs_width(plan.pick, cols), (n - plan.rows) * probs_width(plan.rest_pick, cols)));
+            left_out = s.get<float>(n);
+        }
         bytes = s.used;
     }
+    // The launches for P of `cols` words.
+    RowPlan probs_plan(int64_t n, int64_t cols) const
+    {
+        return plan_rows(M::kPairP || wide ? kProbPairs : kProbs, M::kPairs ? 3 : 1, n, cols, pitch / kPer);
+    }
+    static int64_t probs_width(int pick, int64_t cols) { return 2 * parts(cols, kTileCosts[pick].side); }
 };
 
 template <class T, int Terms>
@@ -1284,17 +1355,21 @@ void gradient(const Entropy& q, char* scratch, hipStream_t s)
                 const Plane<G> turned = {g.pt.at ? g.pt.at + row : nullptr, g.pt.pitch, g.pt.low};
                 const Probs<H> p = {x, w, (uint32_t)rows, (uint32_t)count, (uint32_t)first, words.from(row), q.lse + row,
                                     q.loss ? q.loss + row : nullptr, q.loss_grad ? q.loss_grad + row : nullptr, out, turned,
-                                    (uint32_t)(row + rows < n ? rows : g.cols_n - row), g.scales};
-                auto go = [&](auto kernel) { kernel<<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places); };
+                                    (uint32_t)(row + rows < n ? rows : g.cols_n - row), g.scales, q.loss ? nullptr : g.row_sums,
+                                    (uint32_t)g.probs_width(pick, wide), g.left_out};
+                auto go = [&](auto kernel, auto own_words) {
+                    kernel<<<tile_blocks(pick, places.total), Tl::kThreads, 0, s>>>(p, span, places);
+                    if (p.row_sums) own_words<<<(uint32_t)parts(rows, 16), 256, 0, s>>>(p);
+                };
                 if constexpr (M::kPairP)
-                    go(k_probs<M, true, Tl>);
+                    go(k_probs<M, true, Tl>, k_own_words<M, true>);
                 else if (g.wide)
-                    go(k_probs<M, true, Tl>);
+                    go(k_probs<M, true, Tl>, k_own_words<M, true>);
                 else
-                    go(k_probs<M, false, Tl>);
+                    go(k_probs<M, false, Tl>, k_own_words<M, false>);
             });
         };
-        const RowPlan plan = plan_rows(M::kPairP || g.wide ? kProbPairs : kProbs, M::kPairs ? 3 : 1, n, wide, span.lines);
+        const RowPlan plan = g.probs_plan(n, wide);
         probs(plan.pick, 0, plan.rows);
         if (plan.rows < n) probs(plan.rest_pick, plan.rows, n - plan.rows);
         if (q.x_grad.at) {

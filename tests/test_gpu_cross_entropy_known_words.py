@@ -64,6 +64,64 @@ def test_rows_that_know_their_word(n, gap, t, o):
     assert not bool(dx[n // 2].any())
 
 
+class Sums(Known):
+    """Without the losses a word of which a row knows more than a quarter has minus the sum of the row's others, off by what they are and a sum in
+    32 bits; one of which it knows less is exp(l - lse) - 1.  Near a quarter it may be either."""
+
+    def __init__(self, x, w, words, g):
+        torch = _torch()
+        super().__init__(x, w, words, g)
+        base = ref.CrossEntropy(x, w, words, g)
+        rows, at = torch.arange(len(x), device=x.device), torch.where(self.ok, self.words, 0)
+        p, off = self.p[rows, at].abs(), self.p_off.clone()
+        off[rows, at] = 0.0
+        sums = off.sum(1) + 70 * self.u * p
+        one = base.p_off[rows, at]
+        known = torch.exp(-self.loss)
+        off[rows, at] = torch.where(known > 0.26, sums, torch.where(known < 0.24, one, torch.maximum(sums, one)))
+        self.p_off = off
+
+
+@pytest.mark.parametrize("n,gap", [(3, 0), (40, 1), (100, 0), (300, 3)])
+@pytest.mark.parametrize("t,o", [("f32", "f32"), ("f16", "f16"), ("f16", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("low", [0, 30])
+def test_without_the_losses(n, gap, t, o, low):
+    torch, sidco = _torch(), _sidco()
+    x, w, words = _known(n, t, gap)
+    x = x * torch.rand(n, 1, device="cuda", generator=torch.Generator(device="cuda").manual_seed(n + 1)).round().clamp(min=0.125).to(x.dtype)
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    g = (0.5 + torch.rand(n, device="cuda", generator=gen)) * torch.exp2(-low * torch.rand(n, device="cuda", generator=gen))
+    loss, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    dx, dw = torch.full(x.shape, 3.0, dtype=x.dtype, device="cuda"), torch.full(w.shape, 3.0, dtype=_dtype(o), device="cuda")
+    sidco.sidco_cross_entropy(x, w, words, loss, lse)
+    sidco.sidco_cross_entropy_grad(x, w, words, lse, g, dx, dw)
+    torch.cuda.synchronize()
+    r = Sums(x, w, words, g)
+    for got, (want, off) in ((dx, r.x_grad()), (dw, r.w_grad(_dtype(o)))):
+        off = off + 2.0**-38 * float(g.max()) * 128  # P by words is rounded under two powers of two where a row has one of its own
+        miss = (got.double() - want).abs()
+        assert bool((miss <= off).all()), (float(miss.max()), (miss > off).nonzero()[:4].tolist())
+    a, b = torch.empty_like(dx), torch.empty_like(dw)
+    sidco.sidco_cross_entropy_grad(x, w, words, lse, g, x_grad=a)
+    sidco.sidco_cross_entropy_grad(x, w, words, lse, g, weight_grad=b)
+    torch.cuda.synchronize()
+    assert torch.equal(a, dx) and torch.equal(b, dw)
+
+
+def test_no_number_stays_one_without_the_losses():
+    torch, sidco = _torch(), _sidco()
+    for n in (3, 130):
+        x, w = torch.ones(n, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(300, 64, dtype=torch.bfloat16, device="cuda")
+        w[7, 0] = float("inf")
+        words = torch.full((n,), 7, device="cuda")
+        x[1], words[1] = 0.0, -1
+        lse, dx, dw = torch.full((n,), float("inf"), device="cuda"), torch.empty_like(x), torch.empty_like(w)
+        sidco.sidco_cross_entropy_grad(x, w, words, lse, None, dx, dw)
+        torch.cuda.synchronize()
+        # the padding row's P is zeros, and its x_grad P w: zero times infinity in the first column
+        assert bool(torch.isnan(dx[0]).all()) and not bool(dx[1, 1:].any()) and bool(torch.isnan(dw[7]).all())
+
+
 def test_one_gradient_alone_from_the_losses():
     torch, sidco = _torch(), _sidco()
     for t in ("f32", "bf16"):
