@@ -1059,7 +1059,8 @@ int64_t forward_width(int pick, int64_t vocab) { return 2 * parts(vocab, kTileCo
 // The blocks of k_few, the steps that it takes, and whether it is what a call takes.  It reads the weight once for every 32 rows; the
 // way by tiles reads it once, and where it has to be laid out first a second time, for fp32 a third, beside writing it.  us, here /
 // there: against 10000 x 1500 fp32 64 rows 44 / 63, 96 rows 64 / 74; 100000 x 2048 fp32 292 / 740, 436 / 791; 10000 x 1502 bf16 33 rows
-// 24 / 28; 100000 x 3002 bf16 20 rows 113 / 403.  Rows of 16 bits that start between two words are read at half the rate: 10000 x 1501 bf16
+// 24 / 28; 100000 x 3002 bf16 20 rows 113 / 403.  From 97 rows on the way by tiles is taken whatever the weight: of 128 rows against
+// 100000 x 2048 fp32 it takes 666, and four passes here would be 580 by the figures above, against 10000 x 1500 64 and 85.  Rows of 16 bits that start between two words are read at half the rate: 10000 x 1501 bf16
 // 20 rows 31 / 28, 33 rows 54 / 28; 100000 x 3001 207 / 404, 420 / 404.
 constexpr int64_t kFewBlocks = 512;
 template <class M>
