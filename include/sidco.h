@@ -659,7 +659,7 @@ int sidco_embedding(void *stream, const void *table, int table_dtype, int64_t vo
  * What is formed in fp32 is then rounded to table_grad's type.  Padding has no gradient,
  * whatever its row of grad holds.  grad is n x dim with row stride ldg, table_grad vocab x dim
  * with row stride ldt; n / 32, up to 2048 words n / 8, times dim / 512, each rounded up, is at
- * most 2^22 (SIDCO_ERR_SIZE).  Uses the stream's workspace, of
+ * most 2^22 (SIDCO_ERR_SIZE).  They must not overlap.  Uses the stream's workspace, of
  * sidco_workspace_bytes_embedding_grad(n, dim).
  */
 int sidco_embedding_grad(void *stream, const void *grad, int grad_dtype, int64_t n, int64_t dim, int64_t ldg, const void *words,
@@ -732,9 +732,10 @@ size_t sidco_workspace_bytes_cross_entropy_grad(int64_t n, int64_t dim, int64_t 
  * A row's target has P = loss_grad (exp(l - lse) - 1), a difference that l and lse are not near
  * enough for where the row knows its target: with the losses it is loss_grad (exp(-loss) - 1),
  * which keeps its own last bits.  Without them it is minus the sum of the row's others where a row
- * knows its target to more than a quarter and P of all words takes no more than 2^30 bytes (n rounded
- * up to a multiple of 64, times vocab, times 2, twice that for both gradients, twice that again but for
- * bf16), at some microseconds; else it is that difference, off by 2^-23 |lse| of loss_grad.
+ * knows its target to more than a quarter and P of all words is formed at once, at some microseconds
+ * (where it takes at most 2^30 bytes - n rounded up to a multiple of 64, times vocab, times 2, twice that
+ * for both gradients, twice that again but for bf16 - and vocab is at most 2^22); else it is that
+ * difference, off by 2^-23 |lse| of loss_grad.
  */
 int sidco_cross_entropy_grad_of_loss(void *stream, const void *x, const void *w, int dtype, int64_t n, int64_t dim, int64_t vocab,
                                      int64_t ldx, int64_t ldw, const void *targets, int word_type, const float *loss, const float *lse,

@@ -253,8 +253,8 @@ __device__ __forceinline__ float lay(const Layout<typename M::T, typename M::H>&
     return top;
 }
 
-// x and w laid out with the guessed scales, and the largest finite magnitudes of x, w and the rows' gradient, a partial result from
-// each block (not in the forward pass of 16-bit operands, which nothing is scaled in).  The magnitudes are only known behind a pass over
+// x and w laid out with the guessed scales, and the largest finite magnitudes of x, w and the rows' gradient, and that one's least, a partial
+// result from each block (not in the forward pass of 16-bit operands, which nothing is scaled in).  The magnitudes are only known behind a pass over
 // everything: to find them first and lay out then is one read more.  Bound by memory: 700 and 10000 rows of 1500 fp32, 64 MB read and
 // 128 MB written (two halves of each by rows and transposed), 28 to 34 us; with the pass before it the training step took 391, not 378.
 template <class M, bool Scaled>
@@ -286,8 +286,8 @@ __global__ __launch_bounds__(256) void k_layout(Layout<typename M::T, typename M
 }
 
 // The scales that the largest magnitudes ask for, and what was laid out with another one once more.  A piece of w after the first
-// leaves those of x and P as they are.  4.8 us where the guess does, three lists of 2048 partial results for each block; about
-// 32 where all of that size is laid out again.
+// leaves those of x and P as they are.  4.8 us where the guess does, two lists of 2048 partial results for each block and two more
+// for the first; about 32 where all of that size is laid out again.
 constexpr uint32_t kSettleBlocks = 512;
 template <class M>
 __global__ __launch_bounds__(256) void k_settle(Layout<typename M::T, typename M::H> x, Layout<typename M::T, typename M::H> w, uint32_t blocks, bool later,
@@ -1060,8 +1060,9 @@ int64_t forward_width(int pick, int64_t vocab) { return 2 * parts(vocab, kTileCo
 // way by tiles reads it once, and where it has to be laid out first a second time, for fp32 a third, beside writing it.  us, here /
 // there: against 10000 x 1500 fp32 64 rows 44 / 63, 96 rows 64 / 74; 100000 x 2048 fp32 292 / 740, 436 / 791; 10000 x 1502 bf16 33 rows
 // 24 / 28; 100000 x 3002 bf16 20 rows 113 / 403.  From 97 rows on the way by tiles is taken whatever the weight: of 128 rows against
-// 100000 x 2048 fp32 it takes 666, and four passes here would be 580 by the figures above, against 10000 x 1500 64 and 85.  Rows of 16 bits that start between two words are read at half the rate: 10000 x 1501 bf16
-// 20 rows 31 / 28, 33 rows 54 / 28; 100000 x 3001 207 / 404, 420 / 404.
+// 100000 x 2048 fp32 it takes 666, and four passes here would be 580 by the figures above, against 10000 x 1500 64 and 85.
+// Rows of 16 bits that start between two words are read at half the rate: 10000 x 1501 bf16 20 rows 31 / 28, 33 rows 54 / 28; 100000 x
+// 3001 207 / 404, 420 / 404.
 constexpr int64_t kFewBlocks = 512;
 template <class M>
 int64_t few_steps(int64_t dim)
@@ -1229,7 +1230,7 @@ struct GradPlan {
     Plane<H> x, w;
     Plane<G> xt, wt, p, pt;
     float* sums;
-    float *row_sums, *left_out;  // of P, for the rows' words; NULL where there are several pieces, whose first are multiplied before the last are known
+    float *row_sums, *left_out;  // of P, for the rows' words; NULL with several pieces, whose first are multiplied before the last are known
     size_t bytes;
     static constexpr int kTerms = M::kPairs ? 3 : (M::kPairP ? 2 : 1);  // of the product for x's gradient
     GradPlan(const Entropy& q, char* scratch)
